@@ -304,6 +304,46 @@ int poss_debug_gemm(int32_t dtype, const void *x, const void *w, void *y, int32_
 int poss_gemm_static(int32_t dtype, const void *x, const void *w, void *y, int32_t M, int32_t N,
                      int32_t K, int32_t target_workgroups, void *hip_stream);
 
+/* ---- microscaled 4-bit weights ---------------------------------------------------------------- */
+
+/* A quarter of the bytes of 16-bit weights for what streams them.  The format ("MX"): 32 values of a row share a power of two, a byte b
+ * that stands for 2^(b - 127) (255: NaN); a value is 4 bits, sign and magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6.  A matrix of `rows` x `cols`
+ * is codes[rows][nb][16] bytes (the even column in the low half of a byte) and scales[rows][nb] bytes, nb = ceil(cols / 32), both
+ * contiguous; columns beyond cols are codes of zero.
+ *
+ * All calls below enqueue on hip_stream (NULL = default stream) of the current GPU, whose memory every pointer addresses, and return
+ * without waiting; they allocate nothing, keep nothing, and can be captured into a graph.  Rows start ld* values apart (ld >= the row's
+ * length, as 64-bit counts).  Zero rows are no work and no error.  Inputs and outputs must not overlap.  Failures leave their message for
+ * poss_last_error(NULL). */
+
+/* x[rows][cols] of `dtype` to codes (16-byte aligned) and scales.  The power of two of a block is that of its largest magnitude less two
+ * (at least 2^-127), a value is the nearest of the eight magnitudes times it, of two equally near the one whose code is even, at most
+ * 6; a block that holds a NaN or an infinity gets the scale NaN and codes of zero, a block of zeros the scale 2^-127. */
+int poss_mx_quantize(int32_t dtype, const void *x, int64_t ldx, int32_t rows, int32_t cols, void *codes, void *scales, void *hip_stream);
+/* What codes and scales stand for, rounded once to `dtype`: y[rows][cols]. */
+int poss_mx_dequantize(int32_t dtype, const void *codes, const void *scales, int32_t rows, int32_t cols, void *y, int64_t ldy, void *hip_stream);
+
+/* A weight matrix [N][K] (codes and scales as above) in the operand order of the products below: `packed`, poss_mx_packed_bytes(N, K)
+ * bytes (0 for a bad shape), aligned to 256.  Codes and scales are not needed afterwards.  Products use a block's scale relative to
+ * the largest one of its row: exactly while it lies at most 126 (fp16 activations: 36) powers of two below; what lies further below is smaller than
+ * 2^-124 (2^-38) of the row's largest weight and may lose bits or be taken for zero. */
+size_t poss_mx_packed_bytes(int32_t N, int32_t K);
+int poss_mx_pack(const void *codes, const void *scales, int32_t N, int32_t K, void *packed, void *hip_stream);
+
+/* Y[M][N] of y_dtype = X[M][K] . W[N][K]^T with packed W and X of x_dtype.  Every product of an activation and a weight is exact (float32
+ * activations included), sums are float32, the result is rounded once.  scratch: at least poss_mx_gemm_scratch_bytes(x_dtype, M, N, K)
+ * bytes (at least 256; 0 for a bad shape), aligned to 256, for this call alone until it has run: two calls that may run at the same
+ * time, or two graphs that may, need one each.  The bits of a row may differ with M (other kernels sum in another order); the same call
+ * gives the same bits. */
+#define POSS_MX 4                    /* in place of x_dtype: X is microscaled too (poss_mx_gemm_mx) */
+size_t poss_mx_gemm_scratch_bytes(int32_t x_dtype, int32_t M, int32_t N, int32_t K);
+int poss_mx_gemm(int32_t x_dtype, const void *x, int64_t ldx, const void *packed, int32_t y_dtype, void *y, int64_t ldy,
+                 int32_t M, int32_t N, int32_t K, void *scratch, size_t scratch_bytes, void *hip_stream);
+/* The same with X[M][K] as poss_mx_quantize leaves it: both operands go to the matrix cores in 4 bits.  A row of X with a block of
+ * scale NaN gives a row of NaN, a row of W a column of NaN. */
+int poss_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *packed, int32_t y_dtype, void *y, int64_t ldy,
+                    int32_t M, int32_t N, int32_t K, void *scratch, size_t scratch_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

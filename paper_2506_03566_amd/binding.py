@@ -19,7 +19,8 @@ EXPORTS = ["poss_workspace_bytes", "poss_load", "poss_reset", "poss_prefill", "p
            "poss_prefill_seq", "poss_get_tree_seq", "poss_get_commit_seq", "poss_get_tokens_seq", "poss_set_uniforms_seq", "poss_reset_seq", "poss_set_active",
            "poss_last_error", "poss_free", "poss_profile_gemm", "poss_gemm_profile", "poss_set_tuning", "poss_set_launch_rows", "poss_set_sampling", "poss_set_draft_sampling",
            "poss_debug_build_tree", "poss_debug_set_taps", "poss_debug_read_kv", "poss_debug_draft_logits",
-           "poss_debug_gemm_scratch_bytes", "poss_debug_gemm", "poss_gemm_static"]
+           "poss_debug_gemm_scratch_bytes", "poss_debug_gemm", "poss_gemm_static",
+           "poss_mx_quantize", "poss_mx_dequantize", "poss_mx_packed_bytes", "poss_mx_pack", "poss_mx_gemm_scratch_bytes", "poss_mx_gemm", "poss_mx_gemm_mx"]
 
 c_i32, c_f32, c_vp = ctypes.c_int32, ctypes.c_float, ctypes.c_void_p
 
@@ -101,6 +102,16 @@ def load_library():
     lib.poss_debug_gemm_scratch_bytes.argtypes = [c_i32, c_i32, c_i32, c_i32]
     lib.poss_debug_gemm.argtypes = [c_i32, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_vp, c_vp, c_i32, P(c_f32)]
     lib.poss_gemm_static.argtypes = [c_i32, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_vp]
+    c_i64, c_sz = ctypes.c_int64, ctypes.c_size_t
+    lib.poss_mx_quantize.argtypes = [c_i32, c_vp, c_i64, c_i32, c_i32, c_vp, c_vp, c_vp]
+    lib.poss_mx_dequantize.argtypes = [c_i32, c_vp, c_vp, c_i32, c_i32, c_vp, c_i64, c_vp]
+    lib.poss_mx_packed_bytes.restype = c_sz
+    lib.poss_mx_packed_bytes.argtypes = [c_i32, c_i32]
+    lib.poss_mx_pack.argtypes = [c_vp, c_vp, c_i32, c_i32, c_vp, c_vp]
+    lib.poss_mx_gemm_scratch_bytes.restype = c_sz
+    lib.poss_mx_gemm_scratch_bytes.argtypes = [c_i32, c_i32, c_i32, c_i32]
+    lib.poss_mx_gemm.argtypes = [c_i32, c_vp, c_i64, c_vp, c_i32, c_vp, c_i64, c_i32, c_i32, c_i32, c_vp, c_sz, c_vp]
+    lib.poss_mx_gemm_mx.argtypes = [c_vp, c_vp, c_vp, c_i32, c_vp, c_i64, c_i32, c_i32, c_i32, c_vp, c_sz, c_vp]
     _lib = lib
     return lib
 
@@ -373,3 +384,158 @@ def gemm_static(dtype, x, w, y, target_workgroups=0, stream=None):
                               target_workgroups, c_vp(stream.cuda_stream) if stream is not None else c_vp(0))
     if rc != POSS_OK:
         raise PossError(rc, lib.poss_last_error(None).decode())
+
+
+# ---- microscaled 4-bit weights
+MX_BLOCK = 32
+_MX = 4                              # POSS_MX: activations that are microscaled too
+
+
+def _mx_refuse(msg):
+    raise PossError(E_INVALID_ARG, msg)
+
+
+def _mx_dtype(t):
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t)
+    return _mx_refuse("float32, bfloat16 or float16 is wanted, not %s" % t) if code is None else code
+
+
+def _mx_rows(t, what):
+    """Address and row distance of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        _mx_refuse("%s must be a matrix with contiguous rows" % what)
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        _mx_refuse("%s must not have overlapping rows" % what)
+    return t.data_ptr(), ld
+
+
+def _mx_blocks(codes, scales, rows, cols, what):
+    import torch
+    nb = (cols + MX_BLOCK - 1) // MX_BLOCK
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(codes.shape) != (rows, nb * 16) or tuple(scales.shape) != (rows, nb) \
+            or not codes.is_contiguous() or not scales.is_contiguous():
+        _mx_refuse("%s: contiguous uint8 codes [%d, %d] and scales [%d, %d] are wanted" % (what, rows, nb * 16, rows, nb))
+
+
+class _MxCall:
+    """Makes the tensors' GPU current around a call and finds the stream: the caller's, or torch's current one there."""
+
+    def __init__(self, stream, *tensors):
+        import torch
+        dev = tensors[0].device
+        for t in tensors:
+            if not t.is_cuda or t.device != dev:
+                _mx_refuse("all tensors of a call must be on one GPU")
+        self.back = torch.cuda.current_device()
+        self.dev = dev.index
+        self.stream = c_vp((stream if stream is not None else torch.cuda.current_stream(dev)).cuda_stream)
+
+    def __enter__(self):
+        if self.dev != self.back:
+            import torch
+            torch.cuda.set_device(self.dev)
+        return self.stream
+
+    def __exit__(self, *exc):
+        if self.dev != self.back:
+            import torch
+            torch.cuda.set_device(self.back)
+
+
+def _mx_empty(shape, device, stream):
+    """Memory of the stream that will use it: torch's allocator hands a freed block on within one stream only."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=torch.uint8, device=device)
+
+
+def _mx_check(rc):
+    if rc != POSS_OK:
+        raise PossError(rc, load_library().poss_last_error(None).decode())
+
+
+def mx_quantize(x, codes=None, scales=None, stream=None):
+    """Rows of x (float32, bfloat16, float16) as 4-bit codes with a scale per 32 values.  codes [rows, ceil(cols/32)*16] and scales
+    [rows, ceil(cols/32)], uint8, are allocated if not given.  stream: torch's current one unless given.  Returns (codes, scales)."""
+    p, ld = _mx_rows(x, "x")
+    rows, cols = x.shape
+    nb = (cols + MX_BLOCK - 1) // MX_BLOCK
+    if codes is None:
+        codes = _mx_empty((rows, nb * 16), x.device, stream)
+    if scales is None:
+        scales = _mx_empty((rows, nb), x.device, stream)
+    _mx_blocks(codes, scales, rows, cols, "mx_quantize")
+    with _MxCall(stream, x, codes, scales) as st:
+        _mx_check(load_library().poss_mx_quantize(_mx_dtype(x.dtype), p, ld, rows, cols, codes.data_ptr(), scales.data_ptr(), st))
+    return codes, scales
+
+
+def mx_dequantize(codes, scales, y, stream=None):
+    """What codes and scales stand for, into y [rows, cols] (float32, bfloat16, float16).  Returns y."""
+    p, ld = _mx_rows(y, "y")
+    rows, cols = y.shape
+    _mx_blocks(codes, scales, rows, cols, "mx_dequantize")
+    with _MxCall(stream, y, codes, scales) as st:
+        _mx_check(load_library().poss_mx_dequantize(_mx_dtype(y.dtype), codes.data_ptr(), scales.data_ptr(), rows, cols, p, ld, st))
+    return y
+
+
+class MxWeight:
+    """A weight matrix [N, K] of 4-bit codes in the products' operand order (made by mx_pack)."""
+
+    def __init__(self, packed, N, K):
+        self.packed, self.N, self.K = packed, N, K
+
+
+def mx_pack(codes, scales, K, stream=None):
+    """The weight matrix [N, K] that codes and scales hold, laid out once for mx_gemm and mx_gemm_mx."""
+    lib, N = load_library(), codes.shape[0]
+    _mx_blocks(codes, scales, N, K, "mx_pack")
+    packed = _mx_empty(max(256, lib.poss_mx_packed_bytes(N, K)), codes.device, stream)
+    with _MxCall(stream, codes, scales) as st:
+        _mx_check(lib.poss_mx_pack(codes.data_ptr(), scales.data_ptr(), N, K, packed.data_ptr(), st))
+    return MxWeight(packed, N, K)
+
+
+def mx_gemm_scratch(dtype, M, N, K, device="cuda", stream=None):
+    """Scratch for a product of this shape: dtype of the activations, None for microscaled ones."""
+    need = load_library().poss_mx_gemm_scratch_bytes(_MX if dtype is None else _mx_dtype(dtype), M, N, K)
+    if need == 0:
+        _mx_refuse("shape rejected")
+    return _mx_empty(need, device, stream)
+
+
+def mx_gemm(x, w, y, scratch=None, stream=None):
+    """y [M, N] = x [M, K] . w^T for an MxWeight; x and y float32, bfloat16 or float16.  scratch: a uint8 tensor from mx_gemm_scratch
+    that no other call uses at the same time; allocated per call if not given.  Returns y."""
+    px, ldx = _mx_rows(x, "x")
+    py, ldy = _mx_rows(y, "y")
+    M = x.shape[0]
+    if x.shape[1] != w.K or tuple(y.shape) != (M, w.N):
+        _mx_refuse("mx_gemm: x [M, %d] and y [M, %d] are wanted, got %s and %s" % (w.K, w.N, tuple(x.shape), tuple(y.shape)))
+    if scratch is None:
+        scratch = mx_gemm_scratch(x.dtype, M, w.N, w.K, x.device, stream)
+    with _MxCall(stream, x, y, w.packed, scratch) as st:
+        _mx_check(load_library().poss_mx_gemm(_mx_dtype(x.dtype), px, ldx, w.packed.data_ptr(), _mx_dtype(y.dtype), py, ldy, M, w.N, w.K,
+                                              scratch.data_ptr(), scratch.numel(), st))
+    return y
+
+
+def mx_gemm_mx(codes, scales, w, y, scratch=None, stream=None):
+    """y [M, N] = x . w^T for x [M, K] as mx_quantize left it: both operands in 4 bits.  Returns y."""
+    py, ldy = _mx_rows(y, "y")
+    M = codes.shape[0]
+    _mx_blocks(codes, scales, M, w.K, "mx_gemm_mx")
+    if tuple(y.shape) != (M, w.N):
+        _mx_refuse("mx_gemm_mx: y [%d, %d] is wanted, got %s" % (M, w.N, tuple(y.shape)))
+    if scratch is None:
+        scratch = mx_gemm_scratch(None, M, w.N, w.K, y.device, stream)
+    with _MxCall(stream, y, codes, scales, w.packed, scratch) as st:
+        _mx_check(load_library().poss_mx_gemm_mx(codes.data_ptr(), scales.data_ptr(), w.packed.data_ptr(), _mx_dtype(y.dtype), py, ldy, M, w.N, w.K,
+                                                 scratch.data_ptr(), scratch.numel(), st))
+    return y

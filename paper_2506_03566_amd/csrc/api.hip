@@ -4,6 +4,7 @@
 // sequences; a pass stacks the rows of all of them so that they share the weight streams.
 #include "../../include/poss.h"
 #include "common.h"
+#include "mx.h"
 
 #include <math.h>
 #include <stdarg.h>
@@ -40,6 +41,14 @@ enum { ST_LOADED = 0, ST_READY = 1, ST_VERIFIED = 2 };
 constexpr int PROFILE_EVENTS = 1024;
 
 }  // namespace
+
+int poss::set_error(int code, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_load_error, sizeof g_load_error, fmt, ap);
+    va_end(ap);
+    return code;
+}
 
 // One sequence of the batch: its caches, its tree, its token stream.  Weights and activation
 // buffers are shared; a pass stacks the rows of every sequence into one set of GEMM launches.
