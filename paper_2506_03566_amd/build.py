@@ -7,7 +7,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libposs.so")
-SOURCES = ["gemm.hip", "gemm_block.hip", "elementwise.hip", "attention.hip", "tree.hip", "mx.hip", "api.hip"]
+SOURCES = ["gemm.hip", "gemm_block.hip", "elementwise.hip", "attention.hip", "tree.hip", "mx.hip", "mx_gemm.hip", "api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-result"]

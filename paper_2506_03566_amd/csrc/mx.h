@@ -1,14 +1,37 @@
-// Microscaled 4-bit weights: the packed form and its launches (mx.hip), shared by the entry points.
+// Microscaled 4-bit weights: the packed form, its device pieces and its launches (mx.hip, mx_gemm.hip).
 #pragma once
-#include "common.h"
+#include "device_utils.h"
 
 namespace poss {
+
+typedef float  f32x2 __attribute__((ext_vector_type(2)));
+typedef float  f32x4 __attribute__((ext_vector_type(4)));
+typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16_t  f16x2 __attribute__((ext_vector_type(2)));
+typedef f16_t  f16x8 __attribute__((ext_vector_type(8)));
+typedef int    i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int MX_BLOCK = 32;      // values that share a scale
+constexpr int MX_KSTEP = 128;     // columns of a k-step: a block for each sixteen lanes
 
 // Packed weights as the kernels see them (the layout stands in mx.hip).
 struct MxPacked { const u32x4 *codes; const uint32_t *scales; const int32_t *ref; int ksteps, kgroups, tiles; };
 MxPacked mx_packed_at(const void *packed, int N, int K);
 
+enum { DT_MX = 4 };               // activations that are microscaled too
+size_t mx_gemm_scratch_size(int x_dt, int M, int N, int K);
+void launch_mx_gemm(int x_dt, const void *x, int64_t ldx, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *scratch, hipStream_t st);
+void launch_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *scratch, hipStream_t st);
+
 // Leaves the message that poss_last_error(NULL) returns; the code is handed through.
 int set_error(int code, const char *fmt, ...);
+
+static inline int mx_blocks(int cols) { return (cols + MX_BLOCK - 1) / MX_BLOCK; }
+
+// 2^(b - 127) of a scale byte, exactly (2^-127 is subnormal).
+__device__ __forceinline__ float mx_power(unsigned b) {
+    return __builtin_bit_cast(float, b == 255 ? 0x7fc00000u : b == 0 ? 0x00400000u : b << 23);
+}
 
 }  // namespace poss

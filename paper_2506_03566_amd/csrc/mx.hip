@@ -6,34 +6,15 @@
 //
 // Packed weights (what the products read) are those blocks in operand order of the 16 x 16 x 128 matrix instruction:
 //   codes  [column tile][k-step][lane]  16 bytes: the block of weight row tile * 16 + lane % 16, columns k-step * 128 + lane / 16 * 32 ...
+//          (k-steps of 128, in whole groups of four; zeros beyond the matrix)
 //   scales [column tile][k-step / 4][lane]  4 bytes: the scales of that lane's blocks of four k-steps, relative to the row's largest
 //   ref    [row]  the largest scale byte of the row's blocks that are not all zero; 255 where a block of the row is NaN
 // A wave reads 1 KB of codes per k-step, contiguous along k.  The relative scales let every product form c * 2^(s - ref) in the type
 // that its matrix instruction takes (an fp16 number reaches from 2^-24 to 2^16 only) and apply 2^ref to the float32 sum, exactly.
 #include "../../include/poss.h"
-#include "device_utils.h"
 #include "mx.h"
 
 namespace poss {
-
-typedef float  f32x2 __attribute__((ext_vector_type(2)));
-typedef float  f32x4 __attribute__((ext_vector_type(4)));
-typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
-typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
-typedef f16_t  f16x2 __attribute__((ext_vector_type(2)));
-typedef f16_t  f16x8 __attribute__((ext_vector_type(8)));
-typedef int    i32x8 __attribute__((ext_vector_type(8)));
-
-constexpr int MX_BLOCK = 32;      // values that share a scale
-constexpr int MX_KSTEP = 128;     // columns of a k-step: a block for each sixteen lanes
-constexpr int F16_SHIFT = 13;     // fp16 operands carry 2^13: 6 * 2^13 is finite, and c * 2^(s - ref) exact down to s = ref - 36
-
-static inline int mx_blocks(int cols) { return (cols + MX_BLOCK - 1) / MX_BLOCK; }
-
-// 2^(b - 127) of a scale byte, exactly (2^-127 is subnormal).
-__device__ __forceinline__ float mx_power(unsigned b) {
-    return __builtin_bit_cast(float, b == 255 ? 0x7fc00000u : b == 0 ? 0x00400000u : b << 23);
-}
 
 // ------------------------------------------------------------------------------------------ quantisation
 // Four lanes per block, eight values each; scale byte = exponent field of the block's largest magnitude - 2, at least 0: the largest
@@ -91,7 +72,7 @@ template <typename T> __global__ __launch_bounds__(256) void mx_dequantize_kerne
 }
 
 // ------------------------------------------------------------------------------------------ packing
-static inline int mx_ksteps(int K) { return (K + MX_KSTEP - 1) / MX_KSTEP; }
+static inline int mx_ksteps(int K) { return (K + 4 * MX_KSTEP - 1) / (4 * MX_KSTEP) * 4; }
 static inline int mx_tiles(int N) { return (N + 15) / 16; }
 
 MxPacked mx_packed_at(const void *packed, int N, int K) {
@@ -101,15 +82,15 @@ MxPacked mx_packed_at(const void *packed, int N, int K) {
     w.codes = reinterpret_cast<const u32x4 *>(p);
     p += tiles * ks * 1024;
     w.scales = reinterpret_cast<const uint32_t *>(p);
-    p += tiles * ((ks + 3) / 4) * 256;
+    p += tiles * (ks / 4) * 256;
     w.ref = reinterpret_cast<const int32_t *>(p);
-    w.ksteps = (int)ks; w.kgroups = (int)((ks + 3) / 4); w.tiles = (int)tiles;
+    w.ksteps = (int)ks; w.kgroups = (int)(ks / 4); w.tiles = (int)tiles;
     return w;
 }
 
 static size_t mx_packed_size(int N, int K) {
     const size_t tiles = mx_tiles(N), ks = mx_ksteps(K);
-    return (tiles * ks * 1024 + tiles * ((ks + 3) / 4) * 256 + tiles * 64 + 255) / 256 * 256;
+    return (tiles * ks * 1024 + tiles * (ks / 4) * 256 + tiles * 64 + 255) / 256 * 256;
 }
 
 __device__ __forceinline__ bool mx_all_zero(u32x4 c) { return ((c.x | c.y | c.z | c.w) & 0x77777777u) == 0; }
@@ -133,7 +114,7 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ 
     }
     __syncthreads();
     if (tid < 16) ref[tile * 16 + tid] = top[tid];
-    const int lane = tid & 63, r = lane & 15, n = tile * 16 + r, groups = (ksteps + 3) / 4;
+    const int lane = tid & 63, r = lane & 15, n = tile * 16 + r, groups = ksteps / 4;
     for (int g = tid >> 6; g < groups; g += 4) {
         uint32_t packed = 0;
         for (int i = 0; i < 4; ++i) {
@@ -144,119 +125,11 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ 
                 c = codes[(size_t)n * blocks + b];
                 s = min(127, max(0, scales[(size_t)n * blocks + b] - top[r] + 127));
             }
-            if (ks < ksteps) out[((size_t)tile * ksteps + ks) * 64 + lane] = c;
+            out[((size_t)tile * ksteps + ks) * 64 + lane] = c;
             packed |= (uint32_t)s << (8 * i);
         }
         out_scales[((size_t)tile * groups + g) * 64 + lane] = packed;
     }
-}
-
-// ------------------------------------------------------------------------------------------ products
-// Eight codes (a dword) as operand values c * 2^(s + shift - ref): s in the byte, the power as the scale operand of the conversion.
-template <typename T> struct MxOp;
-template <> struct MxOp<bf16_t> {
-    typedef bf16x8 V;
-    static __device__ __forceinline__ float scale(unsigned s) { return mx_power(s); }
-    static __device__ __forceinline__ V weights(unsigned q, float s) {
-        union { V v; bf16x2 p[4]; } u;
-        u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 0); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 1);
-        u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 2); u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 3);
-        return u.v;
-    }
-    static __device__ __forceinline__ f32x4 mfma(V a, V b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-    static constexpr int SHIFT = 0;
-};
-template <> struct MxOp<f16_t> {
-    typedef f16x8 V;
-    static __device__ __forceinline__ float scale(unsigned s) { return __builtin_bit_cast(float, (s + F16_SHIFT) << 23); }
-    static __device__ __forceinline__ V weights(unsigned q, float s) {
-        union { V v; f16x2 p[4]; } u;
-        u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(q, s, 0); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(q, s, 1);
-        u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(q, s, 2); u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(q, s, 3);
-        return u.v;
-    }
-    static __device__ __forceinline__ f32x4 mfma(V a, V b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-    static constexpr int SHIFT = F16_SHIFT;
-};
-
-// float32 activations enter as the sum of three bf16 numbers, each the leading eight bits of what is left: exact.  Infinities and NaN
-// are the first number alone.
-__device__ __forceinline__ void split3(float x, bf16_t &a, bf16_t &b, bf16_t &c) {
-    const unsigned u = __builtin_bit_cast(unsigned, x);
-    const bool special = (u & 0x7f800000u) == 0x7f800000u;
-    const unsigned top = special && (u & 0x7fffffu) ? (u >> 16) | 0x40u : u >> 16;
-    const float r1 = special ? 0.f : x - __builtin_bit_cast(float, u & 0xffff0000u);
-    const unsigned u1 = __builtin_bit_cast(unsigned, r1);
-    const float r2 = r1 - __builtin_bit_cast(float, u1 & 0xffff0000u);
-    a = __builtin_bit_cast(bf16_t, (uint16_t)top);
-    b = __builtin_bit_cast(bf16_t, (uint16_t)(u1 >> 16));
-    c = (bf16_t)r2;                                       // at most eight bits: no rounding but below 2^-133
-}
-
-// The sum of a column, times 2^ref, to Y; four consecutive columns of one row per lane.
-template <typename Y> __device__ __forceinline__ void mx_store(Y *__restrict__ y, int64_t ldy, int m, int n, int N, f32x4 acc, const int32_t *__restrict__ ref, int shift) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (n + r >= N) break;
-        const int e = ref[n + r];
-        const float v = e == 255 ? __builtin_nanf("") : __builtin_ldexpf(acc[r], e - 127 - shift);
-        y[(int64_t)m * ldy + n + r] = from_f<Y>(v);
-    }
-}
-
-template <typename X> struct MxOperand { typedef X T; static constexpr int PARTS = 1; };
-template <> struct MxOperand<float> { typedef bf16_t T; static constexpr int PARTS = 3; };
-
-// A wave per 16 x 16 tile, the whole K; operands straight from memory, column by column where they are not aligned.
-template <typename X, typename Y>
-__global__ __launch_bounds__(256) void mx_gemm_simple_kernel(MxPacked w, const X *__restrict__ x, int64_t ldx, Y *__restrict__ y, int64_t ldy, int M, int N, int K) {
-    typedef typename MxOperand<X>::T T;
-    typedef MxOp<T> Op;
-    constexpr int PARTS = MxOperand<X>::PARTS;
-    const int lane = threadIdx.x & 63, ct = blockIdx.x * 4 + (threadIdx.x >> 6), m0 = blockIdx.y * 16;
-    if (ct >= w.tiles) return;
-    const int m = m0 + (lane & 15);
-    const X *row = x + (int64_t)min(m, M - 1) * ldx;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int ks = 0; ks < w.ksteps; ++ks) {
-        const u32x4 c = w.codes[((size_t)ct * w.ksteps + ks) * 64 + lane];
-        const float s = Op::scale((w.scales[((size_t)ct * w.kgroups + (ks >> 2)) * 64 + lane] >> (8 * (ks & 3))) & 255);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k0 = ks * MX_KSTEP + (lane >> 4) * 32 + i * 8;
-            typename Op::V v[PARTS];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const X e = k0 + j < K ? row[k0 + j] : from_f<X>(0.f);
-                if constexpr (PARTS == 1) v[0][j] = e;
-                else { bf16_t a, b, d; split3(e, a, b, d); v[0][j] = a; v[1][j] = b; v[2][j] = d; }
-            }
-            const typename Op::V wv = Op::weights(c[i], s);
-#pragma unroll
-            for (int p = PARTS - 1; p >= 0; --p) acc = Op::mfma(wv, v[p], acc);
-        }
-    }
-    if (m < M) mx_store<Y>(y, ldy, m, ct * 16 + (lane >> 4) * 4, N, acc, w.ref, Op::SHIFT);
-}
-
-template <typename Y>
-__global__ __launch_bounds__(256) void mx_both_simple_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint8_t *__restrict__ xs, int blocks, Y *__restrict__ y, int64_t ldy, int M, int N) {
-    const int lane = threadIdx.x & 63, ct = blockIdx.x * 4 + (threadIdx.x >> 6), m0 = blockIdx.y * 16;
-    if (ct >= w.tiles) return;
-    const int m = m0 + (lane & 15), g = lane >> 4;
-    const size_t row = (size_t)min(m, M - 1) * blocks;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int ks = 0; ks < w.ksteps; ++ks) {
-        const u32x4 c = w.codes[((size_t)ct * w.ksteps + ks) * 64 + lane];
-        const int s = (w.scales[((size_t)ct * w.kgroups + (ks >> 2)) * 64 + lane] >> (8 * (ks & 3))) & 255;
-        const int b = ks * 4 + g;
-        u32x4 q = {0u, 0u, 0u, 0u};
-        int t = 127;
-        if (b < blocks) { q = x[row + b]; t = xs[row + b]; }
-        const i32x8 wa = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}, xb = {(int)q.x, (int)q.y, (int)q.z, (int)q.w, 0, 0, 0, 0};
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xb, acc, 4, 4, 0, s, 0, t);
-    }
-    if (m < M) mx_store<Y>(y, ldy, m, ct * 16 + g * 4, N, acc, w.ref, 0);
 }
 
 // ------------------------------------------------------------------------------------------ launches
@@ -286,34 +159,6 @@ void launch_mx_pack(const void *codes, const void *scales, int N, int K, void *p
                                             const_cast<u32x4 *>(w.codes), const_cast<uint32_t *>(w.scales), const_cast<int32_t *>(w.ref));
 }
 
-template <typename X, typename Y>
-static void launch_gemm_xy(const MxPacked &w, const void *x, int64_t ldx, void *y, int64_t ldy, int M, int N, int K, hipStream_t st) {
-    mx_gemm_simple_kernel<X, Y><<<dim3((w.tiles + 3) / 4, (M + 15) / 16), 256, 0, st>>>(w, static_cast<const X *>(x), ldx, static_cast<Y *>(y), ldy, M, N, K);
-}
-template <typename X>
-static void launch_gemm_x(const MxPacked &w, const void *x, int64_t ldx, int y_dt, void *y, int64_t ldy, int M, int N, int K, hipStream_t st) {
-    if (y_dt == DT_F32) launch_gemm_xy<X, float>(w, x, ldx, y, ldy, M, N, K, st);
-    else if (y_dt == DT_BF16) launch_gemm_xy<X, bf16_t>(w, x, ldx, y, ldy, M, N, K, st);
-    else launch_gemm_xy<X, f16_t>(w, x, ldx, y, ldy, M, N, K, st);
-}
-
-void launch_mx_gemm(int x_dt, const void *x, int64_t ldx, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *, hipStream_t st) {
-    const MxPacked w = mx_packed_at(packed, N, K);
-    if (x_dt == DT_F32) launch_gemm_x<float>(w, x, ldx, y_dt, y, ldy, M, N, K, st);
-    else if (x_dt == DT_BF16) launch_gemm_x<bf16_t>(w, x, ldx, y_dt, y, ldy, M, N, K, st);
-    else launch_gemm_x<f16_t>(w, x, ldx, y_dt, y, ldy, M, N, K, st);
-}
-
-void launch_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *, hipStream_t st) {
-    const MxPacked w = mx_packed_at(packed, N, K);
-    const dim3 grid((w.tiles + 3) / 4, (M + 15) / 16);
-    const u32x4 *q = static_cast<const u32x4 *>(x_codes); const uint8_t *s = static_cast<const uint8_t *>(x_scales);
-    const int nb = mx_blocks(K);
-    if (y_dt == DT_F32) mx_both_simple_kernel<float><<<grid, 256, 0, st>>>(w, q, s, nb, static_cast<float *>(y), ldy, M, N);
-    else if (y_dt == DT_BF16) mx_both_simple_kernel<bf16_t><<<grid, 256, 0, st>>>(w, q, s, nb, static_cast<bf16_t *>(y), ldy, M, N);
-    else mx_both_simple_kernel<f16_t><<<grid, 256, 0, st>>>(w, q, s, nb, static_cast<f16_t *>(y), ldy, M, N);
-}
-
 }  // namespace poss
 
 // ------------------------------------------------------------------------------------------ C entry points (include/poss.h)
@@ -326,7 +171,6 @@ int launched(const char *who) {
     return e == hipSuccess ? POSS_OK : set_error(POSS_E_HIP, "%s: %s", who, hipGetErrorString(e));
 }
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-size_t mx_scratch(int x_dtype, int M, int N, int K) { (void)x_dtype; (void)M; (void)N; (void)K; return 256; }
 // what both products check
 int check_product(const char *who, const void *packed, const void *y, int32_t y_dtype, int64_t ldy, int32_t M, int32_t N, int32_t K, const void *scratch, size_t scratch_bytes, size_t need) {
     if (M < 0 || N < 1 || K < 1 || ldy < N || bad_dtype(y_dtype)) return set_error(POSS_E_INVALID_ARG, "%s: bad shape or type", who);
@@ -372,13 +216,13 @@ int poss_mx_pack(const void *codes, const void *scales, int32_t N, int32_t K, vo
 
 size_t poss_mx_gemm_scratch_bytes(int32_t x_dtype, int32_t M, int32_t N, int32_t K) {
     if ((bad_dtype(x_dtype) && x_dtype != POSS_MX) || M < 0 || N < 1 || K < 1) return 0;
-    return mx_scratch(x_dtype, M, N, K);
+    return mx_gemm_scratch_size(x_dtype, M, N, K);
 }
 
 int poss_mx_gemm(int32_t x_dtype, const void *x, int64_t ldx, const void *packed, int32_t y_dtype, void *y, int64_t ldy, int32_t M, int32_t N, int32_t K,
                  void *scratch, size_t scratch_bytes, void *hip_stream) {
     if (bad_dtype(x_dtype) || ldx < K) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm: bad shape or type");
-    const int rc = check_product("poss_mx_gemm", packed, y, y_dtype, ldy, M, N, K, scratch, scratch_bytes, M > 0 && N > 0 && K > 0 ? mx_scratch(x_dtype, M, N, K) : 0);
+    const int rc = check_product("poss_mx_gemm", packed, y, y_dtype, ldy, M, N, K, scratch, scratch_bytes, M > 0 && N > 0 && K > 0 ? mx_gemm_scratch_size(x_dtype, M, N, K) : 0);
     if (rc != POSS_OK || M == 0) return rc;
     if (!x) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm: null argument");
     if (reinterpret_cast<uintptr_t>(x) % dtype_size(x_dtype)) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm: x is not aligned to its type");
@@ -388,7 +232,7 @@ int poss_mx_gemm(int32_t x_dtype, const void *x, int64_t ldx, const void *packed
 
 int poss_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *packed, int32_t y_dtype, void *y, int64_t ldy, int32_t M, int32_t N, int32_t K,
                     void *scratch, size_t scratch_bytes, void *hip_stream) {
-    const int rc = check_product("poss_mx_gemm_mx", packed, y, y_dtype, ldy, M, N, K, scratch, scratch_bytes, M > 0 && N > 0 && K > 0 ? mx_scratch(POSS_MX, M, N, K) : 0);
+    const int rc = check_product("poss_mx_gemm_mx", packed, y, y_dtype, ldy, M, N, K, scratch, scratch_bytes, M > 0 && N > 0 && K > 0 ? mx_gemm_scratch_size(POSS_MX, M, N, K) : 0);
     if (rc != POSS_OK || M == 0) return rc;
     if (!x_codes || !x_scales) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm_mx: null argument");
     if (!aligned16(x_codes)) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm_mx: x_codes must be aligned to 16 bytes");
