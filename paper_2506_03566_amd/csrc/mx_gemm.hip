@@ -63,6 +63,7 @@ template <typename Y> __device__ __forceinline__ void mx_store(Y *__restrict__ y
 
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
+template <int I> struct Num { static constexpr int value = I; };
 
 // X as the 16-bit kernels read it: rows of 16-byte pieces.  PARTS > 1: the parts lie `part` values apart.
 struct MxRows { const void *x; int64_t ldx, part; int K; };
@@ -83,7 +84,7 @@ __device__ __forceinline__ void split3(float x, bf16_t &a, bf16_t &b, bf16_t &c)
 }
 
 // X whose rows cannot be read in 16-byte pieces (odd lengths, distances or addresses), and float32 X: a copy in rows of Kp values,
-// zeros beyond K; of float32 the three parts, a matrix each.
+// zeros beyond K; of float32 the three parts, one after the other.
 template <typename X> __global__ __launch_bounds__(256) void mx_stage_kernel(const X *__restrict__ x, int64_t ldx, int M, int K, int Kp, u32x4 *__restrict__ out) {
     const int k0 = (blockIdx.x * 256 + threadIdx.x) * 8;
     if (k0 >= Kp) return;
@@ -92,7 +93,7 @@ template <typename X> __global__ __launch_bounds__(256) void mx_stage_kernel(con
         X v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = k0 + j < K ? row[k0 + j] : from_f<X>(0.f);
-        u32x4 *dst = out + ((int64_t)m * Kp + k0) / 8;
+        u32x4 *dst = out + ((int64_t)m * Kp * (sizeof(X) == 2 ? 1 : 3) + k0) / 8;
         if constexpr (sizeof(X) == 2) {
             union { X e[8]; u32x4 u; } o;
 #pragma unroll
@@ -102,8 +103,7 @@ template <typename X> __global__ __launch_bounds__(256) void mx_stage_kernel(con
             union { bf16_t e[8]; u32x4 u; } a, b, c;
 #pragma unroll
             for (int j = 0; j < 8; ++j) split3(v[j], a.e[j], b.e[j], c.e[j]);
-            const int64_t part = (int64_t)M * Kp / 8;
-            dst[0] = a.u; dst[part] = b.u; dst[2 * part] = c.u;
+            dst[0] = a.u; dst[Kp / 8] = b.u; dst[Kp / 4] = c.u;
         }
     }
 }
@@ -113,12 +113,11 @@ template <typename X> __global__ __launch_bounds__(256) void mx_stage_kernel(con
 // k-steps; each wave reads its weights (1 KB per tile and k-step, contiguous) and its part of X (from the L2) straight into
 // operand registers, the next group's on the way while this one is multiplied, and the waves' sums are added in LDS, in wave order.
 // No planes, no second launch.
-constexpr int mx_waves_max(int mt, int nt) { return 64 / (mt * nt) < 16 ? 64 / (mt * nt) : 16; }   // the waves' sums stay within 64 KB of LDS
-
-template <typename T, typename Y, int MT, int NT, int PARTS>
-__global__ __launch_bounds__(mx_waves_max(MT, NT) * 64) void mx_stream_kernel(MxPacked w, MxRows x, Y *__restrict__ y, int64_t ldy, bool quads, int M, int N) {
+template <typename T, typename Y, int PARTS>
+__global__ __launch_bounds__(1024) void mx_stream_kernel(MxPacked w, MxRows x, Y *__restrict__ y, int64_t ldy, bool quads, int M, int N) {
     extern __shared__ f32x4 red[];
     typedef MxOp<T> Op;
+    constexpr int MT = 1, NT = 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int ct0 = blockIdx.x * NT, g0 = wave * w.kgroups / waves, g1 = (wave + 1) * w.kgroups / waves;
     f32x4 acc[MT][NT];
@@ -209,10 +208,11 @@ __global__ __launch_bounds__(mx_waves_max(MT, NT) * 64) void mx_stream_kernel(Mx
 }
 
 // The same with microscaled X: a block of 16 bytes and its scale per lane, row tile and k-step.
-template <typename Y, int MT, int NT>
-__global__ __launch_bounds__(mx_waves_max(MT, NT) * 64) void mx_stream_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint8_t *__restrict__ xs, int blocks, Y *__restrict__ y, int64_t ldy,
+template <typename Y>
+__global__ __launch_bounds__(1024) void mx_stream_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint8_t *__restrict__ xs, int blocks, Y *__restrict__ y, int64_t ldy,
                                                               bool quads, int M, int N) {
     extern __shared__ f32x4 red[];
+    constexpr int MT = 1, NT = 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int ct0 = blockIdx.x * NT, g0 = wave * w.kgroups / waves, g1 = (wave + 1) * w.kgroups / waves;
     f32x4 acc[MT][NT];
@@ -296,100 +296,749 @@ __global__ __launch_bounds__(mx_waves_max(MT, NT) * 64) void mx_stream_both_kern
     }
 }
 
-// ------------------------------------------------------------------------------------------ launches
-constexpr int MX_STREAM_ROWS = 64;
+// ------------------------------------------------------------------------------------------ many rows
+// A workgroup owns TM rows x TN columns and all of K or a part of it (whose sums go to a plane).  X goes from memory straight into LDS,
+// one k-step of 128 per stage, two stages; the codes of a wave's own columns go into its registers (the weights of a k-step are a
+// quarter of X's bytes, and LDS reads are what a tile has least of) and are converted there, one k-step ahead.  A k-step is four
+// substeps of one matrix instruction per 16 x 16 tile; while a wave multiplies a substep it converts the next one's weights and reads
+// X's operands a few tiles ahead from LDS.  One barrier per k-step, where those reads pass into the next stage: that has landed by then,
+// and every operand of this one has been read, so that its place can be asked for again.
+struct MxGeom {
+    int M, N, steps;              // k-steps of the product: float32 X is three times as long (its parts one after the other)
+    int full;                     // k-steps that lie inside X's rows as a whole
+    int tiles_m, tiles_n, splits;
+};
 
-template <typename T, typename Y, int MT, int NT, int PARTS>
-static void launch_stream_c(const MxPacked &w, const MxRows &x, void *y, int64_t ldy, bool quads, int M, int N, int waves, hipStream_t st) {
-    if (waves > mx_waves_max(MT, NT)) waves = mx_waves_max(MT, NT);
-    mx_stream_kernel<T, Y, MT, NT, PARTS><<<(w.tiles + NT - 1) / NT, waves * 64, waves * MT * NT * 1024, st>>>(w, x, static_cast<Y *>(y), ldy, quads, M, N);
+// Workgroup -> tile: consecutive ids go to the 8 XCDs in turn; an XCD is given a contiguous run of tiles, ordered so that those it works
+// on at a time share rows and columns in its L2.
+__device__ __forceinline__ void mx_tile_of(const MxGeom &g, int gm_rows, int &tm, int &tn) {
+    const int n = g.tiles_m * g.tiles_n, bid = blockIdx.x, q = n >> 3, r = n & 7, x = bid & 7;
+    const int id = x * q + (x < r ? x : r) + (bid >> 3);
+    const int grp = id / (gm_rows * g.tiles_n), in_grp = id - grp * (gm_rows * g.tiles_n), gm = min(gm_rows, g.tiles_m - grp * gm_rows);
+    tm = grp * gm_rows + in_grp % gm;
+    tn = in_grp / gm;
 }
-template <typename T, typename Y, int PARTS>
-static void launch_stream(const MxPacked &w, const MxRows &x, void *y, int64_t ldy, bool quads, int M, int N, int nt, int waves, hipStream_t st) {
-    const int mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-#define POSS_MX(MT, NT) return launch_stream_c<T, Y, MT, NT, PARTS>(w, x, y, ldy, quads, M, N, waves, st)
-    if (mt == 1) { if (nt == 1) POSS_MX(1, 1); if (nt == 2) POSS_MX(1, 2); POSS_MX(1, 4); }
-    if constexpr (PARTS == 3) { if (nt == 1) POSS_MX(2, 1); POSS_MX(2, 2); }
-    else {
-        if (mt == 2) { if (nt == 1) POSS_MX(2, 1); if (nt == 2) POSS_MX(2, 2); POSS_MX(2, 4); }
-        if (nt == 1) POSS_MX(4, 1); if (nt == 2) POSS_MX(4, 2); POSS_MX(4, 4);
+
+// A wave's tiles to Y, or to this split's plane.  D tile: lane -> row lane % 16, register r -> column 4 (lane / 16) + r.
+template <typename T, typename Y, int MTW, int NTW, bool SPLIT>
+__device__ __forceinline__ void mx_tile_store(const f32x4 (&acc)[MTW][NTW], int row0, int ct0, const MxGeom &g, const MxPacked &w, Y *__restrict__ y, int64_t ldy, bool quads) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int mt = 0; mt < MTW; ++mt) {
+        const int m = row0 + mt * 16 + (lane & 15);
+        if (m >= g.M) continue;
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) {
+            const int col = (ct0 + nt) * 16 + (lane >> 4) * 4;
+            if (col >= g.N) continue;
+            if constexpr (SPLIT) *reinterpret_cast<f32x4 *>(y + ((size_t)blockIdx.y * g.M + m) * (w.tiles * 16) + col) = acc[mt][nt];
+            else mx_store<Y>(y, ldy, quads, m, col, g.N, acc[mt][nt], w.ref, MxOp<T>::SHIFT);
+        }
     }
-#undef POSS_MX
-}
-template <typename Y>
-static void launch_stream_both(const MxPacked &w, const void *x, const void *xs, int blocks, void *y, int64_t ldy, bool quads, int M, int N, int nt, int waves, hipStream_t st) {
-    const int mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    if (waves > mx_waves_max(mt, nt)) waves = mx_waves_max(mt, nt);
-#define POSS_MX(MT, NT) return mx_stream_both_kernel<Y, MT, NT><<<(w.tiles + NT - 1) / NT, waves * 64, waves * MT * NT * 1024, st>>>( \
-        w, static_cast<const u32x4 *>(x), static_cast<const uint8_t *>(xs), blocks, static_cast<Y *>(y), ldy, quads, M, N)
-    if (mt == 1) { if (nt == 1) POSS_MX(1, 1); if (nt == 2) POSS_MX(1, 2); POSS_MX(1, 4); }
-    if (mt == 2) { if (nt == 1) POSS_MX(2, 1); if (nt == 2) POSS_MX(2, 2); POSS_MX(2, 4); }
-    if (nt == 1) POSS_MX(4, 1); if (nt == 2) POSS_MX(4, 2); POSS_MX(4, 4);
-#undef POSS_MX
 }
 
-struct StreamShape { int nt, waves; };
-static StreamShape stream_shape(int, int, int) { return StreamShape{1, 8}; }
+template <typename T, typename Y, int TM, int TN, int WM, int WN, bool SPLIT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, MxRows x, MxGeom g, Y *__restrict__ y, int64_t ldy, bool quads) {
+    typedef __attribute__((address_space(3))) void *LdsPtr;
+    typedef MxOp<T> Op;
+    constexpr int WAVES = WM * WN, MTW = TM / (16 * WM), NTW = TN / (16 * WN), UNITS = TM / 16 * 4, UPW = UNITS / WAVES;   // 1 KB units: 16 rows x 64 bytes
+    static_assert(UPW * WAVES == UNITS && MTW >= 1 && NTW >= 1, "tile shape");
+    __shared__ __attribute__((aligned(1024))) u32x4 xs[2 * UNITS * 64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % WM, wn = wave / WM;
+    int tm, tn;
+    mx_tile_of(g, TM >= 256 ? 8 : 16, tm, tn);
+    const int m0 = tm * TM, ct0 = tn * (TN / 16) + wn * NTW;
+    const int s0 = (int)((int64_t)blockIdx.y * g.steps / g.splits), n = (int)((int64_t)(blockIdx.y + 1) * g.steps / g.splits) - s0;
+
+    // Unit u of a stage: rows 16 (u / 4).., columns 32 (u % 4).. of the k-step, four lanes per row; piece p (eight columns) of row r lies at
+    // position p ^ (r / 4 % 4), so that sixteen lanes that read the same piece of sixteen rows meet every bank once.
+    const int x_piece = (lane & 3) ^ ((lane >> 4) & 3);
+    const T *x_base = static_cast<const T *>(x.x) + (int64_t)m0 * x.ldx;
+    const unsigned lds0 = (unsigned)(uintptr_t)(LdsPtr)&xs[0];
+    auto issue_one = [&](int j, int s, int st) {          // unit j (static) of this wave's share of k-step s, into stage st
+        const int u = wave + WAVES * j, m = min((u >> 2) * 16 + (lane >> 2), g.M - 1 - m0);
+        const unsigned dst = lds0 + (unsigned)((st * UNITS + u) * 1024);
+        const int k = (u & 3) * MX_BLOCK + x_piece * 8;
+        const unsigned off = ((unsigned)m * (unsigned)x.ldx + (unsigned)k) * 2u;     // (TM rows are below 4 GiB: checked on the host)
+        const T *src = x_base + (int64_t)s * MX_KSTEP;
+        if (s < g.full) lds_dma16_s(dst, src, off);
+        else {
+            const char *p = reinterpret_cast<const char *>(src) + off;
+            lds_dma16(dst, s * MX_KSTEP + k < x.K ? static_cast<const void *>(p) : static_cast<const void *>(&mx_zero_piece));
+        }
+    };
+    int ws = s0 % w.ksteps;                               // k-step of the weights: the next one to load
+    const u32x4 *wp[NTW];
+    const uint32_t *sp[NTW];
+#pragma unroll
+    for (int nt = 0; nt < NTW; ++nt) {
+        const int ct = min(ct0 + nt, w.tiles - 1);        // tiles beyond the matrix repeat the last one (never stored)
+        wp[nt] = w.codes + (size_t)ct * w.ksteps * 64;
+        sp[nt] = w.scales + (size_t)ct * w.kgroups * 64;
+    }
+    auto load_w = [&](u32x4 (&c)[NTW], unsigned (&f)[NTW]) {
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) {
+            c[nt] = wp[nt][ws * 64 + lane];
+            f[nt] = (sp[nt][(ws >> 2) * 64 + lane] >> (8 * (ws & 3)) & 255u) + Op::SHIFT << 23;
+        }
+        ws = ws + 1 == w.ksteps ? 0 : ws + 1;
+    };
+    f32x4 acc[MTW][NTW];
+#pragma unroll
+    for (int mt = 0; mt < MTW; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // A k-step is 4 MTW slots, one row tile of one substep each.  Operands of X are read AHEAD slots ahead, into a ring of four.
+    constexpr int SLOTS = 4 * MTW, AHEAD = 3;
+    u32x4 c[NTW], cn[NTW], xf[4], wf[2][NTW];
+    unsigned f[NTW], fn[NTW];
+#pragma unroll
+    for (int j = 0; j < UPW; ++j) issue_one(j, s0, 0);
+    load_w(c, f);
+    dma_wait<0>();
+    __syncthreads();
+    const int rd = (wm * MTW * 4 + (lane >> 4)) * 64 + (lane & 15) * 4, rs = (lane >> 2) & 3;      // + 256 per row tile, piece i at i ^ rs
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) xf[q] = xs[rd + (q % MTW) * 256 + ((q / MTW) ^ rs)];
+#pragma unroll
+    for (int nt = 0; nt < NTW; ++nt) wf[0][nt] = Op::weights(c[nt][0], __builtin_bit_cast(float, f[nt]));
+
+    for (int s = 0; s < n; ++s) {
+        const u32x4 *cur = xs + (s & 1) * UNITS * 64, *nxt = xs + (~s & 1) * UNITS * 64;
+        const bool more = s + 1 < n;
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q) {
+            const int i = q / MTW, mt = q % MTW;
+            if (q == SLOTS - AHEAD) {                     // (nobody reads this stage any more, and the next one has landed)
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                __syncthreads();
+            }
+            if (more && q == 0) load_w(cn, fn);
+            if (more && q < MTW)
+#pragma unroll
+                for (int j = mt; j < UPW; j += MTW) issue_one(j, s0 + s + 1, ~s & 1);
+            const int qa = (q + AHEAD) % SLOTS;
+            xf[(q + AHEAD) & 3] = (q + AHEAD >= SLOTS ? nxt : cur)[rd + (qa % MTW) * 256 + ((qa / MTW) ^ rs)];
+#pragma unroll
+            for (int nt = mt; nt < NTW; nt += MTW)
+                wf[(i + 1) & 1][nt] = i == 3 ? Op::weights(cn[nt][0], __builtin_bit_cast(float, fn[nt])) : Op::weights(c[nt][(i + 1) & 3], __builtin_bit_cast(float, f[nt]));
+#pragma unroll
+            for (int nt = 0; nt < NTW; ++nt) acc[mt][nt] = Op::mfma(wf[i & 1][nt], xf[q & 3], acc[mt][nt]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) { c[nt] = cn[nt]; f[nt] = fn[nt]; }
+    }
+    mx_tile_store<T, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
+}
+
+// ------------------------------------------------------------------------------------------ tens of rows
+// Up to some hundred rows: what bounds a product is how fast a CU draws weights and X through its L1 together (some 45 GB/s measured, whatever
+// the shape of a load), and what comes between: a wave that waits for X cannot ask for weights.  So FW waves of a workgroup do nothing but
+// fetch X into LDS, a group of four k-steps (KS k-steps) a stage, two stages; the others keep the codes of their own columns four k-steps
+// ahead in registers, and multiply.  One barrier per stage, where reads pass into the next one, as in mx_tile_kernel.
+template <typename T, typename Y, int TM, int TN, int WM, int WN, int FW, int KS, bool SPLIT>
+__global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w, MxRows x, MxGeom g, Y *__restrict__ y, int64_t ldy, bool quads) {
+    typedef __attribute__((address_space(3))) void *LdsPtr;
+    typedef MxOp<T> Op;
+    constexpr int WAVES = WM * WN, MTW = TM / (16 * WM), NTW = TN / (16 * WN), UNITS = TM / 4 * KS, UPW = UNITS / FW;     // 1 KB units of a stage
+    constexpr int STAGES = 4 / KS, SLOTS = 4 * MTW * KS, AHEAD = 3;
+    static_assert(UPW * FW == UNITS && STAGES * KS == 4 && SLOTS > AHEAD, "tile shape");
+    __shared__ __attribute__((aligned(1024))) u32x4 xs[2 * UNITS * 64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    int tm, tn;
+    mx_tile_of(g, 16, tm, tn);
+    const int m0 = tm * TM;
+    // groups of four k-steps
+    const int n_groups = (g.steps + 3) >> 2, g0 = (int)((int64_t)blockIdx.y * n_groups / g.splits), n = (int)((int64_t)(blockIdx.y + 1) * n_groups / g.splits) - g0;
+    const int stages = n * STAGES;
+
+    if (wave >= WAVES) {                                  // a wave that fetches
+        const int fw = wave - WAVES, x_piece = (lane & 3) ^ ((lane >> 4) & 3);
+        const unsigned lds0 = (unsigned)(uintptr_t)(LdsPtr)&xs[0];
+        const T *src = static_cast<const T *>(x.x) + (int64_t)m0 * x.ldx + (int64_t)g0 * 4 * MX_KSTEP;
+        auto issue = [&](int t) {                         // stage t
+            const int k0 = g0 * 4 * MX_KSTEP + t * KS * MX_KSTEP;
+            const bool whole = k0 + KS * MX_KSTEP <= g.full * MX_KSTEP;
+#pragma unroll
+            for (int j = 0; j < UPW; ++j) {
+                const int u = fw + FW * j, m = min(u / (4 * KS) * 16 + (lane >> 2), g.M - 1 - m0), k = (u % (4 * KS)) * MX_BLOCK + x_piece * 8;
+                const unsigned off = ((unsigned)m * (unsigned)x.ldx + (unsigned)k) * 2u, dst = lds0 + (unsigned)(((t & 1) * UNITS + u) * 1024);
+                if (whole) lds_dma16_s(dst, src + (int64_t)t * KS * MX_KSTEP, off);
+                else {
+                    const char *p = reinterpret_cast<const char *>(src + (int64_t)t * KS * MX_KSTEP) + off;
+                    lds_dma16(dst, k0 + k < x.K ? static_cast<const void *>(p) : static_cast<const void *>(&mx_zero_piece));
+                }
+            }
+        };
+        issue(0);
+        for (int t = 0; t < stages; ++t) {
+            dma_wait<0>();
+            __syncthreads();                              // stage t has landed; nobody reads stage t - 1 any more
+            if (t + 1 < stages) issue(t + 1);
+        }
+        return;
+    }
+    const int wm = wave % WM, wn = wave / WM, ct0 = tn * (TN / 16) + wn * NTW;
+    const u32x4 *wp[NTW];
+    const uint32_t *sp[NTW];
+#pragma unroll
+    for (int nt = 0; nt < NTW; ++nt) {
+        const int ct = min(ct0 + nt, w.tiles - 1);        // tiles beyond the matrix repeat the last one (never stored)
+        wp[nt] = w.codes + (size_t)ct * w.ksteps * 64 + lane;
+        sp[nt] = w.scales + (size_t)ct * w.kgroups * 64 + lane;
+    }
+    int wg = g0 % w.kgroups;                              // group of the weights (float32 X passes over them three times)
+    f32x4 acc[MTW][NTW];
+#pragma unroll
+    for (int mt = 0; mt < MTW; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    u32x4 c[4][NTW], xf[4], wf[2][NTW];
+    unsigned sc[NTW], sn[NTW];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) c[s][nt] = wp[nt][(wg * 4 + s) * 64];
+#pragma unroll
+    for (int nt = 0; nt < NTW; ++nt) sc[nt] = sp[nt][wg * 64];
+    // X: + (4 KS) * 64 per row tile, block b of a stage at b * 64, piece i at i ^ rs
+    const int rd = (wm * MTW * 4 * KS + (lane >> 4)) * 64 + (lane & 15) * 4, rs = (lane >> 2) & 3;
+    auto x_at = [&](int q) { const int ks = q / (4 * MTW), i = q / MTW & 3, mt = q % MTW; return rd + (mt * 4 * KS + ks * 4) * 64 + (i ^ rs); };
+    auto scale = [&](int s, unsigned four) { return s == 0 ? mx_scale<T, 0>(four) : s == 1 ? mx_scale<T, 1>(four) : s == 2 ? mx_scale<T, 2>(four) : mx_scale<T, 3>(four); };
+    __syncthreads();
+    int st = 0;
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) xf[q] = xs[x_at(q)];
+#pragma unroll
+    for (int nt = 0; nt < NTW; ++nt) wf[0][nt] = Op::weights(c[0][nt][0], scale(0, sc[nt]));
+    auto group = [&](auto more_, bool last) {
+        constexpr bool more = decltype(more_)::value;
+        const int wn_ = wg + 1 == w.kgroups ? 0 : wg + 1;
+        if constexpr (more)
+#pragma unroll
+            for (int nt = 0; nt < NTW; ++nt) sn[nt] = sp[nt][wn_ * 64];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int ks = s % KS;
+            const u32x4 *cur = xs + st * UNITS * 64, *nxt = xs + (st ^ 1) * UNITS * 64;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int mt = 0; mt < MTW; ++mt) {
+                    const int q = (ks * 4 + i) * MTW + mt;
+                    if (q == SLOTS - AHEAD && (more || s < 3)) {
+                        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                        __syncthreads();
+                    }
+                    xf[(q + AHEAD) & 3] = q + AHEAD >= SLOTS ? nxt[x_at(q + AHEAD - SLOTS)] : cur[x_at(q + AHEAD)];
+#pragma unroll
+                    for (int nt = mt; nt < NTW; nt += MTW) {
+                        // the next substep's weights
+                        if (i < 3) wf[(i + 1) & 1][nt] = Op::weights(c[s][nt][(i + 1) & 3], scale(s, sc[nt]));
+                        else if (s < 3) wf[0][nt] = Op::weights(c[(s + 1) & 3][nt][0], scale(s + 1, sc[nt]));
+                        else if constexpr (more) wf[0][nt] = Op::weights(c[0][nt][0], scale(0, sn[nt]));
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NTW; ++nt) acc[mt][nt] = Op::mfma(wf[i & 1][nt], xf[q & 3], acc[mt][nt]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (i == 2)                                // all of these codes are converted: the next group's on their way
+                    if constexpr (more)
+#pragma unroll
+                        for (int nt = 0; nt < NTW; ++nt) c[s][nt] = wp[nt][(wn_ * 4 + s) * 64];
+            }
+            if (ks == KS - 1) st ^= 1;
+        }
+        wg = wn_;
+        if constexpr (more)
+#pragma unroll
+            for (int nt = 0; nt < NTW; ++nt) sc[nt] = sn[nt];
+    };
+    for (int s = 0; s + 1 < n; ++s) group(Yes{}, false);
+    group(No{}, true);
+    mx_tile_store<T, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
+}
+
+__device__ __forceinline__ void lds_dma4_s(unsigned lds_base, const void *g, unsigned off) {     // 4 bytes a lane (device_utils.h has 16)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_base), "v"(off), "s"(g) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------ both operands in 4 bits, tens of rows
+// mx_fed_kernel for microscaled X: a lane's block of 16 bytes is an operand as it is, so a stage is codes (a 1 KB unit per row tile and
+// k-step, in operand order) and, for each row tile and group, the scales of a lane's four blocks in one word, which the fetching waves
+// put together from the rows' bytes.  KG groups of four k-steps a stage.
+template <typename Y, int TM, int TN, int WM, int WN, int FW, int KG, bool SPLIT>
+__global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint8_t *__restrict__ xs_, int blocks, MxGeom g, Y *__restrict__ y,
+                                                                          int64_t ldy, bool quads) {
+    typedef __attribute__((address_space(3))) void *LdsPtr;
+    constexpr int WAVES = WM * WN, MTW = TM / (16 * WM), NTW = TN / (16 * WN), RT = TM / 16, UNITS = RT * 4 * KG;
+    constexpr int STAGE = UNITS * 64 + RT * KG * 16, SLOTS = 4 * KG * MTW, AHEAD = 3;      // (16 bytes each: codes, then scales)
+    constexpr int UPW = (UNITS + FW - 1) / FW, SPW = (RT * KG + FW - 1) / FW;
+    static_assert(SLOTS > AHEAD, "tile shape");
+    __shared__ __attribute__((aligned(1024))) u32x4 xs[2 * STAGE];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    int tm, tn;
+    mx_tile_of(g, 16, tm, tn);
+    const int m0 = tm * TM;
+    const int n_groups = w.kgroups, g0 = (int)((int64_t)blockIdx.y * n_groups / g.splits), n = (int)((int64_t)(blockIdx.y + 1) * n_groups / g.splits) - g0;
+    const int stages = (n + KG - 1) / KG;
+
+    if (wave >= WAVES) {
+        const int fw = wave - WAVES;
+        const unsigned lds0 = (unsigned)(uintptr_t)(LdsPtr)&xs[0];
+        unsigned sc[SPW];
+        auto issue = [&](int t) {
+            const int b0 = (g0 + t * KG) * 16;            // first block of the stage
+#pragma unroll
+            for (int j = 0; j < UPW; ++j) {
+                const int u = fw + FW * j;
+                if (UPW * FW != UNITS && u >= UNITS) break;
+                const int m = min(m0 + u / (4 * KG) * 16 + (lane & 15), g.M - 1), b = b0 + u % (4 * KG) * 4 + (lane >> 4);
+                lds_dma16(lds0 + (unsigned)(((t & 1) * STAGE + u * 64) * 16), b < blocks ? x + ((int64_t)m * blocks + b) : &mx_zero_piece);
+            }
+#pragma unroll
+            for (int j = 0; j < SPW; ++j) {
+                const int u = fw + FW * j, m = min(m0 + u / KG * 16 + (lane & 15), g.M - 1), b = b0 + u % KG * 16 + (lane >> 4);
+                sc[j] = 0;
+                if (SPW * FW != RT * KG && u >= RT * KG) break;
+#pragma unroll
+                for (int s = 0; s < 4; ++s) sc[j] |= (unsigned)(b + s * 4 < blocks ? xs_[(int64_t)m * blocks + b + s * 4] : 127) << (8 * s);
+            }
+        };
+        auto put = [&](int t) {
+#pragma unroll
+            for (int j = 0; j < SPW; ++j) {
+                const int u = fw + FW * j;
+                if (SPW * FW != RT * KG && u >= RT * KG) break;
+                reinterpret_cast<unsigned *>(xs + (t & 1) * STAGE + UNITS * 64)[u * 64 + lane] = sc[j];
+            }
+        };
+        issue(0);
+        for (int t = 0; t < stages; ++t) {
+            put(t);
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (t + 1 < stages) issue(t + 1);
+        }
+        return;
+    }
+    const int wm = wave % WM, wn = wave / WM, ct0 = tn * (TN / 16) + wn * NTW;
+    const u32x4 *wp[NTW];
+    const uint32_t *sp[NTW];
+#pragma unroll
+    for (int nt = 0; nt < NTW; ++nt) {
+        const int ct = min(ct0 + nt, w.tiles - 1);
+        wp[nt] = w.codes + ((size_t)ct * w.ksteps + g0 * 4) * 64 + lane;
+        sp[nt] = w.scales + ((size_t)ct * w.kgroups + g0) * 64 + lane;
+    }
+    f32x4 acc[MTW][NTW];
+#pragma unroll
+    for (int mt = 0; mt < MTW; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    u32x4 c[4][NTW], xf[4];
+    unsigned sc[NTW], sn[NTW], xsc[MTW];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) c[s][nt] = wp[nt][s * 64];
+#pragma unroll
+    for (int nt = 0; nt < NTW; ++nt) sn[nt] = *sp[nt];
+    const int rd = wm * MTW * 4 * KG * 64 + lane;
+    auto x_at = [&](int q) { return rd + ((q % MTW) * 4 * KG + q / MTW) * 64; };            // slot q of a stage: k-step q / MTW
+    __syncthreads();
+    int st = 0;                                           // stage buffer
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) xf[q] = xs[x_at(q)];
+    auto group = [&](auto more_, auto gi_, bool next_stage) {
+        constexpr bool more = decltype(more_)::value;
+        constexpr int GI = decltype(gi_)::value;          // group within the stage (static)
+        const u32x4 *cur = xs + st * STAGE, *nxt = xs + (st ^ 1) * STAGE;
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) { sc[nt] = sn[nt]; if constexpr (more) { sp[nt] += 64; sn[nt] = *sp[nt]; } }
+#pragma unroll
+        for (int mt = 0; mt < MTW; ++mt) xsc[mt] = reinterpret_cast<const unsigned *>(cur + UNITS * 64)[((wm * MTW + mt) * KG + GI) * 64 + lane];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+#pragma unroll
+            for (int mt = 0; mt < MTW; ++mt) {
+                const int q = (GI * 4 + s) * MTW + mt;
+                if (q == SLOTS - AHEAD && next_stage) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    __syncthreads();
+                }
+                xf[(q + AHEAD) & 3] = q + AHEAD >= SLOTS ? nxt[x_at(q + AHEAD - SLOTS)] : cur[x_at(q + AHEAD)];
+                const u32x4 &xv = xf[q & 3];
+                const i32x8 b = {(int)xv.x, (int)xv.y, (int)xv.z, (int)xv.w, 0, 0, 0, 0};
+#pragma unroll
+                for (int nt = 0; nt < NTW; ++nt) {
+                    const i32x8 a = {(int)c[s][nt].x, (int)c[s][nt].y, (int)c[s][nt].z, (int)c[s][nt].w, 0, 0, 0, 0};
+                    if (s == 0) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[mt][nt], 4, 4, 0, (int)sc[nt], 0, (int)xsc[mt]);
+                    else if (s == 1) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[mt][nt], 4, 4, 1, (int)sc[nt], 1, (int)xsc[mt]);
+                    else if (s == 2) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[mt][nt], 4, 4, 2, (int)sc[nt], 2, (int)xsc[mt]);
+                    else acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[mt][nt], 4, 4, 3, (int)sc[nt], 3, (int)xsc[mt]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (more)
+#pragma unroll
+                for (int nt = 0; nt < NTW; ++nt) c[s][nt] = wp[nt][(s + 4) * 64];
+        }
+#pragma unroll
+        for (int nt = 0; nt < NTW; ++nt) wp[nt] += 256;
+    };
+    // whole stages but the last, then what is left of it
+    for (int t = 0; t + 1 < stages; ++t) {
+        group(Yes{}, Num<0>{}, true);
+        if constexpr (KG == 2) group(Yes{}, Num<1>{}, true);
+        st ^= 1;
+    }
+    if (KG == 1 || n % KG != 0) group(No{}, Num<0>{}, false);
+    else {
+        group(Yes{}, Num<0>{}, false);
+        if constexpr (KG == 2) group(No{}, Num<1>{}, false);
+    }
+    mx_tile_store<bf16_t, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
+}
+
+// ------------------------------------------------------------------------------------------ both operands in 4 bits, many rows
+// X's scales as the packed weights have theirs: [row tile][group][lane], the four k-steps of a lane's block row in a word.
+__global__ __launch_bounds__(256) void mx_scales_kernel(const uint8_t *__restrict__ xs, int M, int blocks, int groups, uint32_t *__restrict__ out) {
+    const int i = blockIdx.x * 256 + threadIdx.x, grp = i >> 6, lane = i & 63;
+    if (grp >= groups) return;
+    for (int rt = blockIdx.y; rt * 16 < M; rt += gridDim.y) {
+        const int m = min(rt * 16 + (lane & 15), M - 1);
+        unsigned v = 0;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int b = grp * 16 + s * 4 + (lane >> 4);
+            v |= (unsigned)(b < blocks ? xs[(int64_t)m * blocks + b] : 127) << (8 * s);
+        }
+        out[((size_t)rt * groups + grp) * 64 + lane] = v;
+    }
+}
+
+// 256 x 256 tiles, eight waves of 128 x 64 with the 32 x 32 x 64 instruction (registers alone, random codes: 6.3 PFLOP/s where the
+// 16 x 16 x 128 one gives 5.2).  Codes of both operands go into LDS by LDS-direct loads, a k-step of 128 a stage, four stages in a ring,
+// one barrier per k-step; the scales of a group of four k-steps likewise, an eighth of them by each wave, a quarter of that per k-step, two buffers.
+template <typename Y, bool SPLIT>
+__global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint32_t *__restrict__ xscales, int blocks, MxGeom g, Y *__restrict__ y,
+                                                               int64_t ldy, bool quads) {
+    typedef __attribute__((address_space(3))) void *LdsPtr;
+    constexpr int NST = 4, STAGE = 32 * 64;               // units 0..15: X's row tiles, 16..31: column tiles
+    __shared__ __attribute__((aligned(1024))) u32x4 xs[NST * STAGE];
+    __shared__ __attribute__((aligned(1024))) unsigned scs[2][32 * 64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave & 1, wn = wave >> 1;
+    int tm, tn;
+    mx_tile_of(g, 8, tm, tn);
+    const int m0 = tm * 256, ct0 = tn * 16, rts = (g.M + 15) / 16;
+    const int g0 = (int)((int64_t)blockIdx.y * w.kgroups / g.splits), n = ((int)((int64_t)(blockIdx.y + 1) * w.kgroups / g.splits) - g0) * 4;     // k-steps: whole groups
+    const unsigned lds0 = (unsigned)(uintptr_t)(LdsPtr)&xs[0], lds1 = (unsigned)(uintptr_t)(LdsPtr)&scs[0][0];
+    const u32x4 *xp[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) xp[j] = x + (int64_t)min(m0 + (wave + 8 * j) * 16 + (lane & 15), g.M - 1) * blocks + (lane >> 4);
+    const int wt0 = min(ct0 + wave, w.tiles - 1), wt1 = min(ct0 + wave + 8, w.tiles - 1);
+    const u32x4 *wp0 = w.codes + ((size_t)wt0 * w.ksteps + g0 * 4) * 64, *wp1 = w.codes + ((size_t)wt1 * w.ksteps + g0 * 4) * 64;
+    // the scales this wave brings: unit wave + 8 j of a group at its k-step j (0, 1: row tiles; 2, 3: column tiles)
+    const uint32_t *sp[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        sp[j] = j < 2 ? xscales + ((size_t)min(m0 / 16 + wave + 8 * j, rts - 1) * w.kgroups + g0) * 64 : w.scales + ((size_t)min(ct0 + wave + 8 * (j - 2), w.tiles - 1) * w.kgroups + g0) * 64;
+    auto issue = [&](int j, int s, int st) {              // load j (static, 0..3) of k-step s (relative), into stage st
+        const unsigned base = lds0 + (unsigned)(st * STAGE * 16);
+        if (j < 2) {
+            const int b = (g0 * 4 + s) * 4;
+            const u32x4 *p = xp[j] + b;
+            if (b + 4 > blocks) p = b + (lane >> 4) < blocks ? p : &mx_zero_piece;
+            lds_dma16(base + (wave + 8 * j) * 1024, p);
+        } else lds_dma16_s(base + (16 + wave + 8 * (j - 2)) * 1024, (j == 2 ? wp0 : wp1) + s * 64, lane * 16);
+    };
+    auto issue_scales = [&](int j, int grp) {             // unit j (static) of group grp (relative)
+        lds_dma4_s(lds1 + (unsigned)(((grp & 1) * 32 + wave + 8 * j) * 256), sp[j] + grp * 64, lane * 4);
+    };
+    f32x16 acc[4][2];
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[mt][nt][r] = 0.f;
+    // Loads of a wave: four pieces a k-step, and in the first two of a group two units each of the next group's scales, which have landed
+    // with the pieces by the group's end.  Behind the stage that k-step s waits for: those of s - 1 and of s.
+#pragma unroll
+    for (int j = 0; j < 4; ++j) issue_scales(j, 0);
+#pragma unroll
+    for (int s = 0; s < NST - 1; ++s) {                   // (n is at least four)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) issue(j, s, s);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NST - 2) * 4) : "memory");
+    __syncthreads();
+    // an operand of 32 rows x 64 columns (half h of a k-step): lane -> row lane % 32 (of two units), block 2 h + lane / 32
+    const int fr = ((lane >> 4) & 1) * 64 + (lane >> 5) * 16 + (lane & 15);
+    const int xr = wm * 8 * 64 + fr, wr = (16 + wn * 4) * 64 + fr;                       // + 128 per 32 rows, + 32 for the second half
+    u32x4 xf[2][4], wf[2][2];
+    unsigned xsc[2][4], wsc[2][2];
+    auto read = [&](const u32x4 *st, int h, u32x4 (&xo)[4], u32x4 (&wo)[2]) {
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) wo[nt] = st[wr + nt * 128 + h * 32];
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) xo[mt] = st[xr + mt * 128 + h * 32];
+    };
+    auto read_scales = [&](int grp) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) wsc[h][nt] = scs[grp & 1][wr + nt * 128 + h * 32];
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) xsc[h][mt] = scs[grp & 1][xr + mt * 128 + h * 32];
+        }
+    };
+    read(xs, 0, xf[0], wf[0]);
+    read_scales(0);
+    int at = 0;
+    for (int s4 = 0; s4 < n; s4 += 4) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int step = s4 + s, an = at == NST - 1 ? 0 : at + 1, ai = at == 0 ? NST - 1 : at - 1;
+            const u32x4 *cur = xs + at * STAGE, *nxt = xs + an * STAGE;
+            // asked for beyond the end too (of the last k-step and group again: valid memory, never read): every step is the same straight line
+            const int si = min(step + NST - 1, n - 1), gi = min((s4 >> 2) + 1, (n >> 2) - 1);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (h == 1) {                             // the next stage has landed; behind the barrier the last one's place is free
+                    if (s == 1) asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");
+                    else if (s == 3) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+                    else asm volatile("s_waitcnt vmcnt(10) lgkmcnt(0)" ::: "memory");
+                    __syncthreads();
+                }
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt) {
+                    if (h == 0 && mt < 4) issue(mt, si, ai);
+                    if (h == 0 && mt >= 2 && s < 2) issue_scales(2 * s + mt - 2, gi);
+                    const u32x4 *from = h == 1 ? nxt : cur;
+                    if (mt < 2) wf[h ^ 1][mt] = from[wr + mt * 128 + (h ^ 1) * 32];
+                    xf[h ^ 1][mt] = from[xr + mt * 128 + (h ^ 1) * 32];
+                    const i32x8 b = {(int)xf[h][mt].x, (int)xf[h][mt].y, (int)xf[h][mt].z, (int)xf[h][mt].w, 0, 0, 0, 0};
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt) {
+                        const i32x8 a = {(int)wf[h][nt].x, (int)wf[h][nt].y, (int)wf[h][nt].z, (int)wf[h][nt].w, 0, 0, 0, 0};
+                        if (s == 0) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[mt][nt], 4, 4, 0, (int)wsc[h][nt], 0, (int)xsc[h][mt]);
+                        else if (s == 1) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[mt][nt], 4, 4, 1, (int)wsc[h][nt], 1, (int)xsc[h][mt]);
+                        else if (s == 2) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[mt][nt], 4, 4, 2, (int)wsc[h][nt], 2, (int)xsc[h][mt]);
+                        else acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[mt][nt], 4, 4, 3, (int)wsc[h][nt], 3, (int)xsc[h][mt]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            at = an;
+        }
+        if (s4 + 4 < n) read_scales((s4 >> 2) + 1);
+    }
+    // D tile: lane -> row lane % 32, register r -> column 8 (r / 4) + 4 (lane / 32) + r % 4
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt) {
+        const int m = m0 + wm * 128 + mt * 32 + (lane & 31);
+        if (m >= g.M) continue;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int col = (ct0 + wn * 4 + nt * 2) * 16 + q * 8 + (lane >> 5) * 4;
+                if (col >= g.N) continue;
+                const f32x4 v = {acc[mt][nt][q * 4], acc[mt][nt][q * 4 + 1], acc[mt][nt][q * 4 + 2], acc[mt][nt][q * 4 + 3]};
+                if constexpr (SPLIT) *reinterpret_cast<f32x4 *>(y + ((size_t)blockIdx.y * g.M + m) * (w.tiles * 16) + col) = v;
+                else mx_store<Y>(y, ldy, quads, m, col, g.N, v, w.ref, 0);
+            }
+    }
+    dma_wait<0>();                                        // what nobody reads: LDS must not be given back before it lands
+}
+
+// The planes of a product, added in order.
+template <typename Y>
+__global__ __launch_bounds__(256) void mx_planes_kernel(const f32x4 *__restrict__ part, int splits, int M, int N, int quads_row, const int32_t *__restrict__ ref, int shift,
+                                                        Y *__restrict__ y, int64_t ldy, bool quads) {
+    const int q = blockIdx.x * 256 + threadIdx.x;          // four columns
+    if (q * 4 >= N) return;
+    const size_t plane = (size_t)M * quads_row;
+    for (int m = blockIdx.y; m < M; m += gridDim.y) {
+        const f32x4 *p = part + (size_t)m * quads_row + q;
+        f32x4 a = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < splits; s += 8) {              // eight planes on the way at a time
+            f32x4 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = p[min(s + j, splits - 1) * plane];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) if (s + j < splits) a += v[j];
+        }
+        mx_store<Y>(y, ldy, quads, m, q * 4, N, a, ref, shift);
+    }
+}
+
+// ------------------------------------------------------------------------------------------ launches
+// How a product runs: a kernel and tile shape (below), K splits.
+struct MxPlan { int shape, splits; };
+struct MxTile { int tm, tn; };
+enum { MX_STREAM = 0 };
+//                                   stream     fed                                                    tile
+constexpr MxTile MX_TILES[] =      {{16, 16}, {16, 64}, {32, 128}, {32, 256}, {64, 128}, {64, 256}, {256, 256}};
+//                                   stream     fed                                                      block
+constexpr MxTile MX_BOTH_TILES[] = {{16, 16}, {16, 64}, {32, 128}, {64, 128}, {64, 256}, {128, 256}, {256, 256}};
+
+static int mx_groups(int K) { return (K + 4 * MX_KSTEP - 1) / (4 * MX_KSTEP); }
+static int stream_waves(int kgroups) { return kgroups < 16 ? (kgroups < 8 ? kgroups : 8) : 16; }
+
+static MxPlan gemm_plan_of(int M, int N, int groups) {
+    const int shape = M <= 4 ? 0 : M <= 16 ? 1 : M <= 32 ? 2 : M <= 64 ? 3 : M <= 512 ? 5 : 6;
+    const MxTile t = MX_TILES[shape];
+    const int tiles = ((M + t.tm - 1) / t.tm) * ((N + t.tn - 1) / t.tn);
+    int s = shape == MX_STREAM ? 1 : 256 / tiles;
+    if (s > groups) s = groups;
+    return MxPlan{shape, s < 1 ? 1 : s};
+}
+static MxPlan both_plan_of(int M, int N, int groups) {
+    const int shape = M <= 4 ? 0 : M <= 16 ? 1 : M <= 32 ? 2 : M <= 64 ? 3 : M <= 128 ? 4 : M <= 512 ? 5 : 6;
+    const MxTile t = MX_BOTH_TILES[shape];
+    const int tiles = ((M + t.tm - 1) / t.tm) * ((N + t.tn - 1) / t.tn);
+    int s = shape == MX_STREAM ? 1 : 256 / tiles;
+    if (s > groups) s = groups;
+    return MxPlan{shape, s < 1 ? 1 : s};
+}
 
 // Whether X can be read as it is: rows of whole 16-byte pieces.
 static bool rows_ok(int x_dt, const void *x, int64_t ldx, int K) {
-    return x_dt != DT_F32 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0 && K % 8 == 0;
+    return x_dt != DT_F32 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0 && K % 8 == 0 && ldx < (1 << 22);   // (offsets within a tile's rows are 32 bits)
 }
 static bool quads_ok(const void *y, int64_t ldy, int N, int y_dt) {
     return N % 4 == 0 && ldy % 4 == 0 && reinterpret_cast<uintptr_t>(y) % (4 * dtype_size(y_dt)) == 0;
 }
 
-size_t mx_gemm_scratch_size(int x_dt, int M, int N, int K) {
-    if (x_dt == DT_MX) return 256;
-    const size_t kp = (size_t)(K + 4 * MX_KSTEP - 1) / (4 * MX_KSTEP) * (4 * MX_KSTEP);
-    return ((size_t)M * kp * 2 * (x_dt == DT_F32 ? 3 : 1) + 255) / 256 * 256 + 256;
-}
-
 static MxRows stage(int x_dt, const void *x, int64_t ldx, int M, int K, int kp, void *scratch, hipStream_t st) {
     const dim3 grid((kp / 8 + 255) / 256, M < 65535 ? M : 65535);
     u32x4 *o = static_cast<u32x4 *>(scratch);
-    if (x_dt == DT_F32) mx_stage_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float *>(x), ldx, M, K, kp, o);
-    else mx_stage_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(x), ldx, M, K, kp, o);
-    return MxRows{scratch, kp, (int64_t)M * kp, kp};
+    if (x_dt == DT_F32) { mx_stage_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float *>(x), ldx, M, K, kp, o); return MxRows{scratch, 3 * (int64_t)kp, kp, kp}; }
+    mx_stage_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(x), ldx, M, K, kp, o);
+    return MxRows{scratch, kp, 0, kp};
+}
+
+// Scratch: what stands in X's place (a staged copy; X's scales in operand order), then the planes.
+static size_t stage_bytes(int x_dt, int M, int K, const MxPlan &p) {
+    const size_t groups = mx_groups(K);
+    if (x_dt == DT_MX) return MX_BOTH_TILES[p.shape].tm == 256 ? (size_t)((M + 15) / 16) * groups * 256 : 0;
+    return ((size_t)M * groups * 4 * MX_KSTEP * 2 * (x_dt == DT_F32 ? 3 : 1) + 255) / 256 * 256;
+}
+static MxPlan plan_of(int x_dt, int M, int N, int K) {
+    return x_dt == DT_MX ? both_plan_of(M, N, mx_groups(K)) : gemm_plan_of(M, N, mx_groups(K) * (x_dt == DT_F32 ? 3 : 1));
+}
+size_t mx_gemm_scratch_size(int x_dt, int M, int N, int K) {
+    if (M == 0) return 256;
+    const MxPlan p = plan_of(x_dt, M, N, K);
+    return stage_bytes(x_dt, M, K, p) + (p.splits > 1 ? (size_t)p.splits * M * ((N + 15) / 16 * 16) * sizeof(float) : 0) + 256;
+}
+
+template <typename Y>
+static void add_planes(const MxPacked &w, const float *part, int splits, int M, int N, int shift, Y *y, int64_t ldy, bool quads, hipStream_t st) {
+    mx_planes_kernel<Y><<<dim3(((N + 3) / 4 + 255) / 256, M < 65535 ? M : 65535), 256, 0, st>>>(reinterpret_cast<const f32x4 *>(part), splits, M, N, w.tiles * 4, w.ref, shift, y, ldy, quads);
+}
+
+template <typename T, typename Y, int PARTS>
+static void run_gemm(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan &p, Y *y, int64_t ldy, bool quads, float *part, hipStream_t st) {
+    if (p.shape == MX_STREAM) {
+        const int waves = stream_waves(w.kgroups);
+        mx_stream_kernel<T, Y, PARTS><<<w.tiles, waves * 64, waves * 1024, st>>>(w, x, y, ldy, quads, g.M, g.N);
+        return;
+    }
+    const MxTile t = MX_TILES[p.shape];
+    g.splits = p.splits; g.tiles_m = (g.M + t.tm - 1) / t.tm; g.tiles_n = (g.N + t.tn - 1) / t.tn;
+    const dim3 grid(g.tiles_m * g.tiles_n, g.splits);
+#define POSS_MX_FED(TM, TN, WM, WN, FW, KS)                                                                                                  \
+    do {                                                                                                                                     \
+        if (g.splits > 1) mx_fed_kernel<T, float, TM, TN, WM, WN, FW, KS, true><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, part, 0, false); \
+        else mx_fed_kernel<T, Y, TM, TN, WM, WN, FW, KS, false><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, y, ldy, quads);               \
+    } while (0)
+    switch (p.shape) {
+        case 1: POSS_MX_FED(16, 64, 1, 4, 2, 4); break;
+        case 2: POSS_MX_FED(32, 128, 1, 8, 4, 4); break;
+        case 3: POSS_MX_FED(32, 256, 1, 8, 4, 4); break;
+        case 4: POSS_MX_FED(64, 128, 2, 4, 4, 4); break;
+        case 5: POSS_MX_FED(64, 256, 1, 8, 4, 4); break;
+        default:
+            if (g.splits > 1) mx_tile_kernel<T, float, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(w, x, g, part, 0, false);
+            else mx_tile_kernel<T, Y, 256, 256, 2, 4, false><<<grid, 512, 0, st>>>(w, x, g, y, ldy, quads);
+    }
+#undef POSS_MX_FED
+    if (g.splits > 1) add_planes<Y>(w, part, g.splits, g.M, g.N, MxOp<T>::SHIFT, y, ldy, quads, st);
+}
+
+// X microscaled.  xscales: scratch for its scales in operand order.
+template <typename Y>
+static void run_both(const MxPacked &w, const u32x4 *x, const uint8_t *xs, int blocks, MxGeom g, const MxPlan &p, Y *y, int64_t ldy, bool quads, uint32_t *xscales, float *part, hipStream_t st) {
+    if (p.shape == MX_STREAM) {
+        const int waves = stream_waves(w.kgroups);
+        mx_stream_both_kernel<Y><<<w.tiles, waves * 64, waves * 1024, st>>>(w, x, xs, blocks, y, ldy, quads, g.M, g.N);
+        return;
+    }
+    const MxTile t = MX_BOTH_TILES[p.shape];
+    g.splits = p.splits; g.tiles_m = (g.M + t.tm - 1) / t.tm; g.tiles_n = (g.N + t.tn - 1) / t.tn;
+    const dim3 grid(g.tiles_m * g.tiles_n, g.splits);
+#define POSS_MX_FED(TM, TN, WM, WN, FW, KG)                                                                                                        \
+    do {                                                                                                                                           \
+        if (g.splits > 1) mx_fed_both_kernel<float, TM, TN, WM, WN, FW, KG, true><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, xs, blocks, g, part, 0, false); \
+        else mx_fed_both_kernel<Y, TM, TN, WM, WN, FW, KG, false><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, xs, blocks, g, y, ldy, quads);       \
+    } while (0)
+    switch (p.shape) {
+        case 1: POSS_MX_FED(16, 64, 1, 4, 2, 1); break;
+        case 2: POSS_MX_FED(32, 128, 1, 8, 4, 1); break;
+        case 3: POSS_MX_FED(64, 128, 1, 8, 4, 2); break;
+        case 4: POSS_MX_FED(64, 256, 1, 8, 4, 2); break;
+        case 5: POSS_MX_FED(128, 256, 2, 4, 4, 2); break;
+        default: {
+            const int rts = (g.M + 15) / 16;
+            mx_scales_kernel<<<dim3((w.kgroups * 64 + 255) / 256, rts < 65535 ? rts : 65535), 256, 0, st>>>(xs, g.M, blocks, w.kgroups, xscales);
+            if (g.splits > 1) mx_block_both_kernel<float, true><<<grid, 512, 0, st>>>(w, x, xscales, blocks, g, part, 0, false);
+            else mx_block_both_kernel<Y, false><<<grid, 512, 0, st>>>(w, x, xscales, blocks, g, y, ldy, quads);
+        }
+    }
+#undef POSS_MX_FED
+    if (g.splits > 1) add_planes<Y>(w, part, g.splits, g.M, g.N, 0, y, ldy, quads, st);
 }
 
 template <typename T, int PARTS>
-static void launch_gemm_t(const MxPacked &w, MxRows x, int y_dt, char *y, int64_t ldy, bool quads, int M, int N, hipStream_t st) {
-    const int rows = PARTS == 3 ? 32 : MX_STREAM_ROWS;
-    const StreamShape sh = stream_shape(M, N, w.kgroups);
-    for (int m = 0; m < M; m += rows) {
-        MxRows xr = x;
-        xr.x = static_cast<const T *>(x.x) + m * x.ldx;
-        char *yr = y + m * ldy * (int64_t)dtype_size(y_dt);
-        const int n = M - m < rows ? M - m : rows;
-        if (y_dt == DT_F32) launch_stream<T, float, PARTS>(w, xr, yr, ldy, quads, n, N, sh.nt, sh.waves, st);
-        else if (y_dt == DT_BF16) launch_stream<T, bf16_t, PARTS>(w, xr, yr, ldy, quads, n, N, sh.nt, sh.waves, st);
-        else launch_stream<T, f16_t, PARTS>(w, xr, yr, ldy, quads, n, N, sh.nt, sh.waves, st);
-    }
+static void run_gemm_t(const MxPacked &w, const MxRows &x, const MxGeom &g, const MxPlan &p, int y_dt, void *y, int64_t ldy, float *part, hipStream_t st) {
+    const bool quads = quads_ok(y, ldy, g.N, y_dt);
+    if (y_dt == DT_F32) run_gemm<T, float, PARTS>(w, x, g, p, static_cast<float *>(y), ldy, quads, part, st);
+    else if (y_dt == DT_BF16) run_gemm<T, bf16_t, PARTS>(w, x, g, p, static_cast<bf16_t *>(y), ldy, quads, part, st);
+    else run_gemm<T, f16_t, PARTS>(w, x, g, p, static_cast<f16_t *>(y), ldy, quads, part, st);
 }
 
 void launch_mx_gemm(int x_dt, const void *x, int64_t ldx, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *scratch, hipStream_t st) {
     const MxPacked w = mx_packed_at(packed, N, K);
-    const MxRows r = rows_ok(x_dt, x, ldx, K) ? MxRows{x, ldx, 0, K} : stage(x_dt, x, ldx, M, K, w.ksteps * MX_KSTEP, scratch, st);
-    const bool quads = quads_ok(y, ldy, N, y_dt);
-    if (x_dt == DT_F32) launch_gemm_t<bf16_t, 3>(w, r, y_dt, static_cast<char *>(y), ldy, quads, M, N, st);
-    else if (x_dt == DT_BF16) launch_gemm_t<bf16_t, 1>(w, r, y_dt, static_cast<char *>(y), ldy, quads, M, N, st);
-    else launch_gemm_t<f16_t, 1>(w, r, y_dt, static_cast<char *>(y), ldy, quads, M, N, st);
+    const MxPlan p = plan_of(x_dt, M, N, K);
+    const bool as_is = rows_ok(x_dt, x, ldx, K);
+    const MxRows r = as_is ? MxRows{x, ldx, 0, K} : stage(x_dt, x, ldx, M, K, w.ksteps * MX_KSTEP, scratch, st);
+    MxGeom g{M, N, x_dt == DT_F32 ? 3 * w.ksteps : (K + MX_KSTEP - 1) / MX_KSTEP, 0, 0, 0, 1};
+    g.full = as_is ? K / MX_KSTEP : x_dt == DT_F32 ? g.steps : w.ksteps;
+    float *part = reinterpret_cast<float *>(static_cast<char *>(scratch) + stage_bytes(x_dt, M, K, p));
+    if (x_dt == DT_F32) run_gemm_t<bf16_t, 3>(w, r, g, p, y_dt, y, ldy, part, st);
+    else if (x_dt == DT_BF16) run_gemm_t<bf16_t, 1>(w, r, g, p, y_dt, y, ldy, part, st);
+    else run_gemm_t<f16_t, 1>(w, r, g, p, y_dt, y, ldy, part, st);
 }
 
-void launch_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *, hipStream_t st) {
+void launch_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *scratch, hipStream_t st) {
     const MxPacked w = mx_packed_at(packed, N, K);
+    const MxPlan p = plan_of(DT_MX, M, N, K);
     const bool quads = quads_ok(y, ldy, N, y_dt);
-    const int nb = mx_blocks(K);
-    const StreamShape sh = stream_shape(M, N, w.kgroups);
-    for (int m = 0; m < M; m += MX_STREAM_ROWS) {
-        const char *c = static_cast<const char *>(x_codes) + (int64_t)m * nb * 16, *s = static_cast<const char *>(x_scales) + (int64_t)m * nb;
-        char *yr = static_cast<char *>(y) + m * ldy * (int64_t)dtype_size(y_dt);
-        const int n = M - m < MX_STREAM_ROWS ? M - m : MX_STREAM_ROWS;
-        if (y_dt == DT_F32) launch_stream_both<float>(w, c, s, nb, yr, ldy, quads, n, N, sh.nt, sh.waves, st);
-        else if (y_dt == DT_BF16) launch_stream_both<bf16_t>(w, c, s, nb, yr, ldy, quads, n, N, sh.nt, sh.waves, st);
-        else launch_stream_both<f16_t>(w, c, s, nb, yr, ldy, quads, n, N, sh.nt, sh.waves, st);
-    }
+    const MxGeom g{M, N, w.ksteps, 0, 0, 0, 1};
+    const u32x4 *c = static_cast<const u32x4 *>(x_codes);
+    const uint8_t *s = static_cast<const uint8_t *>(x_scales);
+    uint32_t *xs = static_cast<uint32_t *>(scratch);
+    float *part = reinterpret_cast<float *>(static_cast<char *>(scratch) + stage_bytes(DT_MX, M, K, p));
+    if (y_dt == DT_F32) run_both<float>(w, c, s, mx_blocks(K), g, p, static_cast<float *>(y), ldy, quads, xs, part, st);
+    else if (y_dt == DT_BF16) run_both<bf16_t>(w, c, s, mx_blocks(K), g, p, static_cast<bf16_t *>(y), ldy, quads, xs, part, st);
+    else run_both<f16_t>(w, c, s, mx_blocks(K), g, p, static_cast<f16_t *>(y), ldy, quads, xs, part, st);
 }
 
 }  // namespace poss
