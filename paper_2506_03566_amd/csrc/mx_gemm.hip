@@ -48,12 +48,16 @@ __device__ const u32x4 mx_zero_piece = {0u, 0u, 0u, 0u};  // what a lane reads w
 
 // The sums of four consecutive columns n.. of row m, times 2^ref, to Y.
 template <typename Y> struct __attribute__((aligned(4 * sizeof(Y)))) MxQuad { Y v[4]; };
-template <typename Y> __device__ __forceinline__ void mx_store(Y *__restrict__ y, int64_t ldy, bool quads, int m, int n, int N, f32x4 acc, const int32_t *__restrict__ ref, int shift) {
+template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_scaled(f32x4 a, const int32_t *__restrict__ ref, int n, int shift) {
     MxQuad<Y> o;
     const int4 e = *reinterpret_cast<const int4 *>(ref + n);
     const int es[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
-    for (int r = 0; r < 4; ++r) o.v[r] = from_f<Y>(es[r] == 255 ? __builtin_nanf("") : __builtin_ldexpf(acc[r], es[r] - 127 - shift));
+    for (int r = 0; r < 4; ++r) o.v[r] = from_f<Y>(es[r] == 255 ? __builtin_nanf("") : __builtin_ldexpf(a[r], es[r] - 127 - shift));
+    return o;
+}
+template <typename Y> __device__ __forceinline__ void mx_store(Y *__restrict__ y, int64_t ldy, bool quads, int m, int n, int N, f32x4 acc, const int32_t *__restrict__ ref, int shift) {
+    const MxQuad<Y> o = mx_scaled<Y>(acc, ref, n, shift);
     Y *dst = y + (int64_t)m * ldy + n;
     if (quads) *reinterpret_cast<MxQuad<Y> *>(dst) = o;   // (n, N and ldy are multiples of four then, and y is aligned)
     else
@@ -61,6 +65,24 @@ template <typename Y> __device__ __forceinline__ void mx_store(Y *__restrict__ y
         for (int r = 0; r < 4; ++r) if (n + r < N) dst[r] = o.v[r];
 }
 
+// ROWS rows x COLS columns of float32 sums that a wave holds, to Y (times 2^ref) or to a plane, in pieces of 16 bytes: from the lanes' quads
+// through LDS of the wave's own (rows padded by 16 bytes).  A lane's quads of a row, as they are, would be written 8 bytes here and
+// there: 256 x 256 tiles of 8192 x 28672 results took 24 us a round for them, of 59.
+// put(f): calls f(row, column, sums) for each quad.
+template <typename Y, int ROWS, int COLS, typename Put>
+__device__ __forceinline__ void mx_store_rows(char *lds, Put put, int m0, int n0, int M, int N, Y *__restrict__ y, int64_t ldy) {
+    constexpr int ROW = COLS * (int)sizeof(Y) + 16, LPR = COLS * (int)sizeof(Y) / 16, RPI = 64 / LPR;      // lanes a row, rows an instruction
+    const int lane = threadIdx.x & 63;
+    put([&](int r, int c, const MxQuad<Y> &v) { *reinterpret_cast<MxQuad<Y> *>(lds + r * ROW + c * (int)sizeof(Y)) = v; });
+    wave_lds_sync();
+    const int c = (lane % LPR) * (16 / (int)sizeof(Y));
+#pragma unroll
+    for (int r = lane / LPR; r < ROWS; r += RPI) {
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + r * ROW + c * (int)sizeof(Y));
+        if (m0 + r < M && n0 + c < N) *reinterpret_cast<u32x4 *>(y + (int64_t)(m0 + r) * ldy + n0 + c) = v;
+    }
+    wave_lds_sync();                                      // (the next rows go to the same place)
+}
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 template <int I> struct Num { static constexpr int value = I; };
@@ -337,8 +359,25 @@ __device__ __forceinline__ void mx_tile_store(const f32x4 (&acc)[MTW][NTW], int 
     }
 }
 
+// The same through LDS of the wave's own (16 rows of NTW * 16 columns and padding), where pieces of 16 bytes can be written.
+template <typename T, typename Y, int MTW, int NTW, bool SPLIT>
+__device__ __forceinline__ void mx_tile_store_wide(char *own, const f32x4 (&acc)[MTW][NTW], int row0, int ct0, const MxGeom &g, const MxPacked &w, Y *__restrict__ y, int64_t ldy) {
+    const int lane = threadIdx.x & 63, cols = SPLIT ? w.tiles * 16 : g.N;
+    Y *dst = SPLIT ? y + (size_t)blockIdx.y * g.M * cols : y;
+#pragma unroll
+    for (int mt = 0; mt < MTW; ++mt)
+        mx_store_rows<Y, 16, NTW * 16>(own, [&](auto f) {
+#pragma unroll
+            for (int nt = 0; nt < NTW; ++nt) {
+                const int c = nt * 16 + (lane >> 4) * 4;
+                if constexpr (SPLIT) f(lane & 15, c, __builtin_bit_cast(MxQuad<Y>, acc[mt][nt]));
+                else f(lane & 15, c, mx_scaled<Y>(acc[mt][nt], w.ref, min(ct0 + nt, w.tiles - 1) * 16 + (lane >> 4) * 4, MxOp<T>::SHIFT));
+            }
+        }, row0 + mt * 16, ct0 * 16, g.M, cols, dst, SPLIT ? cols : ldy);
+}
+
 template <typename T, typename Y, int TM, int TN, int WM, int WN, bool SPLIT>
-__global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, MxRows x, MxGeom g, Y *__restrict__ y, int64_t ldy, bool quads) {
+__global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, MxRows x, MxGeom g, Y *__restrict__ y, int64_t ldy, bool quads, bool wide) {
     typedef __attribute__((address_space(3))) void *LdsPtr;
     typedef MxOp<T> Op;
     constexpr int WAVES = WM * WN, MTW = TM / (16 * WM), NTW = TN / (16 * WN), UNITS = TM / 16 * 4, UPW = UNITS / WAVES;   // 1 KB units: 16 rows x 64 bytes
@@ -431,7 +470,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
 #pragma unroll
         for (int nt = 0; nt < NTW; ++nt) { c[nt] = cn[nt]; f[nt] = fn[nt]; }
     }
-    mx_tile_store<T, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
+    if (!wide) {
+        mx_tile_store<T, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
+        return;
+    }
+    __syncthreads();                                      // nobody reads X any more
+    mx_tile_store_wide<T, Y, MTW, NTW, SPLIT>(reinterpret_cast<char *>(xs) + wave * (16 * (NTW * 16 * (int)sizeof(Y) + 16)), acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy);
 }
 
 // ------------------------------------------------------------------------------------------ tens of rows
@@ -440,7 +484,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
 // fetch X into LDS, a group of four k-steps (KS k-steps) a stage, two stages; the others keep the codes of their own columns four k-steps
 // ahead in registers, and multiply.  One barrier per stage, where reads pass into the next one, as in mx_tile_kernel.
 template <typename T, typename Y, int TM, int TN, int WM, int WN, int FW, int KS, bool SPLIT>
-__global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w, MxRows x, MxGeom g, Y *__restrict__ y, int64_t ldy, bool quads) {
+__global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w, MxRows x, MxGeom g, Y *__restrict__ y, int64_t ldy, bool quads, bool wide) {
     typedef __attribute__((address_space(3))) void *LdsPtr;
     typedef MxOp<T> Op;
     constexpr int WAVES = WM * WN, MTW = TM / (16 * WM), NTW = TN / (16 * WN), UNITS = TM / 4 * KS, UPW = UNITS / FW;     // 1 KB units of a stage
@@ -479,6 +523,7 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
             __syncthreads();                              // stage t has landed; nobody reads stage t - 1 any more
             if (t + 1 < stages) issue(t + 1);
         }
+        if (TM >= 64 && wide) __syncthreads();            // (the others write their results through LDS)
         return;
     }
     const int wm = wave % WM, wn = wave / WM, ct0 = tn * (TN / 16) + wn * NTW;
@@ -559,7 +604,10 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
     };
     for (int s = 0; s + 1 < n; ++s) group(Yes{}, false);
     group(No{}, true);
-    mx_tile_store<T, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
+    if (TM >= 64 && wide) {
+        __syncthreads();                                  // nobody reads X any more
+        mx_tile_store_wide<T, Y, MTW, NTW, SPLIT>(reinterpret_cast<char *>(xs) + wave * (16 * (NTW * 16 * (int)sizeof(Y) + 16)), acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy);
+    } else mx_tile_store<T, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
 }
 
 __device__ __forceinline__ void lds_dma4_s(unsigned lds_base, const void *g, unsigned off) {     // 4 bytes a lane (device_utils.h has 16)
@@ -568,11 +616,11 @@ __device__ __forceinline__ void lds_dma4_s(unsigned lds_base, const void *g, uns
 
 // ------------------------------------------------------------------------------------------ both operands in 4 bits, tens of rows
 // mx_fed_kernel for microscaled X: a lane's block of 16 bytes is an operand as it is, so a stage is codes (a 1 KB unit per row tile and
-// k-step, in operand order) and, for each row tile and group, the scales of a lane's four blocks in one word, which the fetching waves
+// k-step: four lanes fetch a row's 64 bytes, block b of row r to position b ^ (r / 4 % 4)) and, for each row tile and group, the scales of a lane's four blocks in one word, which the fetching waves
 // put together from the rows' bytes.  KG groups of four k-steps a stage.
 template <typename Y, int TM, int TN, int WM, int WN, int FW, int KG, bool SPLIT>
 __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint8_t *__restrict__ xs_, int blocks, MxGeom g, Y *__restrict__ y,
-                                                                          int64_t ldy, bool quads) {
+                                                                          int64_t ldy, bool quads, bool wide) {
     typedef __attribute__((address_space(3))) void *LdsPtr;
     constexpr int WAVES = WM * WN, MTW = TM / (16 * WM), NTW = TN / (16 * WN), RT = TM / 16, UNITS = RT * 4 * KG;
     constexpr int STAGE = UNITS * 64 + RT * KG * 16, SLOTS = 4 * KG * MTW, AHEAD = 3;      // (16 bytes each: codes, then scales)
@@ -596,7 +644,7 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_both_kernel(MxPack
             for (int j = 0; j < UPW; ++j) {
                 const int u = fw + FW * j;
                 if (UPW * FW != UNITS && u >= UNITS) break;
-                const int m = min(m0 + u / (4 * KG) * 16 + (lane & 15), g.M - 1), b = b0 + u % (4 * KG) * 4 + (lane >> 4);
+                const int m = min(m0 + u / (4 * KG) * 16 + (lane >> 2), g.M - 1), b = b0 + u % (4 * KG) * 4 + ((lane & 3) ^ (lane >> 4));
                 lds_dma16(lds0 + (unsigned)(((t & 1) * STAGE + u * 64) * 16), b < blocks ? x + ((int64_t)m * blocks + b) : &mx_zero_piece);
             }
 #pragma unroll
@@ -623,6 +671,7 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_both_kernel(MxPack
             __syncthreads();
             if (t + 1 < stages) issue(t + 1);
         }
+        if (TM >= 64 && wide) __syncthreads();            // (the others write their results through LDS)
         return;
     }
     const int wm = wave % WM, wn = wave / WM, ct0 = tn * (TN / 16) + wn * NTW;
@@ -647,7 +696,7 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_both_kernel(MxPack
         for (int nt = 0; nt < NTW; ++nt) c[s][nt] = wp[nt][s * 64];
 #pragma unroll
     for (int nt = 0; nt < NTW; ++nt) sn[nt] = *sp[nt];
-    const int rd = wm * MTW * 4 * KG * 64 + lane;
+    const int rd = wm * MTW * 4 * KG * 64 + (lane & 15) * 4 + ((lane >> 4) ^ ((lane >> 2) & 3));
     auto x_at = [&](int q) { return rd + ((q % MTW) * 4 * KG + q / MTW) * 64; };            // slot q of a stage: k-step q / MTW
     __syncthreads();
     int st = 0;                                           // stage buffer
@@ -701,7 +750,10 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_both_kernel(MxPack
         group(Yes{}, Num<0>{}, false);
         if constexpr (KG == 2) group(No{}, Num<1>{}, false);
     }
-    mx_tile_store<bf16_t, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
+    if (TM >= 64 && wide) {
+        __syncthreads();                                  // nobody reads X any more
+        mx_tile_store_wide<bf16_t, Y, MTW, NTW, SPLIT>(reinterpret_cast<char *>(xs) + wave * (16 * (NTW * 16 * (int)sizeof(Y) + 16)), acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy);
+    } else mx_tile_store<bf16_t, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
 }
 
 // ------------------------------------------------------------------------------------------ both operands in 4 bits, many rows
@@ -726,7 +778,7 @@ __global__ __launch_bounds__(256) void mx_scales_kernel(const uint8_t *__restric
 // one barrier per k-step; the scales of a group of four k-steps likewise, an eighth of them by each wave, a quarter of that per k-step, two buffers.
 template <typename Y, bool SPLIT>
 __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint32_t *__restrict__ xscales, int blocks, MxGeom g, Y *__restrict__ y,
-                                                               int64_t ldy, bool quads) {
+                                                               int64_t ldy, bool quads, bool wide) {
     typedef __attribute__((address_space(3))) void *LdsPtr;
     constexpr int NST = 4, STAGE = 32 * 64;               // units 0..15: X's row tiles, 16..31: column tiles
     __shared__ __attribute__((aligned(1024))) u32x4 xs[NST * STAGE];
@@ -737,9 +789,10 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
     const int m0 = tm * 256, ct0 = tn * 16, rts = (g.M + 15) / 16;
     const int g0 = (int)((int64_t)blockIdx.y * w.kgroups / g.splits), n = ((int)((int64_t)(blockIdx.y + 1) * w.kgroups / g.splits) - g0) * 4;     // k-steps: whole groups
     const unsigned lds0 = (unsigned)(uintptr_t)(LdsPtr)&xs[0], lds1 = (unsigned)(uintptr_t)(LdsPtr)&scs[0][0];
+    const int x_b = (lane & 3) ^ (lane >> 4);             // block b of row r of a unit of X lies at position b ^ (r / 4 % 4)
     const u32x4 *xp[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) xp[j] = x + (int64_t)min(m0 + (wave + 8 * j) * 16 + (lane & 15), g.M - 1) * blocks + (lane >> 4);
+    for (int j = 0; j < 2; ++j) xp[j] = x + (int64_t)min(m0 + (wave + 8 * j) * 16 + (lane >> 2), g.M - 1) * blocks + x_b;
     const int wt0 = min(ct0 + wave, w.tiles - 1), wt1 = min(ct0 + wave + 8, w.tiles - 1);
     const u32x4 *wp0 = w.codes + ((size_t)wt0 * w.ksteps + g0 * 4) * 64, *wp1 = w.codes + ((size_t)wt1 * w.ksteps + g0 * 4) * 64;
     // the scales this wave brings: unit wave + 8 j of a group at its k-step j (0, 1: row tiles; 2, 3: column tiles)
@@ -752,7 +805,7 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
         if (j < 2) {
             const int b = (g0 * 4 + s) * 4;
             const u32x4 *p = xp[j] + b;
-            if (b + 4 > blocks) p = b + (lane >> 4) < blocks ? p : &mx_zero_piece;
+            if (b + 4 > blocks) p = b + x_b < blocks ? p : &mx_zero_piece;
             lds_dma16(base + (wave + 8 * j) * 1024, p);
         } else lds_dma16_s(base + (16 + wave + 8 * (j - 2)) * 1024, (j == 2 ? wp0 : wp1) + s * 64, lane * 16);
     };
@@ -780,13 +833,16 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
     // an operand of 32 rows x 64 columns (half h of a k-step): lane -> row lane % 32 (of two units), block 2 h + lane / 32
     const int fr = ((lane >> 4) & 1) * 64 + (lane >> 5) * 16 + (lane & 15);
     const int xr = wm * 8 * 64 + fr, wr = (16 + wn * 4) * 64 + fr;                       // + 128 per 32 rows, + 32 for the second half
+    int xc[2];                                            // X's codes
+#pragma unroll
+    for (int h = 0; h < 2; ++h) xc[h] = wm * 8 * 64 + ((lane >> 4) & 1) * 64 + (lane & 15) * 4 + ((h * 2 + (lane >> 5)) ^ ((lane >> 2) & 3));
     u32x4 xf[2][4], wf[2][2];
     unsigned xsc[2][4], wsc[2][2];
     auto read = [&](const u32x4 *st, int h, u32x4 (&xo)[4], u32x4 (&wo)[2]) {
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) wo[nt] = st[wr + nt * 128 + h * 32];
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) xo[mt] = st[xr + mt * 128 + h * 32];
+        for (int mt = 0; mt < 4; ++mt) xo[mt] = st[xc[h] + mt * 128];
     };
     auto read_scales = [&](int grp) {
 #pragma unroll
@@ -821,7 +877,7 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
                     if (h == 0 && mt >= 2 && s < 2) issue_scales(2 * s + mt - 2, gi);
                     const u32x4 *from = h == 1 ? nxt : cur;
                     if (mt < 2) wf[h ^ 1][mt] = from[wr + mt * 128 + (h ^ 1) * 32];
-                    xf[h ^ 1][mt] = from[xr + mt * 128 + (h ^ 1) * 32];
+                    xf[h ^ 1][mt] = from[xc[h ^ 1] + mt * 128];
                     const i32x8 b = {(int)xf[h][mt].x, (int)xf[h][mt].y, (int)xf[h][mt].z, (int)xf[h][mt].w, 0, 0, 0, 0};
 #pragma unroll
                     for (int nt = 0; nt < 2; ++nt) {
@@ -839,6 +895,28 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
         if (s4 + 4 < n) read_scales((s4 >> 2) + 1);
     }
     // D tile: lane -> row lane % 32, register r -> column 8 (r / 4) + 4 (lane / 32) + r % 4
+    auto quad = [&](int mt, int nt, int q) { return f32x4{acc[mt][nt][q * 4], acc[mt][nt][q * 4 + 1], acc[mt][nt][q * 4 + 2], acc[mt][nt][q * 4 + 3]}; };
+    dma_wait<0>();                                        // what nobody reads: LDS is written over, or given back
+    __syncthreads();
+    const int n0 = (ct0 + wn * 4) * 16;
+    if (wide) {
+        Y *dst = SPLIT ? y + (size_t)blockIdx.y * g.M * (w.tiles * 16) : y;
+        const int64_t ldd = SPLIT ? (int64_t)w.tiles * 16 : ldy;
+        char *own = reinterpret_cast<char *>(xs) + wave * (32 * (64 * (int)sizeof(Y) + 16));
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt)
+            mx_store_rows<Y, 32, 64>(own, [&](auto f) {
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int c = nt * 32 + q * 8 + (lane >> 5) * 4;
+                        if constexpr (SPLIT) f(lane & 31, c, __builtin_bit_cast(MxQuad<Y>, quad(mt, nt, q)));
+                        else f(lane & 31, c, mx_scaled<Y>(quad(mt, nt, q), w.ref, min(n0 + c, w.tiles * 16 - 4), 0));
+                    }
+            }, m0 + wm * 128 + mt * 32, n0, g.M, SPLIT ? w.tiles * 16 : g.N, dst, ldd);
+        return;
+    }
 #pragma unroll
     for (int mt = 0; mt < 4; ++mt) {
         const int m = m0 + wm * 128 + mt * 32 + (lane & 31);
@@ -847,14 +925,12 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int col = (ct0 + wn * 4 + nt * 2) * 16 + q * 8 + (lane >> 5) * 4;
+                const int col = n0 + nt * 32 + q * 8 + (lane >> 5) * 4;
                 if (col >= g.N) continue;
-                const f32x4 v = {acc[mt][nt][q * 4], acc[mt][nt][q * 4 + 1], acc[mt][nt][q * 4 + 2], acc[mt][nt][q * 4 + 3]};
-                if constexpr (SPLIT) *reinterpret_cast<f32x4 *>(y + ((size_t)blockIdx.y * g.M + m) * (w.tiles * 16) + col) = v;
-                else mx_store<Y>(y, ldy, quads, m, col, g.N, v, w.ref, 0);
+                if constexpr (SPLIT) *reinterpret_cast<f32x4 *>(y + ((size_t)blockIdx.y * g.M + m) * (w.tiles * 16) + col) = quad(mt, nt, q);
+                else mx_store<Y>(y, ldy, quads, m, col, g.N, quad(mt, nt, q), w.ref, 0);
             }
     }
-    dma_wait<0>();                                        // what nobody reads: LDS must not be given back before it lands
 }
 
 // The planes of a product, added in order.
@@ -886,7 +962,7 @@ enum { MX_STREAM = 0 };
 //                                   stream     fed                                                    tile
 constexpr MxTile MX_TILES[] =      {{16, 16}, {16, 64}, {32, 128}, {32, 256}, {64, 128}, {64, 256}, {256, 256}};
 //                                   stream     fed                                                      block
-constexpr MxTile MX_BOTH_TILES[] = {{16, 16}, {16, 64}, {32, 128}, {64, 128}, {64, 256}, {128, 256}, {256, 256}};
+constexpr MxTile MX_BOTH_TILES[] = {{16, 16}, {16, 64}, {32, 128}, {64, 128}, {64, 256}, {256, 256}};
 
 static int mx_groups(int K) { return (K + 4 * MX_KSTEP - 1) / (4 * MX_KSTEP); }
 static int stream_waves(int kgroups) { return kgroups < 16 ? (kgroups < 8 ? kgroups : 8) : 16; }
@@ -900,7 +976,7 @@ static MxPlan gemm_plan_of(int M, int N, int groups) {
     return MxPlan{shape, s < 1 ? 1 : s};
 }
 static MxPlan both_plan_of(int M, int N, int groups) {
-    const int shape = M <= 4 ? 0 : M <= 16 ? 1 : M <= 32 ? 2 : M <= 64 ? 3 : M <= 128 ? 4 : M <= 512 ? 5 : 6;
+    const int shape = M <= 4 ? 0 : M <= 16 ? 1 : M <= 32 ? 2 : M <= 64 ? 3 : M <= 256 ? 4 : 5;
     const MxTile t = MX_BOTH_TILES[shape];
     const int tiles = ((M + t.tm - 1) / t.tm) * ((N + t.tn - 1) / t.tn);
     int s = shape == MX_STREAM ? 1 : 256 / tiles;
@@ -914,6 +990,11 @@ static bool rows_ok(int x_dt, const void *x, int64_t ldx, int K) {
 }
 static bool quads_ok(const void *y, int64_t ldy, int N, int y_dt) {
     return N % 4 == 0 && ldy % 4 == 0 && reinterpret_cast<uintptr_t>(y) % (4 * dtype_size(y_dt)) == 0;
+}
+
+// Whether rows of Y can be written in pieces of 16 bytes.
+template <typename Y> static bool wide_ok(const Y *y, int64_t ldy, int N) {
+    return reinterpret_cast<uintptr_t>(y) % 16 == 0 && ldy * sizeof(Y) % 16 == 0 && N * sizeof(Y) % 16 == 0;
 }
 
 static MxRows stage(int x_dt, const void *x, int64_t ldx, int M, int K, int kp, void *scratch, hipStream_t st) {
@@ -954,10 +1035,11 @@ static void run_gemm(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan 
     const MxTile t = MX_TILES[p.shape];
     g.splits = p.splits; g.tiles_m = (g.M + t.tm - 1) / t.tm; g.tiles_n = (g.N + t.tn - 1) / t.tn;
     const dim3 grid(g.tiles_m * g.tiles_n, g.splits);
+    const bool wide = wide_ok(y, ldy, g.N);
 #define POSS_MX_FED(TM, TN, WM, WN, FW, KS)                                                                                                  \
     do {                                                                                                                                     \
-        if (g.splits > 1) mx_fed_kernel<T, float, TM, TN, WM, WN, FW, KS, true><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, part, 0, false); \
-        else mx_fed_kernel<T, Y, TM, TN, WM, WN, FW, KS, false><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, y, ldy, quads);               \
+        if (g.splits > 1) mx_fed_kernel<T, float, TM, TN, WM, WN, FW, KS, true><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, part, 0, true, true); \
+        else mx_fed_kernel<T, Y, TM, TN, WM, WN, FW, KS, false><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, y, ldy, quads, wide);         \
     } while (0)
     switch (p.shape) {
         case 1: POSS_MX_FED(16, 64, 1, 4, 2, 4); break;
@@ -966,8 +1048,8 @@ static void run_gemm(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan 
         case 4: POSS_MX_FED(64, 128, 2, 4, 4, 4); break;
         case 5: POSS_MX_FED(64, 256, 1, 8, 4, 4); break;
         default:
-            if (g.splits > 1) mx_tile_kernel<T, float, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(w, x, g, part, 0, false);
-            else mx_tile_kernel<T, Y, 256, 256, 2, 4, false><<<grid, 512, 0, st>>>(w, x, g, y, ldy, quads);
+            if (g.splits > 1) mx_tile_kernel<T, float, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(w, x, g, part, 0, true, true);
+            else mx_tile_kernel<T, Y, 256, 256, 2, 4, false><<<grid, 512, 0, st>>>(w, x, g, y, ldy, quads, wide);
     }
 #undef POSS_MX_FED
     if (g.splits > 1) add_planes<Y>(w, part, g.splits, g.M, g.N, MxOp<T>::SHIFT, y, ldy, quads, st);
@@ -984,22 +1066,22 @@ static void run_both(const MxPacked &w, const u32x4 *x, const uint8_t *xs, int b
     const MxTile t = MX_BOTH_TILES[p.shape];
     g.splits = p.splits; g.tiles_m = (g.M + t.tm - 1) / t.tm; g.tiles_n = (g.N + t.tn - 1) / t.tn;
     const dim3 grid(g.tiles_m * g.tiles_n, g.splits);
+    const bool wide = wide_ok(y, ldy, g.N);
 #define POSS_MX_FED(TM, TN, WM, WN, FW, KG)                                                                                                        \
     do {                                                                                                                                           \
-        if (g.splits > 1) mx_fed_both_kernel<float, TM, TN, WM, WN, FW, KG, true><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, xs, blocks, g, part, 0, false); \
-        else mx_fed_both_kernel<Y, TM, TN, WM, WN, FW, KG, false><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, xs, blocks, g, y, ldy, quads);       \
+        if (g.splits > 1) mx_fed_both_kernel<float, TM, TN, WM, WN, FW, KG, true><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, xs, blocks, g, part, 0, true, true); \
+        else mx_fed_both_kernel<Y, TM, TN, WM, WN, FW, KG, false><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, xs, blocks, g, y, ldy, quads, wide); \
     } while (0)
     switch (p.shape) {
         case 1: POSS_MX_FED(16, 64, 1, 4, 2, 1); break;
         case 2: POSS_MX_FED(32, 128, 1, 8, 4, 1); break;
         case 3: POSS_MX_FED(64, 128, 1, 8, 4, 2); break;
         case 4: POSS_MX_FED(64, 256, 1, 8, 4, 2); break;
-        case 5: POSS_MX_FED(128, 256, 2, 4, 4, 2); break;
         default: {
             const int rts = (g.M + 15) / 16;
             mx_scales_kernel<<<dim3((w.kgroups * 64 + 255) / 256, rts < 65535 ? rts : 65535), 256, 0, st>>>(xs, g.M, blocks, w.kgroups, xscales);
-            if (g.splits > 1) mx_block_both_kernel<float, true><<<grid, 512, 0, st>>>(w, x, xscales, blocks, g, part, 0, false);
-            else mx_block_both_kernel<Y, false><<<grid, 512, 0, st>>>(w, x, xscales, blocks, g, y, ldy, quads);
+            if (g.splits > 1) mx_block_both_kernel<float, true><<<grid, 512, 0, st>>>(w, x, xscales, blocks, g, part, 0, true, true);
+            else mx_block_both_kernel<Y, false><<<grid, 512, 0, st>>>(w, x, xscales, blocks, g, y, ldy, quads, wide);
         }
     }
 #undef POSS_MX_FED
