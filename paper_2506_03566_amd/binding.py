@@ -386,102 +386,104 @@ def gemm_static(dtype, x, w, y, target_workgroups=0, stream=None):
         raise PossError(rc, lib.poss_last_error(None).decode())
 
 
-# ---- microscaled 4-bit weights
+# ---- microscaled 4-bit weights.  Small products take a few microseconds: what these functions do for a call is kept short.
 MX_BLOCK = 32
 _MX = 4                              # POSS_MX: activations that are microscaled too
+
+
+class _MxState:
+    """What the calls below look up once: the library, torch, its types' codes, and how to read a device's current stream."""
+    lib = None
+
+    def open(self):
+        import torch
+        self.lib, self.torch, self.u8 = load_library(), torch, torch.uint8
+        self.types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.current = raw if raw is not None else lambda dev: torch.cuda.current_stream(dev).cuda_stream
+        return self
+
+
+_mx = _MxState()
 
 
 def _mx_refuse(msg):
     raise PossError(E_INVALID_ARG, msg)
 
 
-def _mx_dtype(t):
-    import torch
-    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t)
+def _mx_type(t):
+    code = (_mx if _mx.lib else _mx.open()).types.get(t)
     return _mx_refuse("float32, bfloat16 or float16 is wanted, not %s" % t) if code is None else code
 
 
-def _mx_rows(t, what):
-    """Address and row distance of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        _mx_refuse("%s must be a matrix with contiguous rows" % what)
-    rows, cols = t.shape
+def _mx_rows(t, rows, cols, what):
+    """The row distance of a matrix [rows, cols] whose rows are contiguous."""
+    if t.dim() != 2 or t.size(0) != rows or t.size(1) != cols:
+        _mx_refuse("%s [%d, %d] is wanted, got %s" % (what, rows, cols, tuple(t.shape)))
     ld = t.stride(0) if rows > 1 else cols
-    if ld < cols:
-        _mx_refuse("%s must not have overlapping rows" % what)
-    return t.data_ptr(), ld
+    if ld < cols or (cols > 1 and t.stride(1) != 1):
+        _mx_refuse("%s must have contiguous rows that do not overlap" % what)
+    return ld
 
 
-def _mx_blocks(codes, scales, rows, cols, what):
-    import torch
+def _mx_pair(codes, scales, rows, cols, what):
     nb = (cols + MX_BLOCK - 1) // MX_BLOCK
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or tuple(codes.shape) != (rows, nb * 16) or tuple(scales.shape) != (rows, nb) \
+    if codes.dtype is not _mx.u8 or scales.dtype is not _mx.u8 or codes.shape != (rows, nb * 16) or scales.shape != (rows, nb) \
             or not codes.is_contiguous() or not scales.is_contiguous():
         _mx_refuse("%s: contiguous uint8 codes [%d, %d] and scales [%d, %d] are wanted" % (what, rows, nb * 16, rows, nb))
 
 
-class _MxCall:
-    """Makes the tensors' GPU current around a call and finds the stream: the caller's, or torch's current one there."""
-
-    def __init__(self, stream, *tensors):
-        import torch
-        dev = tensors[0].device
-        for t in tensors:
-            if not t.is_cuda or t.device != dev:
-                _mx_refuse("all tensors of a call must be on one GPU")
-        self.back = torch.cuda.current_device()
-        self.dev = dev.index
-        self.stream = c_vp((stream if stream is not None else torch.cuda.current_stream(dev)).cuda_stream)
-
-    def __enter__(self):
-        if self.dev != self.back:
-            import torch
-            torch.cuda.set_device(self.dev)
-        return self.stream
-
-    def __exit__(self, *exc):
-        if self.dev != self.back:
-            import torch
-            torch.cuda.set_device(self.back)
+def _mx_call(f, stream, tensors, *args):
+    """f(*args, stream) with the tensors' GPU current, on the stream given or torch's current one there."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != dev or dev < 0:
+            _mx_refuse("all tensors of a call must be on one GPU")
+    st = stream.cuda_stream if stream is not None else _mx.current(dev)
+    back = _mx.torch.cuda.current_device()
+    if back == dev:
+        rc = f(*args, st)
+    else:
+        _mx.torch.cuda.set_device(dev)
+        try:
+            rc = f(*args, st)
+        finally:
+            _mx.torch.cuda.set_device(back)
+    if rc != POSS_OK:
+        raise PossError(rc, _mx.lib.poss_last_error(None).decode())
 
 
 def _mx_empty(shape, device, stream):
     """Memory of the stream that will use it: torch's allocator hands a freed block on within one stream only."""
-    import torch
+    torch = _mx.torch
     if stream is None:
         return torch.empty(shape, dtype=torch.uint8, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=torch.uint8, device=device)
 
 
-def _mx_check(rc):
-    if rc != POSS_OK:
-        raise PossError(rc, load_library().poss_last_error(None).decode())
-
-
 def mx_quantize(x, codes=None, scales=None, stream=None):
     """Rows of x (float32, bfloat16, float16) as 4-bit codes with a scale per 32 values.  codes [rows, ceil(cols/32)*16] and scales
     [rows, ceil(cols/32)], uint8, are allocated if not given.  stream: torch's current one unless given.  Returns (codes, scales)."""
-    p, ld = _mx_rows(x, "x")
-    rows, cols = x.shape
-    nb = (cols + MX_BLOCK - 1) // MX_BLOCK
-    if codes is None:
-        codes = _mx_empty((rows, nb * 16), x.device, stream)
-    if scales is None:
-        scales = _mx_empty((rows, nb), x.device, stream)
-    _mx_blocks(codes, scales, rows, cols, "mx_quantize")
-    with _MxCall(stream, x, codes, scales) as st:
-        _mx_check(load_library().poss_mx_quantize(_mx_dtype(x.dtype), p, ld, rows, cols, codes.data_ptr(), scales.data_ptr(), st))
+    t = _mx_type(x.dtype)
+    rows, cols = x.shape if x.dim() == 2 else _mx_refuse("x must be a matrix")
+    ld = _mx_rows(x, rows, cols, "x")
+    if codes is None or scales is None:
+        nb = (cols + MX_BLOCK - 1) // MX_BLOCK
+        codes = _mx_empty((rows, nb * 16), x.device, stream) if codes is None else codes
+        scales = _mx_empty((rows, nb), x.device, stream) if scales is None else scales
+    _mx_pair(codes, scales, rows, cols, "mx_quantize")
+    _mx_call(_mx.lib.poss_mx_quantize, stream, (x, codes, scales), t, x.data_ptr(), ld, rows, cols, codes.data_ptr(), scales.data_ptr())
     return codes, scales
 
 
 def mx_dequantize(codes, scales, y, stream=None):
     """What codes and scales stand for, into y [rows, cols] (float32, bfloat16, float16).  Returns y."""
-    p, ld = _mx_rows(y, "y")
-    rows, cols = y.shape
-    _mx_blocks(codes, scales, rows, cols, "mx_dequantize")
-    with _MxCall(stream, y, codes, scales) as st:
-        _mx_check(load_library().poss_mx_dequantize(_mx_dtype(y.dtype), codes.data_ptr(), scales.data_ptr(), rows, cols, p, ld, st))
+    t = _mx_type(y.dtype)
+    rows, cols = y.shape if y.dim() == 2 else _mx_refuse("y must be a matrix")
+    ld = _mx_rows(y, rows, cols, "y")
+    _mx_pair(codes, scales, rows, cols, "mx_dequantize")
+    _mx_call(_mx.lib.poss_mx_dequantize, stream, (y, codes, scales), t, codes.data_ptr(), scales.data_ptr(), rows, cols, y.data_ptr(), ld)
     return y
 
 
@@ -494,17 +496,21 @@ class MxWeight:
 
 def mx_pack(codes, scales, K, stream=None):
     """The weight matrix [N, K] that codes and scales hold, laid out once for mx_gemm and mx_gemm_mx."""
-    lib, N = load_library(), codes.shape[0]
-    _mx_blocks(codes, scales, N, K, "mx_pack")
-    packed = _mx_empty(max(256, lib.poss_mx_packed_bytes(N, K)), codes.device, stream)
-    with _MxCall(stream, codes, scales) as st:
-        _mx_check(lib.poss_mx_pack(codes.data_ptr(), scales.data_ptr(), N, K, packed.data_ptr(), st))
+    lib, N = (_mx if _mx.lib else _mx.open()).lib, codes.shape[0]
+    _mx_pair(codes, scales, N, K, "mx_pack")
+    need = lib.poss_mx_packed_bytes(N, K)
+    if need == 0:
+        _mx_refuse("mx_pack: shape rejected")
+    packed = _mx_empty(need, codes.device, stream)
+    _mx_call(lib.poss_mx_pack, stream, (codes, scales), codes.data_ptr(), scales.data_ptr(), N, K, packed.data_ptr())
     return MxWeight(packed, N, K)
 
 
 def mx_gemm_scratch(dtype, M, N, K, device="cuda", stream=None):
-    """Scratch for a product of this shape: dtype of the activations, None for microscaled ones."""
-    need = load_library().poss_mx_gemm_scratch_bytes(_MX if dtype is None else _mx_dtype(dtype), M, N, K)
+    """Scratch for a product of this shape: dtype of the activations, None for microscaled ones.  One that is large enough serves
+    other shapes too."""
+    t = _MX if dtype is None else _mx_type(dtype)
+    need = (_mx if _mx.lib else _mx.open()).lib.poss_mx_gemm_scratch_bytes(t, M, N, K)
     if need == 0:
         _mx_refuse("shape rejected")
     return _mx_empty(need, device, stream)
@@ -513,29 +519,24 @@ def mx_gemm_scratch(dtype, M, N, K, device="cuda", stream=None):
 def mx_gemm(x, w, y, scratch=None, stream=None):
     """y [M, N] = x [M, K] . w^T for an MxWeight; x and y float32, bfloat16 or float16.  scratch: a uint8 tensor from mx_gemm_scratch
     that no other call uses at the same time; allocated per call if not given.  Returns y."""
-    px, ldx = _mx_rows(x, "x")
-    py, ldy = _mx_rows(y, "y")
-    M = x.shape[0]
-    if x.shape[1] != w.K or tuple(y.shape) != (M, w.N):
-        _mx_refuse("mx_gemm: x [M, %d] and y [M, %d] are wanted, got %s and %s" % (w.K, w.N, tuple(x.shape), tuple(y.shape)))
+    tx, ty = _mx_type(x.dtype), _mx_type(y.dtype)
+    M, N, K = x.size(0), w.N, w.K
+    ldx, ldy = _mx_rows(x, M, K, "x"), _mx_rows(y, M, N, "y")
     if scratch is None:
-        scratch = mx_gemm_scratch(x.dtype, M, w.N, w.K, x.device, stream)
-    with _MxCall(stream, x, y, w.packed, scratch) as st:
-        _mx_check(load_library().poss_mx_gemm(_mx_dtype(x.dtype), px, ldx, w.packed.data_ptr(), _mx_dtype(y.dtype), py, ldy, M, w.N, w.K,
-                                              scratch.data_ptr(), scratch.numel(), st))
+        scratch = mx_gemm_scratch(x.dtype, M, N, K, x.device, stream)
+    _mx_call(_mx.lib.poss_mx_gemm, stream, (x, y, w.packed, scratch), tx, x.data_ptr(), ldx, w.packed.data_ptr(), ty, y.data_ptr(), ldy, M, N, K,
+             scratch.data_ptr(), scratch.nbytes)
     return y
 
 
 def mx_gemm_mx(codes, scales, w, y, scratch=None, stream=None):
     """y [M, N] = x . w^T for x [M, K] as mx_quantize left it: both operands in 4 bits.  Returns y."""
-    py, ldy = _mx_rows(y, "y")
-    M = codes.shape[0]
-    _mx_blocks(codes, scales, M, w.K, "mx_gemm_mx")
-    if tuple(y.shape) != (M, w.N):
-        _mx_refuse("mx_gemm_mx: y [%d, %d] is wanted, got %s" % (M, w.N, tuple(y.shape)))
+    ty = _mx_type(y.dtype)
+    M, N, K = codes.size(0), w.N, w.K
+    ldy = _mx_rows(y, M, N, "y")
+    _mx_pair(codes, scales, M, K, "mx_gemm_mx")
     if scratch is None:
-        scratch = mx_gemm_scratch(None, M, w.N, w.K, y.device, stream)
-    with _MxCall(stream, y, codes, scales, w.packed, scratch) as st:
-        _mx_check(load_library().poss_mx_gemm_mx(codes.data_ptr(), scales.data_ptr(), w.packed.data_ptr(), _mx_dtype(y.dtype), py, ldy, M, w.N, w.K,
-                                                 scratch.data_ptr(), scratch.numel(), st))
+        scratch = mx_gemm_scratch(None, M, N, K, y.device, stream)
+    _mx_call(_mx.lib.poss_mx_gemm_mx, stream, (y, codes, scales, w.packed, scratch), codes.data_ptr(), scales.data_ptr(), w.packed.data_ptr(), ty, y.data_ptr(), ldy,
+             M, N, K, scratch.data_ptr(), scratch.nbytes)
     return y

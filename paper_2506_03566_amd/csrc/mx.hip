@@ -17,58 +17,111 @@
 namespace poss {
 
 // ------------------------------------------------------------------------------------------ quantisation
-// Four lanes per block, eight values each; scale byte = exponent field of the block's largest magnitude - 2, at least 0: the largest
-// magnitude lies in [4, 8) then, and 6 to 8 saturates.  The division is by a power of two, the rounding (to nearest, ties to even)
-// the instruction's.
-template <typename T> __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ x, int64_t ldx, int rows, int cols, int blocks,
-                                                                                uint32_t *__restrict__ codes, uint8_t *__restrict__ scales) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (blocks * 4);
-    const int piece = (int)(i - row * (blocks * 4));       // of eight values
-    float v[8];
-    float top = 0.f;
-    unsigned special = 0;
+// Bound by memory.  Four lanes per block, a piece of eight values each: 16 or 32 bytes read, a word of codes written.  Scale byte = exponent field of
+// the block's largest magnitude - 2, at least 0: that magnitude lies in [4, 8) then, and 6 to 8 saturates.  Magnitudes compare as integers,
+// NaN above infinity above the rest.  The conversion instruction divides by the power of two and rounds to nearest, ties to even.
+// A matrix without gaps whose rows are whole blocks is one long row (`flat`: no division per piece).
+template <typename T> struct MxIn;
+template <> struct MxIn<float> {
+    union { u32x4 u[2]; float e[8]; unsigned w[8]; } v;
+    __device__ __forceinline__ void load(const float *p) { v.u[0] = reinterpret_cast<const u32x4 *>(p)[0]; v.u[1] = reinterpret_cast<const u32x4 *>(p)[1]; }
+    __device__ __forceinline__ void set(int j, float x) { v.e[j] = x; }
+    __device__ __forceinline__ unsigned top() const {
+        unsigned m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int c = piece * 8 + j;
-        v[j] = row < rows && c < cols ? to_f(x[row * ldx + c]) : 0.f;
-        const unsigned bits = __builtin_bit_cast(unsigned, v[j]) & 0x7fffffffu;
-        special |= bits >= 0x7f800000u;
-        top = fmaxf(top, fabsf(v[j]));
+        for (int j = 0; j < 8; ++j) m = max(m, v.w[j] & 0x7fffffffu);
+        return m;
     }
-    unsigned field = special ? 255u : __builtin_bit_cast(unsigned, top) >> 23;
-    field = max(field, (unsigned)__shfl_xor((int)field, 1));
-    field = max(field, (unsigned)__shfl_xor((int)field, 2));
-    const unsigned s = field == 255 ? 255u : field < 2 ? 0u : field - 2;
-    const float inv = field == 255 ? 0.f : __builtin_bit_cast(float, (254u - s) << 23);   // 2^(127 - s)
-    unsigned q = 0;
-    if (field != 255) {
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[0] * inv, v[1] * inv, 1.0f, 0);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[2] * inv, v[3] * inv, 1.0f, 1);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[4] * inv, v[5] * inv, 1.0f, 2);
-        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[6] * inv, v[7] * inv, 1.0f, 3);
+    __device__ __forceinline__ unsigned codes(float s) const {
+        unsigned q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v.e[0], v.e[1], s, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v.e[2], v.e[3], s, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v.e[4], v.e[5], s, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v.e[6], v.e[7], s, 3);
     }
-    if (row >= rows) return;
-    codes[i] = q;
-    if ((piece & 3) == 0) scales[i >> 2] = (uint8_t)s;
+};
+template <typename T> struct MxIn16 {
+    union { u32x4 u; T e[8]; } v;
+    __device__ __forceinline__ void load(const T *p) { v.u = *reinterpret_cast<const u32x4 *>(p); }
+    __device__ __forceinline__ void set(int j, T x) { v.e[j] = x; }
+    __device__ __forceinline__ unsigned top() const {      // the largest magnitude's 16 bits
+        unsigned m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = max(m, max(v.u[j] & 0x7fffu, v.u[j] >> 16 & 0x7fffu));
+        return m;
+    }
+};
+template <> struct MxIn<bf16_t> : MxIn16<bf16_t> {
+    __device__ __forceinline__ unsigned top() const { return MxIn16<bf16_t>::top() << 16; }
+    __device__ __forceinline__ unsigned codes(float s) const {
+        const bf16x2 *p = reinterpret_cast<const bf16x2 *>(&v);
+        unsigned q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, p[0], s, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, p[1], s, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, p[2], s, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, p[3], s, 3);
+    }
+};
+template <> struct MxIn<f16_t> : MxIn16<f16_t> {
+    __device__ __forceinline__ unsigned top() const {
+        const uint16_t b = (uint16_t)MxIn16<f16_t>::top();
+        return __builtin_bit_cast(unsigned, (float)__builtin_bit_cast(f16_t, b));      // (infinity and NaN stay above the rest)
+    }
+    __device__ __forceinline__ unsigned codes(float s) const {
+        const f16x2 *p = reinterpret_cast<const f16x2 *>(&v);
+        unsigned q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(0u, p[0], s, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(q, p[1], s, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(q, p[2], s, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(q, p[3], s, 3);
+    }
+};
+__device__ __forceinline__ unsigned quad_max(unsigned v) {
+    v = max(v, __builtin_bit_cast(unsigned, xor1(__builtin_bit_cast(float, v))));
+    return max(v, __builtin_bit_cast(unsigned, xor2(__builtin_bit_cast(float, v))));
 }
 
-template <typename T> __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales,
-                                                                                  int rows, int cols, int blocks, T *__restrict__ y, int64_t ldy) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (blocks * 4);
-    if (row >= rows) return;
-    const int piece = (int)(i - row * (blocks * 4));
-    const unsigned q = codes[i];
-    const float s = mx_power(scales[i >> 2]);
-    float v[8];
+// Piece i of a matrix of `pieces` pieces a row (a multiple of four): its row and place.  Index: 32 bits wherever they hold all pieces.
+template <typename I> __device__ __forceinline__ void piece_at(I i, int pieces, bool flat, int64_t &row, int64_t &piece) {
+    if (flat) { row = 0; piece = (int64_t)i; }
+    else { const I r = i / (I)pieces; row = (int64_t)r; piece = (int64_t)(i - r * (I)pieces); }
+}
+
+// wide: rows of x can be read in pieces of 16 bytes.
+template <typename T, typename I> __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ x, int64_t ldx, int64_t total, int64_t cols, int pieces, bool flat,
+                                                                                            bool wide, uint32_t *__restrict__ codes, uint8_t *__restrict__ scales) {
+    for (I i = (I)blockIdx.x * 256 + threadIdx.x; i < (I)total; i += (I)gridDim.x * 256) {       // (total is a multiple of four: the lanes of a block go together)
+        int64_t row, piece;
+        piece_at<I>(i, pieces, flat, row, piece);
+        const T *p = x + row * ldx + piece * 8;
+        MxIn<T> in;
+        if (wide && piece * 8 + 8 <= cols) in.load(p);
+        else
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const f32x2 p = j == 0 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0) : j == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1)
-                      : j == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3);
-        v[2 * j] = p.x * s; v[2 * j + 1] = p.y * s;
+            for (int j = 0; j < 8; ++j) in.set(j, piece * 8 + j < cols ? p[j] : from_f<T>(0.f));
+        const unsigned field = quad_max(in.top()) >> 23, s = field == 255 ? 255u : field < 2 ? 0u : field - 2;
+        codes[i] = field == 255 ? 0u : in.codes(mx_power(s));
+        if ((i & 3) == 0) scales[i >> 2] = (uint8_t)s;
     }
+}
+
+template <typename T> struct __attribute__((aligned(16))) MxOut { T v[8]; };
+template <typename T, typename I> __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t total,
+                                                                                              int64_t cols, int pieces, bool flat, bool wide, T *__restrict__ y, int64_t ldy) {
+    for (I i = (I)blockIdx.x * 256 + threadIdx.x; i < (I)total; i += (I)gridDim.x * 256) {
+        int64_t row, piece;
+        piece_at<I>(i, pieces, flat, row, piece);
+        const unsigned q = codes[i];
+        const float s = mx_power(scales[i >> 2]);
+        MxOut<T> o;
+        // (values times the power of two in float32, exactly; then rounded to T once)
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),
+                    c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 3);
+        o.v[0] = from_f<T>(a.x * s); o.v[1] = from_f<T>(a.y * s); o.v[2] = from_f<T>(b.x * s); o.v[3] = from_f<T>(b.y * s);
+        o.v[4] = from_f<T>(c.x * s); o.v[5] = from_f<T>(c.y * s); o.v[6] = from_f<T>(d.x * s); o.v[7] = from_f<T>(d.y * s);
+        T *p = y + row * ldy + piece * 8;
+        if (wide && piece * 8 + 8 <= cols) *reinterpret_cast<MxOut<T> *>(p) = o;
+        else
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (piece * 8 + j < cols) y[row * ldy + piece * 8 + j] = from_f<T>(v[j]);
+            for (int j = 0; j < 8; ++j) if (piece * 8 + j < cols) p[j] = o.v[j];
+    }
 }
 
 // ------------------------------------------------------------------------------------------ packing
@@ -133,25 +186,40 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ 
 }
 
 // ------------------------------------------------------------------------------------------ launches
-static unsigned grid_of(int64_t threads) { return (unsigned)((threads + 255) / 256); }
+// A matrix as the kernels walk it.
+struct MxWalk { int64_t total, cols; int pieces; bool flat, wide, small; unsigned grid; };
+static MxWalk walk_of(int dt, const void *rows_at, int64_t ld, int rows, int cols) {
+    MxWalk k;
+    k.pieces = mx_blocks(cols) * 4;
+    k.total = (int64_t)rows * k.pieces;
+    k.flat = cols % MX_BLOCK == 0 && (ld == cols || rows == 1);
+    k.cols = k.flat ? (int64_t)rows * cols : cols;
+    k.wide = reinterpret_cast<uintptr_t>(rows_at) % 16 == 0 && (rows == 1 || ld * dtype_size(dt) % 16 == 0);
+    k.small = k.total < (1ll << 31);
+    const int64_t g = (k.total + 255) / 256;
+    k.grid = (unsigned)(g < (1 << 20) ? g : 1 << 20);
+    return k;
+}
+
+#define POSS_MX_TYPES(KERNEL, ...)                                                                                   \
+    do {                                                                                                             \
+        if (dt == DT_F32) { typedef float T; if (k.small) KERNEL<T, uint32_t> __VA_ARGS__; else KERNEL<T, uint64_t> __VA_ARGS__; }          \
+        else if (dt == DT_BF16) { typedef bf16_t T; if (k.small) KERNEL<T, uint32_t> __VA_ARGS__; else KERNEL<T, uint64_t> __VA_ARGS__; }   \
+        else { typedef f16_t T; if (k.small) KERNEL<T, uint32_t> __VA_ARGS__; else KERNEL<T, uint64_t> __VA_ARGS__; }                       \
+    } while (0)
 
 void launch_mx_quantize(int dt, const void *x, int64_t ldx, int rows, int cols, void *codes, void *scales, hipStream_t st) {
-    const int nb = mx_blocks(cols);
-    const dim3 grid(grid_of((int64_t)rows * nb * 4));
-    uint32_t *c = static_cast<uint32_t *>(codes); uint8_t *s = static_cast<uint8_t *>(scales);
-    if (dt == DT_F32) mx_quantize_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float *>(x), ldx, rows, cols, nb, c, s);
-    else if (dt == DT_BF16) mx_quantize_kernel<bf16_t><<<grid, 256, 0, st>>>(static_cast<const bf16_t *>(x), ldx, rows, cols, nb, c, s);
-    else mx_quantize_kernel<f16_t><<<grid, 256, 0, st>>>(static_cast<const f16_t *>(x), ldx, rows, cols, nb, c, s);
+    const MxWalk k = walk_of(dt, x, ldx, rows, cols);
+    POSS_MX_TYPES(mx_quantize_kernel, <<<k.grid, 256, 0, st>>>(static_cast<const T *>(x), ldx, k.total, k.cols, k.pieces, k.flat, k.wide, static_cast<uint32_t *>(codes),
+                                                               static_cast<uint8_t *>(scales)));
 }
 
 void launch_mx_dequantize(int dt, const void *codes, const void *scales, int rows, int cols, void *y, int64_t ldy, hipStream_t st) {
-    const int nb = mx_blocks(cols);
-    const dim3 grid(grid_of((int64_t)rows * nb * 4));
-    const uint32_t *c = static_cast<const uint32_t *>(codes); const uint8_t *s = static_cast<const uint8_t *>(scales);
-    if (dt == DT_F32) mx_dequantize_kernel<float><<<grid, 256, 0, st>>>(c, s, rows, cols, nb, static_cast<float *>(y), ldy);
-    else if (dt == DT_BF16) mx_dequantize_kernel<bf16_t><<<grid, 256, 0, st>>>(c, s, rows, cols, nb, static_cast<bf16_t *>(y), ldy);
-    else mx_dequantize_kernel<f16_t><<<grid, 256, 0, st>>>(c, s, rows, cols, nb, static_cast<f16_t *>(y), ldy);
+    const MxWalk k = walk_of(dt, y, ldy, rows, cols);
+    POSS_MX_TYPES(mx_dequantize_kernel, <<<k.grid, 256, 0, st>>>(static_cast<const uint32_t *>(codes), static_cast<const uint8_t *>(scales), k.total, k.cols, k.pieces, k.flat,
+                                                                 k.wide, static_cast<T *>(y), ldy));
 }
+#undef POSS_MX_TYPES
 
 void launch_mx_pack(const void *codes, const void *scales, int N, int K, void *packed, hipStream_t st) {
     const MxPacked w = mx_packed_at(packed, N, K);

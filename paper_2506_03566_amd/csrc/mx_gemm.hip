@@ -9,6 +9,8 @@
 // columns of a row of Y.
 #include "mx.h"
 
+#include <math.h>
+
 namespace poss {
 
 constexpr int F16_SHIFT = 13;     // fp16 operands carry 2^13: 6 * 2^13 is finite, and c * 2^(s - ref) exact down to s = ref - 36
@@ -131,191 +133,121 @@ template <typename X> __global__ __launch_bounds__(256) void mx_stage_kernel(con
 }
 
 // ------------------------------------------------------------------------------------------ few rows
-// Up to 64 rows: the weights are what is read.  A workgroup owns NT column tiles and all of K, cut among its waves in whole groups of four
-// k-steps; each wave reads its weights (1 KB per tile and k-step, contiguous) and its part of X (from the L2) straight into
-// operand registers, the next group's on the way while this one is multiplied, and the waves' sums are added in LDS, in wave order.
-// No planes, no second launch.
+// Up to sixteen rows: a workgroup owns a column tile and all of K, cut among its waves in whole groups of four k-steps.  Each wave reads its
+// weights (1 KB per k-step, contiguous) and its part of X (from the L2) straight into operand registers, the next group's on the way while this
+// one is multiplied; the waves' sums are added in LDS, in wave order.  Nothing is waited for but memory: one row of 28672 x 4096 13.0 us
+// (62.5 MB; a copy reads and writes as much in 12.5), 4096 x 4096 3.4.  With rows X counts (16 bytes at a time, once per column tile): 16 rows 30 us,
+// where mx_fed_kernel takes 12.8.
+// The waves' sums in the first wave (true there).
+__device__ __forceinline__ bool mx_stream_sum(f32x4 *red, f32x4 &acc) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    red[wave * 64 + lane] = acc;
+    __syncthreads();
+    if (wave) return false;
+    for (int v = 1; v < waves; ++v) acc += red[v * 64 + lane];
+    return true;
+}
+
 template <typename T, typename Y, int PARTS>
 __global__ __launch_bounds__(1024) void mx_stream_kernel(MxPacked w, MxRows x, Y *__restrict__ y, int64_t ldy, bool quads, int M, int N) {
     extern __shared__ f32x4 red[];
     typedef MxOp<T> Op;
-    constexpr int MT = 1, NT = 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int ct0 = blockIdx.x * NT, g0 = wave * w.kgroups / waves, g1 = (wave + 1) * w.kgroups / waves;
-    f32x4 acc[MT][NT];
+    const int ct = blockIdx.x, g0 = wave * w.kgroups / waves, g1 = (wave + 1) * w.kgroups / waves, kl = (lane >> 4) * MX_BLOCK;     // (every wave has a group)
+    const u32x4 *wp = w.codes + ((size_t)ct * w.ksteps + g0 * 4) * 64 + lane;
+    const uint32_t *sp = w.scales + ((size_t)ct * w.kgroups + g0) * 64 + lane;
+    const T *xp = static_cast<const T *>(x.x) + (int64_t)min(lane & 15, M - 1) * x.ldx + g0 * 4 * MX_KSTEP + kl;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    u32x4 c[4], xv[4][PARTS];
+    uint32_t next = *sp;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int s = 0; s < 4; ++s) c[s] = wp[s * 64];
+    // piece i of k-step s of the group at g
+    auto load_x = [&](auto tail, int g, int s, int i) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (g0 < g1) {
-        const u32x4 *wp[NT];
-        const uint32_t *sp[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int ct = min(ct0 + nt, w.tiles - 1);    // tiles beyond the matrix repeat the last one (never stored)
-            wp[nt] = w.codes + ((size_t)ct * w.ksteps + g0 * 4) * 64 + lane;
-            sp[nt] = w.scales + ((size_t)ct * w.kgroups + g0) * 64 + lane;
+        for (int p = 0; p < PARTS; ++p) {
+            const T *a = xp + p * x.part + s * MX_KSTEP + i * 8;
+            if constexpr (decltype(tail)::value) a = (g * 4 + s) * MX_KSTEP + kl + i * 8 < x.K ? a : reinterpret_cast<const T *>(&mx_zero_piece);
+            xv[i][p] = *reinterpret_cast<const u32x4 *>(a);
         }
-        const T *xp[MT];
-        const int kl = (lane >> 4) * MX_BLOCK;
+    };
+    // one group; `more`: another follows, whose weights are asked for as this one's are used up; `tail`: X ends in it
+    auto group = [&](auto more, auto tail, int g) {
+        const uint32_t sc = next;
+        if constexpr (decltype(more)::value) { sp += 64; next = *sp; }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) xp[mt] = static_cast<const T *>(x.x) + (int64_t)min(mt * 16 + (lane & 15), M - 1) * x.ldx + g0 * 4 * MX_KSTEP + kl;
-        u32x4 c[4][NT], xv[4][PARTS][MT];
-        uint32_t sc[NT], sn[NT];
+        for (int i = 0; i < 4; ++i) load_x(tail, g, 0, i);
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+        for (int s = 0; s < 4; ++s) {
+            const float f = s == 0 ? mx_scale<T, 0>(sc) : s == 1 ? mx_scale<T, 1>(sc) : s == 2 ? mx_scale<T, 2>(sc) : mx_scale<T, 3>(sc);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) c[s][nt] = wp[nt][s * 64];
+            for (int i = 0; i < 4; ++i) {
+                const u32x4 v = Op::weights(c[s][i], f);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) sn[nt] = *sp[nt];
-        // piece i of k-step s (of the group at g) for every row tile
-        auto load_x = [&](auto tail, int g, int s, int i) {
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const T *a = xp[mt] + p * x.part + s * MX_KSTEP + i * 8;
-                    if constexpr (decltype(tail)::value) a = (g * 4 + s) * MX_KSTEP + kl + i * 8 < x.K ? a : reinterpret_cast<const T *>(&mx_zero_piece);
-                    xv[i][p][mt] = *reinterpret_cast<const u32x4 *>(a);
-                }
-        };
-        // one group; `more`: another follows, whose weights are asked for as this one's are used up
-        auto group = [&](auto more, auto tail, int g) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) { sc[nt] = sn[nt]; if constexpr (decltype(more)::value) { sp[nt] += 64; sn[nt] = *sp[nt]; } }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) load_x(tail, g, 0, i);
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                float f[NT];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) f[nt] = s == 0 ? mx_scale<T, 0>(sc[nt]) : s == 1 ? mx_scale<T, 1>(sc[nt]) : s == 2 ? mx_scale<T, 2>(sc[nt]) : mx_scale<T, 3>(sc[nt]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const u32x4 v = Op::weights(c[s][nt][i], f[nt]);
-#pragma unroll
-                        for (int p = PARTS - 1; p >= 0; --p)
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) acc[mt][nt] = Op::mfma(v, xv[i][p][mt], acc[mt][nt]);
-                    }
-                    if (s < 3) load_x(tail, g, s + 1, i);
-                }
-                if constexpr (decltype(more)::value)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) c[s][nt] = wp[nt][(s + 4) * 64];
+                for (int p = PARTS - 1; p >= 0; --p) acc = Op::mfma(v, xv[i][p], acc);
+                if (s < 3) load_x(tail, g, s + 1, i);
             }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) wp[nt] += 256;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) xp[mt] += 4 * MX_KSTEP;
-        };
-        int g = g0;
-        for (; g + 1 < g1; ++g) group(Yes{}, No{}, g);
-        if ((g + 1) * 4 * MX_KSTEP <= x.K) group(No{}, No{}, g); else group(No{}, Yes{}, g);
-    }
-    // the waves' sums
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) red[((wave * MT + mt) * NT + nt) * 64 + lane] = acc[mt][nt];
-    __syncthreads();
-    for (int i = threadIdx.x; i < MT * NT * 64; i += blockDim.x) {
-        f32x4 a = red[i];
-        for (int v = 1; v < waves; ++v) a += red[v * MT * NT * 64 + i];
-        const int l = i & 63, nt = (i >> 6) % NT, m = ((i >> 6) / NT) * 16 + (l & 15), n = (ct0 + nt) * 16 + (l >> 4) * 4;
-        if (m < M && n < N) mx_store<Y>(y, ldy, quads, m, n, N, a, w.ref, Op::SHIFT);
-    }
+            if constexpr (decltype(more)::value) c[s] = wp[(s + 4) * 64];
+        }
+        wp += 256;
+        xp += 4 * MX_KSTEP;
+    };
+    int g = g0;
+    for (; g + 1 < g1; ++g) group(Yes{}, No{}, g);
+    if ((g + 1) * 4 * MX_KSTEP <= x.K) group(No{}, No{}, g); else group(No{}, Yes{}, g);
+    if (!mx_stream_sum(red, acc)) return;
+    const int m = lane & 15, n = ct * 16 + (lane >> 4) * 4;
+    if (m < M && n < N) mx_store<Y>(y, ldy, quads, m, n, N, acc, w.ref, Op::SHIFT);
 }
 
-// The same with microscaled X: a block of 16 bytes and its scale per lane, row tile and k-step.
+// The same with microscaled X: a block of 16 bytes and its scale per lane and k-step.
 template <typename Y>
 __global__ __launch_bounds__(1024) void mx_stream_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint8_t *__restrict__ xs, int blocks, Y *__restrict__ y, int64_t ldy,
                                                               bool quads, int M, int N) {
     extern __shared__ f32x4 red[];
-    constexpr int MT = 1, NT = 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int ct0 = blockIdx.x * NT, g0 = wave * w.kgroups / waves, g1 = (wave + 1) * w.kgroups / waves;
-    f32x4 acc[MT][NT];
+    const int ct = blockIdx.x, g0 = wave * w.kgroups / waves, g1 = (wave + 1) * w.kgroups / waves;
+    const u32x4 *wp = w.codes + ((size_t)ct * w.ksteps + g0 * 4) * 64 + lane;
+    const uint32_t *sp = w.scales + ((size_t)ct * w.kgroups + g0) * 64 + lane;
+    const int64_t xr = (int64_t)min(lane & 15, M - 1) * blocks;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    u32x4 c[4], xv[4];
+    uint32_t next = *sp;
+    int xc[4];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int s = 0; s < 4; ++s) c[s] = wp[s * 64];
+    auto load_x = [&](int g, int s) {
+        const int b = (g * 4 + s) * 4 + (lane >> 4);
+        const bool in = b < blocks;                        // (a block of another row must not lend its scale: it may be NaN)
+        xv[s] = *(in ? x + xr + b : &mx_zero_piece);
+        const int t = xs[xr + (in ? b : blocks - 1)];
+        xc[s] = in ? t : 127;
+    };
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (g0 < g1) {
-        const u32x4 *wp[NT];
-        const uint32_t *sp[NT];
+    for (int s = 0; s < 4; ++s) load_x(g0, s);
+    auto group = [&](auto more, int g) {
+        const uint32_t sc = next;
+        if constexpr (decltype(more)::value) { sp += 64; next = *sp; }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int ct = min(ct0 + nt, w.tiles - 1);
-            wp[nt] = w.codes + ((size_t)ct * w.ksteps + g0 * 4) * 64 + lane;
-            sp[nt] = w.scales + ((size_t)ct * w.kgroups + g0) * 64 + lane;
+        for (int s = 0; s < 4; ++s) {
+            const i32x8 a = {(int)c[s].x, (int)c[s].y, (int)c[s].z, (int)c[s].w, 0, 0, 0, 0}, b = {(int)xv[s].x, (int)xv[s].y, (int)xv[s].z, (int)xv[s].w, 0, 0, 0, 0};
+            if (s == 0) acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, 0, (int)sc, 0, xc[s]);
+            else if (s == 1) acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, 1, (int)sc, 0, xc[s]);
+            else if (s == 2) acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, 2, (int)sc, 0, xc[s]);
+            else acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, 3, (int)sc, 0, xc[s]);
+            if constexpr (decltype(more)::value) {
+                c[s] = wp[(s + 4) * 64];
+                load_x(g + 1, s);
+            }
         }
-        int64_t xr[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) xr[mt] = (int64_t)min(mt * 16 + (lane & 15), M - 1) * blocks;
-        u32x4 c[4][NT], xv[4][MT];
-        uint32_t sc[NT], sn[NT];
-        int xc[4][MT];
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) c[s][nt] = wp[nt][s * 64];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) sn[nt] = *sp[nt];
-        auto load_x = [&](int g, int s) {
-            const int b = (g * 4 + s) * 4 + (lane >> 4);
-            const bool in = b < blocks;                    // (a block of another row must not lend its scale: it may be NaN)
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                xv[s][mt] = *(in ? x + xr[mt] + b : &mx_zero_piece);
-                const int t = xs[xr[mt] + (in ? b : blocks - 1)];
-                xc[s][mt] = in ? t : 127;
-            }
-        };
-#pragma unroll
-        for (int s = 0; s < 4; ++s) load_x(g0, s);
-        auto group = [&](auto more, int g) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) { sc[nt] = sn[nt]; if constexpr (decltype(more)::value) { sp[nt] += 64; sn[nt] = *sp[nt]; } }
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const i32x8 a = {(int)c[s][nt].x, (int)c[s][nt].y, (int)c[s][nt].z, (int)c[s][nt].w, 0, 0, 0, 0};
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        const i32x8 b = {(int)xv[s][mt].x, (int)xv[s][mt].y, (int)xv[s][mt].z, (int)xv[s][mt].w, 0, 0, 0, 0};
-                        if (s == 0) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[mt][nt], 4, 4, 0, (int)sc[nt], 0, xc[s][mt]);
-                        else if (s == 1) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[mt][nt], 4, 4, 1, (int)sc[nt], 0, xc[s][mt]);
-                        else if (s == 2) acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[mt][nt], 4, 4, 2, (int)sc[nt], 0, xc[s][mt]);
-                        else acc[mt][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[mt][nt], 4, 4, 3, (int)sc[nt], 0, xc[s][mt]);
-                    }
-                }
-                if constexpr (decltype(more)::value) {
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) c[s][nt] = wp[nt][(s + 4) * 64];
-                    load_x(g + 1, s);
-                }
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) wp[nt] += 256;
-        };
-        int g = g0;
-        for (; g + 1 < g1; ++g) group(Yes{}, g);
-        group(No{}, g);
-    }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) red[((wave * MT + mt) * NT + nt) * 64 + lane] = acc[mt][nt];
-    __syncthreads();
-    for (int i = threadIdx.x; i < MT * NT * 64; i += blockDim.x) {
-        f32x4 a = red[i];
-        for (int v = 1; v < waves; ++v) a += red[v * MT * NT * 64 + i];
-        const int l = i & 63, nt = (i >> 6) % NT, m = ((i >> 6) / NT) * 16 + (l & 15), n = (ct0 + nt) * 16 + (l >> 4) * 4;
-        if (m < M && n < N) mx_store<Y>(y, ldy, quads, m, n, N, a, w.ref, 0);
-    }
+        wp += 256;
+    };
+    int g = g0;
+    for (; g + 1 < g1; ++g) group(Yes{}, g);
+    group(No{}, g);
+    if (!mx_stream_sum(red, acc)) return;
+    const int m = lane & 15, n = ct * 16 + (lane >> 4) * 4;
+    if (m < M && n < N) mx_store<Y>(y, ldy, quads, m, n, N, acc, w.ref, 0);
 }
 
 // ------------------------------------------------------------------------------------------ many rows
@@ -955,33 +887,56 @@ __global__ __launch_bounds__(256) void mx_planes_kernel(const f32x4 *__restrict_
 }
 
 // ------------------------------------------------------------------------------------------ launches
-// How a product runs: a kernel and tile shape (below), K splits.
+// How a product runs: a kernel with its tile shape, and K splits.  Chosen by an estimate of the time in us: for each shape the sum of eight
+// terms whose weights were fitted (none negative) to measured times of 19 row counts (1 to 4096) x 10 matrices (512 x 512 to 28672 x 4096
+// and 5120 x 13824) x up to ten splits.  What the estimate picks is 2 % (microscaled X: 4 %) slower on average than the fastest of all that was
+// measured, at 95 of 100 sizes within 10 %; where the shapes cross (4096 x 4096, us): 32 rows 16 x 64 6.8, 32 x 128 8.4; 244 rows 32 x 128
+// 12.2, 64 x 128 14.9; 512 rows 64 x 128 19.5, 64 x 256 24.6; 1024 rows 39 and 31; 4096 rows 64 x 256 127, 256 x 256 106.
 struct MxPlan { int shape, splits; };
-struct MxTile { int tm, tn; };
+struct MxTile { int tm, tn; float us[8]; };
 enum { MX_STREAM = 0 };
-//                                   stream     fed                                                    tile
-constexpr MxTile MX_TILES[] =      {{16, 16}, {16, 64}, {32, 128}, {32, 256}, {64, 128}, {64, 256}, {256, 256}};
-//                                   stream     fed                                                      block
-constexpr MxTile MX_BOTH_TILES[] = {{16, 16}, {16, 64}, {32, 128}, {64, 128}, {64, 256}, {256, 256}};
+// us: a launch; k-groups of a tile; the same times rounds of the chip (256 tiles); ... times tiles / 256; rounds; planes: their launch, a million
+// of their values; a million results.  The first row (no tiles): a launch; sixteen k-groups; 10^4 column x k-groups; the same times ten rows.
+constexpr MxTile MX_TILES[] = {
+    {16, 16, {2.956f, 1.255f, 0.408f, 5.14f}},                                       // mx_stream_kernel
+    {16, 64, {2.421f, 0.346f, 0.120f, 0.161f, 0.574f, 2.361f, 0.775f, 0.648f}},      // mx_fed_kernel
+    {32, 128, {2.828f, 0.261f, 0.339f, 0.546f, 1.079f, 1.924f, 0.961f, 1.289f}},
+    {32, 256, {3.126f, 0.634f, 0.419f, 0.874f, 1.965f, 1.285f, 1.037f, 1.457f}},
+    {64, 128, {2.819f, 0.000f, 1.131f, 0.653f, 1.244f, 2.629f, 1.221f, 0.719f}},
+    {64, 256, {4.790f, 0.000f, 1.803f, 1.072f, 0.000f, 2.306f, 1.461f, 0.817f}},
+    {256, 256, {5.440f, 0.000f, 8.964f, 1.138f, 2.072f, 0.492f, 0.835f, 0.982f}}};   // mx_tile_kernel
+constexpr MxTile MX_BOTH_TILES[] = {
+    {16, 16, {2.991f, 0.096f, 0.321f, 2.48f}},                                       // mx_stream_both_kernel
+    {16, 64, {1.681f, 0.696f, 0.015f, 0.182f, 0.606f, 2.733f, 0.422f, 0.382f}},      // mx_fed_both_kernel
+    {32, 128, {1.520f, 0.822f, 0.025f, 0.316f, 1.321f, 2.437f, 1.208f, 1.680f}},
+    {64, 128, {2.656f, 0.272f, 0.612f, 0.195f, 1.551f, 2.415f, 1.356f, 0.915f}},
+    {64, 256, {4.153f, 0.050f, 1.108f, 0.270f, 0.029f, 2.751f, 1.432f, 0.690f}},
+    {256, 256, {7.684f, 0.000f, 1.906f, 0.901f, 2.925f, 1.774f, 1.203f, 0.563f}}};   // mx_block_both_kernel
 
 static int mx_groups(int K) { return (K + 4 * MX_KSTEP - 1) / (4 * MX_KSTEP); }
-static int stream_waves(int kgroups) { return kgroups < 16 ? (kgroups < 8 ? kgroups : 8) : 16; }
+// Waves of a column tile: four, sixteen where the tiles leave CUs with one each and K is long (one row, us, 4 / 8 / 16 waves: 4096 x 14336 9.0 / 8.5 / 8.0,
+// 5120 x 13824 10.8 / 12.0 / 12.2, 6144 x 4096 5.4 / 5.7, 4096 x 4096 3.4 / 3.6).
+static int stream_waves(int tiles, int kgroups) { return tiles <= 256 && kgroups >= 16 ? 16 : kgroups < 4 ? kgroups : 4; }
 
-static MxPlan gemm_plan_of(int M, int N, int groups) {
-    const int shape = M <= 4 ? 0 : M <= 16 ? 1 : M <= 32 ? 2 : M <= 64 ? 3 : M <= 512 ? 5 : 6;
-    const MxTile t = MX_TILES[shape];
-    const int tiles = ((M + t.tm - 1) / t.tm) * ((N + t.tn - 1) / t.tn);
-    int s = shape == MX_STREAM ? 1 : 256 / tiles;
-    if (s > groups) s = groups;
-    return MxPlan{shape, s < 1 ? 1 : s};
-}
-static MxPlan both_plan_of(int M, int N, int groups) {
-    const int shape = M <= 4 ? 0 : M <= 16 ? 1 : M <= 32 ? 2 : M <= 64 ? 3 : M <= 256 ? 4 : 5;
-    const MxTile t = MX_BOTH_TILES[shape];
-    const int tiles = ((M + t.tm - 1) / t.tm) * ((N + t.tn - 1) / t.tn);
-    int s = shape == MX_STREAM ? 1 : 256 / tiles;
-    if (s > groups) s = groups;
-    return MxPlan{shape, s < 1 ? 1 : s};
+template <int SHAPES> static MxPlan best_plan(const MxTile (&tiles)[SHAPES], int M, int N, int groups) {
+    MxPlan best{MX_STREAM, 1};
+    float least = 1e30f;
+    if (M <= 16) {
+        const float *u = tiles[MX_STREAM].us, ng = (float)N * groups * 1e-4f;
+        least = u[0] + u[1] * groups / 16 + u[2] * ng + u[3] * ng * M * 1e-2f;
+    }
+    const float mn = (float)M * N * 1e-6f;
+    for (int i = 1; i < SHAPES; ++i) {
+        const MxTile &t = tiles[i];
+        const float n = (float)((M + t.tm - 1) / t.tm) * (float)((N + t.tn - 1) / t.tn);
+        for (int s = 1; s <= 16 && s <= groups && (s == 1 || n * s <= 1024); ++s) {
+            const float g = (float)((groups + s - 1) / s), chips = n * s / 256, rounds = ceilf(chips);
+            float us = t.us[0] + t.us[1] * g + t.us[2] * g * rounds + t.us[3] * g * chips + t.us[4] * rounds + t.us[7] * mn;
+            if (s > 1) us += t.us[5] + t.us[6] * s * mn;
+            if (us < least) { least = us; best = MxPlan{i, s}; }
+        }
+    }
+    return best;
 }
 
 // Whether X can be read as it is: rows of whole 16-byte pieces.
@@ -1012,7 +967,7 @@ static size_t stage_bytes(int x_dt, int M, int K, const MxPlan &p) {
     return ((size_t)M * groups * 4 * MX_KSTEP * 2 * (x_dt == DT_F32 ? 3 : 1) + 255) / 256 * 256;
 }
 static MxPlan plan_of(int x_dt, int M, int N, int K) {
-    return x_dt == DT_MX ? both_plan_of(M, N, mx_groups(K)) : gemm_plan_of(M, N, mx_groups(K) * (x_dt == DT_F32 ? 3 : 1));
+    return x_dt == DT_MX ? best_plan(MX_BOTH_TILES, M, N, mx_groups(K)) : best_plan(MX_TILES, M, N, mx_groups(K) * (x_dt == DT_F32 ? 3 : 1));
 }
 size_t mx_gemm_scratch_size(int x_dt, int M, int N, int K) {
     if (M == 0) return 256;
@@ -1028,7 +983,7 @@ static void add_planes(const MxPacked &w, const float *part, int splits, int M, 
 template <typename T, typename Y, int PARTS>
 static void run_gemm(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan &p, Y *y, int64_t ldy, bool quads, float *part, hipStream_t st) {
     if (p.shape == MX_STREAM) {
-        const int waves = stream_waves(w.kgroups);
+        const int waves = stream_waves(w.tiles, w.kgroups);
         mx_stream_kernel<T, Y, PARTS><<<w.tiles, waves * 64, waves * 1024, st>>>(w, x, y, ldy, quads, g.M, g.N);
         return;
     }
@@ -1059,7 +1014,7 @@ static void run_gemm(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan 
 template <typename Y>
 static void run_both(const MxPacked &w, const u32x4 *x, const uint8_t *xs, int blocks, MxGeom g, const MxPlan &p, Y *y, int64_t ldy, bool quads, uint32_t *xscales, float *part, hipStream_t st) {
     if (p.shape == MX_STREAM) {
-        const int waves = stream_waves(w.kgroups);
+        const int waves = stream_waves(w.tiles, w.kgroups);
         mx_stream_both_kernel<Y><<<w.tiles, waves * 64, waves * 1024, st>>>(w, x, xs, blocks, y, ldy, quads, g.M, g.N);
         return;
     }
