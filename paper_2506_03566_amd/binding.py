@@ -20,7 +20,7 @@ EXPORTS = ["poss_workspace_bytes", "poss_load", "poss_reset", "poss_prefill", "p
            "poss_last_error", "poss_free", "poss_profile_gemm", "poss_gemm_profile", "poss_set_tuning", "poss_set_launch_rows", "poss_set_sampling", "poss_set_draft_sampling",
            "poss_debug_build_tree", "poss_debug_set_taps", "poss_debug_read_kv", "poss_debug_draft_logits",
            "poss_debug_gemm_scratch_bytes", "poss_debug_gemm", "poss_gemm_static",
-           "poss_mx_quantize", "poss_mx_dequantize", "poss_mx_packed_bytes", "poss_mx_pack", "poss_mx_gemm_scratch_bytes", "poss_mx_gemm", "poss_mx_gemm_mx"]
+           "poss_workspace_bytes_mx", "poss_load_mx", "poss_mx_quantize", "poss_mx_dequantize", "poss_mx_packed_bytes", "poss_mx_pack", "poss_mx_gemm_scratch_bytes", "poss_mx_gemm", "poss_mx_gemm_mx"]
 
 c_i32, c_f32, c_vp = ctypes.c_int32, ctypes.c_float, ctypes.c_void_p
 
@@ -70,6 +70,9 @@ def load_library():
     lib.poss_workspace_bytes.restype = ctypes.c_size_t
     lib.poss_workspace_bytes.argtypes = [P(PossConfig)]
     lib.poss_load.argtypes = [P(PossConfig), P(PossWeights), c_vp, ctypes.c_size_t, c_vp, P(c_vp)]
+    lib.poss_workspace_bytes_mx.restype = ctypes.c_size_t
+    lib.poss_workspace_bytes_mx.argtypes = lib.poss_workspace_bytes.argtypes
+    lib.poss_load_mx.argtypes = lib.poss_load.argtypes
     lib.poss_reset.argtypes = [c_vp]
     lib.poss_reset_seq.argtypes = [c_vp, c_i32]
     lib.poss_set_active.argtypes = [c_vp, c_i32, c_i32]
@@ -165,16 +168,16 @@ class TreeArrays:
 
 class Poss:
     """One context.  `weights`: dict name -> torch tensor on the GPU (names of synth.tensor_specs);
-    the workspace is a torch uint8 tensor this object keeps alive."""
+    the workspace is a torch uint8 tensor this object keeps alive.  mx: the layers' weights are held in 4 bits (poss_load_mx)."""
 
-    def __init__(self, cfg, weights, stream=None, **over):
+    def __init__(self, cfg, weights, stream=None, mx=False, **over):
         import torch
         self.lib = load_library()
         self.cfg = cfg
         self.c_cfg = make_config(cfg, **over)
-        need = self.lib.poss_workspace_bytes(ctypes.byref(self.c_cfg))
+        need = (self.lib.poss_workspace_bytes_mx if mx else self.lib.poss_workspace_bytes)(ctypes.byref(self.c_cfg))
         if need == 0:
-            raise PossError(E_INVALID_ARG, "configuration rejected by poss_workspace_bytes")
+            raise PossError(E_INVALID_ARG, "configuration rejected by poss_workspace_bytes%s" % ("_mx" if mx else ""))
         self.workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
         names = ("attn_norm", "wq", "wk", "wv", "wo", "mlp_norm", "w_gate", "w_up", "w_down")
         lay = (c_vp * (cfg.n_layers * 9))(*[weights[f"layer{l}.{n}"].data_ptr()
@@ -188,7 +191,7 @@ class Poss:
         self.stream = stream
         sh = c_vp(stream.cuda_stream) if stream is not None else c_vp(0)
         h = c_vp()
-        rc = self.lib.poss_load(ctypes.byref(self.c_cfg), ctypes.byref(w), c_vp(self.workspace.data_ptr()),
+        rc = (self.lib.poss_load_mx if mx else self.lib.poss_load)(ctypes.byref(self.c_cfg), ctypes.byref(w), c_vp(self.workspace.data_ptr()),
                                 need, sh, ctypes.byref(h))
         if rc != POSS_OK:
             raise PossError(rc, self.lib.poss_last_error(None).decode())

@@ -72,6 +72,7 @@ struct Seq {
 struct poss_ctx {
     poss_config cfg;
     ModelDims md;
+    bool mx;                           // the layers' and the fc matrices are microscaled (poss_load_mx)
     hipStream_t st;
     char err[512];
     // weights (workspace)
@@ -208,17 +209,18 @@ struct WeightSlots {
     std::vector<void *> spec;    // [S][8]: fc_w, fc_b, then the 6
 };
 
-size_t carve(const poss_config &c, Arena &a, poss_ctx *ctx, WeightSlots *ws) {
+size_t carve(const poss_config &c, Arena &a, poss_ctx *ctx, WeightSlots *ws, bool mx) {
     const int dt = c.dtype;
     const size_t es = esize(c);
     const int d = c.d_model, qd = c.n_q_heads * c.head_dim, kd = c.n_kv_heads * c.head_dim, F = c.d_ffn, V = c.vocab;
+    auto matrix = [&](int N, int K) { return a.take(mx ? mx_packed_size(N, K) : packed_elems(dt, N, K) * es); };
     auto layer_slots = [&](std::vector<void *> &out) {
         out.push_back(a.take(d * es));
-        out.push_back(a.take(packed_elems(dt, qd + 2 * kd, d) * es));
-        out.push_back(a.take(packed_elems(dt, d, qd) * es));
+        out.push_back(matrix(qd + 2 * kd, d));
+        out.push_back(matrix(d, qd));
         out.push_back(a.take(d * es));
-        out.push_back(a.take(packed_elems(dt, gate_up_rows(F), d) * es));
-        out.push_back(a.take(packed_elems(dt, d, F) * es));
+        out.push_back(matrix(gate_up_rows(F), d));
+        out.push_back(matrix(d, F));
     };
     WeightSlots local;
     WeightSlots &w = ws ? *ws : local;
@@ -227,7 +229,7 @@ size_t carve(const poss_config &c, Arena &a, poss_ctx *ctx, WeightSlots *ws) {
     w.final_norm = a.take(d * es);
     for (int l = 0; l < c.n_layers; ++l) layer_slots(w.layer);
     for (int s = 0; s < c.n_specialists; ++s) {
-        w.spec.push_back(a.take(packed_elems(dt, d, 2 * d) * es));
+        w.spec.push_back(matrix(d, 2 * d));
         w.spec.push_back(a.take(d * es));
         layer_slots(w.spec);
     }
@@ -248,11 +250,12 @@ size_t carve(const poss_config &c, Arena &a, poss_ctx *ctx, WeightSlots *ws) {
     for (int i = 0; i < 5; ++i) {
         // split count does not depend on M; planes are at most R rows
         GemmShape g = gemm_plan(dt, R, shapes[i][0], shapes[i][1], 4096);   // upper bound on splits
-        const size_t f = (size_t)g.S * R * g.Npad;
+        const int planes = mx && mx_plane_splits(shapes[i][0], shapes[i][1]) > g.S ? mx_plane_splits(shapes[i][0], shapes[i][1]) : g.S;
+        const size_t f = (size_t)planes * R * g.Npad;
         if (f > part_floats) part_floats = f;
     }
     const int QR = B * 16 < R ? B * 16 : R;                  // full rows of a draft pass: at most k <= 16 per sequence
-    const int PR = prefill_rows(c);                          // rows of the passes over a prompt
+    const int PR = mx ? LAUNCH_ROWS : prefill_rows(c);       // rows of the passes over a prompt
     float *h = a.take_n<float>((size_t)PR * d), *h_other = a.take_n<float>(d);
     float2 *cs = a.take_n<float2>((size_t)PR * (c.head_dim / 2));
     float *part = a.take_n<float>(part_floats);
@@ -353,8 +356,22 @@ ProfileSlot profile_slot(poss_ctx *c, int cols, int K) {
     return ProfileSlot{c->prof_ev[2 * i], c->prof_ev[2 * i + 1]};
 }
 
+// A product with a microscaled matrix: its planes, then what is done with them (EPI_ROPE_KV, EPI_RESIDUAL, EPI_SILU).
+GemmShape run_gemm_mx(poss_ctx *c, const void *Wp, int N, int K, const void *X, int ldx, int M, float *part, const EpiArgs &epi, const RopeRanges *ranges) {
+    const int splits = mx_plane_splits(N, K);
+    GemmShape g = gemm_plan(c->md.dt, M, N, K, 1);
+    g.Mpad = M;
+    g.S = mx_planes_written(M, N, K, splits);
+    bool ok = launch_mx_planes(c->md.dt, Wp, N, K, X, ldx, M, part, g.Npad, splits, c->st);
+    if (ok && epi.mode == EPI_SILU) launch_mx_silu(c->md.dt, part, g.S, M, g.Npad, epi.F, epi.act, c->st);
+    else if (ok) ok = launch_planes_epilogue(c->md.dt, g, part, epi, c->md.eps, c->st, ranges);
+    if (!ok) c->launch_refused = true;
+    return g;
+}
+
 GemmShape run_gemm(poss_ctx *c, const void *Wp, int N, int K, const void *X, int ldx, int M, float *part,
                    bool single_split, EpiArgs epi, const RopeRanges *ranges = nullptr) {
+    if (c->mx && Wp != c->lm_head) return run_gemm_mx(c, Wp, N, K, X, ldx, M, part, epi, ranges);
     GemmShape g = gemm_plan(c->md.dt, M, N, K, single_split ? 1 : c->gemm_target_wgs);
     const ProfileSlot p = profile_slot(c, N, K);
     if (!launch_gemm(c->md.dt, g, Wp, X, ldx, part, epi, c->md.eps, c->st, p.start, p.stop, ranges))
@@ -451,7 +468,7 @@ void run_layer(poss_ctx *c, const LayerW &w, const std::vector<Seg> &segs, int r
         if (mlp_row) eo.mode = EPI_PLANES;
     }
     const AttnMerge am = attention_partials(md, as[0].rows, as[0].n_prefix, as[0].region_len, kps, c->attn_sc);
-    if (na == 1 && as[0].row0 == 0 && gemm_merged_ok(md.dt, go, am)) {           // few rows: the output projection merges the splits itself
+    if (!c->mx && na == 1 && as[0].row0 == 0 && gemm_merged_ok(md.dt, go, am)) {           // few rows: the output projection merges the splits itself
         launch_attention(md, c->q, rows_q, rm, as[0].n_prefix, as[0].region_len, *as[0].kv, kps, c->attn_sc, c->attn_out, c->st, false);
         const ProfileSlot p = profile_slot(c, md.d, qd);
         if (!launch_gemm_merged(md.dt, go, w.wo, am, c->part, eo, md.eps, c->st, p.start, p.stop)) c->launch_refused = true;
@@ -488,7 +505,7 @@ void target_forward(poss_ctx *c, int rows, const int32_t *tokens_dev, const RowM
     const ModelDims &md = c->md;
     launch_embed_norm(md, c->embed, tokens_dev, rows, c->layers[0].attn_norm, c->h, c->u, rm.pos, c->inv_freq, c->cs, c->st);
     const int nl = c->cfg.n_layers;
-    RowFlow rf{rows == 1 && md.dt != DT_F32 && !c->taps_user, false, RowNorm{}, c->h};   // (taps read the stream between the layers)
+    RowFlow rf{rows == 1 && md.dt != DT_F32 && !c->taps_user && !c->mx, false, RowNorm{}, c->h};   // (taps read the stream between the layers)
     for (int l = 0; l < nl; ++l) {
         if (c->taps_user)
             launch_copy_rows_f32(c->h, md.d, c->taps_user + (size_t)l * rows * md.d, md.d, rows, md.d, c->st);
@@ -616,7 +633,7 @@ void spec_pass(poss_ctx *c, int s, std::vector<SeqPlan> &plans, int depth_index,
     }
     const void *bias = c->cfg.fc_bias ? w.fc_b : nullptr;
     EpiArgs ef = epi_residual(c, false, bias, nullptr, w.layer.attn_norm);
-    RowFlow rf{rows_all == 1 && rows_q == 1 && md.dt != DT_F32, false, RowNorm{}, c->h};
+    RowFlow rf{rows_all == 1 && rows_q == 1 && md.dt != DT_F32 && !c->mx, false, RowNorm{}, c->h};
     if (rf.on) {
         rf.norm = row_norm_of(c, rf, gemm_plan(md.dt, 1, md.d, 2 * md.d, c->gemm_target_wgs), false, bias, w.layer.attn_norm);
         rf.pending = row_next_ok(c, rf.norm, (md.hq + 2 * md.hkv) * md.dh, EPI_ROPE_KV);
@@ -701,7 +718,7 @@ void catchup_pass(poss_ctx *c, int b, int s, int i0, int n) {
 // many-row kernels, otherwise in chunks of MAX_ROWS rows.
 void spec_catchup(poss_ctx *c, int b, int s, int upto) {
     Seq &sq = c->seq[b];
-    const int most = prefill_rows(c->cfg);
+    const int most = c->mx ? LAUNCH_ROWS : prefill_rows(c->cfg);
     while (most > LAUNCH_ROWS && upto - sq.spec_len[s] > STREAMED_PROMPT) {
         const int n = prompt_chunk(upto - sq.spec_len[s], most);
         catchup_pass(c, b, s, sq.spec_len[s], n);
@@ -719,16 +736,22 @@ void spec_catchup(poss_ctx *c, int b, int s, int upto) {
     }
 }
 
+// One of a layer's matrices, or an fc matrix.
+void pack_matrix(poss_ctx *c, const PackSrc &src, int N, int K, void *dst) {
+    if (c->mx) launch_mx_pack_rows(c->cfg.dtype, src, N, K, dst, c->st);
+    else launch_pack(c->cfg.dtype, src, K, dst, c->st);
+}
+
 void pack_layer(poss_ctx *c, const void *const *src, const std::vector<void *> &dst, size_t base) {
     const poss_config &cf = c->cfg;
     const int dt = cf.dtype, d = cf.d_model, qd = cf.n_q_heads * cf.head_dim, kd = cf.n_kv_heads * cf.head_dim, F = cf.d_ffn;
     const size_t es = esize(cf);
     (void)hipMemcpyAsync(dst[base + 0], src[0], d * es, hipMemcpyDeviceToDevice, c->st);
-    launch_pack(dt, PackSrc{{src[1], src[2], src[3]}, {qd, kd, kd}, 0, dt == DT_F32 ? 0 : cf.head_dim}, d, dst[base + 1], c->st);
-    launch_pack(dt, PackSrc{{src[4], nullptr, nullptr}, {d, 0, 0}}, qd, dst[base + 2], c->st);
+    pack_matrix(c, PackSrc{{src[1], src[2], src[3]}, {qd, kd, kd}, 0, dt == DT_F32 ? 0 : cf.head_dim}, qd + 2 * kd, d, dst[base + 1]);
+    pack_matrix(c, PackSrc{{src[4], nullptr, nullptr}, {d, 0, 0}}, d, qd, dst[base + 2]);
     (void)hipMemcpyAsync(dst[base + 3], src[5], d * es, hipMemcpyDeviceToDevice, c->st);
-    launch_pack(dt, PackSrc{{src[6], src[7], nullptr}, {F, F, 0}, 1}, d, dst[base + 4], c->st);
-    launch_pack(dt, PackSrc{{src[8], nullptr, nullptr}, {d, 0, 0}}, F, dst[base + 5], c->st);
+    pack_matrix(c, PackSrc{{src[6], src[7], nullptr}, {F, F, 0}, 1}, gate_up_rows(F), d, dst[base + 4]);
+    pack_matrix(c, PackSrc{{src[8], nullptr, nullptr}, {d, 0, 0}}, d, F, dst[base + 5]);
 }
 
 LayerW layer_view(const std::vector<void *> &v, size_t base) {
@@ -797,11 +820,17 @@ extern "C" {
 size_t poss_workspace_bytes(const poss_config *cfg) {
     if (!cfg || check_config(*cfg)) return 0;
     Arena a(nullptr);
-    return carve(*cfg, a, nullptr, nullptr);
+    return carve(*cfg, a, nullptr, nullptr, false);
 }
 
-int poss_load(const poss_config *cfg, const poss_weights *w, void *workspace, size_t workspace_bytes,
-              void *hip_stream, poss_ctx **out) {
+size_t poss_workspace_bytes_mx(const poss_config *cfg) {
+    if (!cfg || check_config(*cfg) || cfg->dtype == POSS_DTYPE_F32) return 0;
+    Arena a(nullptr);
+    return carve(*cfg, a, nullptr, nullptr, true);
+}
+
+static int load_context(const poss_config *cfg, const poss_weights *w, void *workspace, size_t workspace_bytes,
+                        void *hip_stream, poss_ctx **out, bool mx) {
     if (!cfg || !w || !workspace || !out) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load: null argument");
     if (const char *why = check_config(*cfg)) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load: %s", why);
     if (!w->embed || !w->lm_head || !w->final_norm || !w->layer || !w->spec)
@@ -811,13 +840,15 @@ int poss_load(const poss_config *cfg, const poss_weights *w, void *workspace, si
     for (int i = 0; i < cfg->n_specialists * 11; ++i)
         if (!w->spec[i]) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load: null specialist tensor %d", i);
     if (reinterpret_cast<uintptr_t>(workspace) % 256) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load: workspace not 256-byte aligned");
-    const size_t need = poss_workspace_bytes(cfg);
+    if (mx && cfg->dtype == POSS_DTYPE_F32) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load_mx: activations and caches are of a 16-bit type (dtype 1 or 2)");
+    const size_t need = mx ? poss_workspace_bytes_mx(cfg) : poss_workspace_bytes(cfg);
     if (workspace_bytes < need)
         return fail(nullptr, POSS_E_CAPACITY, "poss_load: workspace of %zu bytes, %zu needed", workspace_bytes, need);
 
     poss_ctx *c = new (std::nothrow) poss_ctx();
     if (!c) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load: out of host memory");
     c->cfg = *cfg;
+    c->mx = mx;
     c->md = ModelDims{cfg->d_model, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, cfg->d_ffn, cfg->vocab,
                       cfg->rms_eps, cfg->rope_theta, cfg->dtype};
     c->st = static_cast<hipStream_t>(hip_stream);
@@ -827,7 +858,7 @@ int poss_load(const poss_config *cfg, const poss_weights *w, void *workspace, si
     c->prof_on = 0; c->prof_n = 0; c->prof_bytes = 0;
     Arena a(workspace);
     WeightSlots ws;
-    carve(*cfg, a, c, &ws);
+    carve(*cfg, a, c, &ws, mx);
 
     auto bail = [&](int code) { g_load_error[0] = 0; strncpy(g_load_error, c->err, 511); release_host(c); delete c; return code; };
 #define LOAD_TRY(call)                                                                    \
@@ -849,7 +880,7 @@ int poss_load(const poss_config *cfg, const poss_weights *w, void *workspace, si
     }
     for (int s = 0; s < cfg->n_specialists; ++s) {
         const void *const *src = w->spec + (size_t)s * 11;
-        launch_pack(cfg->dtype, PackSrc{{src[0], nullptr, nullptr}, {d, 0, 0}}, 2 * d, ws.spec[(size_t)s * 8], c->st);
+        pack_matrix(c, PackSrc{{src[0], nullptr, nullptr}, {d, 0, 0}}, d, 2 * d, ws.spec[(size_t)s * 8]);
         LOAD_TRY(hipMemcpyAsync(ws.spec[(size_t)s * 8 + 1], src[1], d * es, hipMemcpyDeviceToDevice, c->st));
         pack_layer(c, src + 2, ws.spec, (size_t)s * 8 + 2);
         c->specs.push_back(SpecW{ws.spec[(size_t)s * 8], ws.spec[(size_t)s * 8 + 1], layer_view(ws.spec, (size_t)s * 8 + 2)});
@@ -907,6 +938,13 @@ int poss_load(const poss_config *cfg, const poss_weights *w, void *workspace, si
     reset_sequence(c);
     *out = c;
     return POSS_OK;
+}
+
+int poss_load(const poss_config *cfg, const poss_weights *w, void *workspace, size_t workspace_bytes, void *hip_stream, poss_ctx **out) {
+    return load_context(cfg, w, workspace, workspace_bytes, hip_stream, out, false);
+}
+int poss_load_mx(const poss_config *cfg, const poss_weights *w, void *workspace, size_t workspace_bytes, void *hip_stream, poss_ctx **out) {
+    return load_context(cfg, w, workspace, workspace_bytes, hip_stream, out, true);
 }
 
 int poss_reset(poss_ctx *c) {
@@ -979,7 +1017,7 @@ int poss_prefill_seq(poss_ctx *c, int32_t seq, const int32_t *prompt, int32_t n_
     // A long prompt goes through the many-row kernels, up to prefill_rows tokens a pass.  Up to STREAMED_PROMPT tokens
     // it is the weight-streaming kernels, LAUNCH_ROWS a pass, on two row ranges of at most MAX_ROWS (the width of a
     // row's mask): the second range finds the keys of the first, written by the same layer's QKV epilogue, in its prefix.
-    const int most = n_prompt <= STREAMED_PROMPT ? LAUNCH_ROWS : prefill_rows(c->cfg);
+    const int most = n_prompt <= STREAMED_PROMPT || c->mx ? LAUNCH_ROWS : prefill_rows(c->cfg);
     for (int c0 = 0, rows; c0 < n_prompt; c0 += rows) {
         rows = prompt_chunk(n_prompt - c0, most);
         memcpy(stage, prompt + c0, rows * sizeof(int32_t));

@@ -210,6 +210,24 @@ __device__ __forceinline__ void rope_pair(float x1, float x2, float2 cs, float &
     o2 = __builtin_fmaf(x2, cs.x, q);
 }
 
+// The source of row n of a packed matrix: which of src's matrices, and its row there (false: a row of padding).
+__device__ __forceinline__ bool pack_source_row(const PackSrc &src, int n, int &which, int &row) {
+    if (src.interleave16) {          // 32 rows = 16 rows of matrix 0, then the same 16 rows of matrix 1
+        const int w = n & 31;
+        which = w >> 4; row = (n >> 5) * 16 + (w & 15);
+        return row < src.rows[which];
+    }
+    if (src.rope_dh > 0) {           // packed column p of a head -> dim (p / 32) * 16 + p % 16 + (p / 16 % 2) * dh / 2
+        const int dh = src.rope_dh, p = n % dh;
+        n = n - p + (p >> 5) * 16 + (p & 15) + ((p >> 4) & 1) * (dh >> 1);
+    }
+    for (which = 0; which < 3; ++which) {
+        if (n < src.rows[which]) { row = n; return true; }
+        n -= src.rows[which];
+    }
+    return false;
+}
+
 // Element offsets into the paged caches; _in: with the slot's physical page already looked up.
 __device__ __forceinline__ size_t k_offset_in(const KVCache &kv, int pg, int slot, int head, int hkv, int dh) {
     const int P = 1 << kv.page_shift;

@@ -1804,6 +1804,27 @@ static bool ranges_ok(const GemmShape &g, RopeRanges &rr) {
     return true;
 }
 
+template <typename T>
+static void launch_planes_epilogue_t(const GemmShape &g, const float *part, const EpiArgs &epi, float eps, hipStream_t st, const RopeRanges &rr) {
+    if (epi.mode != EPI_ROPE_KV) { launch_epilogue_t<T>(g, part, epi, eps, st); return; }
+    const int blocks = rr.blk0[rr.n - 1] + (rr.r1[rr.n - 1] - rr.r0[rr.n - 1] + EPI_ROWS_PAIR - 1) / EPI_ROWS_PAIR;
+    hipLaunchKernelGGL((epilogue_rope_ranges_kernel<T>), dim3(g.Npad / GEMM_BLOCK_N, blocks), dim3(ROPE_THREADS), 0, st, part, (size_t)g.Mpad * g.Npad, g.S,
+                       g.Npad, rr, epi);
+}
+
+bool launch_planes_epilogue(int dt, const GemmShape &g, const float *part, const EpiArgs &epi, float eps, hipStream_t st, const RopeRanges *ranges) {
+    if (dt == DT_F32 || (epi.mode != EPI_ROPE_KV && epi.mode != EPI_RESIDUAL) || !gemm_args_ok(dt, g, part, part, part, epi)) return false;
+    RopeRanges rr{};
+    if (epi.mode == EPI_ROPE_KV) {
+        if (ranges) rr = *ranges;
+        else { rr.n = 1; rr.r0[0] = 0; rr.r1[0] = g.M; rr.rows_q[0] = epi.rows_q; rr.kv[0] = epi.kv; }
+        if (!ranges_ok(g, rr)) return false;
+    }
+    if (dt == DT_BF16) launch_planes_epilogue_t<bf16_t>(g, part, epi, eps, st, rr);
+    else launch_planes_epilogue_t<f16_t>(g, part, epi, eps, st, rr);
+    return true;
+}
+
 bool launch_gemm(int dt, const GemmShape &g, const void *Wp, const void *X, int ldx, float *part,
                  const EpiArgs &epi, float eps, hipStream_t st, hipEvent_t ev_start, hipEvent_t ev_stop, const RopeRanges *ranges) {
     if (!gemm_args_ok(dt, g, Wp, X, part, epi)) return false;
@@ -1948,23 +1969,6 @@ bool launch_gemm_row(int dt, const GemmShape &g, const void *Wp, const RowNorm &
 // ------------------------------------------------------------------------------------------
 // Repack row-major [rows_i, K] matrices, stacked along N (or gate/up interleaved in groups of 16
 // rows), into B-operand order.
-__device__ __forceinline__ bool pack_source_row(const PackSrc &src, int n, int &which, int &row) {
-    if (src.interleave16) {          // 32 rows = 16 rows of matrix 0, then the same 16 rows of matrix 1
-        const int w = n & 31;
-        which = w >> 4; row = (n >> 5) * 16 + (w & 15);
-        return row < src.rows[which];
-    }
-    if (src.rope_dh > 0) {           // packed column p of a head -> dim (p / 32) * 16 + p % 16 + (p / 16 % 2) * dh / 2
-        const int dh = src.rope_dh, p = n % dh;
-        n = n - p + (p >> 5) * 16 + (p & 15) + ((p >> 4) & 1) * (dh >> 1);
-    }
-    for (which = 0; which < 3; ++which) {
-        if (n < src.rows[which]) { row = n; return true; }
-        n -= src.rows[which];
-    }
-    return false;
-}
-
 __global__ void pack16_kernel(PackSrc src, int K, int Kpad, int Npad, u32x4 *__restrict__ dst) {
     const size_t unit = (size_t)blockIdx.x * blockDim.x + threadIdx.x;     // one 16-byte unit of dst
     const size_t total = (size_t)Npad * Kpad / 8;

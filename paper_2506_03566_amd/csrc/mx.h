@@ -25,6 +25,17 @@ size_t mx_gemm_scratch_size(int x_dt, int M, int N, int K);
 void launch_mx_gemm(int x_dt, const void *x, int64_t ldx, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *scratch, hipStream_t st);
 void launch_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *scratch, hipStream_t st);
 
+
+// For a context's layers (16-bit types).  A matrix of packed rows, as launch_pack takes them, quantised and packed; N: its rows, padding ones among them.
+size_t mx_packed_size(int N, int K);
+void launch_mx_pack_rows(int dt, const PackSrc &src, int N, int K, void *packed, hipStream_t st);
+// The planes of X W^T: plane s < splits of part, [M][ld], ld a multiple of four and at least N.  A row's planes are the same for every M.
+int mx_plane_splits(int N, int K);
+bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, int ldx, int M, float *part, int ld, int splits, hipStream_t st);
+int mx_planes_written(int M, int N, int K, int splits);    // how many of them that is: splits, or one where the kernel has added them
+// act[M][F] = SiLU(gate) * up from the planes of a product whose rows alternate in groups of 16 (PackSrc::interleave16).
+void launch_mx_silu(int dt, const float *part, int splits, int M, int ld, int F, void *act, hipStream_t st);
+
 // Leaves the message that poss_last_error(NULL) returns; the code is handed through.
 int set_error(int code, const char *fmt, ...);
 

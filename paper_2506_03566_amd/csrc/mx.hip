@@ -141,7 +141,7 @@ MxPacked mx_packed_at(const void *packed, int N, int K) {
     return w;
 }
 
-static size_t mx_packed_size(int N, int K) {
+size_t mx_packed_size(int N, int K) {
     const size_t tiles = mx_tiles(N), ks = mx_ksteps(K);
     return (tiles * ks * 1024 + tiles * (ks / 4) * 256 + tiles * 64 + 255) / 256 * 256;
 }
@@ -177,6 +177,61 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ 
             if (n < N && b < blocks) {
                 c = codes[(size_t)n * blocks + b];
                 s = min(127, max(0, scales[(size_t)n * blocks + b] - top[r] + 127));
+            }
+            out[((size_t)tile * ksteps + ks) * 64 + lane] = c;
+            packed |= (uint32_t)s << (8 * i);
+        }
+        out_scales[((size_t)tile * groups + g) * 64 + lane] = packed;
+    }
+}
+
+// Quantisation and packing of a context's matrices in one kernel, when it is loaded: a workgroup per column tile reads its rows (the packed order's:
+// gate and up alternate, heads have their rotary pairs side by side) once for the scales and once for the codes.  What poss_mx_quantize and
+// poss_mx_pack give for the same rows.
+constexpr int MX_ROW_BLOCKS = 1024;                       // K up to twice the largest d_model
+template <typename T> __global__ __launch_bounds__(256) void mx_pack_rows_kernel(PackSrc src, int K, int ksteps, u32x4 *__restrict__ out, uint32_t *__restrict__ out_scales,
+                                                                                 int32_t *__restrict__ ref) {
+    __shared__ int top[16];
+    __shared__ uint8_t sc[16 * MX_ROW_BLOCKS];
+    const int tile = blockIdx.x, tid = threadIdx.x, blocks = (K + MX_BLOCK - 1) / MX_BLOCK, groups = ksteps / 4;
+    if (tid < 16) top[tid] = 0;
+    __syncthreads();
+    auto row_of = [&](int r) {
+        int which, row;
+        return pack_source_row(src, tile * 16 + r, which, row) ? static_cast<const T *>(src.ptr[which]) + (size_t)row * K : nullptr;
+    };
+    auto load = [&](const T *row, int b, MxIn<T> (&in)[4]) {      // (K is a multiple of eight)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (row && b * MX_BLOCK + i * 8 < K) in[i].load(row + b * MX_BLOCK + i * 8);
+            else in[i].v.u = u32x4{0u, 0u, 0u, 0u};
+        }
+    };
+    for (int i = tid; i < 16 * blocks; i += 256) {
+        const int r = i / blocks, b = i - r * blocks;
+        MxIn<T> in[4];
+        load(row_of(r), b, in);
+        const unsigned field = max(max(in[0].top(), in[1].top()), max(in[2].top(), in[3].top())) >> 23;
+        const int s = field == 255 ? 255 : field < 2 ? 0 : (int)field - 2;
+        sc[r * blocks + b] = (uint8_t)s;
+        atomicMax(&top[r], s);
+    }
+    __syncthreads();
+    if (tid < 16) ref[tile * 16 + tid] = top[tid];
+    const int lane = tid & 63, r = lane & 15;
+    const T *row = row_of(r);
+    for (int g = tid >> 6; g < groups; g += 4) {
+        uint32_t packed = 0;
+        for (int i = 0; i < 4; ++i) {
+            const int ks = g * 4 + i, b = ks * 4 + (lane >> 4);
+            u32x4 c = {0u, 0u, 0u, 0u};
+            int s = 127;
+            if (row && b < blocks) {
+                MxIn<T> in[4];
+                load(row, b, in);
+                const int sb = sc[r * blocks + b];
+                if (sb != 255) c = u32x4{in[0].codes(mx_power(sb)), in[1].codes(mx_power(sb)), in[2].codes(mx_power(sb)), in[3].codes(mx_power(sb))};
+                s = min(127, max(0, sb - top[r] + 127));
             }
             out[((size_t)tile * ksteps + ks) * 64 + lane] = c;
             packed |= (uint32_t)s << (8 * i);
@@ -225,6 +280,13 @@ void launch_mx_pack(const void *codes, const void *scales, int N, int K, void *p
     const MxPacked w = mx_packed_at(packed, N, K);
     mx_pack_kernel<<<w.tiles, 256, 0, st>>>(static_cast<const u32x4 *>(codes), static_cast<const uint8_t *>(scales), N, mx_blocks(K), w.ksteps,
                                             const_cast<u32x4 *>(w.codes), const_cast<uint32_t *>(w.scales), const_cast<int32_t *>(w.ref));
+}
+
+void launch_mx_pack_rows(int dt, const PackSrc &src, int N, int K, void *packed, hipStream_t st) {
+    const MxPacked w = mx_packed_at(packed, N, K);
+    u32x4 *c = const_cast<u32x4 *>(w.codes); uint32_t *s = const_cast<uint32_t *>(w.scales); int32_t *r = const_cast<int32_t *>(w.ref);
+    if (dt == DT_BF16) mx_pack_rows_kernel<bf16_t><<<w.tiles, 256, 0, st>>>(src, K, w.ksteps, c, s, r);
+    else mx_pack_rows_kernel<f16_t><<<w.tiles, 256, 0, st>>>(src, K, w.ksteps, c, s, r);
 }
 
 }  // namespace poss

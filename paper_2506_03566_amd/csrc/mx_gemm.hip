@@ -58,6 +58,7 @@ template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_scaled(f32x4 a, co
     for (int r = 0; r < 4; ++r) o.v[r] = from_f<Y>(es[r] == 255 ? __builtin_nanf("") : __builtin_ldexpf(a[r], es[r] - 127 - shift));
     return o;
 }
+template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_raw(f32x4 a) { MxQuad<Y> o; for (int r = 0; r < 4; ++r) o.v[r] = (Y)a[r]; return o; }
 template <typename Y> __device__ __forceinline__ void mx_store(Y *__restrict__ y, int64_t ldy, bool quads, int m, int n, int N, f32x4 acc, const int32_t *__restrict__ ref, int shift) {
     const MxQuad<Y> o = mx_scaled<Y>(acc, ref, n, shift);
     Y *dst = y + (int64_t)m * ldy + n;
@@ -261,6 +262,8 @@ struct MxGeom {
     int M, N, steps;              // k-steps of the product: float32 X is three times as long (its parts one after the other)
     int full;                     // k-steps that lie inside X's rows as a whole
     int tiles_m, tiles_n, splits;
+    int plane_ld;                 // planes: [M][plane_ld] each,
+    bool plane_scaled;            // times 2^ref already
 };
 
 // Workgroup -> tile: consecutive ids go to the 8 XCDs in turn; an XCD is given a contiguous run of tiles, ordered so that those it works
@@ -271,6 +274,11 @@ __device__ __forceinline__ void mx_tile_of(const MxGeom &g, int gm_rows, int &tm
     const int grp = id / (gm_rows * g.tiles_n), in_grp = id - grp * (gm_rows * g.tiles_n), gm = min(gm_rows, g.tiles_m - grp * gm_rows);
     tm = grp * gm_rows + in_grp % gm;
     tn = in_grp / gm;
+}
+
+// Four consecutive columns to a plane.
+template <int SHIFT> __device__ __forceinline__ void mx_store_plane(float *p, f32x4 a, const MxGeom &g, const MxPacked &w, int col) {
+    *reinterpret_cast<MxQuad<float> *>(p) = g.plane_scaled ? mx_scaled<float>(a, w.ref, col, SHIFT) : __builtin_bit_cast(MxQuad<float>, a);
 }
 
 // A wave's tiles to Y, or to this split's plane.  D tile: lane -> row lane % 16, register r -> column 4 (lane / 16) + r.
@@ -285,7 +293,7 @@ __device__ __forceinline__ void mx_tile_store(const f32x4 (&acc)[MTW][NTW], int 
         for (int nt = 0; nt < NTW; ++nt) {
             const int col = (ct0 + nt) * 16 + (lane >> 4) * 4;
             if (col >= g.N) continue;
-            if constexpr (SPLIT) *reinterpret_cast<f32x4 *>(y + ((size_t)blockIdx.y * g.M + m) * (w.tiles * 16) + col) = acc[mt][nt];
+            if constexpr (SPLIT) mx_store_plane<MxOp<T>::SHIFT>(y + ((size_t)blockIdx.y * g.M + m) * g.plane_ld + col, acc[mt][nt], g, w, col);
             else mx_store<Y>(y, ldy, quads, m, col, g.N, acc[mt][nt], w.ref, MxOp<T>::SHIFT);
         }
     }
@@ -295,17 +303,17 @@ __device__ __forceinline__ void mx_tile_store(const f32x4 (&acc)[MTW][NTW], int 
 template <typename T, typename Y, int MTW, int NTW, bool SPLIT>
 __device__ __forceinline__ void mx_tile_store_wide(char *own, const f32x4 (&acc)[MTW][NTW], int row0, int ct0, const MxGeom &g, const MxPacked &w, Y *__restrict__ y, int64_t ldy) {
     const int lane = threadIdx.x & 63, cols = SPLIT ? w.tiles * 16 : g.N;
-    Y *dst = SPLIT ? y + (size_t)blockIdx.y * g.M * cols : y;
+    Y *dst = SPLIT ? y + (size_t)blockIdx.y * g.M * g.plane_ld : y;
 #pragma unroll
     for (int mt = 0; mt < MTW; ++mt)
         mx_store_rows<Y, 16, NTW * 16>(own, [&](auto f) {
 #pragma unroll
             for (int nt = 0; nt < NTW; ++nt) {
                 const int c = nt * 16 + (lane >> 4) * 4;
-                if constexpr (SPLIT) f(lane & 15, c, __builtin_bit_cast(MxQuad<Y>, acc[mt][nt]));
+                if (SPLIT && !g.plane_scaled) f(lane & 15, c, mx_raw<Y>(acc[mt][nt]));
                 else f(lane & 15, c, mx_scaled<Y>(acc[mt][nt], w.ref, min(ct0 + nt, w.tiles - 1) * 16 + (lane >> 4) * 4, MxOp<T>::SHIFT));
             }
-        }, row0 + mt * 16, ct0 * 16, g.M, cols, dst, SPLIT ? cols : ldy);
+        }, row0 + mt * 16, ct0 * 16, g.M, cols, dst, SPLIT ? g.plane_ld : ldy);
 }
 
 template <typename T, typename Y, int TM, int TN, int WM, int WN, bool SPLIT>
@@ -832,8 +840,8 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
     __syncthreads();
     const int n0 = (ct0 + wn * 4) * 16;
     if (wide) {
-        Y *dst = SPLIT ? y + (size_t)blockIdx.y * g.M * (w.tiles * 16) : y;
-        const int64_t ldd = SPLIT ? (int64_t)w.tiles * 16 : ldy;
+        Y *dst = SPLIT ? y + (size_t)blockIdx.y * g.M * g.plane_ld : y;
+        const int64_t ldd = SPLIT ? (int64_t)g.plane_ld : ldy;
         char *own = reinterpret_cast<char *>(xs) + wave * (32 * (64 * (int)sizeof(Y) + 16));
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
@@ -843,7 +851,7 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int c = nt * 32 + q * 8 + (lane >> 5) * 4;
-                        if constexpr (SPLIT) f(lane & 31, c, __builtin_bit_cast(MxQuad<Y>, quad(mt, nt, q)));
+                        if (SPLIT && !g.plane_scaled) f(lane & 31, c, mx_raw<Y>(quad(mt, nt, q)));
                         else f(lane & 31, c, mx_scaled<Y>(quad(mt, nt, q), w.ref, min(n0 + c, w.tiles * 16 - 4), 0));
                     }
             }, m0 + wm * 128 + mt * 32, n0, g.M, SPLIT ? w.tiles * 16 : g.N, dst, ldd);
@@ -859,7 +867,7 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
             for (int q = 0; q < 4; ++q) {
                 const int col = n0 + nt * 32 + q * 8 + (lane >> 5) * 4;
                 if (col >= g.N) continue;
-                if constexpr (SPLIT) *reinterpret_cast<f32x4 *>(y + ((size_t)blockIdx.y * g.M + m) * (w.tiles * 16) + col) = quad(mt, nt, q);
+                if constexpr (SPLIT) mx_store_plane<0>(y + ((size_t)blockIdx.y * g.M + m) * g.plane_ld + col, quad(mt, nt, q), g, w, col);
                 else mx_store<Y>(y, ldy, quads, m, col, g.N, quad(mt, nt, q), w.ref, 0);
             }
     }
@@ -918,8 +926,9 @@ static int mx_groups(int K) { return (K + 4 * MX_KSTEP - 1) / (4 * MX_KSTEP); }
 // 5120 x 13824 10.8 / 12.0 / 12.2, 6144 x 4096 5.4 / 5.7, 4096 x 4096 3.4 / 3.6).
 static int stream_waves(int tiles, int kgroups) { return tiles <= 256 && kgroups >= 16 ? 16 : kgroups < 4 ? kgroups : 4; }
 
-template <int SHAPES> static MxPlan best_plan(const MxTile (&tiles)[SHAPES], int M, int N, int groups) {
-    MxPlan best{MX_STREAM, 1};
+// fixed > 0: the number of splits.
+template <int SHAPES> static MxPlan best_plan(const MxTile (&tiles)[SHAPES], int M, int N, int groups, int fixed = 0) {
+    MxPlan best{MX_STREAM, fixed > 0 ? fixed : 1};
     float least = 1e30f;
     if (M <= 16) {
         const float *u = tiles[MX_STREAM].us, ng = (float)N * groups * 1e-4f;
@@ -929,7 +938,7 @@ template <int SHAPES> static MxPlan best_plan(const MxTile (&tiles)[SHAPES], int
     for (int i = 1; i < SHAPES; ++i) {
         const MxTile &t = tiles[i];
         const float n = (float)((M + t.tm - 1) / t.tm) * (float)((N + t.tn - 1) / t.tn);
-        for (int s = 1; s <= 16 && s <= groups && (s == 1 || n * s <= 1024); ++s) {
+        for (int s = fixed > 0 ? fixed : 1; s <= (fixed > 0 ? fixed : 16) && s <= groups && (fixed > 0 || s == 1 || n * s <= 1024); ++s) {
             const float g = (float)((groups + s - 1) / s), chips = n * s / 256, rounds = ceilf(chips);
             float us = t.us[0] + t.us[1] * g + t.us[2] * g * rounds + t.us[3] * g * chips + t.us[4] * rounds + t.us[7] * mn;
             if (s > 1) us += t.us[5] + t.us[6] * s * mn;
@@ -981,9 +990,8 @@ static void add_planes(const MxPacked &w, const float *part, int splits, int M, 
 }
 
 template <typename T, typename Y, int PARTS>
-static void run_gemm(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan &p, Y *y, int64_t ldy, bool quads, float *part, hipStream_t st) {
+static void run_tiles(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan &p, int waves, Y *y, int64_t ldy, bool quads, float *part, hipStream_t st) {
     if (p.shape == MX_STREAM) {
-        const int waves = stream_waves(w.tiles, w.kgroups);
         mx_stream_kernel<T, Y, PARTS><<<w.tiles, waves * 64, waves * 1024, st>>>(w, x, y, ldy, quads, g.M, g.N);
         return;
     }
@@ -1007,7 +1015,12 @@ static void run_gemm(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan 
             else mx_tile_kernel<T, Y, 256, 256, 2, 4, false><<<grid, 512, 0, st>>>(w, x, g, y, ldy, quads, wide);
     }
 #undef POSS_MX_FED
-    if (g.splits > 1) add_planes<Y>(w, part, g.splits, g.M, g.N, MxOp<T>::SHIFT, y, ldy, quads, st);
+}
+template <typename T, typename Y, int PARTS>
+static void run_gemm(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan &p, Y *y, int64_t ldy, bool quads, float *part, hipStream_t st) {
+    g.plane_ld = w.tiles * 16; g.plane_scaled = false;
+    run_tiles<T, Y, PARTS>(w, x, g, p, stream_waves(w.tiles, w.kgroups), y, ldy, quads, part, st);
+    if (p.splits > 1) add_planes<Y>(w, part, p.splits, g.M, g.N, MxOp<T>::SHIFT, y, ldy, quads, st);
 }
 
 // X microscaled.  xscales: scratch for its scales in operand order.
@@ -1019,6 +1032,7 @@ static void run_both(const MxPacked &w, const u32x4 *x, const uint8_t *xs, int b
         return;
     }
     const MxTile t = MX_BOTH_TILES[p.shape];
+    g.plane_ld = w.tiles * 16; g.plane_scaled = false;
     g.splits = p.splits; g.tiles_m = (g.M + t.tm - 1) / t.tm; g.tiles_n = (g.N + t.tn - 1) / t.tn;
     const dim3 grid(g.tiles_m * g.tiles_n, g.splits);
     const bool wide = wide_ok(y, ldy, g.N);
@@ -1051,12 +1065,63 @@ static void run_gemm_t(const MxPacked &w, const MxRows &x, const MxGeom &g, cons
     else run_gemm<T, f16_t, PARTS>(w, x, g, p, static_cast<f16_t *>(y), ldy, quads, part, st);
 }
 
+// ------------------------------------------------------------------------------------------ a context's layers
+// Splits of a matrix whose planes the layer's own epilogues add up: as many as give every CU a 128-column tile, the groups dealt out
+// evenly.  They follow the matrix alone, and every kernel adds a split's products in the same order (mx_stream_kernel its waves' sums as the
+// epilogue would the planes): a row's sums do not depend on the rows beside it, and a tree's rows get what plain decoding gives them.
+int mx_plane_splits(int N, int K) {
+    const int groups = mx_groups(K), cols = (N + 127) / 128;
+    int s = (256 + cols / 2) / cols;
+    if (s > groups) s = groups;
+    if (s > 16) s = 16;
+    if (s < 1) s = 1;
+    const int longest = (groups + s - 1) / s;
+    return (groups + longest - 1) / longest;
+}
+
+bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, int ldx, int M, float *part, int ld, int splits, hipStream_t st) {
+    if (!packed || !X || !part || M < 1 || N < 4 || N % 4 || K < 8 || K % 8 || ld % 4 || ld < (N + 15) / 16 * 16 || splits < 1 || splits > 16 || splits > mx_groups(K) ||
+        !rows_ok(dt, X, ldx, K) || ldx < K) return false;
+    const MxPacked w = mx_packed_at(packed, N, K);
+    MxPlan p = best_plan(MX_TILES, M, N, w.kgroups, splits);
+    const MxGeom g{M, N, (K + MX_KSTEP - 1) / MX_KSTEP, K / MX_KSTEP, 0, 0, 1, ld, true};
+    const MxRows x{X, ldx, 0, K};
+    if (dt == DT_BF16) run_tiles<bf16_t, float, 1>(w, x, g, p, splits, part, ld, true, part, st);
+    else run_tiles<f16_t, float, 1>(w, x, g, p, splits, part, ld, true, part, st);
+    return true;
+}
+// Whether the planes are one (mx_stream_kernel adds its waves' sums itself).
+int mx_planes_written(int M, int N, int K, int splits) { return best_plan(MX_TILES, M, N, mx_groups(K), splits).shape == MX_STREAM ? 1 : splits; }
+
+// A thread per four units.  Of 61 rows of 28672 columns: 15 MB read, from the L2s for the most part.
+template <typename T>
+__global__ __launch_bounds__(256) void mx_silu_kernel(const float *__restrict__ part, int splits, int M, int ld, int F, T *__restrict__ act) {
+    const int f = (blockIdx.x * 256 + threadIdx.x) * 4, m = blockIdx.y;
+    if (f >= F) return;                                   // (F is a multiple of eight)
+    const float *p = part + (size_t)m * ld + (f >> 4) * 32 + (f & 15);
+    const size_t plane = (size_t)M * ld;
+    f32x4 gate = *reinterpret_cast<const f32x4 *>(p), up = *reinterpret_cast<const f32x4 *>(p + 16);
+    for (int s = 1; s < splits; ++s) {
+        gate += *reinterpret_cast<const f32x4 *>(p + s * plane);
+        up += *reinterpret_cast<const f32x4 *>(p + s * plane + 16);
+    }
+    MxQuad<T> o;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o.v[r] = mul_round<T>(gate[r] / (1.0f + expf(-gate[r])), up[r]);
+    *reinterpret_cast<MxQuad<T> *>(act + (size_t)m * F + f) = o;
+}
+void launch_mx_silu(int dt, const float *part, int splits, int M, int ld, int F, void *act, hipStream_t st) {
+    const dim3 grid((F / 4 + 255) / 256, M);
+    if (dt == DT_BF16) mx_silu_kernel<bf16_t><<<grid, 256, 0, st>>>(part, splits, M, ld, F, static_cast<bf16_t *>(act));
+    else mx_silu_kernel<f16_t><<<grid, 256, 0, st>>>(part, splits, M, ld, F, static_cast<f16_t *>(act));
+}
+
 void launch_mx_gemm(int x_dt, const void *x, int64_t ldx, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *scratch, hipStream_t st) {
     const MxPacked w = mx_packed_at(packed, N, K);
     const MxPlan p = plan_of(x_dt, M, N, K);
     const bool as_is = rows_ok(x_dt, x, ldx, K);
     const MxRows r = as_is ? MxRows{x, ldx, 0, K} : stage(x_dt, x, ldx, M, K, w.ksteps * MX_KSTEP, scratch, st);
-    MxGeom g{M, N, x_dt == DT_F32 ? 3 * w.ksteps : (K + MX_KSTEP - 1) / MX_KSTEP, 0, 0, 0, 1};
+    MxGeom g{M, N, x_dt == DT_F32 ? 3 * w.ksteps : (K + MX_KSTEP - 1) / MX_KSTEP, 0, 0, 0, 1, 0, false};
     g.full = as_is ? K / MX_KSTEP : x_dt == DT_F32 ? g.steps : w.ksteps;
     float *part = reinterpret_cast<float *>(static_cast<char *>(scratch) + stage_bytes(x_dt, M, K, p));
     if (x_dt == DT_F32) run_gemm_t<bf16_t, 3>(w, r, g, p, y_dt, y, ldy, part, st);
@@ -1068,7 +1133,7 @@ void launch_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *pa
     const MxPacked w = mx_packed_at(packed, N, K);
     const MxPlan p = plan_of(DT_MX, M, N, K);
     const bool quads = quads_ok(y, ldy, N, y_dt);
-    const MxGeom g{M, N, w.ksteps, 0, 0, 0, 1};
+    const MxGeom g{M, N, w.ksteps, 0, 0, 0, 1, 0, false};
     const u32x4 *c = static_cast<const u32x4 *>(x_codes);
     const uint8_t *s = static_cast<const uint8_t *>(x_scales);
     uint32_t *xs = static_cast<uint32_t *>(scratch);

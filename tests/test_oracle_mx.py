@@ -123,3 +123,17 @@ def test_the_binding_refuses_what_the_kernels_would_misread():
     assert refused(P.mx_pack, codes, scales, 128)
     assert refused(P.mx_gemm_scratch, torch.int8, 4, 16, 64)
     assert refused(P.mx_gemm_scratch, None, -1, 16, 64)
+
+
+def test_workspace_of_microscaled_layers():
+    import ctypes
+    from synth import CONFIGS
+    lib = _lib()
+    for name, cfg in CONFIGS.items():
+        c = P.make_config(cfg)
+        small, full = lib.poss_workspace_bytes_mx(ctypes.byref(c)), lib.poss_workspace_bytes(ctypes.byref(c))
+        assert small == 0 if cfg.dtype == 0 else 0 < small < full, name
+    assert lib.poss_workspace_bytes_mx(None) == 0
+    out = ctypes.c_void_p()
+    c = P.make_config(CONFIGS["t_mid_bf16"])
+    assert lib.poss_load_mx(ctypes.byref(c), None, None, 0, None, ctypes.byref(out)) == P.E_INVALID_ARG
