@@ -362,9 +362,9 @@ GemmShape run_gemm_mx(poss_ctx *c, const void *Wp, int N, int K, const void *X, 
     GemmShape g = gemm_plan(c->md.dt, M, N, K, 1);
     g.Mpad = M;
     g.S = mx_planes_written(M, N, K, splits);
-    bool ok = launch_mx_planes(c->md.dt, Wp, N, K, X, ldx, M, part, g.Npad, splits, c->st);
-    if (ok && epi.mode == EPI_SILU) launch_mx_silu(c->md.dt, part, g.S, M, g.Npad, epi.F, epi.act, c->st);
-    else if (ok) ok = launch_planes_epilogue(c->md.dt, g, part, epi, c->md.eps, c->st, ranges);
+    const bool ok = epi.mode == EPI_SILU ? launch_mx_gate_up(c->md.dt, Wp, epi.F, K, X, ldx, M, part, g.Npad, epi.act, c->st)
+                                         : launch_mx_planes(c->md.dt, Wp, N, K, X, ldx, M, part, g.Npad, splits, c->st) &&
+                                           launch_planes_epilogue(c->md.dt, g, part, epi, c->md.eps, c->st, ranges);
     if (!ok) c->launch_refused = true;
     return g;
 }

@@ -33,8 +33,8 @@ void launch_mx_pack_rows(int dt, const PackSrc &src, int N, int K, void *packed,
 int mx_plane_splits(int N, int K);
 bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, int ldx, int M, float *part, int ld, int splits, hipStream_t st);
 int mx_planes_written(int M, int N, int K, int splits);    // how many of them that is: splits, or one where the kernel has added them
-// act[M][F] = SiLU(gate) * up from the planes of a product whose rows alternate in groups of 16 (PackSrc::interleave16).
-void launch_mx_silu(int dt, const float *part, int splits, int M, int ld, int F, void *act, hipStream_t st);
+// act[M][F] = SiLU(gate) * up of X with a matrix whose rows alternate in groups of 16 (PackSrc::interleave16).  part as above, for the planes of a split product.
+bool launch_mx_gate_up(int dt, const void *packed, int F, int K, const void *X, int ldx, int M, float *part, int ld, void *act, hipStream_t st);
 
 // Leaves the message that poss_last_error(NULL) returns; the code is handed through.
 int set_error(int code, const char *fmt, ...);

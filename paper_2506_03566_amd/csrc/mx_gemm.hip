@@ -86,6 +86,13 @@ __device__ __forceinline__ void mx_store_rows(char *lds, Put put, int m0, int n0
     }
     wave_lds_sync();                                      // (the next rows go to the same place)
 }
+template <typename T> __device__ __forceinline__ MxQuad<T> mx_silu_quad(const MxQuad<float> &gate, const MxQuad<float> &up) {
+    MxQuad<T> o;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o.v[r] = mul_round<T>(gate.v[r] / (1.0f + expf(-gate.v[r])), up.v[r]);
+    return o;
+}
+
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
 template <int I> struct Num { static constexpr int value = I; };
@@ -423,7 +430,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
 // the shape of a load), and what comes between: a wave that waits for X cannot ask for weights.  So FW waves of a workgroup do nothing but
 // fetch X into LDS, a group of four k-steps (KS k-steps) a stage, two stages; the others keep the codes of their own columns four k-steps
 // ahead in registers, and multiply.  One barrier per stage, where reads pass into the next one, as in mx_tile_kernel.
-template <typename T, typename Y, int TM, int TN, int WM, int WN, int FW, int KS, bool SPLIT>
+// SILU: the columns alternate in groups of 16 gates and 16 ups (PackSrc::interleave16), and what is written is SiLU(gate) * up, [M][ldy].
+template <typename T, typename Y, int TM, int TN, int WM, int WN, int FW, int KS, bool SPLIT, bool SILU = false>
 __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w, MxRows x, MxGeom g, Y *__restrict__ y, int64_t ldy, bool quads, bool wide) {
     typedef __attribute__((address_space(3))) void *LdsPtr;
     typedef MxOp<T> Op;
@@ -463,7 +471,7 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
             __syncthreads();                              // stage t has landed; nobody reads stage t - 1 any more
             if (t + 1 < stages) issue(t + 1);
         }
-        if (TM >= 64 && wide) __syncthreads();            // (the others write their results through LDS)
+        if (TM >= 64 && !SILU && wide) __syncthreads();   // (the others write their results through LDS)
         return;
     }
     const int wm = wave % WM, wn = wave / WM, ct0 = tn * (TN / 16) + wn * NTW;
@@ -544,7 +552,21 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
     };
     for (int s = 0; s + 1 < n; ++s) group(Yes{}, false);
     group(No{}, true);
-    if (TM >= 64 && wide) {
+    if constexpr (SILU) {
+        static_assert(NTW % 2 == 0, "a wave holds gates with their ups");
+#pragma unroll
+        for (int mt = 0; mt < MTW; ++mt) {
+            const int m = m0 + (wm * MTW + mt) * 16 + (lane & 15);
+            if (m >= g.M) continue;
+#pragma unroll
+            for (int nt = 0; nt < NTW; nt += 2) {
+                const int f = (ct0 + nt) * 8 + (lane >> 4) * 4, n = min(ct0 + nt, w.tiles - 2) * 16 + (lane >> 4) * 4;
+                if (f >= ldy) continue;                   // (a multiple of eight)
+                const MxQuad<float> gate = mx_scaled<float>(acc[mt][nt], w.ref, n, Op::SHIFT), up = mx_scaled<float>(acc[mt][nt + 1], w.ref, n + 16, Op::SHIFT);
+                *reinterpret_cast<MxQuad<T> *>(y + (int64_t)m * ldy + f) = mx_silu_quad<T>(gate, up);
+            }
+        }
+    } else if (TM >= 64 && wide) {
         __syncthreads();                                  // nobody reads X any more
         mx_tile_store_wide<T, Y, MTW, NTW, SPLIT>(reinterpret_cast<char *>(xs) + wave * (16 * (NTW * 16 * (int)sizeof(Y) + 16)), acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy);
     } else mx_tile_store<T, Y, MTW, NTW, SPLIT>(acc, m0 + wm * MTW * 16, ct0, g, w, y, ldy, quads);
@@ -1093,6 +1115,38 @@ bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, i
 // Whether the planes are one (mx_stream_kernel adds its waves' sums itself).
 int mx_planes_written(int M, int N, int K, int splits) { return best_plan(MX_TILES, M, N, mx_groups(K), splits).shape == MX_STREAM ? 1 : splits; }
 
+static void launch_mx_silu(int dt, const float *part, int splits, int M, int ld, int F, void *act, hipStream_t st);
+
+// act[M][F] = SiLU(gate) * up.  Unsplit (enough column tiles for the chip) the product does it itself: tiles whose waves hold a gate column with its up.
+template <typename T>
+static void run_silu(const MxPacked &w, const MxRows &x, MxGeom g, T *act, int F, hipStream_t st) {
+#define POSS_MX_SILU(TM, TN, WM, WN, FW)                                                                                                     \
+    do {                                                                                                                                     \
+        g.tiles_m = (g.M + TM - 1) / TM; g.tiles_n = (g.N + TN - 1) / TN;                                                                    \
+        mx_fed_kernel<T, T, TM, TN, WM, WN, FW, 4, false, true><<<dim3(g.tiles_m * g.tiles_n), (WM * WN + FW) * 64, 0, st>>>(w, x, g, act, F, true, false); \
+    } while (0)
+    if (g.M <= 16) POSS_MX_SILU(16, 128, 1, 4, 2);
+    else if (g.M <= 32) POSS_MX_SILU(32, 256, 1, 8, 4);
+    else if (g.M <= 64) POSS_MX_SILU(64, 128, 2, 4, 4);
+    else POSS_MX_SILU(64, 256, 1, 8, 4);
+#undef POSS_MX_SILU
+}
+bool launch_mx_gate_up(int dt, const void *packed, int F, int K, const void *X, int ldx, int M, float *part, int ld, void *act, hipStream_t st) {
+    const int N = gate_up_rows(F), splits = mx_plane_splits(N, K);
+    if (!act || F % 8) return false;
+    if (splits > 1) {
+        if (!launch_mx_planes(dt, packed, N, K, X, ldx, M, part, ld, splits, st)) return false;
+        launch_mx_silu(dt, part, mx_planes_written(M, N, K, splits), M, ld, F, act, st);
+        return true;
+    }
+    if (!packed || !X || M < 1 || K < 8 || ldx < K || !rows_ok(dt, X, ldx, K)) return false;
+    const MxPacked w = mx_packed_at(packed, N, K);
+    const MxGeom g{M, N, (K + MX_KSTEP - 1) / MX_KSTEP, K / MX_KSTEP, 0, 0, 1, 0, false};
+    if (dt == DT_BF16) run_silu<bf16_t>(w, MxRows{X, ldx, 0, K}, g, static_cast<bf16_t *>(act), F, st);
+    else run_silu<f16_t>(w, MxRows{X, ldx, 0, K}, g, static_cast<f16_t *>(act), F, st);
+    return true;
+}
+
 // A thread per four units.  Of 61 rows of 28672 columns: 15 MB read, from the L2s for the most part.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_silu_kernel(const float *__restrict__ part, int splits, int M, int ld, int F, T *__restrict__ act) {
@@ -1105,12 +1159,9 @@ __global__ __launch_bounds__(256) void mx_silu_kernel(const float *__restrict__ 
         gate += *reinterpret_cast<const f32x4 *>(p + s * plane);
         up += *reinterpret_cast<const f32x4 *>(p + s * plane + 16);
     }
-    MxQuad<T> o;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) o.v[r] = mul_round<T>(gate[r] / (1.0f + expf(-gate[r])), up[r]);
-    *reinterpret_cast<MxQuad<T> *>(act + (size_t)m * F + f) = o;
+    *reinterpret_cast<MxQuad<T> *>(act + (size_t)m * F + f) = mx_silu_quad<T>(__builtin_bit_cast(MxQuad<float>, gate), __builtin_bit_cast(MxQuad<float>, up));
 }
-void launch_mx_silu(int dt, const float *part, int splits, int M, int ld, int F, void *act, hipStream_t st) {
+static void launch_mx_silu(int dt, const float *part, int splits, int M, int ld, int F, void *act, hipStream_t st) {
     const dim3 grid((F / 4 + 255) / 256, M);
     if (dt == DT_BF16) mx_silu_kernel<bf16_t><<<grid, 256, 0, st>>>(part, splits, M, ld, F, static_cast<bf16_t *>(act));
     else mx_silu_kernel<f16_t><<<grid, 256, 0, st>>>(part, splits, M, ld, F, static_cast<f16_t *>(act));
