@@ -334,15 +334,16 @@ int poss_mx_quantize(int32_t dtype, const void *x, int64_t ldx, int32_t rows, in
 int poss_mx_dequantize(int32_t dtype, const void *codes, const void *scales, int32_t rows, int32_t cols, void *y, int64_t ldy, void *hip_stream);
 
 /* A weight matrix [N][K] (codes and scales as above) in the operand order of the products below: `packed`, poss_mx_packed_bytes(N, K)
- * bytes (0 for a bad shape), aligned to 256.  Codes and scales are not needed afterwards.  Products use a block's scale relative to
- * the largest one of its row: exactly while it lies at most 126 (fp16 activations: 36) powers of two below; what lies further below is smaller than
- * 2^-124 (2^-38) of the row's largest weight and may lose bits or be taken for zero. */
+ * bytes (0 for a bad shape; K at most 2^21, N at most 2^27), aligned to 256.  Codes and scales are not needed afterwards.  Products use a
+ * block's scale relative to the largest one of its row: exactly while it lies at most 126 (fp16 activations: 36) powers of two below; what
+ * lies further below is smaller than 2^-124 (2^-38) of the row's largest weight and may lose bits or be taken for zero.  The float32 sums
+ * are of activations times those relative weights (magnitudes up to 6), and are multiplied by the row's power of two at the end. */
 size_t poss_mx_packed_bytes(int32_t N, int32_t K);
 int poss_mx_pack(const void *codes, const void *scales, int32_t N, int32_t K, void *packed, void *hip_stream);
 
 /* Y[M][N] of y_dtype = X[M][K] . W[N][K]^T with packed W and X of x_dtype.  Every product of an activation and a weight is exact (float32
  * activations included), sums are float32, the result is rounded once.  scratch: at least poss_mx_gemm_scratch_bytes(x_dtype, M, N, K)
- * bytes (at least 256; 0 for a bad shape), aligned to 256, for this call alone until it has run: two calls that may run at the same
+ * bytes (at least 256; 0 for a bad shape: M at most 2^24, M * N at most 2^38), aligned to 256, for this call alone until it has run: two calls that may run at the same
  * time, or two graphs that may, need one each.  The bits of a row may differ with M (other kernels sum in another order); the same call
  * gives the same bits. */
 #define POSS_MX 4                    /* in place of x_dtype: X is microscaled too (poss_mx_gemm_mx) */

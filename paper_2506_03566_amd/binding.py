@@ -421,7 +421,7 @@ def _mx_type(t):
 
 def _mx_rows(t, rows, cols, what):
     """The row distance of a matrix [rows, cols] whose rows are contiguous."""
-    if t.dim() != 2 or t.size(0) != rows or t.size(1) != cols:
+    if t.dim() != 2 or t.size(0) != rows or t.size(1) != cols or rows > 0x7fffffff or cols > 0x7fffffff:
         _mx_refuse("%s [%d, %d] is wanted, got %s" % (what, rows, cols, tuple(t.shape)))
     ld = t.stride(0) if rows > 1 else cols
     if ld < cols or (cols > 1 and t.stride(1) != 1):
@@ -494,6 +494,9 @@ class MxWeight:
     """A weight matrix [N, K] of 4-bit codes in the products' operand order (made by mx_pack)."""
 
     def __init__(self, packed, N, K):
+        need = (_mx if _mx.lib else _mx.open()).lib.poss_mx_packed_bytes(N, K) if max(N, K) < 1 << 31 else 0
+        if need == 0 or packed.nbytes < need or not packed.is_contiguous():
+            _mx_refuse("packed weights [%d, %d] take %d contiguous bytes, got %d" % (N, K, need, packed.nbytes))
         self.packed, self.N, self.K = packed, N, K
 
 
@@ -513,7 +516,7 @@ def mx_gemm_scratch(dtype, M, N, K, device="cuda", stream=None):
     """Scratch for a product of this shape: dtype of the activations, None for microscaled ones.  One that is large enough serves
     other shapes too."""
     t = _MX if dtype is None else _mx_type(dtype)
-    need = (_mx if _mx.lib else _mx.open()).lib.poss_mx_gemm_scratch_bytes(t, M, N, K)
+    need = (_mx if _mx.lib else _mx.open()).lib.poss_mx_gemm_scratch_bytes(t, M, N, K) if max(M, N, K) < 1 << 31 else 0
     if need == 0:
         _mx_refuse("shape rejected")
     return _mx_empty(need, device, stream)
@@ -527,6 +530,8 @@ def mx_gemm(x, w, y, scratch=None, stream=None):
     ldx, ldy = _mx_rows(x, M, K, "x"), _mx_rows(y, M, N, "y")
     if scratch is None:
         scratch = mx_gemm_scratch(x.dtype, M, N, K, x.device, stream)
+    elif not scratch.is_contiguous():
+        _mx_refuse("scratch must be contiguous")
     _mx_call(_mx.lib.poss_mx_gemm, stream, (x, y, w.packed, scratch), tx, x.data_ptr(), ldx, w.packed.data_ptr(), ty, y.data_ptr(), ldy, M, N, K,
              scratch.data_ptr(), scratch.nbytes)
     return y
@@ -540,6 +545,8 @@ def mx_gemm_mx(codes, scales, w, y, scratch=None, stream=None):
     _mx_pair(codes, scales, M, K, "mx_gemm_mx")
     if scratch is None:
         scratch = mx_gemm_scratch(None, M, N, K, y.device, stream)
+    elif not scratch.is_contiguous():
+        _mx_refuse("scratch must be contiguous")
     _mx_call(_mx.lib.poss_mx_gemm_mx, stream, (y, codes, scales, w.packed, scratch), codes.data_ptr(), scales.data_ptr(), w.packed.data_ptr(), ty, y.data_ptr(), ldy,
              M, N, K, scratch.data_ptr(), scratch.nbytes)
     return y

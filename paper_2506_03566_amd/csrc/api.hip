@@ -797,6 +797,13 @@ void update_ready(poss_ctx *c) {
     if (c->state == ST_READY && !all) c->state = ST_LOADED;
 }
 
+// What microscaled layers ask for beyond check_config.
+const char *check_mx_config(const poss_config &c) {
+    if (c.dtype == POSS_DTYPE_F32) return "activations and caches are of a 16-bit type (dtype 1 or 2)";
+    if (c.d_ffn > MX_MOST_K || (int64_t)c.n_q_heads * c.head_dim > MX_MOST_K) return "a matrix of more than 2^21 columns";
+    return nullptr;
+}
+
 // Events and pinned host memory of a context (whatever of them exists: a failed poss_load stops half way).
 void release_host(poss_ctx *c) {
     for (int i = 0; i < 6; ++i)
@@ -824,7 +831,7 @@ size_t poss_workspace_bytes(const poss_config *cfg) {
 }
 
 size_t poss_workspace_bytes_mx(const poss_config *cfg) {
-    if (!cfg || check_config(*cfg) || cfg->dtype == POSS_DTYPE_F32) return 0;
+    if (!cfg || check_config(*cfg) || check_mx_config(*cfg)) return 0;
     Arena a(nullptr);
     return carve(*cfg, a, nullptr, nullptr, true);
 }
@@ -840,7 +847,7 @@ static int load_context(const poss_config *cfg, const poss_weights *w, void *wor
     for (int i = 0; i < cfg->n_specialists * 11; ++i)
         if (!w->spec[i]) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load: null specialist tensor %d", i);
     if (reinterpret_cast<uintptr_t>(workspace) % 256) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load: workspace not 256-byte aligned");
-    if (mx && cfg->dtype == POSS_DTYPE_F32) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load_mx: activations and caches are of a 16-bit type (dtype 1 or 2)");
+    if (const char *why = mx ? check_mx_config(*cfg) : nullptr) return fail(nullptr, POSS_E_INVALID_ARG, "poss_load_mx: %s", why);
     const size_t need = mx ? poss_workspace_bytes_mx(cfg) : poss_workspace_bytes(cfg);
     if (workspace_bytes < need)
         return fail(nullptr, POSS_E_CAPACITY, "poss_load: workspace of %zu bytes, %zu needed", workspace_bytes, need);

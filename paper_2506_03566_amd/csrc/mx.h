@@ -39,7 +39,10 @@ bool launch_mx_gate_up(int dt, const void *packed, int F, int K, const void *X, 
 // Leaves the message that poss_last_error(NULL) returns; the code is handed through.
 int set_error(int code, const char *fmt, ...);
 
-static inline int mx_blocks(int cols) { return (cols + MX_BLOCK - 1) / MX_BLOCK; }
+static inline int mx_blocks(int cols) { return (cols - 1) / MX_BLOCK + 1; }     // cols > 0
+// What a product takes: offsets within a tile's rows are 32 bits (256 rows of three times K 16-bit values), and so are a launch's threads.
+constexpr int MX_MOST_M = 1 << 24, MX_MOST_N = 1 << 27, MX_MOST_K = 1 << 21;
+constexpr int64_t MX_MOST_MN = 1ll << 38;
 
 // 2^(b - 127) of a scale byte, exactly (2^-127 is subnormal).
 __device__ __forceinline__ float mx_power(unsigned b) {

@@ -186,13 +186,11 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ 
 }
 
 // Quantisation and packing of a context's matrices in one kernel, when it is loaded: a workgroup per column tile reads its rows (the packed order's:
-// gate and up alternate, heads have their rotary pairs side by side) once for the scales and once for the codes.  What poss_mx_quantize and
+// gate and up alternate, heads have their rotary pairs side by side) once for the rows' largest scales and once for the codes.  What poss_mx_quantize and
 // poss_mx_pack give for the same rows.
-constexpr int MX_ROW_BLOCKS = 1024;                       // K up to twice the largest d_model
 template <typename T> __global__ __launch_bounds__(256) void mx_pack_rows_kernel(PackSrc src, int K, int ksteps, u32x4 *__restrict__ out, uint32_t *__restrict__ out_scales,
                                                                                  int32_t *__restrict__ ref) {
     __shared__ int top[16];
-    __shared__ uint8_t sc[16 * MX_ROW_BLOCKS];
     const int tile = blockIdx.x, tid = threadIdx.x, blocks = (K + MX_BLOCK - 1) / MX_BLOCK, groups = ksteps / 4;
     if (tid < 16) top[tid] = 0;
     __syncthreads();
@@ -207,14 +205,19 @@ template <typename T> __global__ __launch_bounds__(256) void mx_pack_rows_kernel
             else in[i].v.u = u32x4{0u, 0u, 0u, 0u};
         }
     };
-    for (int i = tid; i < 16 * blocks; i += 256) {
-        const int r = i / blocks, b = i - r * blocks;
-        MxIn<T> in[4];
-        load(row_of(r), b, in);
+    auto scale_of = [&](const MxIn<T> (&in)[4]) {
         const unsigned field = max(max(in[0].top(), in[1].top()), max(in[2].top(), in[3].top())) >> 23;
-        const int s = field == 255 ? 255 : field < 2 ? 0 : (int)field - 2;
-        sc[r * blocks + b] = (uint8_t)s;
-        atomicMax(&top[r], s);
+        return field == 255 ? 255 : field < 2 ? 0 : (int)field - 2;
+    };
+    {
+        const T *row = row_of(tid >> 4);
+        int t = 0;
+        for (int b = tid & 15; b < blocks; b += 16) {
+            MxIn<T> in[4];
+            load(row, b, in);
+            t = max(t, scale_of(in));
+        }
+        atomicMax(&top[tid >> 4], t);                     // (the largest: the same in any order)
     }
     __syncthreads();
     if (tid < 16) ref[tile * 16 + tid] = top[tid];
@@ -229,7 +232,7 @@ template <typename T> __global__ __launch_bounds__(256) void mx_pack_rows_kernel
             if (row && b < blocks) {
                 MxIn<T> in[4];
                 load(row, b, in);
-                const int sb = sc[r * blocks + b];
+                const int sb = scale_of(in);
                 if (sb != 255) c = u32x4{in[0].codes(mx_power(sb)), in[1].codes(mx_power(sb)), in[2].codes(mx_power(sb)), in[3].codes(mx_power(sb))};
                 s = min(127, max(0, sb - top[r] + 127));
             }
@@ -300,10 +303,12 @@ int launched(const char *who) {
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? POSS_OK : set_error(POSS_E_HIP, "%s: %s", who, hipGetErrorString(e));
 }
+bool weight_ok(int32_t N, int32_t K) { return N > 0 && N <= MX_MOST_N && K > 0 && K <= MX_MOST_K; }
+bool product_ok(int32_t M, int32_t N, int32_t K) { return weight_ok(N, K) && M >= 0 && M <= MX_MOST_M && (int64_t)M * N <= MX_MOST_MN; }
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 // what both products check
 int check_product(const char *who, const void *packed, const void *y, int32_t y_dtype, int64_t ldy, int32_t M, int32_t N, int32_t K, const void *scratch, size_t scratch_bytes, size_t need) {
-    if (M < 0 || N < 1 || K < 1 || ldy < N || bad_dtype(y_dtype)) return set_error(POSS_E_INVALID_ARG, "%s: bad shape or type", who);
+    if (!product_ok(M, N, K) || ldy < N || bad_dtype(y_dtype)) return set_error(POSS_E_INVALID_ARG, "%s: bad shape or type", who);
     if (M == 0) return POSS_OK;
     if (!packed || !y || !scratch) return set_error(POSS_E_INVALID_ARG, "%s: null argument", who);
     if (reinterpret_cast<uintptr_t>(packed) % 256 || reinterpret_cast<uintptr_t>(scratch) % 256)
@@ -334,10 +339,10 @@ int poss_mx_dequantize(int32_t dtype, const void *codes, const void *scales, int
     return launched("poss_mx_dequantize");
 }
 
-size_t poss_mx_packed_bytes(int32_t N, int32_t K) { return N < 1 || K < 1 ? 0 : mx_packed_size(N, K); }
+size_t poss_mx_packed_bytes(int32_t N, int32_t K) { return weight_ok(N, K) ? mx_packed_size(N, K) : 0; }
 
 int poss_mx_pack(const void *codes, const void *scales, int32_t N, int32_t K, void *packed, void *hip_stream) {
-    if (N < 1 || K < 1) return set_error(POSS_E_INVALID_ARG, "poss_mx_pack: bad shape");
+    if (!weight_ok(N, K)) return set_error(POSS_E_INVALID_ARG, "poss_mx_pack: bad shape");
     if (!codes || !scales || !packed) return set_error(POSS_E_INVALID_ARG, "poss_mx_pack: null argument");
     if (!aligned16(codes) || reinterpret_cast<uintptr_t>(packed) % 256) return set_error(POSS_E_INVALID_ARG, "poss_mx_pack: codes must be aligned to 16 bytes, packed to 256");
     launch_mx_pack(codes, scales, N, K, packed, static_cast<hipStream_t>(hip_stream));
@@ -345,14 +350,14 @@ int poss_mx_pack(const void *codes, const void *scales, int32_t N, int32_t K, vo
 }
 
 size_t poss_mx_gemm_scratch_bytes(int32_t x_dtype, int32_t M, int32_t N, int32_t K) {
-    if ((bad_dtype(x_dtype) && x_dtype != POSS_MX) || M < 0 || N < 1 || K < 1) return 0;
+    if ((bad_dtype(x_dtype) && x_dtype != POSS_MX) || !product_ok(M, N, K)) return 0;
     return mx_gemm_scratch_size(x_dtype, M, N, K);
 }
 
 int poss_mx_gemm(int32_t x_dtype, const void *x, int64_t ldx, const void *packed, int32_t y_dtype, void *y, int64_t ldy, int32_t M, int32_t N, int32_t K,
                  void *scratch, size_t scratch_bytes, void *hip_stream) {
     if (bad_dtype(x_dtype) || ldx < K) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm: bad shape or type");
-    const int rc = check_product("poss_mx_gemm", packed, y, y_dtype, ldy, M, N, K, scratch, scratch_bytes, M > 0 && N > 0 && K > 0 ? mx_gemm_scratch_size(x_dtype, M, N, K) : 0);
+    const int rc = check_product("poss_mx_gemm", packed, y, y_dtype, ldy, M, N, K, scratch, scratch_bytes, poss_mx_gemm_scratch_bytes(x_dtype, M, N, K));
     if (rc != POSS_OK || M == 0) return rc;
     if (!x) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm: null argument");
     if (reinterpret_cast<uintptr_t>(x) % dtype_size(x_dtype)) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm: x is not aligned to its type");
@@ -362,7 +367,7 @@ int poss_mx_gemm(int32_t x_dtype, const void *x, int64_t ldx, const void *packed
 
 int poss_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *packed, int32_t y_dtype, void *y, int64_t ldy, int32_t M, int32_t N, int32_t K,
                     void *scratch, size_t scratch_bytes, void *hip_stream) {
-    const int rc = check_product("poss_mx_gemm_mx", packed, y, y_dtype, ldy, M, N, K, scratch, scratch_bytes, M > 0 && N > 0 && K > 0 ? mx_gemm_scratch_size(POSS_MX, M, N, K) : 0);
+    const int rc = check_product("poss_mx_gemm_mx", packed, y, y_dtype, ldy, M, N, K, scratch, scratch_bytes, poss_mx_gemm_scratch_bytes(POSS_MX, M, N, K));
     if (rc != POSS_OK || M == 0) return rc;
     if (!x_codes || !x_scales) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm_mx: null argument");
     if (!aligned16(x_codes)) return set_error(POSS_E_INVALID_ARG, "poss_mx_gemm_mx: x_codes must be aligned to 16 bytes");

@@ -3,7 +3,7 @@
 //
 // 16-bit X: a weight becomes c * 2^(s - ref) in the type of X (one conversion instruction for two, exact) and enters
 // v_mfma_f32_16x16x32; the 32 codes that a lane holds per k-step are the k values of four such instructions, lane / 16 choosing the block of
-// 32 and the instruction eight values of it, so that X is read in the same order: 64 contiguous bytes of a row per lane.
+// 32 and the instruction eight values of it, so that a lane takes 64 contiguous bytes of a row of X.
 // float32 X: the sum of three bf16 numbers, three instructions.  Microscaled X: v_mfma_scale with both scales, one block per lane.
 // The sums are multiplied by 2^ref at the end.  Products are formed transposed (weights as MFMA rows): a lane holds four consecutive
 // columns of a row of Y.
@@ -283,6 +283,13 @@ __device__ __forceinline__ void mx_tile_of(const MxGeom &g, int gm_rows, int &tm
     tn = in_grp / gm;
 }
 
+// This split's k-steps: whole groups of four, the last split's as far as the product goes.
+__device__ __forceinline__ void mx_split_of(const MxGeom &g, int &s0, int &n) {
+    const int groups = (g.steps + 3) >> 2;
+    s0 = (int)((int64_t)blockIdx.y * groups / g.splits) * 4;
+    n = min((int)((int64_t)(blockIdx.y + 1) * groups / g.splits) * 4, g.steps) - s0;
+}
+
 // Four consecutive columns to a plane.
 template <int SHIFT> __device__ __forceinline__ void mx_store_plane(float *p, f32x4 a, const MxGeom &g, const MxPacked &w, int col) {
     *reinterpret_cast<MxQuad<float> *>(p) = g.plane_scaled ? mx_scaled<float>(a, w.ref, col, SHIFT) : __builtin_bit_cast(MxQuad<float>, a);
@@ -332,9 +339,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
     __shared__ __attribute__((aligned(1024))) u32x4 xs[2 * UNITS * 64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % WM, wn = wave / WM;
     int tm, tn;
-    mx_tile_of(g, TM >= 256 ? 8 : 16, tm, tn);
+    mx_tile_of(g, 8, tm, tn);
     const int m0 = tm * TM, ct0 = tn * (TN / 16) + wn * NTW;
-    const int s0 = (int)((int64_t)blockIdx.y * g.steps / g.splits), n = (int)((int64_t)(blockIdx.y + 1) * g.steps / g.splits) - s0;
+    int s0, n;
+    mx_split_of(g, s0, n);
 
     // Unit u of a stage: rows 16 (u / 4).., columns 32 (u % 4).. of the k-step, four lanes per row; piece p (eight columns) of row r lies at
     // position p ^ (r / 4 % 4), so that sixteen lanes that read the same piece of sixteen rows meet every bank once.
@@ -428,48 +436,48 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
 // ------------------------------------------------------------------------------------------ tens of rows
 // Up to some hundred rows: what bounds a product is how fast a CU draws weights and X through its L1 together (some 45 GB/s measured, whatever
 // the shape of a load), and what comes between: a wave that waits for X cannot ask for weights.  So FW waves of a workgroup do nothing but
-// fetch X into LDS, a group of four k-steps (KS k-steps) a stage, two stages; the others keep the codes of their own columns four k-steps
+// fetch X into LDS, a group of four k-steps a stage, two stages; the others keep the codes of their own columns four k-steps
 // ahead in registers, and multiply.  One barrier per stage, where reads pass into the next one, as in mx_tile_kernel.
 // SILU: the columns alternate in groups of 16 gates and 16 ups (PackSrc::interleave16), and what is written is SiLU(gate) * up, [M][ldy].
-template <typename T, typename Y, int TM, int TN, int WM, int WN, int FW, int KS, bool SPLIT, bool SILU = false>
+template <typename T, typename Y, int TM, int TN, int WM, int WN, int FW, bool SPLIT, bool SILU = false>
 __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w, MxRows x, MxGeom g, Y *__restrict__ y, int64_t ldy, bool quads, bool wide) {
     typedef __attribute__((address_space(3))) void *LdsPtr;
     typedef MxOp<T> Op;
-    constexpr int WAVES = WM * WN, MTW = TM / (16 * WM), NTW = TN / (16 * WN), UNITS = TM / 4 * KS, UPW = UNITS / FW;     // 1 KB units of a stage
-    constexpr int STAGES = 4 / KS, SLOTS = 4 * MTW * KS, AHEAD = 3;
-    static_assert(UPW * FW == UNITS && STAGES * KS == 4 && SLOTS > AHEAD, "tile shape");
+    constexpr int WAVES = WM * WN, MTW = TM / (16 * WM), NTW = TN / (16 * WN), UNITS = TM, UPW = UNITS / FW;         // 1 KB units of a stage
+    constexpr int SLOTS = 16 * MTW, AHEAD = 3;
+    static_assert(UPW * FW == UNITS, "tile shape");
     __shared__ __attribute__((aligned(1024))) u32x4 xs[2 * UNITS * 64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     int tm, tn;
     mx_tile_of(g, 16, tm, tn);
     const int m0 = tm * TM;
-    // groups of four k-steps
-    const int n_groups = (g.steps + 3) >> 2, g0 = (int)((int64_t)blockIdx.y * n_groups / g.splits), n = (int)((int64_t)(blockIdx.y + 1) * n_groups / g.splits) - g0;
-    const int stages = n * STAGES;
+    int g0, n;                                            // groups of four k-steps
+    mx_split_of(g, g0, n);
+    g0 >>= 2; n = (n + 3) >> 2;
 
     if (wave >= WAVES) {                                  // a wave that fetches
         const int fw = wave - WAVES, x_piece = (lane & 3) ^ ((lane >> 4) & 3);
         const unsigned lds0 = (unsigned)(uintptr_t)(LdsPtr)&xs[0];
         const T *src = static_cast<const T *>(x.x) + (int64_t)m0 * x.ldx + (int64_t)g0 * 4 * MX_KSTEP;
         auto issue = [&](int t) {                         // stage t
-            const int k0 = g0 * 4 * MX_KSTEP + t * KS * MX_KSTEP;
-            const bool whole = k0 + KS * MX_KSTEP <= g.full * MX_KSTEP;
+            const int k0 = (g0 + t) * 4 * MX_KSTEP;
+            const bool whole = (g0 + t + 1) * 4 <= g.full;
 #pragma unroll
             for (int j = 0; j < UPW; ++j) {
-                const int u = fw + FW * j, m = min(u / (4 * KS) * 16 + (lane >> 2), g.M - 1 - m0), k = (u % (4 * KS)) * MX_BLOCK + x_piece * 8;
+                const int u = fw + FW * j, m = min((u >> 4) * 16 + (lane >> 2), g.M - 1 - m0), k = (u & 15) * MX_BLOCK + x_piece * 8;
                 const unsigned off = ((unsigned)m * (unsigned)x.ldx + (unsigned)k) * 2u, dst = lds0 + (unsigned)(((t & 1) * UNITS + u) * 1024);
-                if (whole) lds_dma16_s(dst, src + (int64_t)t * KS * MX_KSTEP, off);
+                if (whole) lds_dma16_s(dst, src + (int64_t)t * 4 * MX_KSTEP, off);
                 else {
-                    const char *p = reinterpret_cast<const char *>(src + (int64_t)t * KS * MX_KSTEP) + off;
+                    const char *p = reinterpret_cast<const char *>(src + (int64_t)t * 4 * MX_KSTEP) + off;
                     lds_dma16(dst, k0 + k < x.K ? static_cast<const void *>(p) : static_cast<const void *>(&mx_zero_piece));
                 }
             }
         };
         issue(0);
-        for (int t = 0; t < stages; ++t) {
+        for (int t = 0; t < n; ++t) {
             dma_wait<0>();
             __syncthreads();                              // stage t has landed; nobody reads stage t - 1 any more
-            if (t + 1 < stages) issue(t + 1);
+            if (t + 1 < n) issue(t + 1);
         }
         if (TM >= 64 && !SILU && wide) __syncthreads();   // (the others write their results through LDS)
         return;
@@ -497,9 +505,9 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
         for (int nt = 0; nt < NTW; ++nt) c[s][nt] = wp[nt][(wg * 4 + s) * 64];
 #pragma unroll
     for (int nt = 0; nt < NTW; ++nt) sc[nt] = sp[nt][wg * 64];
-    // X: + (4 KS) * 64 per row tile, block b of a stage at b * 64, piece i at i ^ rs
-    const int rd = (wm * MTW * 4 * KS + (lane >> 4)) * 64 + (lane & 15) * 4, rs = (lane >> 2) & 3;
-    auto x_at = [&](int q) { const int ks = q / (4 * MTW), i = q / MTW & 3, mt = q % MTW; return rd + (mt * 4 * KS + ks * 4) * 64 + (i ^ rs); };
+    // X: sixteen units per row tile, a block of columns each; slot q of a stage: k-step q / (4 MTW), substep q / MTW % 4, row tile q % MTW
+    const int rd = (wm * MTW * 16 + (lane >> 4)) * 64 + (lane & 15) * 4, rs = (lane >> 2) & 3;
+    auto x_at = [&](int q) { return rd + ((q % MTW) * 16 + q / (4 * MTW) * 4) * 64 + ((q / MTW & 3) ^ rs); };
     auto scale = [&](int s, unsigned four) { return s == 0 ? mx_scale<T, 0>(four) : s == 1 ? mx_scale<T, 1>(four) : s == 2 ? mx_scale<T, 2>(four) : mx_scale<T, 3>(four); };
     __syncthreads();
     int st = 0;
@@ -507,22 +515,21 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
     for (int q = 0; q < AHEAD; ++q) xf[q] = xs[x_at(q)];
 #pragma unroll
     for (int nt = 0; nt < NTW; ++nt) wf[0][nt] = Op::weights(c[0][nt][0], scale(0, sc[nt]));
-    auto group = [&](auto more_, bool last) {
+    auto group = [&](auto more_) {
         constexpr bool more = decltype(more_)::value;
+        const u32x4 *cur = xs + st * UNITS * 64, *nxt = xs + (st ^ 1) * UNITS * 64;
         const int wn_ = wg + 1 == w.kgroups ? 0 : wg + 1;
         if constexpr (more)
 #pragma unroll
             for (int nt = 0; nt < NTW; ++nt) sn[nt] = sp[nt][wn_ * 64];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int ks = s % KS;
-            const u32x4 *cur = xs + st * UNITS * 64, *nxt = xs + (st ^ 1) * UNITS * 64;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
 #pragma unroll
                 for (int mt = 0; mt < MTW; ++mt) {
-                    const int q = (ks * 4 + i) * MTW + mt;
-                    if (q == SLOTS - AHEAD && (more || s < 3)) {
+                    const int q = (s * 4 + i) * MTW + mt;
+                    if (more && q == SLOTS - AHEAD) {
                         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                         __syncthreads();
                     }
@@ -543,15 +550,15 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
 #pragma unroll
                         for (int nt = 0; nt < NTW; ++nt) c[s][nt] = wp[nt][(wn_ * 4 + s) * 64];
             }
-            if (ks == KS - 1) st ^= 1;
         }
+        st ^= 1;
         wg = wn_;
         if constexpr (more)
 #pragma unroll
             for (int nt = 0; nt < NTW; ++nt) sc[nt] = sn[nt];
     };
-    for (int s = 0; s + 1 < n; ++s) group(Yes{}, false);
-    group(No{}, true);
+    for (int t = 0; t + 1 < n; ++t) group(Yes{});
+    group(No{});
     if constexpr (SILU) {
         static_assert(NTW % 2 == 0, "a wave holds gates with their ups");
 #pragma unroll
@@ -578,8 +585,10 @@ __device__ __forceinline__ void lds_dma4_s(unsigned lds_base, const void *g, uns
 
 // ------------------------------------------------------------------------------------------ both operands in 4 bits, tens of rows
 // mx_fed_kernel for microscaled X: a lane's block of 16 bytes is an operand as it is, so a stage is codes (a 1 KB unit per row tile and
-// k-step: four lanes fetch a row's 64 bytes, block b of row r to position b ^ (r / 4 % 4)) and, for each row tile and group, the scales of a lane's four blocks in one word, which the fetching waves
-// put together from the rows' bytes.  KG groups of four k-steps a stage.
+// k-step: four lanes fetch a row's 64 bytes, block b of row r to position b ^ (r / 4 % 4)) and, for each row tile and group, the scales of
+// a lane's four blocks in one word, which the fetching waves put together from the rows' bytes.  KG groups of four k-steps a stage.
+// (Sixteen lanes fetching one block each of sixteen rows took four times as long to issue: 8192 x 28672 x 4096 843 us, now 558 with the
+// results' way out.)
 template <typename Y, int TM, int TN, int WM, int WN, int FW, int KG, bool SPLIT>
 __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint8_t *__restrict__ xs_, int blocks, MxGeom g, Y *__restrict__ y,
                                                                           int64_t ldy, bool quads, bool wide) {
@@ -960,6 +969,7 @@ template <int SHAPES> static MxPlan best_plan(const MxTile (&tiles)[SHAPES], int
     for (int i = 1; i < SHAPES; ++i) {
         const MxTile &t = tiles[i];
         const float n = (float)((M + t.tm - 1) / t.tm) * (float)((N + t.tn - 1) / t.tn);
+        if (n > 4e6f && i + 1 < SHAPES) continue;         // (a launch has fewer than 2^32 threads)
         for (int s = fixed > 0 ? fixed : 1; s <= (fixed > 0 ? fixed : 16) && s <= groups && (fixed > 0 || s == 1 || n * s <= 1024); ++s) {
             const float g = (float)((groups + s - 1) / s), chips = n * s / 256, rounds = ceilf(chips);
             float us = t.us[0] + t.us[1] * g + t.us[2] * g * rounds + t.us[3] * g * chips + t.us[4] * rounds + t.us[7] * mn;
@@ -1021,17 +1031,17 @@ static void run_tiles(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan
     g.splits = p.splits; g.tiles_m = (g.M + t.tm - 1) / t.tm; g.tiles_n = (g.N + t.tn - 1) / t.tn;
     const dim3 grid(g.tiles_m * g.tiles_n, g.splits);
     const bool wide = wide_ok(y, ldy, g.N);
-#define POSS_MX_FED(TM, TN, WM, WN, FW, KS)                                                                                                  \
+#define POSS_MX_FED(TM, TN, WM, WN, FW)                                                                                                      \
     do {                                                                                                                                     \
-        if (g.splits > 1) mx_fed_kernel<T, float, TM, TN, WM, WN, FW, KS, true><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, part, 0, true, true); \
-        else mx_fed_kernel<T, Y, TM, TN, WM, WN, FW, KS, false><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, y, ldy, quads, wide);         \
+        if (g.splits > 1) mx_fed_kernel<T, float, TM, TN, WM, WN, FW, true><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, part, 0, true, true); \
+        else mx_fed_kernel<T, Y, TM, TN, WM, WN, FW, false><<<grid, (WM * WN + FW) * 64, 0, st>>>(w, x, g, y, ldy, quads, wide);         \
     } while (0)
     switch (p.shape) {
-        case 1: POSS_MX_FED(16, 64, 1, 4, 2, 4); break;
-        case 2: POSS_MX_FED(32, 128, 1, 8, 4, 4); break;
-        case 3: POSS_MX_FED(32, 256, 1, 8, 4, 4); break;
-        case 4: POSS_MX_FED(64, 128, 2, 4, 4, 4); break;
-        case 5: POSS_MX_FED(64, 256, 1, 8, 4, 4); break;
+        case 1: POSS_MX_FED(16, 64, 1, 4, 2); break;
+        case 2: POSS_MX_FED(32, 128, 1, 8, 4); break;
+        case 3: POSS_MX_FED(32, 256, 1, 8, 4); break;
+        case 4: POSS_MX_FED(64, 128, 2, 4, 4); break;
+        case 5: POSS_MX_FED(64, 256, 1, 8, 4); break;
         default:
             if (g.splits > 1) mx_tile_kernel<T, float, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(w, x, g, part, 0, true, true);
             else mx_tile_kernel<T, Y, 256, 256, 2, 4, false><<<grid, 512, 0, st>>>(w, x, g, y, ldy, quads, wide);
@@ -1115,7 +1125,25 @@ bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, i
 // Whether the planes are one (mx_stream_kernel adds its waves' sums itself).
 int mx_planes_written(int M, int N, int K, int splits) { return best_plan(MX_TILES, M, N, mx_groups(K), splits).shape == MX_STREAM ? 1 : splits; }
 
-static void launch_mx_silu(int dt, const float *part, int splits, int M, int ld, int F, void *act, hipStream_t st);
+// A thread per four units.  Of 61 rows of 28672 columns: 15 MB read, from the L2s for the most part.
+template <typename T>
+__global__ __launch_bounds__(256) void mx_silu_kernel(const float *__restrict__ part, int splits, int M, int ld, int F, T *__restrict__ act) {
+    const int f = (blockIdx.x * 256 + threadIdx.x) * 4, m = blockIdx.y;
+    if (f >= F) return;                                   // (F is a multiple of eight)
+    const float *p = part + (size_t)m * ld + (f >> 4) * 32 + (f & 15);
+    const size_t plane = (size_t)M * ld;
+    f32x4 gate = *reinterpret_cast<const f32x4 *>(p), up = *reinterpret_cast<const f32x4 *>(p + 16);
+    for (int s = 1; s < splits; ++s) {
+        gate += *reinterpret_cast<const f32x4 *>(p + s * plane);
+        up += *reinterpret_cast<const f32x4 *>(p + s * plane + 16);
+    }
+    *reinterpret_cast<MxQuad<T> *>(act + (size_t)m * F + f) = mx_silu_quad<T>(__builtin_bit_cast(MxQuad<float>, gate), __builtin_bit_cast(MxQuad<float>, up));
+}
+static void launch_mx_silu(int dt, const float *part, int splits, int M, int ld, int F, void *act, hipStream_t st) {
+    const dim3 grid((F / 4 + 255) / 256, M);
+    if (dt == DT_BF16) mx_silu_kernel<bf16_t><<<grid, 256, 0, st>>>(part, splits, M, ld, F, static_cast<bf16_t *>(act));
+    else mx_silu_kernel<f16_t><<<grid, 256, 0, st>>>(part, splits, M, ld, F, static_cast<f16_t *>(act));
+}
 
 // act[M][F] = SiLU(gate) * up.  Unsplit (enough column tiles for the chip) the product does it itself: tiles whose waves hold a gate column with its up.
 template <typename T>
@@ -1123,7 +1151,7 @@ static void run_silu(const MxPacked &w, const MxRows &x, MxGeom g, T *act, int F
 #define POSS_MX_SILU(TM, TN, WM, WN, FW)                                                                                                     \
     do {                                                                                                                                     \
         g.tiles_m = (g.M + TM - 1) / TM; g.tiles_n = (g.N + TN - 1) / TN;                                                                    \
-        mx_fed_kernel<T, T, TM, TN, WM, WN, FW, 4, false, true><<<dim3(g.tiles_m * g.tiles_n), (WM * WN + FW) * 64, 0, st>>>(w, x, g, act, F, true, false); \
+        mx_fed_kernel<T, T, TM, TN, WM, WN, FW, false, true><<<dim3(g.tiles_m * g.tiles_n), (WM * WN + FW) * 64, 0, st>>>(w, x, g, act, F, true, false); \
     } while (0)
     if (g.M <= 16) POSS_MX_SILU(16, 128, 1, 4, 2);
     else if (g.M <= 32) POSS_MX_SILU(32, 256, 1, 8, 4);
@@ -1145,26 +1173,6 @@ bool launch_mx_gate_up(int dt, const void *packed, int F, int K, const void *X, 
     if (dt == DT_BF16) run_silu<bf16_t>(w, MxRows{X, ldx, 0, K}, g, static_cast<bf16_t *>(act), F, st);
     else run_silu<f16_t>(w, MxRows{X, ldx, 0, K}, g, static_cast<f16_t *>(act), F, st);
     return true;
-}
-
-// A thread per four units.  Of 61 rows of 28672 columns: 15 MB read, from the L2s for the most part.
-template <typename T>
-__global__ __launch_bounds__(256) void mx_silu_kernel(const float *__restrict__ part, int splits, int M, int ld, int F, T *__restrict__ act) {
-    const int f = (blockIdx.x * 256 + threadIdx.x) * 4, m = blockIdx.y;
-    if (f >= F) return;                                   // (F is a multiple of eight)
-    const float *p = part + (size_t)m * ld + (f >> 4) * 32 + (f & 15);
-    const size_t plane = (size_t)M * ld;
-    f32x4 gate = *reinterpret_cast<const f32x4 *>(p), up = *reinterpret_cast<const f32x4 *>(p + 16);
-    for (int s = 1; s < splits; ++s) {
-        gate += *reinterpret_cast<const f32x4 *>(p + s * plane);
-        up += *reinterpret_cast<const f32x4 *>(p + s * plane + 16);
-    }
-    *reinterpret_cast<MxQuad<T> *>(act + (size_t)m * F + f) = mx_silu_quad<T>(__builtin_bit_cast(MxQuad<float>, gate), __builtin_bit_cast(MxQuad<float>, up));
-}
-static void launch_mx_silu(int dt, const float *part, int splits, int M, int ld, int F, void *act, hipStream_t st) {
-    const dim3 grid((F / 4 + 255) / 256, M);
-    if (dt == DT_BF16) mx_silu_kernel<bf16_t><<<grid, 256, 0, st>>>(part, splits, M, ld, F, static_cast<bf16_t *>(act));
-    else mx_silu_kernel<f16_t><<<grid, 256, 0, st>>>(part, splits, M, ld, F, static_cast<f16_t *>(act));
 }
 
 void launch_mx_gemm(int x_dt, const void *x, int64_t ldx, const void *packed, int y_dt, void *y, int64_t ldy, int M, int N, int K, void *scratch, hipStream_t st) {

@@ -295,6 +295,26 @@ def test_the_same_call_gives_the_same_bits():
             assert torch.equal(P.mx_gemm(x, packed, y), first) and torch.equal(P.mx_gemm_mx(c, s, packed, z), both)
 
 
+def test_two_streams_at_once_with_scratch_of_their_own():
+    rng = np.random.default_rng(12)
+    M, N, K = 40, 512, 8192                                # (planes of several splits in scratch)
+    _, packed = weights(rng, N, K)
+    xs = [rows_of(rng, M, K, "bf16") for _ in range(2)]
+    want = [P.mx_gemm(x, packed, torch.empty(M, N, device="cuda")) for x in xs]
+    want_q = [P.mx_gemm_mx(*P.mx_quantize(x), packed, torch.empty(M, N, device="cuda")) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    scratch = [P.mx_gemm_scratch(t, M, N, K) for t in (torch.bfloat16, torch.bfloat16, None, None)]
+    got = [torch.empty(M, N, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            P.mx_gemm(xs[i], packed, got[i], scratch[i], st)
+            c, s = P.mx_quantize(xs[i], stream=st)
+            P.mx_gemm_mx(c, s, packed, got[2 + i], scratch[2 + i], st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[i], want[i]) and torch.equal(got[2 + i], want_q[i]) for i in range(2))
+
+
 def test_rows_behind_four_gib():
     """Offsets that pass 32 bits: the last rows of matrices of 4.5 GB."""
     K, rows = 4096, 550_000

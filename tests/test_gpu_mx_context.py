@@ -43,7 +43,8 @@ def pair(name, **over):
 
 
 # widths whose products have one split and several, K that ends inside a k-step (1728) and inside a block's group (1000)
-@pytest.mark.parametrize("name,over", [("t_mid_bf16", dict()), ("t_mid_f16", dict()), ("t_mid_bf16", dict(n_layers=2, d_model=1024, n_q_heads=8, n_kv_heads=2, head_dim=128, d_ffn=1000))])
+@pytest.mark.parametrize("name,over", [("t_mid_bf16", dict()), ("t_mid_f16", dict()), ("t_mid_bf16", dict(n_layers=2, d_model=1024, n_q_heads=8, n_kv_heads=2, head_dim=128, d_ffn=1000)),
+                                       ("t_mid_f16", dict(n_layers=1, n_specialists=1, d_ffn=40000))])
 def test_rounds_follow_the_oracle_with_the_rounded_weights(name, over):
     """Prompt, then three rounds in lock-step: logits and features of every tree row, the cache, tokens where the oracle's choice is clear."""
     cfg, ctx, o = pair(name, **over)
@@ -100,6 +101,32 @@ def test_one_row_has_the_bits_of_a_tree_row(name, over):
     from synth.gpu import make_weights_on_device
     ctx = P.Poss(cfg, make_weights_on_device(cfg), mx=True)
     one_row_against_tree_rows(cfg, ctx, (20, 300, 1300))
+    ctx.close()
+
+
+# gate and up of one split with SiLU in the product, in each of its tile shapes, and of several
+@pytest.mark.parametrize("name,over", [("t_mid_bf16", dict(d_model=4096, n_q_heads=32, n_kv_heads=8, head_dim=128, d_ffn=14336)), ("t_mid_f16", dict(d_ffn=11000)),
+                                       ("t_mid_bf16", dict())])
+def test_a_row_has_the_same_bits_in_trees_of_any_size(name, over):
+    """(Trees of one group have as many blocks of 64 keys: attention cuts them alike.)"""
+    cfg = get_config(name, **dict(over, n_layers=2, vocab=1000, max_seq=512, n_specialists=1, top_k=10, depth=6, total_tokens=120))
+    from synth.gpu import make_weights_on_device
+    ctx = P.Poss(cfg, make_weights_on_device(cfg), mx=True)
+    rs = np.random.RandomState(6)
+    prompt, wide = rs.randint(0, 1000, 70).astype(np.int32), [0] + [int(x) for x in rs.permutation(1000)[:120]]
+    for group in ((33, 1, 16, 17, 32), (120, 64, 65)):
+        got = []
+        for rows in group:
+            ctx.reset()
+            ctx.prefill(prompt)
+            logits, feats = torch.zeros(rows, 1000, device="cuda"), torch.zeros(rows, cfg.d_model, device="cuda")
+            ctx.verify_tree(P.TreeArrays.from_lists(wide[:rows], [-1] + [0] * (rows - 1)), logits_out=logits, feat_out=feats)
+            got.append((logits, feats))
+        torch.cuda.synchronize()
+        assert torch.isfinite(got[0][0]).all()
+        for logits, feats in got[1:]:
+            n = logits.shape[0]
+            assert torch.equal(feats, got[0][1][:n]) and torch.equal(logits, got[0][0][:n]), n
     ctx.close()
 
 

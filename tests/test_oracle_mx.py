@@ -77,6 +77,9 @@ def test_refusals_need_no_gpu():
         assert lib.poss_mx_gemm_scratch_bytes(dt, 0, 1, 1) >= 256
         assert lib.poss_mx_gemm_scratch_bytes(dt, -1, 1, 1) == lib.poss_mx_gemm_scratch_bytes(dt, 1, 0, 1) == lib.poss_mx_gemm_scratch_bytes(dt, 1, 1, 0) == 0
     assert lib.poss_mx_gemm_scratch_bytes(3, 1, 1, 1) == 0
+    assert lib.poss_mx_packed_bytes(16, (1 << 21) + 1) == lib.poss_mx_packed_bytes((1 << 27) + 1, 32) == 0
+    for big in ((1, 16, (1 << 21) + 1), (1, (1 << 27) + 1, 32), ((1 << 24) + 1, 16, 32), (1 << 24, (1 << 14) + 1, 32)):
+        assert [lib.poss_mx_gemm_scratch_bytes(dt, *big) for dt in (0, 1, 2, 4)] == [0] * 4
     need = lib.poss_mx_gemm_scratch_bytes(1, 2, 16, 32)
 
     def gemm(xt=1, x=a, ldx=32, w=o, yt=1, y=a, ldy=16, M=2, N=16, K=32, scratch=o, n=need):
@@ -106,7 +109,8 @@ def test_the_binding_refuses_what_the_kernels_would_misread():
     _lib()
     x, y = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, 16)
     codes, scales = torch.zeros(4, 32, dtype=u8), torch.zeros(4, 2, dtype=u8)
-    w = P.MxWeight(torch.zeros(4096, dtype=u8), 16, 64)
+    w = P.MxWeight(torch.zeros(P.load_library().poss_mx_packed_bytes(16, 64), dtype=u8), 16, 64)
+    assert refused(P.MxWeight, torch.zeros(4096, dtype=u8), 16, 64)        # too few bytes
     assert refused(P.mx_quantize, x, codes, scales)                        # host memory
     assert refused(P.mx_quantize, x.t())                                   # rows that are not contiguous
     assert refused(P.mx_quantize, x[0])                                    # not a matrix
@@ -123,6 +127,8 @@ def test_the_binding_refuses_what_the_kernels_would_misread():
     assert refused(P.mx_pack, codes, scales, 128)
     assert refused(P.mx_gemm_scratch, torch.int8, 4, 16, 64)
     assert refused(P.mx_gemm_scratch, None, -1, 16, 64)
+    assert refused(P.mx_gemm_scratch, None, 4, (1 << 32) + 16, 64)         # (would pass as 16 in 32 bits)
+    assert refused(P.mx_gemm, x, w, y, torch.zeros(4, 600, dtype=u8)[:, :512])   # scratch with gaps
 
 
 def test_workspace_of_microscaled_layers():
@@ -137,3 +143,21 @@ def test_workspace_of_microscaled_layers():
     out = ctypes.c_void_p()
     c = P.make_config(CONFIGS["t_mid_bf16"])
     assert lib.poss_load_mx(ctypes.byref(c), None, None, 0, None, ctypes.byref(out)) == P.E_INVALID_ARG
+
+
+def test_microscaled_layers_of_any_width_up_to_the_products_limit():
+    import ctypes
+    from synth import CONFIGS
+    lib = _lib()
+    base = CONFIGS["t_mid_bf16"]
+
+    def size(**over):
+        c = P.make_config(base)
+        for k, v in over.items():
+            setattr(c, k, v)
+        return lib.poss_workspace_bytes_mx(ctypes.byref(c)), lib.poss_workspace_bytes(ctypes.byref(c))
+
+    small, full = size(d_ffn=1 << 21, n_layers=1)
+    assert 0 < small < full
+    small, full = size(d_ffn=(1 << 21) + 8, n_layers=1)
+    assert small == 0 < full
