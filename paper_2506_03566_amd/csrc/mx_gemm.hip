@@ -50,22 +50,25 @@ __device__ const u32x4 mx_zero_piece = {0u, 0u, 0u, 0u};  // what a lane reads w
 
 // The sums of four consecutive columns n.. of row m, times 2^ref, to Y.
 template <typename Y> struct __attribute__((aligned(4 * sizeof(Y)))) MxQuad { Y v[4]; };
-template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_scaled(f32x4 a, const int32_t *__restrict__ ref, int n, int shift) {
+template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_scaled(f32x4 a, int4 e, int shift) {
     MxQuad<Y> o;
-    const int4 e = *reinterpret_cast<const int4 *>(ref + n);
     const int es[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
     for (int r = 0; r < 4; ++r) o.v[r] = from_f<Y>(es[r] == 255 ? __builtin_nanf("") : __builtin_ldexpf(a[r], es[r] - 127 - shift));
     return o;
 }
+template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_scaled(f32x4 a, const int32_t *__restrict__ ref, int n, int shift) {
+    return mx_scaled<Y>(a, *reinterpret_cast<const int4 *>(ref + n), shift);
+}
 template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_raw(f32x4 a) { MxQuad<Y> o; for (int r = 0; r < 4; ++r) o.v[r] = (Y)a[r]; return o; }
-template <typename Y> __device__ __forceinline__ void mx_store(Y *__restrict__ y, int64_t ldy, bool quads, int m, int n, int N, f32x4 acc, const int32_t *__restrict__ ref, int shift) {
-    const MxQuad<Y> o = mx_scaled<Y>(acc, ref, n, shift);
-    Y *dst = y + (int64_t)m * ldy + n;
-    if (quads) *reinterpret_cast<MxQuad<Y> *>(dst) = o;   // (n, N and ldy are multiples of four then, and y is aligned)
+template <typename Y> __device__ __forceinline__ void mx_store_quad(Y *__restrict__ dst, bool quads, int left, const MxQuad<Y> &o) {
+    if (quads) *reinterpret_cast<MxQuad<Y> *>(dst) = o;   // (columns, N and ldy are multiples of four then, and y is aligned)
     else
 #pragma unroll
-        for (int r = 0; r < 4; ++r) if (n + r < N) dst[r] = o.v[r];
+        for (int r = 0; r < 4; ++r) if (r < left) dst[r] = o.v[r];
+}
+template <typename Y> __device__ __forceinline__ void mx_store(Y *__restrict__ y, int64_t ldy, bool quads, int m, int n, int N, f32x4 acc, const int32_t *__restrict__ ref, int shift) {
+    mx_store_quad<Y>(y + (int64_t)m * ldy + n, quads, N - n, mx_scaled<Y>(acc, ref, n, shift));
 }
 
 // ROWS rows x COLS columns of float32 sums that a wave holds, to Y (times 2^ref) or to a plane, in pieces of 16 bytes: from the lanes' quads
@@ -275,8 +278,8 @@ struct MxGeom {
 
 // Workgroup -> tile: consecutive ids go to the 8 XCDs in turn; an XCD is given a contiguous run of tiles, ordered so that those it works
 // on at a time share rows and columns in its L2.
-__device__ __forceinline__ void mx_tile_of(const MxGeom &g, int gm_rows, int &tm, int &tn) {
-    const int n = g.tiles_m * g.tiles_n, bid = blockIdx.x, q = n >> 3, r = n & 7, x = bid & 7;
+__device__ __forceinline__ void mx_tile_of(const MxGeom &g, int bid, int gm_rows, int &tm, int &tn) {
+    const int n = g.tiles_m * g.tiles_n, q = n >> 3, r = n & 7, x = bid & 7;
     const int id = x * q + (x < r ? x : r) + (bid >> 3);
     const int grp = id / (gm_rows * g.tiles_n), in_grp = id - grp * (gm_rows * g.tiles_n), gm = min(gm_rows, g.tiles_m - grp * gm_rows);
     tm = grp * gm_rows + in_grp % gm;
@@ -339,7 +342,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
     __shared__ __attribute__((aligned(1024))) u32x4 xs[2 * UNITS * 64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % WM, wn = wave / WM;
     int tm, tn;
-    mx_tile_of(g, 8, tm, tn);
+    mx_tile_of(g, blockIdx.x, 8, tm, tn);
     const int m0 = tm * TM, ct0 = tn * (TN / 16) + wn * NTW;
     int s0, n;
     mx_split_of(g, s0, n);
@@ -449,7 +452,7 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
     __shared__ __attribute__((aligned(1024))) u32x4 xs[2 * UNITS * 64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     int tm, tn;
-    mx_tile_of(g, 16, tm, tn);
+    mx_tile_of(g, blockIdx.x, 16, tm, tn);
     const int m0 = tm * TM;
     int g0, n;                                            // groups of four k-steps
     mx_split_of(g, g0, n);
@@ -600,7 +603,7 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_both_kernel(MxPack
     __shared__ __attribute__((aligned(1024))) u32x4 xs[2 * STAGE];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     int tm, tn;
-    mx_tile_of(g, 16, tm, tn);
+    mx_tile_of(g, blockIdx.x, 16, tm, tn);
     const int m0 = tm * TM;
     const int n_groups = w.kgroups, g0 = (int)((int64_t)blockIdx.y * n_groups / g.splits), n = (int)((int64_t)(blockIdx.y + 1) * n_groups / g.splits) - g0;
     const int stages = (n + KG - 1) / KG;
@@ -747,60 +750,65 @@ __global__ __launch_bounds__(256) void mx_scales_kernel(const uint8_t *__restric
 // 256 x 256 tiles, eight waves of 128 x 64 with the 32 x 32 x 64 instruction (registers alone, random codes: 6.3 PFLOP/s where the
 // 16 x 16 x 128 one gives 5.2).  Codes of both operands go into LDS by LDS-direct loads, a k-step of 128 a stage, four stages in a ring,
 // one barrier per k-step; the scales of a group of four k-steps likewise, an eighth of them by each wave, a quarter of that per k-step, two buffers.
-template <typename Y, bool SPLIT>
+// A workgroup per CU takes one tile after the other, and the loads run on into the next one: when a tile's sums are written, the next
+// tile's first three stages and scales are there or on their way.
+template <typename Y>
 __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint32_t *__restrict__ xscales, int blocks, MxGeom g, Y *__restrict__ y,
                                                                int64_t ldy, bool quads, bool wide) {
     typedef __attribute__((address_space(3))) void *LdsPtr;
     constexpr int NST = 4, STAGE = 32 * 64;               // units 0..15: X's row tiles, 16..31: column tiles
     __shared__ __attribute__((aligned(1024))) u32x4 xs[NST * STAGE];
     __shared__ __attribute__((aligned(1024))) unsigned scs[2][32 * 64];
+    __shared__ __attribute__((aligned(1024))) int refs[8 * 64];       // of each wave's 64 columns
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave & 1, wn = wave >> 1;
-    int tm, tn;
-    mx_tile_of(g, 8, tm, tn);
-    const int m0 = tm * 256, ct0 = tn * 16, rts = (g.M + 15) / 16;
-    const int g0 = (int)((int64_t)blockIdx.y * w.kgroups / g.splits), n = ((int)((int64_t)(blockIdx.y + 1) * w.kgroups / g.splits) - g0) * 4;     // k-steps: whole groups
-    const unsigned lds0 = (unsigned)(uintptr_t)(LdsPtr)&xs[0], lds1 = (unsigned)(uintptr_t)(LdsPtr)&scs[0][0];
+    const unsigned lds0 = (unsigned)(uintptr_t)(LdsPtr)&xs[0], lds1 = (unsigned)(uintptr_t)(LdsPtr)&scs[0][0], lds2 = (unsigned)(uintptr_t)(LdsPtr)&refs[0];
     const int x_b = (lane & 3) ^ (lane >> 4);             // block b of row r of a unit of X lies at position b ^ (r / 4 % 4)
-    const u32x4 *xp[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) xp[j] = x + (int64_t)min(m0 + (wave + 8 * j) * 16 + (lane >> 2), g.M - 1) * blocks + x_b;
-    const int wt0 = min(ct0 + wave, w.tiles - 1), wt1 = min(ct0 + wave + 8, w.tiles - 1);
-    const u32x4 *wp0 = w.codes + ((size_t)wt0 * w.ksteps + g0 * 4) * 64, *wp1 = w.codes + ((size_t)wt1 * w.ksteps + g0 * 4) * 64;
-    // the scales this wave brings: unit wave + 8 j of a group at its k-step j (0, 1: row tiles; 2, 3: column tiles)
+    const bool planes = g.splits > 1;                     // (Y is float then)
+    const int tiles = g.tiles_m * g.tiles_n, items = tiles * g.splits, rts = (g.M + 15) / 16;
+    // A tile (of a split) as the loads see it.  Scales: unit wave + 8 j of a group at its k-step j (0, 1: row tiles; 2, 3: column tiles).
+    struct Item { int m0, ct0, split, g0, n; };
+    auto item_of = [&](int i) {
+        Item t;
+        int tm, tn;
+        t.split = i / tiles;
+        mx_tile_of(g, i - t.split * tiles, 8, tm, tn);
+        t.m0 = tm * 256; t.ct0 = tn * 16;
+        t.g0 = (int)((int64_t)t.split * w.kgroups / g.splits);
+        t.n = ((int)((int64_t)(t.split + 1) * w.kgroups / g.splits) - t.g0) * 4;       // k-steps: whole groups
+        return t;
+    };
+    const u32x4 *xp, *wp[2];
     const uint32_t *sp[4];
+    unsigned xo[2];                                       // (256 rows of 2^16 blocks: 32 bits)
+    int x_left;                                           // blocks of a row of X from the item's first on
+    auto codes_at = [&](const Item &t) {
+        xp = x + (int64_t)t.m0 * blocks + t.g0 * 16;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        sp[j] = j < 2 ? xscales + ((size_t)min(m0 / 16 + wave + 8 * j, rts - 1) * w.kgroups + g0) * 64 : w.scales + ((size_t)min(ct0 + wave + 8 * (j - 2), w.tiles - 1) * w.kgroups + g0) * 64;
-    auto issue = [&](int j, int s, int st) {              // load j (static, 0..3) of k-step s (relative), into stage st
+        for (int j = 0; j < 2; ++j) {
+            xo[j] = (unsigned)(min((wave + 8 * j) * 16 + (lane >> 2), g.M - 1 - t.m0) * blocks + x_b) * 16u;
+            wp[j] = w.codes + ((size_t)min(t.ct0 + wave + 8 * j, w.tiles - 1) * w.ksteps + t.g0 * 4) * 64;
+        }
+        x_left = blocks - t.g0 * 16;
+    };
+    auto scales_at = [&](const Item &t) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            sp[j] = xscales + ((size_t)min(t.m0 / 16 + wave + 8 * j, rts - 1) * w.kgroups + t.g0) * 64;
+            sp[2 + j] = w.scales + ((size_t)min(t.ct0 + wave + 8 * j, w.tiles - 1) * w.kgroups + t.g0) * 64;
+        }
+    };
+    auto issue = [&](int j, int s, int st) {              // load j (static, 0..3) of k-step s of the item, into stage st
         const unsigned base = lds0 + (unsigned)(st * STAGE * 16);
         if (j < 2) {
-            const int b = (g0 * 4 + s) * 4;
-            const u32x4 *p = xp[j] + b;
-            if (b + 4 > blocks) p = b + x_b < blocks ? p : &mx_zero_piece;
-            lds_dma16(base + (wave + 8 * j) * 1024, p);
-        } else lds_dma16_s(base + (16 + wave + 8 * (j - 2)) * 1024, (j == 2 ? wp0 : wp1) + s * 64, lane * 16);
+            const void *p = reinterpret_cast<const char *>(xp + s * 4) + xo[j];
+            lds_dma16(base + (wave + 8 * j) * 1024, s * 4 + x_b < x_left ? p : &mx_zero_piece);
+        } else lds_dma16_s(base + (16 + wave + 8 * (j - 2)) * 1024, wp[j - 2] + s * 64, lane * 16);
     };
-    auto issue_scales = [&](int j, int grp) {             // unit j (static) of group grp (relative)
-        lds_dma4_s(lds1 + (unsigned)(((grp & 1) * 32 + wave + 8 * j) * 256), sp[j] + grp * 64, lane * 4);
+    auto issue_scales = [&](int j, int grp, int buf) {    // unit j (static) of group grp of the item
+        lds_dma4_s(lds1 + (unsigned)((buf * 32 + wave + 8 * j) * 256), sp[j] + grp * 64, lane * 4);
     };
+    auto issue_refs = [&](const Item &t) { lds_dma4_s(lds2 + (unsigned)(wave * 256), w.ref, (unsigned)min((t.ct0 + wn * 4) * 16 + lane, w.tiles * 16 - 1) * 4u); };
     f32x16 acc[4][2];
-#pragma unroll
-    for (int mt = 0; mt < 4; ++mt)
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[mt][nt][r] = 0.f;
-    // Loads of a wave: four pieces a k-step, and in the first two of a group two units each of the next group's scales, which have landed
-    // with the pieces by the group's end.  Behind the stage that k-step s waits for: those of s - 1 and of s.
-#pragma unroll
-    for (int j = 0; j < 4; ++j) issue_scales(j, 0);
-#pragma unroll
-    for (int s = 0; s < NST - 1; ++s) {                   // (n is at least four)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) issue(j, s, s);
-    }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NST - 2) * 4) : "memory");
-    __syncthreads();
     // an operand of 32 rows x 64 columns (half h of a k-step): lane -> row lane % 32 (of two units), block 2 h + lane / 32
     const int fr = ((lane >> 4) & 1) * 64 + (lane >> 5) * 16 + (lane & 15);
     const int xr = wm * 8 * 64 + fr, wr = (16 + wn * 4) * 64 + fr;                       // + 128 per 32 rows, + 32 for the second half
@@ -809,44 +817,63 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
     for (int h = 0; h < 2; ++h) xc[h] = wm * 8 * 64 + ((lane >> 4) & 1) * 64 + (lane & 15) * 4 + ((h * 2 + (lane >> 5)) ^ ((lane >> 2) & 3));
     u32x4 xf[2][4], wf[2][2];
     unsigned xsc[2][4], wsc[2][2];
-    auto read = [&](const u32x4 *st, int h, u32x4 (&xo)[4], u32x4 (&wo)[2]) {
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) wo[nt] = st[wr + nt * 128 + h * 32];
-#pragma unroll
-        for (int mt = 0; mt < 4; ++mt) xo[mt] = st[xc[h] + mt * 128];
-    };
-    auto read_scales = [&](int grp) {
+    auto read_scales = [&](int buf) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) wsc[h][nt] = scs[grp & 1][wr + nt * 128 + h * 32];
+            for (int nt = 0; nt < 2; ++nt) wsc[h][nt] = scs[buf][wr + nt * 128 + h * 32];
 #pragma unroll
-            for (int mt = 0; mt < 4; ++mt) xsc[h][mt] = scs[grp & 1][xr + mt * 128 + h * 32];
+            for (int mt = 0; mt < 4; ++mt) xsc[h][mt] = scs[buf][xr + mt * 128 + h * 32];
         }
     };
-    read(xs, 0, xf[0], wf[0]);
+
+    // Loads of a wave: four pieces a k-step, in the first two of a group two units each of the next group's scales, in the second the refs
+    // too: they have landed with the pieces by the group's end.  Behind the stage that k-step s waits for: those of s - 1 and of s.
+    // (Stores of the tile before are behind it too, or done: the wait is longer for them, never shorter.)
+    Item cur = item_of(blockIdx.x);
+    codes_at(cur);
+    scales_at(cur);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) issue_scales(j, 0, 0);
+#pragma unroll
+    for (int s = 0; s < NST - 1; ++s) {                   // (n is at least four)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) issue(j, s, s);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NST - 2) * 4) : "memory");
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) wf[0][nt] = xs[wr + nt * 128];
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt) xf[0][mt] = xs[xc[0] + mt * 128];
     read_scales(0);
-    int at = 0;
-    for (int s4 = 0; s4 < n; s4 += 4) {
+    int buf = 0;
+    Item next;
+    // a group of four k-steps, the item's last one or not: there the scales that follow are the next item's, from its second k-step on the codes
+    auto group = [&](auto last_, int s4) {
+        constexpr bool last = decltype(last_)::value;
+        const int gi = last ? 0 : (s4 >> 2) + 1;
+        if (last) scales_at(next);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int step = s4 + s, an = at == NST - 1 ? 0 : at + 1, ai = at == 0 ? NST - 1 : at - 1;
-            const u32x4 *cur = xs + at * STAGE, *nxt = xs + an * STAGE;
-            // asked for beyond the end too (of the last k-step and group again: valid memory, never read): every step is the same straight line
-            const int si = min(step + NST - 1, n - 1), gi = min((s4 >> 2) + 1, (n >> 2) - 1);
+            if (last && s == 1) codes_at(next);
+            const int ai = (s + 3) & 3, si = last && s > 0 ? s - 1 : s4 + s + 3;      // (k-step s of a group lies in stage s)
+            const u32x4 *st = xs + s * STAGE, *nxt = xs + ((s + 1) & 3) * STAGE;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (h == 1) {                             // the next stage has landed; behind the barrier the last one's place is free
-                    if (s == 1) asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");
-                    else if (s == 3) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
-                    else asm volatile("s_waitcnt vmcnt(10) lgkmcnt(0)" ::: "memory");
+                if (h == 1) {                         // the next stage has landed; behind the barrier the last one's place is free
+                    if (s == 0) asm volatile("s_waitcnt vmcnt(10) lgkmcnt(0)" ::: "memory");
+                    else if (s == 1) asm volatile("s_waitcnt vmcnt(13) lgkmcnt(0)" ::: "memory");
+                    else if (s == 2) asm volatile("s_waitcnt vmcnt(11) lgkmcnt(0)" ::: "memory");
+                    else asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
                     __syncthreads();
                 }
 #pragma unroll
                 for (int mt = 0; mt < 4; ++mt) {
-                    if (h == 0 && mt < 4) issue(mt, si, ai);
-                    if (h == 0 && mt >= 2 && s < 2) issue_scales(2 * s + mt - 2, gi);
-                    const u32x4 *from = h == 1 ? nxt : cur;
+                    if (h == 0) issue(mt, si, ai);
+                    if (h == 0 && mt >= 2 && s < 2) issue_scales(2 * s + mt - 2, gi, buf ^ 1);
+                    if (h == 0 && mt == 3 && s == 1) issue_refs(cur);
+                    const u32x4 *from = h == 1 ? nxt : st;
                     if (mt < 2) wf[h ^ 1][mt] = from[wr + mt * 128 + (h ^ 1) * 32];
                     xf[h ^ 1][mt] = from[xc[h ^ 1] + mt * 128];
                     const i32x8 b = {(int)xf[h][mt].x, (int)xf[h][mt].y, (int)xf[h][mt].z, (int)xf[h][mt].w, 0, 0, 0, 0};
@@ -861,47 +888,78 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            at = an;
         }
-        if (s4 + 4 < n) read_scales((s4 >> 2) + 1);
-    }
-    // D tile: lane -> row lane % 32, register r -> column 8 (r / 4) + 4 (lane / 32) + r % 4
-    auto quad = [&](int mt, int nt, int q) { return f32x4{acc[mt][nt][q * 4], acc[mt][nt][q * 4 + 1], acc[mt][nt][q * 4 + 2], acc[mt][nt][q * 4 + 3]}; };
-    dma_wait<0>();                                        // what nobody reads: LDS is written over, or given back
-    __syncthreads();
-    const int n0 = (ct0 + wn * 4) * 16;
-    if (wide) {
-        Y *dst = SPLIT ? y + (size_t)blockIdx.y * g.M * g.plane_ld : y;
-        const int64_t ldd = SPLIT ? (int64_t)g.plane_ld : ldy;
-        char *own = reinterpret_cast<char *>(xs) + wave * (32 * (64 * (int)sizeof(Y) + 16));
+        buf ^= 1;
+        read_scales(buf);
+    };
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        next = item_of(item + (int)gridDim.x < items ? item + (int)gridDim.x : item);      // (none: this one's again, valid memory that is never used)
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt)
-            mx_store_rows<Y, 32, 64>(own, [&](auto f) {
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[mt][nt][r] = 0.f;
+        for (int s4 = 0; s4 + 4 < cur.n; s4 += 4) group(No{}, s4);
+        group(Yes{}, cur.n - 4);
+        // D tile: lane -> row lane % 32, register r -> column 8 (r / 4) + 4 (lane / 32) + r % 4.  Thirty-two rows of 128 bytes at a time
+        // through the stage that nobody reads and nothing is on its way to: the four units of it that this wave itself fills
+        // next (eight rows each; piece p of a row at p ^ (row % 8)).  So waves need not wait for each other here.
+        auto quad = [&](int mt, int nt, int q) { return f32x4{acc[mt][nt][q * 4], acc[mt][nt][q * 4 + 1], acc[mt][nt][q * 4 + 2], acc[mt][nt][q * 4 + 3]}; };
+        auto scaled = [&](int mt, int nt, int q) {
+            const int4 e = *reinterpret_cast<const int4 *>(&refs[wave * 64 + nt * 32 + q * 8 + (lane >> 5) * 4]);
+            return mx_scaled<Y>(quad(mt, nt, q), planes ? int4{127, 127, 127, 127} : e, 0);
+        };
+        const int row0 = cur.m0 + wm * 128, n0 = (cur.ct0 + wn * 4) * 16;
+        if (wide) {
+            constexpr int NTS = sizeof(Y) == 2 ? 2 : 1;   // 32-column tiles of a piece of 128 bytes
+            const int64_t ldd = planes ? (int64_t)g.plane_ld : ldy;
+            const int half = lane >> 5, r_out = lane >> 3, cols = (planes ? w.tiles * 16 : g.N) - n0 - (lane & 7) * (16 / (int)sizeof(Y));
+            char *const lds = reinterpret_cast<char *>(xs);
+            const int own = (NST - 1) * (STAGE * 16) + wave * 1024, get = own + r_out * 128 + (((lane & 7) ^ r_out) << 4);
+            const int put = own + ((lane >> 3) & 3) * 8192 + (lane & 7) * 128 + (NTS == 2 ? ((lane & 7) << 4) + half * 8 : ((lane & 7) ^ half) << 4);
+            Y *to = y + (planes ? (size_t)cur.split * g.M * g.plane_ld : 0) + (int64_t)(row0 + r_out) * ldd + n0 + (lane & 7) * (16 / (int)sizeof(Y));
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
+#pragma unroll
+                for (int nt0 = 0; nt0 < 2; nt0 += NTS) {
+#pragma unroll
+                    for (int nt = nt0; nt < nt0 + NTS; ++nt)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)       // (quad q: piece nt * 4 + q or, of four bytes a value, 2 q + half)
+                            *reinterpret_cast<MxQuad<Y> *>(lds + (put ^ (NTS == 2 ? nt * 4 + q : 2 * q) << 4)) = scaled(mt, nt, q);
+                    wave_lds_sync();
+                    Y *p = to;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + get + i * 8192);
+                        if (row0 + mt * 32 + i * 8 + r_out < g.M && nt0 * 32 < cols) *reinterpret_cast<u32x4 *>(p + nt0 * 32) = v;
+                        p += 8 * ldd;
+                    }
+                    wave_lds_sync();
+                    if (nt0 + NTS == 2) to = p;
+                    asm volatile("" : "+v"(to));          // (one address at a time: registers)
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int mt = 0; mt < 4; ++mt) {
+                const int m = row0 + mt * 32 + (lane & 31);
+                if (m >= g.M) continue;
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const int c = nt * 32 + q * 8 + (lane >> 5) * 4;
-                        if (SPLIT && !g.plane_scaled) f(lane & 31, c, mx_raw<Y>(quad(mt, nt, q)));
-                        else f(lane & 31, c, mx_scaled<Y>(quad(mt, nt, q), w.ref, min(n0 + c, w.tiles * 16 - 4), 0));
+                        const int col = n0 + nt * 32 + q * 8 + (lane >> 5) * 4;
+                        if (col < g.N) mx_store_quad<Y>(y + (int64_t)m * ldy + col, quads, g.N - col, scaled(mt, nt, q));
                     }
-            }, m0 + wm * 128 + mt * 32, n0, g.M, SPLIT ? w.tiles * 16 : g.N, dst, ldd);
-        return;
-    }
-#pragma unroll
-    for (int mt = 0; mt < 4; ++mt) {
-        const int m = m0 + wm * 128 + mt * 32 + (lane & 31);
-        if (m >= g.M) continue;
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int col = n0 + nt * 32 + q * 8 + (lane >> 5) * 4;
-                if (col >= g.N) continue;
-                if constexpr (SPLIT) mx_store_plane<0>(y + ((size_t)blockIdx.y * g.M + m) * g.plane_ld + col, quad(mt, nt, q), g, w, col);
-                else mx_store<Y>(y, ldy, quads, m, col, g.N, quad(mt, nt, q), w.ref, 0);
             }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (loads go to that stage again)
+        cur = next;
     }
+    dma_wait<0>();                                        // (what nobody reads: LDS is given back)
 }
 
 // The planes of a product, added in order.
@@ -934,6 +992,7 @@ __global__ __launch_bounds__(256) void mx_planes_kernel(const f32x4 *__restrict_
 struct MxPlan { int shape, splits; };
 struct MxTile { int tm, tn; float us[8]; };
 enum { MX_STREAM = 0 };
+constexpr int CHIP_CUS = 256;
 // us: a launch; k-groups of a tile; the same times rounds of the chip (256 tiles); ... times tiles / 256; rounds; planes: their launch, a million
 // of their values; a million results.  The first row (no tiles): a launch; sixteen k-groups; 10^4 column x k-groups; the same times ten rows.
 constexpr MxTile MX_TILES[] = {
@@ -1081,8 +1140,9 @@ static void run_both(const MxPacked &w, const u32x4 *x, const uint8_t *xs, int b
         default: {
             const int rts = (g.M + 15) / 16;
             mx_scales_kernel<<<dim3((w.kgroups * 64 + 255) / 256, rts < 65535 ? rts : 65535), 256, 0, st>>>(xs, g.M, blocks, w.kgroups, xscales);
-            if (g.splits > 1) mx_block_both_kernel<float, true><<<grid, 512, 0, st>>>(w, x, xscales, blocks, g, part, 0, true, true);
-            else mx_block_both_kernel<Y, false><<<grid, 512, 0, st>>>(w, x, xscales, blocks, g, y, ldy, quads, wide);
+            const int items = g.tiles_m * g.tiles_n * g.splits, wgs = items < CHIP_CUS ? items : CHIP_CUS;
+            if (g.splits > 1) mx_block_both_kernel<float><<<wgs, 512, 0, st>>>(w, x, xscales, blocks, g, part, 0, true, true);
+            else mx_block_both_kernel<Y><<<wgs, 512, 0, st>>>(w, x, xscales, blocks, g, y, ldy, quads, wide);
         }
     }
 #undef POSS_MX_FED
