@@ -874,8 +874,15 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
                     if (h == 0 && mt >= 2 && s < 2) issue_scales(2 * s + mt - 2, gi, buf ^ 1);
                     if (h == 0 && mt == 3 && s == 1) issue_refs(cur);
                     const u32x4 *from = h == 1 ? nxt : st;
-                    if (mt < 2) wf[h ^ 1][mt] = from[wr + mt * 128 + (h ^ 1) * 32];
-                    xf[h ^ 1][mt] = from[xc[h ^ 1] + mt * 128];
+                    if (mt == 0) {                        // the next half's operands in the first two of four turns: six matrix instructions to arrive in
+                        wf[h ^ 1][0] = from[wr + (h ^ 1) * 32];
+                        wf[h ^ 1][1] = from[wr + 128 + (h ^ 1) * 32];
+                        xf[h ^ 1][0] = from[xc[h ^ 1]];
+                    } else if (mt == 1) {
+                        xf[h ^ 1][1] = from[xc[h ^ 1] + 128];
+                        xf[h ^ 1][2] = from[xc[h ^ 1] + 256];
+                        xf[h ^ 1][3] = from[xc[h ^ 1] + 384];
+                    }
                     const i32x8 b = {(int)xf[h][mt].x, (int)xf[h][mt].y, (int)xf[h][mt].z, (int)xf[h][mt].w, 0, 0, 0, 0};
 #pragma unroll
                     for (int nt = 0; nt < 2; ++nt) {
