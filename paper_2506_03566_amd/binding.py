@@ -404,6 +404,7 @@ class _MxState:
         self.types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.current = raw if raw is not None else lambda dev: torch.cuda.current_stream(dev).cuda_stream
+        self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         return self
 
 
@@ -421,12 +422,12 @@ def _mx_type(t):
 
 def _mx_rows(t, rows, cols, what):
     """The row distance of a matrix [rows, cols] whose rows are contiguous."""
-    if t.dim() != 2 or t.size(0) != rows or t.size(1) != cols or rows > 0x7fffffff or cols > 0x7fffffff:
+    if t.shape != (rows, cols) or rows > 0x7fffffff or cols > 0x7fffffff:
         _mx_refuse("%s [%d, %d] is wanted, got %s" % (what, rows, cols, tuple(t.shape)))
-    ld = t.stride(0) if rows > 1 else cols
-    if ld < cols or (cols > 1 and t.stride(1) != 1):
+    ld, step = t.stride()
+    if step != 1 and cols > 1 or ld < cols and rows > 1:
         _mx_refuse("%s must have contiguous rows that do not overlap" % what)
-    return ld
+    return ld if rows > 1 else cols
 
 
 def _mx_pair(codes, scales, rows, cols, what):
@@ -440,10 +441,12 @@ def _mx_call(f, stream, tensors, *args):
     """f(*args, stream) with the tensors' GPU current, on the stream given or torch's current one there."""
     dev = tensors[0].get_device()
     for t in tensors:
-        if t.get_device() != dev or dev < 0:
-            _mx_refuse("all tensors of a call must be on one GPU")
+        if t.get_device() != dev:
+            dev = -1
+    if dev < 0:
+        _mx_refuse("all tensors of a call must be on one GPU")
     st = stream.cuda_stream if stream is not None else _mx.current(dev)
-    back = _mx.torch.cuda.current_device()
+    back = _mx.device()
     if back == dev:
         rc = f(*args, st)
     else:
