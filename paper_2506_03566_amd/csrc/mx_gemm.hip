@@ -71,11 +71,18 @@ template <typename Y> __device__ __forceinline__ void mx_store(Y *__restrict__ y
     mx_store_quad<Y>(y + (int64_t)m * ldy + n, quads, N - n, mx_scaled<Y>(acc, ref, n, shift));
 }
 
+// Results of the largest tiles go past the caches: 8192 x 28672 x 4096 in 480 us instead of 503 (16-bit X 1314, 1361); a pass over the results right
+// behind it makes the pair take as long either way (659 us).  Planes are read at once and stay.
+template <typename Y> __device__ __forceinline__ void mx_store_piece(Y *p, u32x4 v, bool past) {
+    if (past) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+    else *reinterpret_cast<u32x4 *>(p) = v;
+}
+
 // ROWS rows x COLS columns of float32 sums that a wave holds, to Y (times 2^ref) or to a plane, in pieces of 16 bytes: from the lanes' quads
 // through LDS of the wave's own (rows padded by 16 bytes).  A lane's quads of a row, as they are, would be written 8 bytes here and
 // there: 256 x 256 tiles of 8192 x 28672 results took 24 us a round for them, of 59.
 // put(f): calls f(row, column, sums) for each quad.
-template <typename Y, int ROWS, int COLS, typename Put>
+template <typename Y, int ROWS, int COLS, bool PAST, typename Put>
 __device__ __forceinline__ void mx_store_rows(char *lds, Put put, int m0, int n0, int M, int N, Y *__restrict__ y, int64_t ldy) {
     constexpr int ROW = COLS * (int)sizeof(Y) + 16, LPR = COLS * (int)sizeof(Y) / 16, RPI = 64 / LPR;      // lanes a row, rows an instruction
     const int lane = threadIdx.x & 63;
@@ -85,7 +92,7 @@ __device__ __forceinline__ void mx_store_rows(char *lds, Put put, int m0, int n0
 #pragma unroll
     for (int r = lane / LPR; r < ROWS; r += RPI) {
         const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + r * ROW + c * (int)sizeof(Y));
-        if (m0 + r < M && n0 + c < N) *reinterpret_cast<u32x4 *>(y + (int64_t)(m0 + r) * ldy + n0 + c) = v;
+        if (m0 + r < M && n0 + c < N) mx_store_piece(y + (int64_t)(m0 + r) * ldy + n0 + c, v, PAST);
     }
     wave_lds_sync();                                      // (the next rows go to the same place)
 }
@@ -323,7 +330,7 @@ __device__ __forceinline__ void mx_tile_store_wide(char *own, const f32x4 (&acc)
     Y *dst = SPLIT ? y + (size_t)blockIdx.y * g.M * g.plane_ld : y;
 #pragma unroll
     for (int mt = 0; mt < MTW; ++mt)
-        mx_store_rows<Y, 16, NTW * 16>(own, [&](auto f) {
+        mx_store_rows<Y, 16, NTW * 16, !SPLIT && MTW >= 8>(own, [&](auto f) {
 #pragma unroll
             for (int nt = 0; nt < NTW; ++nt) {
                 const int c = nt * 16 + (lane >> 4) * 4;
@@ -940,7 +947,7 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + get + i * 8192);
-                        if (row0 + mt * 32 + i * 8 + r_out < g.M && nt0 * 32 < cols) *reinterpret_cast<u32x4 *>(p + nt0 * 32) = v;
+                        if (row0 + mt * 32 + i * 8 + r_out < g.M && nt0 * 32 < cols) mx_store_piece(p + nt0 * 32, v, !planes);
                         p += 8 * ldd;
                     }
                     wave_lds_sync();
