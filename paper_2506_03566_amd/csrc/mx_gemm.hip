@@ -126,25 +126,25 @@ __device__ __forceinline__ void split3(float x, bf16_t &a, bf16_t &b, bf16_t &c)
 }
 
 // X whose rows cannot be read in 16-byte pieces (odd lengths, distances or addresses), and float32 X: a copy in rows of Kp values,
-// zeros beyond K; of float32 the three parts, one after the other.
-template <typename X> __global__ __launch_bounds__(256) void mx_stage_kernel(const X *__restrict__ x, int64_t ldx, int M, int K, int Kp, u32x4 *__restrict__ out) {
+// zeros beyond K; of float32 the three parts, one after the other.  wide: rows of x can be read in pieces of 16 bytes.
+template <typename X> __global__ __launch_bounds__(256) void mx_stage_kernel(const X *__restrict__ x, int64_t ldx, bool wide, int M, int K, int Kp, u32x4 *__restrict__ out) {
     const int k0 = (blockIdx.x * 256 + threadIdx.x) * 8;
     if (k0 >= Kp) return;
     for (int m = blockIdx.y; m < M; m += gridDim.y) {
         const X *row = x + (int64_t)m * ldx;
-        X v[8];
+        union { u32x4 u[sizeof(X) / 2]; X v[8]; } in;
+        if (wide && k0 + 8 <= K)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = k0 + j < K ? row[k0 + j] : from_f<X>(0.f);
+            for (int j = 0; j < (int)sizeof(X) / 2; ++j) in.u[j] = reinterpret_cast<const u32x4 *>(row + k0)[j];
+        else
+#pragma unroll
+            for (int j = 0; j < 8; ++j) in.v[j] = k0 + j < K ? row[k0 + j] : from_f<X>(0.f);
         u32x4 *dst = out + ((int64_t)m * Kp * (sizeof(X) == 2 ? 1 : 3) + k0) / 8;
-        if constexpr (sizeof(X) == 2) {
-            union { X e[8]; u32x4 u; } o;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o.e[j] = v[j];
-            *dst = o.u;
-        } else {
+        if constexpr (sizeof(X) == 2) *dst = in.u[0];
+        else {
             union { bf16_t e[8]; u32x4 u; } a, b, c;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) split3(v[j], a.e[j], b.e[j], c.e[j]);
+            for (int j = 0; j < 8; ++j) split3(in.v[j], a.e[j], b.e[j], c.e[j]);
             dst[0] = a.u; dst[Kp / 8] = b.u; dst[Kp / 4] = c.u;
         }
     }
@@ -1069,8 +1069,9 @@ template <typename Y> static bool wide_ok(const Y *y, int64_t ldy, int N) {
 static MxRows stage(int x_dt, const void *x, int64_t ldx, int M, int K, int kp, void *scratch, hipStream_t st) {
     const dim3 grid((kp / 8 + 255) / 256, M < 65535 ? M : 65535);
     u32x4 *o = static_cast<u32x4 *>(scratch);
-    if (x_dt == DT_F32) { mx_stage_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float *>(x), ldx, M, K, kp, o); return MxRows{scratch, 3 * (int64_t)kp, kp, kp}; }
-    mx_stage_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(x), ldx, M, K, kp, o);
+    const bool wide = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * dtype_size(x_dt) % 16 == 0;
+    if (x_dt == DT_F32) { mx_stage_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float *>(x), ldx, wide, M, K, kp, o); return MxRows{scratch, 3 * (int64_t)kp, kp, kp}; }
+    mx_stage_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(x), ldx, wide, M, K, kp, o);
     return MxRows{scratch, kp, 0, kp};
 }
 
