@@ -130,11 +130,12 @@ int poss_load(const poss_config *cfg, const poss_weights *w, void *workspace,
               size_t workspace_bytes, void *hip_stream, poss_ctx **out);
 
 /* The same context with weights of a quarter of the bytes: every matrix of the layers (target and specialists) and the fc matrices
- * are quantised to 4 bits as poss_mx_quantize does (below; from w's tensors of `dtype`, bf16 or f16; float32 is refused) and multiplied as poss_mx_gemm does.
- * Embedding, LM head, norms, biases, activations and caches stay as poss_load has them.  A smaller workspace, poss_workspace_bytes_mx(cfg) (0 if the
- * configuration is invalid or float32).  All calls on a context work alike; a sequence's tokens are those of a model with the rounded
- * weights, and again the same for every number of rows beside them.  Prompts run POSS_LAUNCH_ROWS rows a pass, whatever their length.  poss_profile_gemm counts
- * the LM head's products only, poss_set_tuning's workgroup target applies to them only. */
+ * are quantised to 4 bits as poss_mx_quantize does (below; from w's tensors of `dtype`, bf16 or f16; float32 is refused, and so are
+ * matrices of more than 2^21 columns) and multiplied as poss_mx_gemm does.  Embedding, LM head, norms, biases, activations and caches stay
+ * as poss_load has them.  A smaller workspace, poss_workspace_bytes_mx(cfg) (0 if the configuration is refused).  All calls on a context
+ * work alike; a sequence's tokens are those of a model with the rounded weights, and a row's products do not depend on the number of rows
+ * beside it.  Prompts run POSS_LAUNCH_ROWS rows a pass, whatever their length.  poss_profile_gemm counts the LM head's products only,
+ * poss_set_tuning's workgroup target applies to them only. */
 size_t poss_workspace_bytes_mx(const poss_config *cfg);
 int poss_load_mx(const poss_config *cfg, const poss_weights *w, void *workspace,
                  size_t workspace_bytes, void *hip_stream, poss_ctx **out);

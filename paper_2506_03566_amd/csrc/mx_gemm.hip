@@ -999,10 +999,11 @@ __global__ __launch_bounds__(256) void mx_planes_kernel(const f32x4 *__restrict_
 
 // ------------------------------------------------------------------------------------------ launches
 // How a product runs: a kernel with its tile shape, and K splits.  Chosen by an estimate of the time in us: for each shape the sum of eight
-// terms whose weights were fitted (none negative) to measured times of 19 row counts (1 to 4096) x 10 matrices (512 x 512 to 28672 x 4096
-// and 5120 x 13824) x up to ten splits.  What the estimate picks is 2 % (microscaled X: 4 %) slower on average than the fastest of all that was
-// measured, at 95 of 100 sizes within 10 %; where the shapes cross (4096 x 4096, us): 32 rows 16 x 64 6.8, 32 x 128 8.4; 244 rows 32 x 128
-// 12.2, 64 x 128 14.9; 512 rows 64 x 128 19.5, 64 x 256 24.6; 1024 rows 39 and 31; 4096 rows 64 x 256 127, 256 x 256 106.
+// terms whose weights were fitted (none negative) to times measured in graphs, 19 row counts (1 to 4096) x 10 matrices (512 x 512 to
+// 28672 x 4096 and 5120 x 13824) x up to ten splits.  What the estimate picks is 0.9 % slower on average than the fastest of all that was
+// measured; of 190 sizes 7 (microscaled X: 6) are more than a tenth slower, a fifth at most.  Where the shapes cross (4096 x 4096, us): 16
+// rows stream 6.2, 16 x 64 7.0; 128 rows 16 x 64 10.3, 32 x 128 11.1; 244 rows 32 x 128 13.7, 64 x 128 15.1; 512 rows 64 x 128 20.0, 64 x 256
+// 24.8; 1024 rows 43.0 and 31.5; 4096 rows 64 x 256 121, 256 x 256 108.
 struct MxPlan { int shape, splits; };
 struct MxTile { int tm, tn; float us[8]; };
 enum { MX_STREAM = 0 };
@@ -1010,20 +1011,20 @@ constexpr int CHIP_CUS = 256;
 // us: a launch; k-groups of a tile; the same times rounds of the chip (256 tiles); ... times tiles / 256; rounds; planes: their launch, a million
 // of their values; a million results.  The first row (no tiles): a launch; sixteen k-groups; 10^4 column x k-groups; the same times ten rows.
 constexpr MxTile MX_TILES[] = {
-    {16, 16, {2.956f, 1.255f, 0.408f, 5.14f}},                                       // mx_stream_kernel
-    {16, 64, {2.421f, 0.346f, 0.120f, 0.161f, 0.574f, 2.361f, 0.775f, 0.648f}},      // mx_fed_kernel
-    {32, 128, {2.828f, 0.261f, 0.339f, 0.546f, 1.079f, 1.924f, 0.961f, 1.289f}},
-    {32, 256, {3.126f, 0.634f, 0.419f, 0.874f, 1.965f, 1.285f, 1.037f, 1.457f}},
-    {64, 128, {2.819f, 0.000f, 1.131f, 0.653f, 1.244f, 2.629f, 1.221f, 0.719f}},
-    {64, 256, {4.790f, 0.000f, 1.803f, 1.072f, 0.000f, 2.306f, 1.461f, 0.817f}},
-    {256, 256, {5.440f, 0.000f, 8.964f, 1.138f, 2.072f, 0.492f, 0.835f, 0.982f}}};   // mx_tile_kernel
+    {16, 16, {2.407f, 0.851f, 0.417f, 6.06f}},                                       // mx_stream_kernel
+    {16, 64, {1.920f, 0.493f, 0.021f, 0.218f, 0.879f, 2.158f, 0.769f, 0.686f}},      // mx_fed_kernel
+    {32, 128, {2.557f, 0.434f, 0.179f, 0.604f, 1.368f, 1.809f, 1.034f, 1.411f}},
+    {32, 256, {3.053f, 0.778f, 0.285f, 0.959f, 2.049f, 1.233f, 1.156f, 1.376f}},
+    {64, 128, {2.855f, 0.000f, 1.160f, 0.657f, 1.158f, 2.713f, 1.373f, 0.771f}},
+    {64, 256, {4.774f, 0.000f, 1.850f, 1.065f, 0.000f, 2.511f, 1.524f, 0.827f}},
+    {256, 256, {7.758f, 0.096f, 8.969f, 1.422f, 0.107f, 1.133f, 0.896f, 0.854f}}};   // mx_tile_kernel
 constexpr MxTile MX_BOTH_TILES[] = {
-    {16, 16, {2.991f, 0.096f, 0.321f, 2.48f}},                                       // mx_stream_both_kernel
-    {16, 64, {1.681f, 0.696f, 0.015f, 0.182f, 0.606f, 2.733f, 0.422f, 0.382f}},      // mx_fed_both_kernel
-    {32, 128, {1.520f, 0.822f, 0.025f, 0.316f, 1.321f, 2.437f, 1.208f, 1.680f}},
-    {64, 128, {2.656f, 0.272f, 0.612f, 0.195f, 1.551f, 2.415f, 1.356f, 0.915f}},
-    {64, 256, {4.153f, 0.050f, 1.108f, 0.270f, 0.029f, 2.751f, 1.432f, 0.690f}},
-    {256, 256, {7.684f, 0.000f, 1.906f, 0.901f, 2.925f, 1.774f, 1.203f, 0.563f}}};   // mx_block_both_kernel
+    {16, 16, {2.334f, 0.381f, 0.347f, 2.44f}},                                       // mx_stream_both_kernel
+    {16, 64, {1.337f, 0.748f, 0.000f, 0.193f, 0.782f, 2.452f, 0.836f, 0.462f}},      // mx_fed_both_kernel
+    {32, 128, {1.353f, 0.881f, 0.000f, 0.331f, 1.418f, 2.265f, 1.356f, 1.889f}},
+    {64, 128, {2.659f, 0.354f, 0.539f, 0.262f, 1.552f, 2.436f, 1.456f, 0.903f}},
+    {64, 256, {4.124f, 0.105f, 1.079f, 0.327f, 0.000f, 2.889f, 1.496f, 0.698f}},
+    {256, 256, {6.552f, 0.000f, 2.005f, 1.094f, 4.886f, 4.424f, 1.030f, 0.407f}}};   // mx_block_both_kernel
 
 static int mx_groups(int K) { return (K + 4 * MX_KSTEP - 1) / (4 * MX_KSTEP); }
 // Waves of a column tile: four, sixteen where the tiles leave CUs with one each and K is long (one row, us, 4 / 8 / 16 waves: 4096 x 14336 9.0 / 8.5 / 8.0,
