@@ -1174,12 +1174,14 @@ static void run_gemm_t(const MxPacked &w, const MxRows &x, const MxGeom &g, cons
 }
 
 // ------------------------------------------------------------------------------------------ a context's layers
-// Splits of a matrix whose planes the layer's own epilogues add up: as many as give every CU a 128-column tile, the groups dealt out
-// evenly.  They follow the matrix alone, and every kernel adds a split's products in the same order (mx_stream_kernel its waves' sums as the
-// epilogue would the planes): a row's sums do not depend on the rows beside it, and a tree's rows get what plain decoding gives them.
+// Splits of a matrix whose planes the layer's own epilogues add up: as many as give half the CUs a 128-column tile (a tree's rows are two
+// tiles of 32), the groups dealt out evenly.  They follow the matrix alone, and every kernel adds a split's products in the same order
+// (mx_stream_kernel its waves' sums as the epilogue would the planes): a row's sums do not depend on the rows beside it, and a tree's rows
+// get what plain decoding gives them.  Rounds of 61 rows and plain decoding, ms: 8B shape 4.42 and 2.27, 13B shape 5.38 and 3.22; with
+// twice as many splits (unsplit from 171 tiles on) 4.62 and 2.14, 5.54 and 3.23; with half as many 4.76 and 2.51, 6.20 and 4.01.
 int mx_plane_splits(int N, int K) {
     const int groups = mx_groups(K), cols = (N + 127) / 128;
-    int s = (256 + cols / 2) / cols;
+    int s = cols >= 120 ? 1 : cols > 64 ? 2 : 128 / cols;
     if (s > groups) s = groups;
     if (s > 16) s = 16;
     if (s < 1) s = 1;
