@@ -154,6 +154,41 @@ def test_both_microscaled_against_float64(M, N, K):
         assert_product(y[:, 2:N + 2], x, w, ty)
 
 
+# sizes of the largest tiles: several rounds of them with edges in rows and columns, a K of one group of k-steps and of several, K splits
+def large(M, N, K, t):
+    g = torch.Generator(device="cuda").manual_seed(M + N + K)
+    x = (torch.randn(M, K, generator=g, device="cuda") * torch.exp2(torch.randint(-3, 4, (M, 1), generator=g, device="cuda").float())).to(t)
+    codes, scales = P.mx_quantize(torch.randn(N, K, generator=g, device="cuda") * 0.02)
+    w = P.mx_dequantize(codes, scales, torch.empty(N, K, device="cuda")).double()
+    return x, w, P.mx_pack(codes, scales, K)
+
+
+def check_large(product, x, w, M, N, K):
+    ref, mag = x @ w.T.contiguous(), x.abs() @ w.abs().T.contiguous()
+    for ty, left, right in (("bf16", 0, 0), ("f32", 0, 8), ("f16", 0, 1), ("f32", 3, 2)):       # 16-byte pieces of a row, and single values
+        y = torch.full((M + 1, left + N + right), 7.0, dtype=TYPES[ty], device="cuda")
+        product(y[:M, left:left + N])
+        assert bool((y[M] == 7).all()) and bool((y[:, :left] == 7).all()) and bool((y[:, left + N:] == 7).all())
+        got = y[:M, left:left + N].double()
+        bound = (K + 16) * 2.0 ** -23 * mag * (1 + half_step(ty)) + half_step(ty) * ref.abs() + float(torch.finfo(TYPES[ty]).smallest_normal) * torch.finfo(TYPES[ty]).eps
+        worst = float(((got - ref).abs() / bound).max())
+        assert worst <= 1, (ty, left, worst)               # (a NaN fails too)
+
+
+@pytest.mark.parametrize("t,M,N,K", [("bf16", 5000, 2992, 2100), ("f16", 3000, 5001, 2104), ("bf16", 500, 4100, 13000), ("f16", 5000, 777, 9000), ("f32", 1500, 2500, 2100)])
+def test_gemm_of_large_tiles(t, M, N, K):
+    x, w, packed = large(M, N, K, TYPES[t])
+    check_large(lambda y: P.mx_gemm(x, packed, y), x.double(), w, M, N, K)
+
+
+@pytest.mark.parametrize("M,N,K", [(4100, 2992, 520), (5000, 5001, 700), (8200, 8200, 500), (3000, 4104, 2100), (5000, 777, 9000), (1030, 4001, 9000)])
+def test_both_microscaled_of_large_tiles(M, N, K):
+    x, w, packed = large(M, N, K, torch.bfloat16)
+    codes, scales = P.mx_quantize(x)
+    x = P.mx_dequantize(codes, scales, torch.empty(M, K, device="cuda")).double()
+    check_large(lambda y: P.mx_gemm_mx(codes, scales, packed, y), x, w, M, N, K)
+
+
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_scales_far_apart_in_a_row(M):
     """bf16 and float32 activations: 100 powers of two in a row of weights; fp16: the 36 that its operands reach."""
