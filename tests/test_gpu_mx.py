@@ -330,6 +330,33 @@ def test_the_same_call_gives_the_same_bits():
             assert torch.equal(P.mx_gemm(x, packed, y), first) and torch.equal(P.mx_gemm_mx(c, s, packed, z), both)
 
 
+@pytest.mark.parametrize("M,N,K", [(5000, 5000, 2100), (5000, 777, 9000)])
+def test_large_tiles_give_the_same_bits_eager_and_replayed(M, N, K):
+    x, _, packed = large(M, N, K, torch.bfloat16)
+    codes, scales = P.mx_quantize(x)
+    ys = [torch.empty(M, N, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    scratch = [P.mx_gemm_scratch(t, M, N, K) for t in (torch.bfloat16, None)]
+
+    def run():
+        P.mx_gemm(x, packed, ys[0], scratch[0])
+        P.mx_gemm_mx(codes, scales, packed, ys[1], scratch[1])
+    run()
+    first = [y.clone() for y in ys]
+    for _ in range(5):
+        run()
+        assert all(torch.equal(a, b) for a, b in zip(ys, first))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(4):
+        for y, s in zip(ys, scratch):
+            y.fill_(3.0)
+            s.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(ys, first))
+
+
 def test_two_streams_at_once_with_scratch_of_their_own():
     rng = np.random.default_rng(12)
     M, N, K = 40, 512, 8192                                # (planes of several splits in scratch)
