@@ -152,10 +152,10 @@ template <typename X> __global__ __launch_bounds__(256) void mx_stage_kernel(con
 
 // ------------------------------------------------------------------------------------------ few rows
 // Up to sixteen rows: a workgroup owns a column tile and all of K, cut among its waves in whole groups of four k-steps.  Each wave reads its
-// weights (1 KB per k-step, contiguous) and its part of X (from the L2) straight into operand registers, the next group's on the way while this
-// one is multiplied; the waves' sums are added in LDS, in wave order.  Nothing is waited for but memory: one row of 28672 x 4096 13.0 us
-// (62.5 MB; a copy reads and writes as much in 12.5), 4096 x 4096 3.4.  With rows X counts (16 bytes at a time, once per column tile): 16 rows 30 us,
-// where mx_fed_kernel takes 12.8.
+// weights (1 KB per k-step, contiguous) and its part of X (from the L2) straight into operand registers, the next group's on the way while
+// this one is multiplied; the waves' sums are added in LDS, in wave order.  Nothing is waited for but memory: one row of 28672 x 4096 11.9 us
+// (62.5 MB at 5.3 TB/s), 4096 x 4096 3.7.  Slower: X through LDS (a barrier behind a trip to memory: 6.0 for 3.7), two groups ahead (6144 x 4096
+// 6.5 for 5.5).  With rows X counts (16 bytes at a time, once per column tile): 16 rows 30 us, where mx_fed_kernel takes 12.8.
 // The waves' sums in the first wave (true there).
 __device__ __forceinline__ bool mx_stream_sum(f32x4 *red, f32x4 &acc) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -758,7 +758,8 @@ __global__ __launch_bounds__(256) void mx_scales_kernel(const uint8_t *__restric
 // 16 x 16 x 128 one gives 5.2).  Codes of both operands go into LDS by LDS-direct loads, a k-step of 128 a stage, four stages in a ring,
 // one barrier per k-step; the scales of a group of four k-steps likewise, an eighth of them by each wave, a quarter of that per k-step, two buffers.
 // A workgroup per CU takes one tile after the other, and the loads run on into the next one: when a tile's sums are written, the next
-// tile's first three stages and scales are there or on their way.
+// tile's first three stages and scales are there or on their way.  8192 x 28672 x 4096: 480 us, 4.0 PFLOP/s; the matrix pipes are busy half the
+// cycles of a clock that their load has brought to 1.7 GHz (registers alone: all cycles at 1.5).
 template <typename Y>
 __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const u32x4 *__restrict__ x, const uint32_t *__restrict__ xscales, int blocks, MxGeom g, Y *__restrict__ y,
                                                                int64_t ldy, bool quads, bool wide) {
@@ -1203,7 +1204,7 @@ bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, i
 // Whether the planes are one (mx_stream_kernel adds its waves' sums itself).
 int mx_planes_written(int M, int N, int K, int splits) { return best_plan(MX_TILES, M, N, mx_groups(K), splits).shape == MX_STREAM ? 1 : splits; }
 
-// A thread per four units.  Of 61 rows of 28672 columns: 15 MB read, from the L2s for the most part.
+// A thread per four units; the planes come from the L2s for the most part.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_silu_kernel(const float *__restrict__ part, int splits, int M, int ld, int F, T *__restrict__ act) {
     const int f = (blockIdx.x * 256 + threadIdx.x) * 4, m = blockIdx.y;
