@@ -154,6 +154,10 @@ size_t mx_packed_size(int N, int K) {
 
 __device__ __forceinline__ bool mx_all_zero(u32x4 c) { return ((c.x | c.y | c.z | c.w) & 0x77777777u) == 0; }
 
+// The byte of a block's scale s relative to its row's largest: 127 at that one (and for blocks of zeros above it), negative where the block lies further
+// below than a byte reaches: it is taken for zero then (its codes at 2^-127 would be larger than they are).
+__device__ __forceinline__ int mx_relative(int s, int top) { return min(127, s - top + 127); }
+
 // A workgroup per column tile: first the rows' largest scales, then the blocks in their order.
 __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ codes, const uint8_t *__restrict__ scales, int N, int blocks, int ksteps,
                                                       u32x4 *__restrict__ out, uint32_t *__restrict__ out_scales, int32_t *__restrict__ ref) {
@@ -181,8 +185,9 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ 
             u32x4 c = {0u, 0u, 0u, 0u};
             int s = 127;
             if (n < N && b < blocks) {
-                c = codes[(size_t)n * blocks + b];
-                s = min(127, max(0, scales[(size_t)n * blocks + b] - top[r] + 127));
+                s = mx_relative(scales[(size_t)n * blocks + b], top[r]);
+                if (s >= 0) c = codes[(size_t)n * blocks + b];
+                else s = 0;
             }
             out[((size_t)tile * ksteps + ks) * 64 + lane] = c;
             packed |= (uint32_t)s << (8 * i);
@@ -239,8 +244,9 @@ template <typename T> __global__ __launch_bounds__(256) void mx_pack_rows_kernel
                 MxIn<T> in[4];
                 load(row, b, in);
                 const int sb = scale_of(in);
-                if (sb != 255) c = u32x4{in[0].codes(mx_power(sb)), in[1].codes(mx_power(sb)), in[2].codes(mx_power(sb)), in[3].codes(mx_power(sb))};
-                s = min(127, max(0, sb - top[r] + 127));
+                s = mx_relative(sb, top[r]);
+                if (s < 0) s = 0;
+                else if (sb != 255) c = u32x4{in[0].codes(mx_power(sb)), in[1].codes(mx_power(sb)), in[2].codes(mx_power(sb)), in[3].codes(mx_power(sb))};
             }
             out[((size_t)tile * ksteps + ks) * 64 + lane] = c;
             packed |= (uint32_t)s << (8 * i);

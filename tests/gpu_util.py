@@ -42,6 +42,21 @@ def tol_for(cfg):
     return 1e-4 if cfg.dtype == 0 else 2e-2
 
 
+def prefill_in_step(ctx, o, prompt, tol):
+    """Prompt to the library and to the oracle; the last layer's cache within tol, and the token behind the prompt the oracle's or, where its two
+    best lie within 2 tol, the second of them, which the oracle then goes on with.  Returns that token."""
+    from oracle.model import head
+    first, want = ctx.prefill(prompt), o.prefill(prompt)
+    logits = head(o.W, o.cfg, np.stack(o.feats[-1:]), o.act)[0]
+    assert int(np.argmax(logits)) == want
+    if first != want:
+        assert logits[want] - logits[first] <= 2 * tol and int(np.argsort(logits)[-2]) == first, (first, want, float(logits[want] - logits[first]))
+        o.tokens[-1] = first
+    k, v = ctx.debug_read_kv(-1, o.cfg.n_layers - 1, 0, len(prompt))
+    assert np.abs(k - o.kv[-1][0][:len(prompt)]).max() <= tol and np.abs(v - o.kv[-1][1][:len(prompt)]).max() <= tol
+    return first
+
+
 # End-to-end error of 16-bit logits after the whole target at the 8B / 13B shapes.  The 2e-2 bound holds per
 # layer and per Head on identical inputs; through 32-40 random-initialised layers every flipped rounding of
 # an activation is carried on and amplified, and two summation orders (the oracle's float64 sums, the
