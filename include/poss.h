@@ -336,9 +336,10 @@ int poss_mx_dequantize(int32_t dtype, const void *codes, const void *scales, int
 
 /* A weight matrix [N][K] (codes and scales as above) in the operand order of the products below: `packed`, poss_mx_packed_bytes(N, K)
  * bytes (0 for a bad shape; K at most 2^21, N at most 2^27), aligned to 256.  Codes and scales are not needed afterwards.  Products use a
- * block's scale relative to the largest one of its row: exactly while it lies at most 126 (fp16 activations: 36) powers of two below; what
- * lies further below is smaller than 2^-124 (2^-38) of the row's largest weight and may lose bits or be taken for zero.  The float32 sums
- * are of activations times those relative weights (magnitudes up to 6), and are multiplied by the row's power of two at the end. */
+ * block's scale exactly while it lies at most 126 (fp16 activations: 36) powers of two below the largest one of its row, and with other activations
+ * than fp16 wherever that one is at most 2^0; what lies further below is smaller than 2^-124 (2^-38) of the row's largest weight and may lose bits or
+ * be taken for zero.  A row's float32 sums are of activations times its weights, brought to a largest scale between 2^-24 and 2^0 where it lies outside
+ * (fp16: to 2^13), and are multiplied by the power of two that is left at the end: they become infinite where those terms take them. */
 size_t poss_mx_packed_bytes(int32_t N, int32_t K);
 int poss_mx_pack(const void *codes, const void *scales, int32_t N, int32_t K, void *packed, void *hip_stream);
 

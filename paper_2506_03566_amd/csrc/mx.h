@@ -44,6 +44,11 @@ static inline int mx_blocks(int cols) { return (cols - 1) / MX_BLOCK + 1; }     
 constexpr int MX_MOST_M = 1 << 24, MX_MOST_N = 1 << 27, MX_MOST_K = 1 << 21;
 constexpr int64_t MX_MOST_MN = 1ll << 38;
 
+// Where a row's largest scale stands in the packed form: as it is between 2^-24 and 2^0, moved there otherwise, the row's sums brought back at the end.  So
+// no sum of ordinary activations with large weights leaves float32's range on the way, and none of activations as large as float32 has them with small
+// weights: 2^21 terms of 3.4e38 * 6 * 2^-24 do not; between the two a sum overflows where its terms take it.
+__device__ __forceinline__ int mx_held(int top) { return min(127, max(103, top)); }
+
 // 2^(b - 127) of a scale byte, exactly (2^-127 is subnormal).
 __device__ __forceinline__ float mx_power(unsigned b) {
     return __builtin_bit_cast(float, b == 255 ? 0x7fc00000u : b == 0 ? 0x00400000u : b << 23);

@@ -7,10 +7,11 @@
 // Packed weights (what the products read) are those blocks in operand order of the 16 x 16 x 128 matrix instruction:
 //   codes  [column tile][k-step][lane]  16 bytes: the block of weight row tile * 16 + lane % 16, columns k-step * 128 + lane / 16 * 32 ...
 //          (k-steps of 128, in whole groups of four; zeros beyond the matrix)
-//   scales [column tile][k-step / 4][lane]  4 bytes: the scales of that lane's blocks of four k-steps, relative to the row's largest
+//   scales [column tile][k-step / 4][lane]  4 bytes: the scales of that lane's blocks of four k-steps, moved with the row's largest to where mx_held has it
 //   ref    [row]  the largest scale byte of the row's blocks that are not all zero; 255 where a block of the row is NaN
-// A wave reads 1 KB of codes per k-step, contiguous along k.  The relative scales let every product form c * 2^(s - ref) in the type
-// that its matrix instruction takes (an fp16 number reaches from 2^-24 to 2^16 only) and apply 2^ref to the float32 sum, exactly.
+// A wave reads 1 KB of codes per k-step, contiguous along k.  bf16 and scaled operands are those numbers, mostly the weights themselves; an fp16
+// number reaches from 2^-24 to 2^16 only: there operands are c * 2^(s - ref), times a constant.  The float32 sums are multiplied by what is left
+// of 2^ref, exactly.
 #include "../../include/poss.h"
 #include "mx.h"
 
@@ -154,9 +155,9 @@ size_t mx_packed_size(int N, int K) {
 
 __device__ __forceinline__ bool mx_all_zero(u32x4 c) { return ((c.x | c.y | c.z | c.w) & 0x77777777u) == 0; }
 
-// The byte of a block's scale s relative to its row's largest: 127 at that one (and for blocks of zeros above it), negative where the block lies further
-// below than a byte reaches: it is taken for zero then (its codes at 2^-127 would be larger than they are).
-__device__ __forceinline__ int mx_relative(int s, int top) { return min(127, s - top + 127); }
+// The byte of a block's scale s in the packed form (blocks of zeros may lie above their row's largest).  Negative where the block lies further below the
+// largest of a row above 2^0 than a byte reaches: it is taken for zero then.
+__device__ __forceinline__ int mx_packed_scale(int s, int top) { return min(top, s) - top + mx_held(top); }
 
 // A workgroup per column tile: first the rows' largest scales, then the blocks in their order.
 __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ codes, const uint8_t *__restrict__ scales, int N, int blocks, int ksteps,
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ 
             u32x4 c = {0u, 0u, 0u, 0u};
             int s = 127;
             if (n < N && b < blocks) {
-                s = mx_relative(scales[(size_t)n * blocks + b], top[r]);
+                s = mx_packed_scale(scales[(size_t)n * blocks + b], top[r]);
                 if (s >= 0) c = codes[(size_t)n * blocks + b];
                 else s = 0;
             }
@@ -244,7 +245,7 @@ template <typename T> __global__ __launch_bounds__(256) void mx_pack_rows_kernel
                 MxIn<T> in[4];
                 load(row, b, in);
                 const int sb = scale_of(in);
-                s = mx_relative(sb, top[r]);
+                s = mx_packed_scale(sb, top[r]);
                 if (s < 0) s = 0;
                 else if (sb != 255) c = u32x4{in[0].codes(mx_power(sb)), in[1].codes(mx_power(sb)), in[2].codes(mx_power(sb)), in[3].codes(mx_power(sb))};
             }

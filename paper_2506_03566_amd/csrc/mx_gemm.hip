@@ -1,11 +1,11 @@
 // Y[m][n] = sum_k X[m][k] W[n][k] with W microscaled in 4 bits and packed in operand order (mx.hip), X in 32 or 16 bits or
 // microscaled as well.
 //
-// 16-bit X: a weight becomes c * 2^(s - ref) in the type of X (one conversion instruction for two, exact) and enters
+// 16-bit X: a weight becomes a number in the type of X (one conversion instruction for two, exact; fp16: relative to its row's largest) and enters
 // v_mfma_f32_16x16x32; the 32 codes that a lane holds per k-step are the k values of four such instructions, lane / 16 choosing the block of
 // 32 and the instruction eight values of it, so that a lane takes 64 contiguous bytes of a row of X.
 // float32 X: the sum of three bf16 numbers, three instructions.  Microscaled X: v_mfma_scale with both scales, one block per lane.
-// The sums are multiplied by 2^ref at the end.  Products are formed transposed (weights as MFMA rows): a lane holds four consecutive
+// What the operands leave out of 2^ref is applied to the sums at the end.  Products are formed transposed (weights as MFMA rows): a lane holds four consecutive
 // columns of a row of Y.
 #include "mx.h"
 
@@ -13,11 +13,15 @@
 
 namespace poss {
 
-constexpr int F16_SHIFT = 13;     // fp16 operands carry 2^13: 6 * 2^13 is finite, and c * 2^(s - ref) exact down to s = ref - 36
+constexpr int F16_SHIFT = 13;     // fp16 operands are c * 2^(s - ref) times 2^13: 6 * 2^13 is finite, and they are exact down to s = ref - 36
 
+// SHIFT: 0 where operands are as the packed scales have them.  scale: a block's scale as the conversion's operand, whose exponent field is the byte,
+// moved by what move gives for the block's row; weights below what fp16 can hold round to zero there, at 2^-127 too.
 template <typename T> struct MxOp;
 template <> struct MxOp<bf16_t> {
     static constexpr int SHIFT = 0;
+    static __device__ __forceinline__ int move(const int32_t *, int) { return 0; }
+    static __device__ __forceinline__ float scale(unsigned byte_at_23, int) { return __builtin_bit_cast(float, byte_at_23); }
     static __device__ __forceinline__ u32x4 weights(unsigned q, float s) {     // eight codes as operand values
         union { u32x4 v; bf16x2 p[4]; } u;
         u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 0); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 1);
@@ -30,6 +34,8 @@ template <> struct MxOp<bf16_t> {
 };
 template <> struct MxOp<f16_t> {
     static constexpr int SHIFT = F16_SHIFT;
+    static __device__ __forceinline__ int move(const int32_t *__restrict__ ref, int n) { return (127 + SHIFT - mx_held(ref[n])) * (1 << 23); }
+    static __device__ __forceinline__ float scale(unsigned byte_at_23, int move) { return __builtin_bit_cast(float, max(0, (int)byte_at_23 + move)); }
     static __device__ __forceinline__ u32x4 weights(unsigned q, float s) {
         union { u32x4 v; f16x2 p[4]; } u;
         u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(q, s, 0); u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(q, s, 1);
@@ -40,21 +46,22 @@ template <> struct MxOp<f16_t> {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     }
 };
-// The scale of k-step s (of a group of four) as the conversion's scale operand: its exponent field is the byte.
-template <typename T, int S> __device__ __forceinline__ float mx_scale(unsigned four) {
-    const unsigned f = (S < 3 ? four << (23 - 8 * S) : four >> 1) & 0x7f800000u;
-    return __builtin_bit_cast(float, f + ((unsigned)MxOp<T>::SHIFT << 23));
+template <typename T, int S> __device__ __forceinline__ float mx_scale(unsigned four, int move) {
+    return MxOp<T>::scale((S < 3 ? four << (23 - 8 * S) : four >> 1) & 0x7f800000u, move);
 }
 
 __device__ const u32x4 mx_zero_piece = {0u, 0u, 0u, 0u};  // what a lane reads where its k lies beyond K
 
-// The sums of four consecutive columns n.. of row m, times 2^ref, to Y.
+// The sums of four consecutive columns n.. of row m to Y, times what their operands leave out: shift 0: of the packed form, otherwise all of 2^ref.
+__device__ __forceinline__ float mx_result(float a, int top, int shift) {
+    return top == 255 ? __builtin_nanf("") : __builtin_ldexpf(a, top - (shift ? 127 + shift : mx_held(top)));
+}
 template <typename Y> struct __attribute__((aligned(4 * sizeof(Y)))) MxQuad { Y v[4]; };
 template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_scaled(f32x4 a, int4 e, int shift) {
     MxQuad<Y> o;
     const int es[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
-    for (int r = 0; r < 4; ++r) o.v[r] = from_f<Y>(es[r] == 255 ? __builtin_nanf("") : __builtin_ldexpf(a[r], es[r] - 127 - shift));
+    for (int r = 0; r < 4; ++r) o.v[r] = from_f<Y>(mx_result(a[r], es[r], shift));
     return o;
 }
 template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_scaled(f32x4 a, const int32_t *__restrict__ ref, int n, int shift) {
@@ -175,6 +182,7 @@ __global__ __launch_bounds__(1024) void mx_stream_kernel(MxPacked w, MxRows x, Y
     const u32x4 *wp = w.codes + ((size_t)ct * w.ksteps + g0 * 4) * 64 + lane;
     const uint32_t *sp = w.scales + ((size_t)ct * w.kgroups + g0) * 64 + lane;
     const T *xp = static_cast<const T *>(x.x) + (int64_t)min(lane & 15, M - 1) * x.ldx + g0 * 4 * MX_KSTEP + kl;
+    const int move = Op::move(w.ref, ct * 16 + (lane & 15));
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     u32x4 c[4], xv[4][PARTS];
     uint32_t next = *sp;
@@ -197,7 +205,7 @@ __global__ __launch_bounds__(1024) void mx_stream_kernel(MxPacked w, MxRows x, Y
         for (int i = 0; i < 4; ++i) load_x(tail, g, 0, i);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const float f = s == 0 ? mx_scale<T, 0>(sc) : s == 1 ? mx_scale<T, 1>(sc) : s == 2 ? mx_scale<T, 2>(sc) : mx_scale<T, 3>(sc);
+            const float f = s == 0 ? mx_scale<T, 0>(sc, move) : s == 1 ? mx_scale<T, 1>(sc, move) : s == 2 ? mx_scale<T, 2>(sc, move) : mx_scale<T, 3>(sc, move);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const u32x4 v = Op::weights(c[s][i], f);
@@ -374,17 +382,19 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
     int ws = s0 % w.ksteps;                               // k-step of the weights: the next one to load
     const u32x4 *wp[NTW];
     const uint32_t *sp[NTW];
+    int move[NTW];
 #pragma unroll
     for (int nt = 0; nt < NTW; ++nt) {
         const int ct = min(ct0 + nt, w.tiles - 1);        // tiles beyond the matrix repeat the last one (never stored)
         wp[nt] = w.codes + (size_t)ct * w.ksteps * 64;
         sp[nt] = w.scales + (size_t)ct * w.kgroups * 64;
+        move[nt] = Op::move(w.ref, ct * 16 + (lane & 15));
     }
-    auto load_w = [&](u32x4 (&c)[NTW], unsigned (&f)[NTW]) {
+    auto load_w = [&](u32x4 (&c)[NTW], float (&f)[NTW]) {
 #pragma unroll
         for (int nt = 0; nt < NTW; ++nt) {
             c[nt] = wp[nt][ws * 64 + lane];
-            f[nt] = (sp[nt][(ws >> 2) * 64 + lane] >> (8 * (ws & 3)) & 255u) + Op::SHIFT << 23;
+            f[nt] = Op::scale((sp[nt][(ws >> 2) * 64 + lane] >> (8 * (ws & 3)) & 255u) << 23, move[nt]);
         }
         ws = ws + 1 == w.ksteps ? 0 : ws + 1;
     };
@@ -397,7 +407,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
     // A k-step is 4 MTW slots, one row tile of one substep each.  Operands of X are read AHEAD slots ahead, into a ring of four.
     constexpr int SLOTS = 4 * MTW, AHEAD = 3;
     u32x4 c[NTW], cn[NTW], xf[4], wf[2][NTW];
-    unsigned f[NTW], fn[NTW];
+    float f[NTW], fn[NTW];
 #pragma unroll
     for (int j = 0; j < UPW; ++j) issue_one(j, s0, 0);
     load_w(c, f);
@@ -407,7 +417,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) xf[q] = xs[rd + (q % MTW) * 256 + ((q / MTW) ^ rs)];
 #pragma unroll
-    for (int nt = 0; nt < NTW; ++nt) wf[0][nt] = Op::weights(c[nt][0], __builtin_bit_cast(float, f[nt]));
+    for (int nt = 0; nt < NTW; ++nt) wf[0][nt] = Op::weights(c[nt][0], f[nt]);
 
     for (int s = 0; s < n; ++s) {
         const u32x4 *cur = xs + (s & 1) * UNITS * 64, *nxt = xs + (~s & 1) * UNITS * 64;
@@ -427,7 +437,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void mx_tile_kernel(MxPacked w, Mx
             xf[(q + AHEAD) & 3] = (q + AHEAD >= SLOTS ? nxt : cur)[rd + (qa % MTW) * 256 + ((qa / MTW) ^ rs)];
 #pragma unroll
             for (int nt = mt; nt < NTW; nt += MTW)
-                wf[(i + 1) & 1][nt] = i == 3 ? Op::weights(cn[nt][0], __builtin_bit_cast(float, fn[nt])) : Op::weights(c[nt][(i + 1) & 3], __builtin_bit_cast(float, f[nt]));
+                wf[(i + 1) & 1][nt] = i == 3 ? Op::weights(cn[nt][0], fn[nt]) : Op::weights(c[nt][(i + 1) & 3], f[nt]);
 #pragma unroll
             for (int nt = 0; nt < NTW; ++nt) acc[mt][nt] = Op::mfma(wf[i & 1][nt], xf[q & 3], acc[mt][nt]);
             __builtin_amdgcn_sched_barrier(0);
@@ -495,11 +505,13 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
     const int wm = wave % WM, wn = wave / WM, ct0 = tn * (TN / 16) + wn * NTW;
     const u32x4 *wp[NTW];
     const uint32_t *sp[NTW];
+    int move[NTW];
 #pragma unroll
     for (int nt = 0; nt < NTW; ++nt) {
         const int ct = min(ct0 + nt, w.tiles - 1);        // tiles beyond the matrix repeat the last one (never stored)
         wp[nt] = w.codes + (size_t)ct * w.ksteps * 64 + lane;
         sp[nt] = w.scales + (size_t)ct * w.kgroups * 64 + lane;
+        move[nt] = Op::move(w.ref, ct * 16 + (lane & 15));
     }
     int wg = g0 % w.kgroups;                              // group of the weights (float32 X passes over them three times)
     f32x4 acc[MTW][NTW];
@@ -518,13 +530,15 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
     // X: sixteen units per row tile, a block of columns each; slot q of a stage: k-step q / (4 MTW), substep q / MTW % 4, row tile q % MTW
     const int rd = (wm * MTW * 16 + (lane >> 4)) * 64 + (lane & 15) * 4, rs = (lane >> 2) & 3;
     auto x_at = [&](int q) { return rd + ((q % MTW) * 16 + q / (4 * MTW) * 4) * 64 + ((q / MTW & 3) ^ rs); };
-    auto scale = [&](int s, unsigned four) { return s == 0 ? mx_scale<T, 0>(four) : s == 1 ? mx_scale<T, 1>(four) : s == 2 ? mx_scale<T, 2>(four) : mx_scale<T, 3>(four); };
+    auto scale = [&](int s, unsigned four, int nt) {
+        return s == 0 ? mx_scale<T, 0>(four, move[nt]) : s == 1 ? mx_scale<T, 1>(four, move[nt]) : s == 2 ? mx_scale<T, 2>(four, move[nt]) : mx_scale<T, 3>(four, move[nt]);
+    };
     __syncthreads();
     int st = 0;
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) xf[q] = xs[x_at(q)];
 #pragma unroll
-    for (int nt = 0; nt < NTW; ++nt) wf[0][nt] = Op::weights(c[0][nt][0], scale(0, sc[nt]));
+    for (int nt = 0; nt < NTW; ++nt) wf[0][nt] = Op::weights(c[0][nt][0], scale(0, sc[nt], nt));
     auto group = [&](auto more_) {
         constexpr bool more = decltype(more_)::value;
         const u32x4 *cur = xs + st * UNITS * 64, *nxt = xs + (st ^ 1) * UNITS * 64;
@@ -547,9 +561,9 @@ __global__ __launch_bounds__((WM * WN + FW) * 64) void mx_fed_kernel(MxPacked w,
 #pragma unroll
                     for (int nt = mt; nt < NTW; nt += MTW) {
                         // the next substep's weights
-                        if (i < 3) wf[(i + 1) & 1][nt] = Op::weights(c[s][nt][(i + 1) & 3], scale(s, sc[nt]));
-                        else if (s < 3) wf[0][nt] = Op::weights(c[(s + 1) & 3][nt][0], scale(s + 1, sc[nt]));
-                        else if constexpr (more) wf[0][nt] = Op::weights(c[0][nt][0], scale(0, sn[nt]));
+                        if (i < 3) wf[(i + 1) & 1][nt] = Op::weights(c[s][nt][(i + 1) & 3], scale(s, sc[nt], nt));
+                        else if (s < 3) wf[0][nt] = Op::weights(c[(s + 1) & 3][nt][0], scale(s + 1, sc[nt], nt));
+                        else if constexpr (more) wf[0][nt] = Op::weights(c[0][nt][0], scale(0, sn[nt], nt));
                     }
 #pragma unroll
                     for (int nt = 0; nt < NTW; ++nt) acc[mt][nt] = Op::mfma(wf[i & 1][nt], xf[q & 3], acc[mt][nt]);
