@@ -48,6 +48,11 @@ constexpr int64_t MX_MOST_MN = 1ll << 38;
 // no sum of ordinary activations with large weights leaves float32's range on the way, and none of activations as large as float32 has them with small
 // weights: 2^21 terms of 3.4e38 * 6 * 2^-24 do not; between the two a sum overflows where its terms take it.
 __device__ __forceinline__ int mx_held(int top) { return min(127, max(103, top)); }
+// A row's largest scale byte as the packed form keeps it: that byte and, ready for the sums, the power of two that they are to be multiplied by.
+constexpr int MX_NAN_ROW = 0x7fffffff;
+__device__ __forceinline__ int mx_row_ref(int top) { return top == 255 ? MX_NAN_ROW : (top - mx_held(top)) * 256 + top; }
+__device__ __forceinline__ int mx_row_top(int ref) { return ref & 255; }
+__device__ __forceinline__ int mx_row_power(int ref) { return ref >> 8; }
 
 // 2^(b - 127) of a scale byte, exactly (2^-127 is subnormal).
 __device__ __forceinline__ float mx_power(unsigned b) {

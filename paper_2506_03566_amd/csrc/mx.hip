@@ -8,7 +8,7 @@
 //   codes  [column tile][k-step][lane]  16 bytes: the block of weight row tile * 16 + lane % 16, columns k-step * 128 + lane / 16 * 32 ...
 //          (k-steps of 128, in whole groups of four; zeros beyond the matrix)
 //   scales [column tile][k-step / 4][lane]  4 bytes: the scales of that lane's blocks of four k-steps, moved with the row's largest to where mx_held has it
-//   ref    [row]  the largest scale byte of the row's blocks that are not all zero; 255 where a block of the row is NaN
+//   ref    [row]  the largest scale byte of the row's blocks that are not all zero, and what the row's sums are multiplied by (mx_row_ref)
 // A wave reads 1 KB of codes per k-step, contiguous along k.  bf16 and scaled operands are those numbers, mostly the weights themselves; an fp16
 // number reaches from 2^-24 to 2^16 only: there operands are c * 2^(s - ref), times a constant.  The float32 sums are multiplied by what is left
 // of 2^ref, exactly.
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const u32x4 *__restrict__ 
         atomicMax(&top[r], t);                            // (the largest: the same in any order)
     }
     __syncthreads();
-    if (tid < 16) ref[tile * 16 + tid] = top[tid];
+    if (tid < 16) ref[tile * 16 + tid] = mx_row_ref(top[tid]);
     const int lane = tid & 63, r = lane & 15, n = tile * 16 + r, groups = ksteps / 4;
     for (int g = tid >> 6; g < groups; g += 4) {
         uint32_t packed = 0;
@@ -232,7 +232,7 @@ template <typename T> __global__ __launch_bounds__(256) void mx_pack_rows_kernel
         atomicMax(&top[tid >> 4], t);                     // (the largest: the same in any order)
     }
     __syncthreads();
-    if (tid < 16) ref[tile * 16 + tid] = top[tid];
+    if (tid < 16) ref[tile * 16 + tid] = mx_row_ref(top[tid]);
     const int lane = tid & 63, r = lane & 15;
     const T *row = row_of(r);
     for (int g = tid >> 6; g < groups; g += 4) {

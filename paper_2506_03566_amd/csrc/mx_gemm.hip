@@ -34,7 +34,7 @@ template <> struct MxOp<bf16_t> {
 };
 template <> struct MxOp<f16_t> {
     static constexpr int SHIFT = F16_SHIFT;
-    static __device__ __forceinline__ int move(const int32_t *__restrict__ ref, int n) { return (127 + SHIFT - mx_held(ref[n])) * (1 << 23); }
+    static __device__ __forceinline__ int move(const int32_t *__restrict__ ref, int n) { return (127 + SHIFT - mx_held(mx_row_top(ref[n]))) * (1 << 23); }
     static __device__ __forceinline__ float scale(unsigned byte_at_23, int move) { return __builtin_bit_cast(float, max(0, (int)byte_at_23 + move)); }
     static __device__ __forceinline__ u32x4 weights(unsigned q, float s) {
         union { u32x4 v; f16x2 p[4]; } u;
@@ -53,8 +53,8 @@ template <typename T, int S> __device__ __forceinline__ float mx_scale(unsigned 
 __device__ const u32x4 mx_zero_piece = {0u, 0u, 0u, 0u};  // what a lane reads where its k lies beyond K
 
 // The sums of four consecutive columns n.. of row m to Y, times what their operands leave out: shift 0: of the packed form, otherwise all of 2^ref.
-__device__ __forceinline__ float mx_result(float a, int top, int shift) {
-    return top == 255 ? __builtin_nanf("") : __builtin_ldexpf(a, top - (shift ? 127 + shift : mx_held(top)));
+__device__ __forceinline__ float mx_result(float a, int ref, int shift) {
+    return ref == MX_NAN_ROW ? __builtin_nanf("") : __builtin_ldexpf(a, shift ? mx_row_top(ref) - 127 - shift : mx_row_power(ref));
 }
 template <typename Y> struct __attribute__((aligned(4 * sizeof(Y)))) MxQuad { Y v[4]; };
 template <typename Y> __device__ __forceinline__ MxQuad<Y> mx_scaled(f32x4 a, int4 e, int shift) {
@@ -85,7 +85,7 @@ template <typename Y> __device__ __forceinline__ void mx_store_piece(Y *p, u32x4
     else *reinterpret_cast<u32x4 *>(p) = v;
 }
 
-// ROWS rows x COLS columns of float32 sums that a wave holds, to Y (times 2^ref) or to a plane, in pieces of 16 bytes: from the lanes' quads
+// ROWS rows x COLS columns of float32 sums that a wave holds, to Y (times what the operands leave out) or to a plane, in pieces of 16 bytes: from the lanes' quads
 // through LDS of the wave's own (rows padded by 16 bytes).  A lane's quads of a row, as they are, would be written 8 bytes here and
 // there: 256 x 256 tiles of 8192 x 28672 results took 24 us a round for them, of 59.
 // put(f): calls f(row, column, sums) for each quad.
@@ -288,7 +288,7 @@ struct MxGeom {
     int full;                     // k-steps that lie inside X's rows as a whole
     int tiles_m, tiles_n, splits;
     int plane_ld;                 // planes: [M][plane_ld] each,
-    bool plane_scaled;            // times 2^ref already
+    bool plane_scaled;            // times what the operands leave out already
 };
 
 // Workgroup -> tile: consecutive ids go to the 8 XCDs in turn; an XCD is given a contiguous run of tiles, ordered so that those it works
@@ -937,7 +937,7 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
         auto quad = [&](int mt, int nt, int q) { return f32x4{acc[mt][nt][q * 4], acc[mt][nt][q * 4 + 1], acc[mt][nt][q * 4 + 2], acc[mt][nt][q * 4 + 3]}; };
         auto scaled = [&](int mt, int nt, int q) {
             const int4 e = *reinterpret_cast<const int4 *>(&refs[wave * 64 + nt * 32 + q * 8 + (lane >> 5) * 4]);
-            return mx_scaled<Y>(quad(mt, nt, q), planes ? int4{127, 127, 127, 127} : e, 0);
+            return mx_scaled<Y>(quad(mt, nt, q), planes ? int4{0, 0, 0, 0} : e, 0);
         };
         const int row0 = cur.m0 + wm * 128, n0 = (cur.ct0 + wn * 4) * 16;
         if (wide) {
