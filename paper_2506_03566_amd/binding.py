@@ -395,16 +395,17 @@ _MX = 4                              # POSS_MX: activations that are microscaled
 
 
 class _MxState:
-    """What the calls below look up once: the library, torch, its types' codes, and how to read a device's current stream."""
+    """What the calls below look up once: the library, torch, its types' codes, and how to read a device's current stream.  They go by `lib`: it comes last."""
     lib = None
 
     def open(self):
         import torch
-        self.lib, self.torch, self.u8 = load_library(), torch, torch.uint8
+        self.torch, self.u8 = torch, torch.uint8
         self.types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.current = raw if raw is not None else lambda dev: torch.cuda.current_stream(dev).cuda_stream
         self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self.lib = load_library()
         return self
 
 
