@@ -237,7 +237,7 @@ int poss_get_stats(poss_ctx *ctx, poss_stats *out);
 /* Number of committed tokens (prompt included); tokens_out (HOST, may be NULL) of capacity cap. */
 int poss_get_tokens(poss_ctx *ctx, int32_t *tokens_out, int32_t cap, int32_t *n_out);
 int poss_get_tokens_seq(poss_ctx *ctx, int32_t seq, int32_t *tokens_out, int32_t cap, int32_t *n_out);
-const char *poss_last_error(poss_ctx *ctx);       /* ctx may be NULL: last poss_load error */
+const char *poss_last_error(poss_ctx *ctx);       /* ctx NULL: the calling thread's last failure of a call that has no context (poss_load among them) */
 void poss_free(poss_ctx *ctx);
 
 /* ---- instrumentation -------------------------------------------------------------------- */

@@ -19,7 +19,7 @@ using namespace poss;
 
 namespace {
 
-char g_load_error[512] = "";
+thread_local char g_load_error[512] = "";    // calls without a context: each thread reads its own failures
 
 struct LayerW { const void *attn_norm, *wqkv, *wo, *mlp_norm, *wgu, *wdown; };
 struct SpecW  { const void *fc_w, *fc_b; LayerW layer; };
