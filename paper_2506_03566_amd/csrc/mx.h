@@ -1,6 +1,7 @@
 // Microscaled 4-bit weights: the packed form, its device pieces and its launches (mx.hip, mx_gemm.hip).
 #pragma once
 #include "device_utils.h"
+#include "mx_plan.h"
 
 namespace poss {
 
@@ -15,6 +16,7 @@ typedef int    i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int MX_BLOCK = 32;      // values that share a scale
 constexpr int MX_KSTEP = 128;     // columns of a k-step: a block for each sixteen lanes
+static_assert(MX_GROUP == 4 * MX_KSTEP, "a scale word holds a group");
 
 // Packed weights as the kernels see them (the layout stands in mx.hip).
 struct MxPacked { const u32x4 *codes; const uint32_t *scales; const int32_t *ref; int ksteps, kgroups, tiles; };
@@ -29,10 +31,9 @@ void launch_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *pa
 // For a context's layers (16-bit types).  A matrix of packed rows, as launch_pack takes them, quantised and packed; N: its rows, padding ones among them.
 size_t mx_packed_size(int N, int K);
 void launch_mx_pack_rows(int dt, const PackSrc &src, int N, int K, void *packed, hipStream_t st);
-// The planes of X W^T: plane s < splits of part, [M][ld], ld a multiple of four and at least N.  A row's planes are the same for every M.
-int mx_plane_splits(int N, int K);
+// The planes of X W^T: plane s < splits of part (mx_plane_splits; mx_planes_written of them), [M][ld], ld a multiple of four and at least N.  A row's planes
+// are the same for every M.
 bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, int ldx, int M, float *part, int ld, int splits, hipStream_t st);
-int mx_planes_written(int M, int N, int K, int splits);    // how many of them that is: splits, or one where the kernel has added them
 // act[M][F] = SiLU(gate) * up of X with a matrix whose rows alternate in groups of 16 (PackSrc::interleave16).  part as above, for the planes of a split product.
 bool launch_mx_gate_up(int dt, const void *packed, int F, int K, const void *X, int ldx, int M, float *part, int ld, void *act, hipStream_t st);
 

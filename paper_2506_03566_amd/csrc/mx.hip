@@ -132,7 +132,7 @@ template <typename T, typename I> __global__ __launch_bounds__(256) void mx_dequ
 }
 
 // ------------------------------------------------------------------------------------------ packing
-static inline int mx_ksteps(int K) { return (K + 4 * MX_KSTEP - 1) / (4 * MX_KSTEP) * 4; }
+static inline int mx_ksteps(int K) { return mx_groups(K) * 4; }
 static inline int mx_tiles(int N) { return (N + 15) / 16; }
 
 MxPacked mx_packed_at(const void *packed, int N, int K) {

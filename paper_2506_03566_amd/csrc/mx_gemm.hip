@@ -9,8 +9,6 @@
 // columns of a row of Y.
 #include "mx.h"
 
-#include <math.h>
-
 namespace poss {
 
 constexpr int F16_SHIFT = 13;     // fp16 operands are c * 2^(s - ref) times 2^13: 6 * 2^13 is finite, and they are exact down to s = ref - 36
@@ -1013,62 +1011,6 @@ __global__ __launch_bounds__(256) void mx_planes_kernel(const f32x4 *__restrict_
 }
 
 // ------------------------------------------------------------------------------------------ launches
-// How a product runs: a kernel with its tile shape, and K splits.  Chosen by an estimate of the time in us: for each shape the sum of eight
-// terms whose weights were fitted (none negative) to times measured in graphs, 19 row counts (1 to 4096) x 10 matrices (512 x 512 to
-// 28672 x 4096 and 5120 x 13824) x up to ten splits.  What the estimate picks is 0.9 % slower on average than the fastest of all that was
-// measured; of 190 sizes 7 (microscaled X: 6) are more than a tenth slower, a fifth at most.  Where the shapes cross (4096 x 4096, us): 16
-// rows stream 6.2, 16 x 64 7.0; 128 rows 16 x 64 10.3, 32 x 128 11.1; 244 rows 32 x 128 13.7, 64 x 128 15.1; 512 rows 64 x 128 20.0, 64 x 256
-// 24.8; 1024 rows 43.0 and 31.5; 4096 rows 64 x 256 121, 256 x 256 108.
-struct MxPlan { int shape, splits; };
-struct MxTile { int tm, tn; float us[8]; };
-enum { MX_STREAM = 0 };
-constexpr int CHIP_CUS = 256;
-// us: a launch; k-groups of a tile; the same times rounds of the chip (256 tiles); ... times tiles / 256; rounds; planes: their launch, a million
-// of their values; a million results.  The first row (no tiles): a launch; sixteen k-groups; 10^4 column x k-groups; the same times ten rows.
-constexpr MxTile MX_TILES[] = {
-    {16, 16, {2.407f, 0.851f, 0.417f, 6.06f}},                                       // mx_stream_kernel
-    {16, 64, {1.920f, 0.493f, 0.021f, 0.218f, 0.879f, 2.158f, 0.769f, 0.686f}},      // mx_fed_kernel
-    {32, 128, {2.557f, 0.434f, 0.179f, 0.604f, 1.368f, 1.809f, 1.034f, 1.411f}},
-    {32, 256, {3.053f, 0.778f, 0.285f, 0.959f, 2.049f, 1.233f, 1.156f, 1.376f}},
-    {64, 128, {2.855f, 0.000f, 1.160f, 0.657f, 1.158f, 2.713f, 1.373f, 0.771f}},
-    {64, 256, {4.774f, 0.000f, 1.850f, 1.065f, 0.000f, 2.511f, 1.524f, 0.827f}},
-    {256, 256, {7.758f, 0.096f, 8.969f, 1.422f, 0.107f, 1.133f, 0.896f, 0.854f}}};   // mx_tile_kernel
-constexpr MxTile MX_BOTH_TILES[] = {
-    {16, 16, {2.334f, 0.381f, 0.347f, 2.44f}},                                       // mx_stream_both_kernel
-    {16, 64, {1.337f, 0.748f, 0.000f, 0.193f, 0.782f, 2.452f, 0.836f, 0.462f}},      // mx_fed_both_kernel
-    {32, 128, {1.353f, 0.881f, 0.000f, 0.331f, 1.418f, 2.265f, 1.356f, 1.889f}},
-    {64, 128, {2.659f, 0.354f, 0.539f, 0.262f, 1.552f, 2.436f, 1.456f, 0.903f}},
-    {64, 256, {4.124f, 0.105f, 1.079f, 0.327f, 0.000f, 2.889f, 1.496f, 0.698f}},
-    {256, 256, {6.552f, 0.000f, 2.005f, 1.094f, 4.886f, 4.424f, 1.030f, 0.407f}}};   // mx_block_both_kernel
-
-static int mx_groups(int K) { return (K + 4 * MX_KSTEP - 1) / (4 * MX_KSTEP); }
-// Waves of a column tile: four, sixteen where the tiles leave CUs with one each and K is long (one row, us, 4 / 8 / 16 waves: 4096 x 14336 9.0 / 8.5 / 8.0,
-// 5120 x 13824 10.8 / 12.0 / 12.2, 6144 x 4096 5.4 / 5.7, 4096 x 4096 3.4 / 3.6).
-static int stream_waves(int tiles, int kgroups) { return tiles <= 256 && kgroups >= 16 ? 16 : kgroups < 4 ? kgroups : 4; }
-
-// fixed > 0: the number of splits.
-template <int SHAPES> static MxPlan best_plan(const MxTile (&tiles)[SHAPES], int M, int N, int groups, int fixed = 0) {
-    MxPlan best{MX_STREAM, fixed > 0 ? fixed : 1};
-    float least = 1e30f;
-    if (M <= 16) {
-        const float *u = tiles[MX_STREAM].us, ng = (float)N * groups * 1e-4f;
-        least = u[0] + u[1] * groups / 16 + u[2] * ng + u[3] * ng * M * 1e-2f;
-    }
-    const float mn = (float)M * N * 1e-6f;
-    for (int i = 1; i < SHAPES; ++i) {
-        const MxTile &t = tiles[i];
-        const float n = (float)((M + t.tm - 1) / t.tm) * (float)((N + t.tn - 1) / t.tn);
-        if (n > 4e6f && i + 1 < SHAPES) continue;         // (a launch has fewer than 2^32 threads)
-        for (int s = fixed > 0 ? fixed : 1; s <= (fixed > 0 ? fixed : 16) && s <= groups && (fixed > 0 || s == 1 || n * s <= 1024); ++s) {
-            const float g = (float)((groups + s - 1) / s), chips = n * s / 256, rounds = ceilf(chips);
-            float us = t.us[0] + t.us[1] * g + t.us[2] * g * rounds + t.us[3] * g * chips + t.us[4] * rounds + t.us[7] * mn;
-            if (s > 1) us += t.us[5] + t.us[6] * s * mn;
-            if (us < least) { least = us; best = MxPlan{i, s}; }
-        }
-    }
-    return best;
-}
-
 // Whether X can be read as it is: rows of whole 16-byte pieces.
 static bool rows_ok(int x_dt, const void *x, int64_t ldx, int K) {
     return x_dt != DT_F32 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0 && K % 8 == 0 && ldx < (1 << 22);   // (offsets within a tile's rows are 32 bits)
@@ -1097,9 +1039,7 @@ static size_t stage_bytes(int x_dt, int M, int K, const MxPlan &p) {
     if (x_dt == DT_MX) return MX_BOTH_TILES[p.shape].tm == 256 ? (size_t)((M + 15) / 16) * groups * 256 : 0;
     return ((size_t)M * groups * 4 * MX_KSTEP * 2 * (x_dt == DT_F32 ? 3 : 1) + 255) / 256 * 256;
 }
-static MxPlan plan_of(int x_dt, int M, int N, int K) {
-    return x_dt == DT_MX ? best_plan(MX_BOTH_TILES, M, N, mx_groups(K)) : best_plan(MX_TILES, M, N, mx_groups(K) * (x_dt == DT_F32 ? 3 : 1));
-}
+static MxPlan plan_of(int x_dt, int M, int N, int K) { return mx_plan_of(x_dt == DT_MX, x_dt == DT_F32 ? 3 : 1, M, N, K); }
 size_t mx_gemm_scratch_size(int x_dt, int M, int N, int K) {
     if (M == 0) return 256;
     const MxPlan p = plan_of(x_dt, M, N, K);
@@ -1189,21 +1129,6 @@ static void run_gemm_t(const MxPacked &w, const MxRows &x, const MxGeom &g, cons
 }
 
 // ------------------------------------------------------------------------------------------ a context's layers
-// Splits of a matrix whose planes the layer's own epilogues add up: as many as give half the CUs a 128-column tile (a tree's rows are two
-// tiles of 32), the groups dealt out evenly.  They follow the matrix alone, and every kernel adds a split's products in the same order
-// (mx_stream_kernel its waves' sums as the epilogue would the planes): a row's sums do not depend on the rows beside it, and a tree's rows
-// get what plain decoding gives them.  Rounds of 61 rows and plain decoding, ms: 8B shape 4.42 and 2.27, 13B shape 5.38 and 3.22; with
-// twice as many splits (unsplit from 171 tiles on) 4.62 and 2.14, 5.54 and 3.23; with half as many 4.76 and 2.51, 6.20 and 4.01.
-int mx_plane_splits(int N, int K) {
-    const int groups = mx_groups(K), cols = (N + 127) / 128;
-    int s = cols >= 120 ? 1 : cols > 64 ? 2 : 128 / cols;
-    if (s > groups) s = groups;
-    if (s > 16) s = 16;
-    if (s < 1) s = 1;
-    const int longest = (groups + s - 1) / s;
-    return (groups + longest - 1) / longest;
-}
-
 bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, int ldx, int M, float *part, int ld, int splits, hipStream_t st) {
     if (!packed || !X || !part || M < 1 || N < 4 || N % 4 || K < 8 || K % 8 || ld % 4 || ld < (N + 15) / 16 * 16 || splits < 1 || splits > 16 || splits > mx_groups(K) ||
         !rows_ok(dt, X, ldx, K) || ldx < K) return false;
@@ -1215,9 +1140,6 @@ bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, i
     else run_tiles<f16_t, float, 1>(w, x, g, p, splits, part, ld, true, part, st);
     return true;
 }
-// Whether the planes are one (mx_stream_kernel adds its waves' sums itself).
-int mx_planes_written(int M, int N, int K, int splits) { return best_plan(MX_TILES, M, N, mx_groups(K), splits).shape == MX_STREAM ? 1 : splits; }
-
 // A thread per four units; the planes come from the L2s for the most part.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_silu_kernel(const float *__restrict__ part, int splits, int M, int ld, int F, T *__restrict__ act) {
