@@ -361,7 +361,7 @@ GemmShape run_gemm_mx(poss_ctx *c, const void *Wp, int N, int K, const void *X, 
     const int splits = mx_plane_splits(N, K);
     GemmShape g = gemm_plan(c->md.dt, M, N, K, 1);
     g.Mpad = M;
-    g.S = mx_planes_written(M, N, K, splits);
+    g.S = splits;
     const bool ok = epi.mode == EPI_SILU ? launch_mx_gate_up(c->md.dt, Wp, epi.F, K, X, ldx, M, part, g.Npad, epi.act, c->st)
                                          : launch_mx_planes(c->md.dt, Wp, N, K, X, ldx, M, part, g.Npad, splits, c->st) &&
                                            launch_planes_epilogue(c->md.dt, g, part, epi, c->md.eps, c->st, ranges);

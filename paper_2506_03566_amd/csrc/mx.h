@@ -31,8 +31,8 @@ void launch_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *pa
 // For a context's layers (16-bit types).  A matrix of packed rows, as launch_pack takes them, quantised and packed; N: its rows, padding ones among them.
 size_t mx_packed_size(int N, int K);
 void launch_mx_pack_rows(int dt, const PackSrc &src, int N, int K, void *packed, hipStream_t st);
-// The planes of X W^T: plane s < splits of part (mx_plane_splits; mx_planes_written of them), [M][ld], ld a multiple of four and at least N.  A row's planes
-// are the same for every M.
+// The planes of X W^T: plane s < splits of part (mx_plane_splits of them), [M][ld], ld a multiple of four and at least N.  A row's planes are the same for
+// every M.
 bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, int ldx, int M, float *part, int ld, int splits, hipStream_t st);
 // act[M][F] = SiLU(gate) * up of X with a matrix whose rows alternate in groups of 16 (PackSrc::interleave16).  part as above, for the planes of a split product.
 bool launch_mx_gate_up(int dt, const void *packed, int F, int K, const void *X, int ldx, int M, float *part, int ld, void *act, hipStream_t st);

@@ -1051,12 +1051,8 @@ static void add_planes(const MxPacked &w, const float *part, int splits, int M, 
     mx_planes_kernel<Y><<<dim3(((N + 3) / 4 + 255) / 256, M < 65535 ? M : 65535), 256, 0, st>>>(reinterpret_cast<const f32x4 *>(part), splits, M, N, w.tiles * 4, w.ref, shift, y, ldy, quads);
 }
 
-template <typename T, typename Y, int PARTS>
-static void run_tiles(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan &p, int waves, Y *y, int64_t ldy, bool quads, float *part, hipStream_t st) {
-    if (p.shape == MX_STREAM) {
-        mx_stream_kernel<T, Y, PARTS><<<w.tiles, waves * 64, waves * 1024, st>>>(w, x, y, ldy, quads, g.M, g.N);
-        return;
-    }
+template <typename T, typename Y>
+static void run_tiles(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan &p, Y *y, int64_t ldy, bool quads, float *part, hipStream_t st) {
     const MxTile t = MX_TILES[p.shape];
     g.splits = p.splits; g.tiles_m = (g.M + t.tm - 1) / t.tm; g.tiles_n = (g.N + t.tn - 1) / t.tn;
     const dim3 grid(g.tiles_m * g.tiles_n, g.splits);
@@ -1080,8 +1076,13 @@ static void run_tiles(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan
 }
 template <typename T, typename Y, int PARTS>
 static void run_gemm(const MxPacked &w, const MxRows &x, MxGeom g, const MxPlan &p, Y *y, int64_t ldy, bool quads, float *part, hipStream_t st) {
+    if (p.shape == MX_STREAM) {
+        const int waves = stream_waves(w.tiles, w.kgroups);
+        mx_stream_kernel<T, Y, PARTS><<<w.tiles, waves * 64, waves * 1024, st>>>(w, x, y, ldy, quads, g.M, g.N);
+        return;
+    }
     g.plane_ld = w.tiles * 16; g.plane_scaled = false;
-    run_tiles<T, Y, PARTS>(w, x, g, p, stream_waves(w.tiles, w.kgroups), y, ldy, quads, part, st);
+    run_tiles<T, Y>(w, x, g, p, y, ldy, quads, part, st);
     if (p.splits > 1) add_planes<Y>(w, part, p.splits, g.M, g.N, MxOp<T>::SHIFT, y, ldy, quads, st);
 }
 
@@ -1133,11 +1134,11 @@ bool launch_mx_planes(int dt, const void *packed, int N, int K, const void *X, i
     if (!packed || !X || !part || M < 1 || N < 4 || N % 4 || K < 8 || K % 8 || ld % 4 || ld < (N + 15) / 16 * 16 || splits < 1 || splits > 16 || splits > mx_groups(K) ||
         !rows_ok(dt, X, ldx, K) || ldx < K) return false;
     const MxPacked w = mx_packed_at(packed, N, K);
-    MxPlan p = best_plan(MX_TILES, M, N, w.kgroups, splits);
+    const MxPlan p = best_plan(MX_TILES, M, N, w.kgroups, splits);
     const MxGeom g{M, N, (K + MX_KSTEP - 1) / MX_KSTEP, K / MX_KSTEP, 0, 0, 1, ld, true};
     const MxRows x{X, ldx, 0, K};
-    if (dt == DT_BF16) run_tiles<bf16_t, float, 1>(w, x, g, p, splits, part, ld, true, part, st);
-    else run_tiles<f16_t, float, 1>(w, x, g, p, splits, part, ld, true, part, st);
+    if (dt == DT_BF16) run_tiles<bf16_t, float>(w, x, g, p, part, ld, true, part, st);
+    else run_tiles<f16_t, float>(w, x, g, p, part, ld, true, part, st);
     return true;
 }
 // A thread per four units; the planes come from the L2s for the most part.
@@ -1179,7 +1180,7 @@ bool launch_mx_gate_up(int dt, const void *packed, int F, int K, const void *X, 
     if (!act || F % 8) return false;
     if (splits > 1) {
         if (!launch_mx_planes(dt, packed, N, K, X, ldx, M, part, ld, splits, st)) return false;
-        launch_mx_silu(dt, part, mx_planes_written(M, N, K, splits), M, ld, F, act, st);
+        launch_mx_silu(dt, part, splits, M, ld, F, act, st);
         return true;
     }
     if (!packed || !X || M < 1 || K < 8 || ldx < K || !rows_ok(dt, X, ldx, K)) return false;

@@ -16,7 +16,7 @@ struct MxTile { int tm, tn; float us[8]; };
 enum { MX_STREAM = 0 };
 constexpr int CHIP_CUS = 256;
 // us: a launch; k-groups of a tile; the same times rounds of the chip (256 tiles); ... times tiles / 256; rounds; planes: their launch, a million
-// of their values; a million results.  The first row (no tiles): a launch; sixteen k-groups; 10^4 column x k-groups; the same times ten rows.
+// of their values; a million results.  The first row (no tiles): a launch; sixteen k-groups; 10^4 column x k-groups; the same times a hundred rows.
 constexpr MxTile MX_TILES[] = {
     {16, 16, {2.407f, 0.851f, 0.417f, 6.06f}},                                       // mx_stream_kernel
     {16, 64, {1.920f, 0.493f, 0.021f, 0.218f, 0.879f, 2.158f, 0.769f, 0.686f}},      // mx_fed_kernel
@@ -38,11 +38,15 @@ static inline int mx_groups(int K) { return (K - 1) / MX_GROUP + 1; }      // K 
 // 5120 x 13824 10.8 / 12.0 / 12.2, 6144 x 4096 5.4 / 5.7, 4096 x 4096 3.4 / 3.6).
 static inline int stream_waves(int tiles, int kgroups) { return tiles <= 256 && kgroups >= 16 ? 16 : kgroups < 4 ? kgroups : 4; }
 
-// fixed > 0: the number of splits.
+// fixed > 0: the number of splits, for a context's layers.  Those are not streamed: there mx_stream_kernel would have a wave per split, not the four or sixteen
+// that its weights were fitted with, and weights come from HBM, not the last cache (one row, us, streamed / 16 x 64 tiles: 6144 x 2048 2 splits 5.0 / 5.3,
+// 4096 x 4096 4 splits 5.3 / 5.4, 6144 x 4096 2 splits 7.6 / 7.2, 15360 x 5120 unsplit 15.7 / 13.3, 4096 x 14336 4 splits 11.7 / 10.1, 5120 x 13824 3 splits
+// 15.8 / 12.3; ten rows 6.2 / 5.4 to 23.6 / 12.4).  Plain decoding in the 8B and 13B shapes, ms, with streaming where the estimate had it / without: 2.24 / 2.17,
+// 3.15 / 3.01.
 template <int SHAPES> static inline MxPlan best_plan(const MxTile (&tiles)[SHAPES], int M, int N, int groups, int fixed = 0) {
-    MxPlan best{MX_STREAM, fixed > 0 ? fixed : 1};
+    MxPlan best{MX_STREAM, 1};
     float least = 1e30f;
-    if (M <= 16) {
+    if (M <= 16 && fixed == 0) {
         const float *u = tiles[MX_STREAM].us, ng = (float)N * groups * 1e-4f;
         least = u[0] + u[1] * groups / 16 + u[2] * ng + u[3] * ng * M * 1e-2f;
     }
@@ -67,9 +71,8 @@ static inline MxPlan mx_plan_of(bool both, int parts, int M, int N, int K) {
 
 // For a context's layers.
 // Splits of a matrix whose planes the layer's own epilogues add up: as many as give half the CUs a 128-column tile (a tree's rows are two
-// tiles of 32), the groups dealt out evenly.  They follow the matrix alone, and every kernel adds a split's products in the same order
-// (mx_stream_kernel its waves' sums as the epilogue would the planes): a row's sums do not depend on the rows beside it, and a tree's rows
-// get what plain decoding gives them.  Rounds of 61 rows and plain decoding, ms: 8B shape 4.42 and 2.27, 13B shape 5.38 and 3.22; with
+// tiles of 32), the groups dealt out evenly.  They follow the matrix alone, and every kernel adds a split's products in the same order:
+// a row's sums do not depend on the rows beside it, and a tree's rows get what plain decoding gives them.  Rounds of 61 rows and plain decoding, ms: 8B shape 4.42 and 2.27, 13B shape 5.38 and 3.22; with
 // twice as many splits (unsplit from 171 tiles on) 4.62 and 2.14, 5.54 and 3.23; with half as many 4.76 and 2.51, 6.20 and 4.01.
 static inline int mx_plane_splits(int N, int K) {
     const int groups = mx_groups(K), cols = (N + 127) / 128;
@@ -80,7 +83,5 @@ static inline int mx_plane_splits(int N, int K) {
     const int longest = (groups + s - 1) / s;
     return (groups + longest - 1) / longest;
 }
-// The planes that come of it: one where mx_stream_kernel has added its waves' sums itself.
-static inline int mx_planes_written(int M, int N, int K, int splits) { return best_plan(MX_TILES, M, N, mx_groups(K), splits).shape == MX_STREAM ? 1 : splits; }
 
 }  // namespace poss

@@ -49,7 +49,7 @@ int main(int argc, char **argv) {
             const int s = mx_plane_splits(n, k), groups = mx_groups(k);
             bool ok = s >= 1 && s <= 16 && s <= groups;
             for (int i = 0; i < s; ++i) ok = ok && (long)(i + 1) * groups / s > (long)i * groups / s;      // (no split is empty)
-            for (int m = 1; m <= 256; m += m < 20 ? 1 : 13) ok = ok && (mx_planes_written(m, n, k, s) == s || (m <= 16 && mx_planes_written(m, n, k, s) == 1));
+            for (int m = 1; m <= 256; m += m < 20 ? 1 : 13) { const MxPlan p = best_plan(MX_TILES, m, n, groups, s); ok = ok && p.shape != MX_STREAM && p.splits == s; }
             ++seen;
             if (!ok && wrong++ < 5) printf("planes of N %d K %d: %d splits\n", n, k, s);
         }
