@@ -71,12 +71,15 @@ static inline MxPlan mx_plan_of(bool both, int parts, int M, int N, int K) {
 
 // For a context's layers.
 // Splits of a matrix whose planes the layer's own epilogues add up: as many as give half the CUs a 128-column tile (a tree's rows are two
-// tiles of 32), the groups dealt out evenly.  They follow the matrix alone, and every kernel adds a split's products in the same order:
-// a row's sums do not depend on the rows beside it, and a tree's rows get what plain decoding gives them.  Rounds of 61 rows and plain decoding, ms: 8B shape 4.42 and 2.27, 13B shape 5.38 and 3.22; with
-// twice as many splits (unsplit from 171 tiles on) 4.62 and 2.14, 5.54 and 3.23; with half as many 4.76 and 2.51, 6.20 and 4.01.
+// tiles of 32), two where the columns alone give a quarter of them one, none where they give more than three quarters of them one; the groups dealt
+// out evenly.  They follow the matrix alone, and every kernel adds a split's products in the same order: a row's sums do not depend on the rows beside
+// it, and a tree's rows get what plain decoding gives them.  Rounds of 61 rows and plain decoding, ms: 8B shape 4.39 and 2.16, 13B shape 5.28 and 2.91;
+// twice as many of the splits below the last line 4.58 and 2.16, 5.40 and 2.88, half as many 4.61 and 2.32, 5.48 and 3.04.  That line, rounds, two
+// splits / none: 16 layers whose QKV, gate and up have 160 to 180 column tiles 2.56 / 2.58, 192 tiles 2.62 / 2.64; gate and up of 224 (8B) 4.46 / 4.39, of
+// 216 (13B) 5.32 / 5.28.
 static inline int mx_plane_splits(int N, int K) {
     const int groups = mx_groups(K), cols = (N + 127) / 128;
-    int s = cols >= 120 ? 1 : cols > 64 ? 2 : 128 / cols;
+    int s = cols > CHIP_CUS * 3 / 4 ? 1 : cols > CHIP_CUS / 4 ? 2 : CHIP_CUS / 2 / cols;
     if (s > groups) s = groups;
     if (s > 16) s = 16;
     if (s < 1) s = 1;

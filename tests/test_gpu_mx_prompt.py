@@ -64,3 +64,11 @@ def test_drafted_scores_after_a_prompt_of_several_passes():
     for t in common:
         assert abs(mine[t] - theirs[t]) <= 2 * tol_for(cfg), t
     ctx.close()
+
+
+# QKV, gate and up on either side of the line between two K splits and none (192 tiles of 128 columns), gate and up of 16-bit types beyond it
+@pytest.mark.parametrize("name,over", [("t_mid_f16", dict(d_ffn=12288)), ("t_mid_f16", dict(d_ffn=12296)), ("t_mid_bf16", dict(d_model=1024, n_q_heads=192, n_kv_heads=96, head_dim=64, d_ffn=12800)),
+                                       ("t_mid_f16", dict(d_model=640, n_q_heads=194, n_kv_heads=97, head_dim=64, d_ffn=1000))])
+def test_a_row_has_the_same_bits_where_splits_begin(name, over):
+    from test_gpu_mx_context import test_a_row_has_the_same_bits_in_trees_of_any_size as same_bits
+    same_bits(name, over)

@@ -81,3 +81,13 @@ def test_the_tested_sizes_reach_every_kernel(planner):
     tiled = {"16": ["16x64", "32x128", "32x256", "64x128", "64x256", "256x256"], "mx": ["16x64", "32x128", "64x128", "64x256", "256x256"]}
     tiled["f32"] = tiled["16"]
     assert reached == {(kind, t, split) for kind, ts in tiled.items() for t in ts for split in (False, True)} | {(kind, "16x16", False) for kind in tiled}
+
+
+def test_splits_of_a_contexts_matrices(tmp_path):
+    """By the columns alone: half of 256 CUs a tile of 128 columns, two splits from a quarter on, none beyond three quarters."""
+    (tmp_path / "splits.cc").write_text('#include "mx_plan.h"\n#include <stdio.h>\nint main() { int n, k; while (scanf("%d %d", &n, &k) == 2) printf("%d\\n", poss::mx_plane_splits(n, k)); }\n')
+    subprocess.run(["g++", "-std=c++17", "-O2", "-I", os.path.join(ROOT, "paper_2506_03566_amd", "csrc"), str(tmp_path / "splits.cc"), "-o", str(tmp_path / "splits")], check=True)
+    cases = {(128, 1 << 21): 16, (1024, 8192): 16, (1024, 4096): 8, (4096, 4096): 4, (4096, 14336): 4, (5120, 5120): 3, (8192, 4096): 2, (8193, 4096): 2, (15360, 5120): 2, (24576, 4096): 2,
+             (24577, 4096): 1, (28672, 4096): 1, (4096, 512): 1, (1024, 1536): 3, (1024, 5632): 11, (2048, 5120): 5}
+    got = subprocess.run([str(tmp_path / "splits")], input="".join("%d %d\n" % c for c in cases), stdout=subprocess.PIPE, text=True, check=True).stdout.split()
+    assert [int(g) for g in got] == list(cases.values())
