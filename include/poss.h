@@ -134,7 +134,8 @@ int poss_load(const poss_config *cfg, const poss_weights *w, void *workspace,
  * matrices of more than 2^21 columns) and multiplied as poss_mx_gemm does.  Embedding, LM head, norms, biases, activations and caches stay
  * as poss_load has them.  A smaller workspace, poss_workspace_bytes_mx(cfg) (0 if the configuration is refused).  All calls on a context
  * work alike; a sequence's tokens are those of a model with the rounded weights, and a row's products do not depend on the number of rows
- * beside it.  Prompts run POSS_LAUNCH_ROWS rows a pass, whatever their length.  poss_profile_gemm counts the LM head's products only,
+ * beside it.  Prompts run POSS_LAUNCH_ROWS rows a pass, whatever their length
+ * (beyond 512 tokens they take longer than with 16-bit layers).  poss_profile_gemm counts the LM head's products only,
  * poss_set_tuning's workgroup target applies to them only. */
 size_t poss_workspace_bytes_mx(const poss_config *cfg);
 int poss_load_mx(const poss_config *cfg, const poss_weights *w, void *workspace,
@@ -343,11 +344,12 @@ int poss_mx_dequantize(int32_t dtype, const void *codes, const void *scales, int
 size_t poss_mx_packed_bytes(int32_t N, int32_t K);
 int poss_mx_pack(const void *codes, const void *scales, int32_t N, int32_t K, void *packed, void *hip_stream);
 
-/* Y[M][N] of y_dtype = X[M][K] . W[N][K]^T with packed W and X of x_dtype.  Every product of an activation and a weight is exact (float32
- * activations included), sums are float32, the result is rounded once.  scratch: at least poss_mx_gemm_scratch_bytes(x_dtype, M, N, K)
- * bytes (at least 256; 0 for a bad shape: M at most 2^24, M * N at most 2^38), aligned to 256, for this call alone until it has run: two calls that may run at the same
- * time, or two graphs that may, need one each.  The bits of a row may differ with M (other kernels sum in another order); the same call
- * gives the same bits. */
+/* Y[M][N] of y_dtype = X[M][K] . W[N][K]^T with packed W and X of x_dtype.  Every product of an activation and a weight is exact where
+ * float32 can hold it (float32 activations included, down to 2^-133), sums are float32, the result is rounded once.  scratch: at least
+ * poss_mx_gemm_scratch_bytes(x_dtype, M, N, K) bytes (at least 256; 0 for a bad shape: M at most 2^24, M * N at most 2^38; room for a copy
+ * of X is part of it, for rows that cannot be read in 16-byte pieces), aligned to 256, for this call alone until it has run: two calls that
+ * may run at the same time, or two graphs that may, need one each.  The bits of a row may differ with M (other kernels sum in another
+ * order); the same call gives the same bits. */
 #define POSS_MX 4                    /* in place of x_dtype: X is microscaled too (poss_mx_gemm_mx) */
 size_t poss_mx_gemm_scratch_bytes(int32_t x_dtype, int32_t M, int32_t N, int32_t K);
 int poss_mx_gemm(int32_t x_dtype, const void *x, int64_t ldx, const void *packed, int32_t y_dtype, void *y, int64_t ldy,

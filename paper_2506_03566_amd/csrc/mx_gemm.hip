@@ -768,7 +768,7 @@ __global__ __launch_bounds__(256) void mx_scales_kernel(const uint8_t *__restric
 
 // 256 x 256 tiles, eight waves of 128 x 64 with the 32 x 32 x 64 instruction (registers alone, random codes: 6.3 PFLOP/s where the
 // 16 x 16 x 128 one gives 5.2).  Codes of both operands go into LDS by LDS-direct loads, a k-step of 128 a stage, four stages in a ring,
-// one barrier per k-step; the scales of a group of four k-steps likewise, an eighth of them by each wave, a quarter of that per k-step, two buffers.
+// one barrier per k-step; the scales of a group of four k-steps likewise, an eighth of them by each wave, half of that in each of the first two k-steps of the group before; two buffers.
 // A workgroup per CU takes one tile after the other, and the loads run on into the next one: when a tile's sums are written, the next
 // tile's first three stages and scales are there or on their way.  8192 x 28672 x 4096: 480 us, 4.0 PFLOP/s; the matrix pipes are busy half the
 // cycles of a clock that their load has brought to 1.7 GHz (registers alone: all cycles at 1.5).
@@ -785,7 +785,7 @@ __global__ __launch_bounds__(512, 2) void mx_block_both_kernel(MxPacked w, const
     const int x_b = (lane & 3) ^ (lane >> 4);             // block b of row r of a unit of X lies at position b ^ (r / 4 % 4)
     const bool planes = g.splits > 1;                     // (Y is float then)
     const int tiles = g.tiles_m * g.tiles_n, items = tiles * g.splits, rts = (g.M + 15) / 16;
-    // A tile (of a split) as the loads see it.  Scales: unit wave + 8 j of a group at its k-step j (0, 1: row tiles; 2, 3: column tiles).
+    // A tile (of a split) as the loads see it.  Scales of a group: unit wave + 8 j (j = 0, 1: row tiles; 2, 3: column tiles).
     struct Item { int m0, ct0, split, g0, n; };
     auto item_of = [&](int i) {
         Item t;
@@ -1033,7 +1033,8 @@ static MxRows stage(int x_dt, const void *x, int64_t ldx, int M, int K, int kp, 
     return MxRows{scratch, kp, 0, kp};
 }
 
-// Scratch: what stands in X's place (a staged copy; X's scales in operand order), then the planes.
+// Scratch: what stands in X's place (a staged copy; X's scales in operand order), then the planes.  Its size is asked for by type and shape: the copy's
+// room is there for 16-bit rows of any distance and address, also where rows can be read as they are.
 static size_t stage_bytes(int x_dt, int M, int K, const MxPlan &p) {
     const size_t groups = mx_groups(K);
     if (x_dt == DT_MX) return MX_BOTH_TILES[p.shape].tm == 256 ? (size_t)((M + 15) / 16) * groups * 256 : 0;
