@@ -359,6 +359,111 @@ int poss_mx_gemm(int32_t x_dtype, const void *x, int64_t ldx, const void *packed
 int poss_mx_gemm_mx(const void *x_codes, const void *x_scales, const void *packed, int32_t y_dtype, void *y, int64_t ldy,
                     int32_t M, int32_t N, int32_t K, void *scratch, size_t scratch_bytes, void *hip_stream);
 
+/* ---- paged caches of a program's own ----------------------------------------------------------- */
+
+/* Serving over caches that the program lays out and owns: rotary positions on the way in, attention of one new token per sequence,
+ * eviction by accumulated attention weight; and what logits say of given tokens.  The cache has the layout of a context's own, so that
+ * poss_get_kv_cache can hand those out to the same calls.
+ *
+ * As above: calls enqueue on hip_stream (NULL = default stream) of the current GPU, whose memory every DEVICE pointer addresses, return without
+ * waiting, allocate nothing, keep nothing and can be captured into a graph; row distances are counts of values; zero rows or sequences are
+ * no work and no error; inputs and outputs must not overlap where nothing else is said; failures leave their message for
+ * poss_last_error(NULL).  Structs are HOST memory, read before the call returns. */
+
+/* Slot s of sequence b lies in page page_table[b * table_stride + s / page_tokens] at place s % page_tokens.  Keys: k[page][head][place][dim];
+ * values: v[page][head][dim][place]; all but the pages contiguous.  A table's entry outside 0 .. n_pages-1 is no page: what a call does
+ * with a slot there stands at the call; nothing outside the pages is read or written.  Several sequences may share pages that no call writes. */
+typedef struct poss_kv_cache {
+    int32_t dtype, n_kv_heads, head_dim;     /* head_dim: a multiple of 32, at most 256; at most 65535 heads                     */
+    int32_t page_tokens;                     /* 32, 64 or 128                                                                    */
+    int32_t n_pages;
+    int32_t n_seq, table_pages, table_stride;/* table_pages * page_tokens slots for each sequence, at most 2^30; n_seq at most 65535 */
+    int64_t k_page_stride, v_page_stride;    /* values from a page to the next, multiples of 16 bytes                            */
+    void *k, *v;                             /* DEVICE, 16-byte aligned                                                          */
+    const int32_t *page_table;               /* DEVICE                                                                           */
+} poss_kv_cache;
+
+/* Rotary positions of a head's first rot_dim values: pair i is (x[i], x[i + rot_dim/2]) or, interleaved, (x[2i], x[2i+1]); it becomes
+ * magnitude * (a cos - b sin, b cos + a sin) at the angle position * freq[i], formed in 64 bits.  The other values stay.  A program may fill in
+ * frequencies of its own (finite ones). */
+#define POSS_ROPE_PAIRS 128
+typedef struct poss_rope {
+    int32_t rot_dim, interleaved;            /* rot_dim: even, 2 .. 2 * POSS_ROPE_PAIRS */
+    float   magnitude;
+    double  freq[POSS_ROPE_PAIRS];
+} poss_rope;
+
+/* Fills in *out.  w[i] = theta^(-2i / rot_dim), scaled for contexts beyond `original` positions by `factor`:
+ * NONE w;  LINEAR w / factor;  BASE w of theta * factor^(rot_dim / (rot_dim - 2));
+ * BANDS and RAMP g w + (1 - g) w / factor, BANDS with g = (turns - low) / (high - low) for turns = original * w / (2 pi), RAMP with
+ * g = 1 - (i - lo) / (hi - lo) for lo, hi = the indices of `high` and `low` turns, floor and ceiling, within 0 .. rot_dim - 1; g kept in 0 .. 1.
+ * factor, low, high and original are read by the scalings that name them.  HOST only, no GPU needed. */
+#define POSS_ROPE_NONE   0
+#define POSS_ROPE_LINEAR 1
+#define POSS_ROPE_BASE   2
+#define POSS_ROPE_BANDS  3
+#define POSS_ROPE_RAMP   4
+int poss_rope_fill(int32_t rot_dim, int32_t interleaved, double theta, int32_t scaling, double factor, double low, double high,
+                   double original, double magnitude, poss_rope *out);
+
+/* y = x rotated, rounded once: value d of head h of row r lies at x[r * x_row + h * x_head + d], the same for y.  positions: DEVICE int32[rows], of
+ * any sign.  inverse != 0: by the opposite angle (the transpose, up to magnitude^2: what a gradient is multiplied by).  y may be x, with the same distances. */
+int poss_rotary(int32_t dtype, const void *x, int64_t x_row, int64_t x_head, void *y, int64_t y_row, int64_t y_head, int32_t rows,
+                int32_t heads, int32_t head_dim, const int32_t *positions, const poss_rope *rope, int32_t inverse, void *hip_stream);
+
+/* New rows on their way into the cache: k and v [rows][n_kv_heads][head_dim] (heads contiguous, rows k_row and v_row values apart) are written to
+ * slot slots[r] of sequence seq[r] (seq NULL: row r is sequence r), keys rotated; q [rows][n_q_heads][head_dim] is rotated into q_out, which may be q
+ * (n_q_heads 0: no queries).  rope NULL: nothing is rotated (positions may then be NULL).  A row whose slot, sequence or page is not there has
+ * its queries rotated and nothing written: slot -1 marks padding.  Two rows with the same slot leave either's values, value by value.
+ * slot_positions, if given: int32 [n_seq][n_kv_heads][slots], the rows' positions are noted there (for poss_kv_evict).  k, v and q may be
+ * parts of one matrix.  All arrays DEVICE. */
+int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t rows, int32_t n_q_heads, const void *q, int64_t q_row,
+                   void *q_out, int64_t q_out_row, const void *k, int64_t k_row, const void *v, int64_t v_row, const int32_t *seq,
+                   const int32_t *slots, const int32_t *positions, int32_t *slot_positions, void *hip_stream);
+
+/* Attention of one query row per sequence over the slots 0 .. lengths[b]-1: out[b][h] = sum_s p v, p = softmax(scale * q . k), query head h on key
+ * head h / (n_q_heads / n_kv_heads).  q and out: [n_seq][n_q_heads][head_dim] of the cache's type, heads contiguous, q_row and out_row values apart, 16-byte
+ * aligned with distances of whole 16 bytes.  lengths: DEVICE int32[n_seq]; max_len: the most that any of them is (0: all slots); it decides
+ * how the work is split.  A length of zero or less gives zeros and an lse of -infinity; one above max_len, or a slot without a page, a row of NaN; scores that are all
+ * -infinity, zeros over nothing: a row of NaN and an lse of -infinity.
+ * lse (may be NULL): float32 [n_seq][n_q_heads], the logarithm of the sum of exponentials.
+ * weights_out (may be NULL): float32 [n_seq][n_kv_heads][slots], the weights that the slots have been given so far: weights (the same form; NULL: zeros;
+ * may be weights_out) plus this row's p, summed over the heads that share the key head.  Slots beyond the length are left as they were.
+ * scratch: poss_kv_attend_scratch_bytes bytes, aligned to 256, for this call alone until it has run (two calls or graphs that may
+ * run at the same time need one each).  Sums and statistics are float32; 16-bit probabilities carry 16 significant bits (bf16) or 11 (f16).
+ * The bits of a row may differ with the other rows' lengths; the same call gives the same bits. */
+size_t poss_kv_attend_scratch_bytes(const poss_kv_cache *cache, int32_t n_q_heads, int32_t max_len, int32_t weighed);
+int poss_kv_attend(const poss_kv_cache *cache, int32_t n_q_heads, const void *q, int64_t q_row, void *out, int64_t out_row,
+                   const int32_t *lengths, int32_t max_len, float scale, float *lse, const float *weights, float *weights_out,
+                   void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/* Cuts every sequence to `budget` slots, each key head for itself: of more than budget slots stay the ones with a position below `first`, the newest
+ * `recent` (position > newest - recent) and, of the others, those of the largest weights; equal ones by the lowest slot, NaN last.  (Should those that always
+ * stay be more than the budget, the lowest slots of them do.)  A kept slot below the budget stays where it is; the places of the others there are
+ * filled, in order, with the kept slots from above, keys, values, weights and positions.  So a slot's index says nothing of its age: its position does.
+ * weights float32 and positions int32: [n_seq][n_kv_heads][slots]; lengths int32[n_seq] (read as 0 .. slots).  kept: int32 [n_seq][n_kv_heads][budget], the
+ * former slot of each, -1 beyond the new length.  weights_out and positions_out: the same for the new slots, 0 and -1 beyond the new length.  lengths_out:
+ * the new lengths.  The four outputs are arrays of their own; keys and values are moved in the cache: what lies at or above the budget there stays,
+ * so the same call again does the same.  Moves from or to a slot without a page are left out.  All arrays DEVICE; first + recent <= budget. */
+int poss_kv_evict(const poss_kv_cache *cache, const float *weights, const int32_t *positions, const int32_t *lengths, int32_t budget,
+                  int32_t first, int32_t recent, int32_t *kept, float *weights_out, int32_t *positions_out, int32_t *lengths_out,
+                  void *hip_stream);
+
+/* Log-probabilities under softmax(x / temperature) for x[rows][vocab] of `dtype`, rows ldx values apart: logp[rows][n_tokens] of tokens[rows][n_tokens] (int32; one
+ * outside the vocabulary gets NaN), entropy[rows] (may be NULL), and of the n_top largest logits of a row, equal ones by the lowest id,
+ * ids and log-probabilities, top_ids and top_logp [rows][n_top].  n_tokens may be 0, n_top is at most POSS_LOGPROBS_TOP and vocab.  Logits of -infinity have
+ * no probability; a row with a NaN or +infinity, or nothing above -infinity, has NaN for all but its ids, among which NaN come last.
+ * Outputs float32, all arrays DEVICE.  scratch: as for poss_kv_attend (0 bytes needed: a bad shape). */
+#define POSS_LOGPROBS_TOP 32
+size_t poss_logprobs_scratch_bytes(int32_t rows, int32_t vocab, int32_t n_top);
+int poss_logprobs(int32_t dtype, const void *x, int64_t ldx, int32_t rows, int32_t vocab, float temperature, const int32_t *tokens,
+                  int32_t n_tokens, float *logp, float *entropy, int32_t n_top, int32_t *top_ids, float *top_logp,
+                  void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/* The cache of one sequence of a context in the form above (one sequence): which = -1: target layer `layer`; which = s >= 0: specialist s.  Slots 0 .. t-1
+ * hold the committed tokens' keys (rotated) and values; queue work on the context's stream, between its calls. */
+int poss_get_kv_cache(poss_ctx *ctx, int32_t seq, int32_t which, int32_t layer, poss_kv_cache *out);
+
 #ifdef __cplusplus
 }
 #endif

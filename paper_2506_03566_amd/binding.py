@@ -20,7 +20,9 @@ EXPORTS = ["poss_workspace_bytes", "poss_load", "poss_reset", "poss_prefill", "p
            "poss_last_error", "poss_free", "poss_profile_gemm", "poss_gemm_profile", "poss_set_tuning", "poss_set_launch_rows", "poss_set_sampling", "poss_set_draft_sampling",
            "poss_debug_build_tree", "poss_debug_set_taps", "poss_debug_read_kv", "poss_debug_draft_logits",
            "poss_debug_gemm_scratch_bytes", "poss_debug_gemm", "poss_gemm_static",
-           "poss_workspace_bytes_mx", "poss_load_mx", "poss_mx_quantize", "poss_mx_dequantize", "poss_mx_packed_bytes", "poss_mx_pack", "poss_mx_gemm_scratch_bytes", "poss_mx_gemm", "poss_mx_gemm_mx"]
+           "poss_workspace_bytes_mx", "poss_load_mx", "poss_mx_quantize", "poss_mx_dequantize", "poss_mx_packed_bytes", "poss_mx_pack", "poss_mx_gemm_scratch_bytes", "poss_mx_gemm", "poss_mx_gemm_mx",
+           "poss_rope_fill", "poss_rotary", "poss_kv_append", "poss_kv_attend_scratch_bytes", "poss_kv_attend", "poss_kv_evict",
+           "poss_logprobs_scratch_bytes", "poss_logprobs", "poss_get_kv_cache"]
 
 c_i32, c_f32, c_vp = ctypes.c_int32, ctypes.c_float, ctypes.c_void_p
 
@@ -47,6 +49,18 @@ class PossStats(ctypes.Structure):
     _fields_ = [("rounds", ctypes.c_int64), ("committed_tokens", ctypes.c_int64),
                 ("c", ctypes.c_int64 * (MAX_DEPTH + 1)),
                 ("ms_draft", ctypes.c_double), ("ms_verify", ctypes.c_double), ("ms_commit", ctypes.c_double)]
+
+
+class PossKvCache(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("dtype", "n_kv_heads", "head_dim", "page_tokens", "n_pages", "n_seq", "table_pages", "table_stride")] + \
+               [("k_page_stride", ctypes.c_int64), ("v_page_stride", ctypes.c_int64), ("k", c_vp), ("v", c_vp), ("page_table", c_vp)]
+
+
+ROPE_PAIRS = 128
+
+
+class PossRope(ctypes.Structure):
+    _fields_ = [("rot_dim", c_i32), ("interleaved", c_i32), ("magnitude", c_f32), ("freq", ctypes.c_double * ROPE_PAIRS)]
 
 
 class PossError(RuntimeError):
@@ -115,6 +129,18 @@ def load_library():
     lib.poss_mx_gemm_scratch_bytes.argtypes = [c_i32, c_i32, c_i32, c_i32]
     lib.poss_mx_gemm.argtypes = [c_i32, c_vp, c_i64, c_vp, c_i32, c_vp, c_i64, c_i32, c_i32, c_i32, c_vp, c_sz, c_vp]
     lib.poss_mx_gemm_mx.argtypes = [c_vp, c_vp, c_vp, c_i32, c_vp, c_i64, c_i32, c_i32, c_i32, c_vp, c_sz, c_vp]
+    c_f64 = ctypes.c_double
+    lib.poss_rope_fill.argtypes = [c_i32, c_i32, c_f64, c_i32, c_f64, c_f64, c_f64, c_f64, c_f64, P(PossRope)]
+    lib.poss_rotary.argtypes = [c_i32, c_vp, c_i64, c_i64, c_vp, c_i64, c_i64, c_i32, c_i32, c_i32, c_vp, P(PossRope), c_i32, c_vp]
+    lib.poss_kv_append.argtypes = [P(PossKvCache), P(PossRope), c_i32, c_i32, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp, c_vp, c_vp, c_vp]
+    lib.poss_kv_attend_scratch_bytes.restype = c_sz
+    lib.poss_kv_attend_scratch_bytes.argtypes = [P(PossKvCache), c_i32, c_i32, c_i32]
+    lib.poss_kv_attend.argtypes = [P(PossKvCache), c_i32, c_vp, c_i64, c_vp, c_i64, c_vp, c_i32, c_f32, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
+    lib.poss_kv_evict.argtypes = [P(PossKvCache), c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp]
+    lib.poss_logprobs_scratch_bytes.restype = c_sz
+    lib.poss_logprobs_scratch_bytes.argtypes = [c_i32, c_i32, c_i32]
+    lib.poss_logprobs.argtypes = [c_i32, c_vp, c_i64, c_i32, c_i32, c_f32, c_vp, c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_sz, c_vp]
+    lib.poss_get_kv_cache.argtypes = [c_vp, c_i32, c_i32, c_i32, P(PossKvCache)]
     _lib = lib
     return lib
 
@@ -344,6 +370,13 @@ class Poss:
         out = torch.empty(n, self.cfg.vocab, dtype=torch.float32, device="cuda")
         self._check(self.lib.poss_debug_draft_logits(self.h, row0, n, c_vp(out.data_ptr())))
         return out
+
+    def kv_cache(self, seq=0, which=-1, layer=0):
+        """The cache of one sequence for kv_attend and the like: the target's layer `layer` (which -1) or specialist `which`.  The memory is this context's."""
+        from .serving import KvCache
+        c = PossKvCache()
+        self._check(self.lib.poss_get_kv_cache(self.h, seq, which, layer, ctypes.byref(c)))
+        return KvCache.of_context(self, c)
 
     def debug_read_kv(self, which, layer, slot0, n):
         cfg = self.cfg

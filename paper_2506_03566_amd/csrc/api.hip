@@ -1630,6 +1630,18 @@ int poss_debug_read_kv(poss_ctx *c, int32_t which, int32_t layer, int32_t slot0,
     return POSS_OK;
 }
 
+int poss_get_kv_cache(poss_ctx *c, int32_t seq, int32_t which, int32_t layer, poss_kv_cache *out) {
+    if (!c || !out) return POSS_E_INVALID_ARG;
+    if (seq < 0 || seq >= c->B) return fail(c, POSS_E_INVALID_ARG, "poss_get_kv_cache: no such sequence");
+    if (which < -1 || which >= c->cfg.n_specialists || (which < 0 && (layer < 0 || layer >= c->cfg.n_layers)))
+        return fail(c, POSS_E_INVALID_ARG, "poss_get_kv_cache: no such cache");
+    const KVCache &kv = which < 0 ? c->seq[seq].target_kv[layer] : c->seq[seq].spec_kv[which];
+    const int P = c->cfg.kv_page_tokens;
+    const int64_t page = (int64_t)c->md.hkv * P * c->md.dh;
+    *out = poss_kv_cache{c->cfg.dtype, c->md.hkv, c->md.dh, P, c->n_pages, 1, c->n_pages, c->n_pages, page, page, kv.k, kv.vt, kv.page_table};
+    return POSS_OK;
+}
+
 __global__ void sum_planes_kernel(const float *__restrict__ part, int S, size_t plane, int Npad, int N, float *__restrict__ y) {
     const int n = blockIdx.x * blockDim.x + threadIdx.x, m = blockIdx.y;
     if (n >= N) return;
