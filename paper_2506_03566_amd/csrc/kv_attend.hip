@@ -1,84 +1,387 @@
 // Attention of one new token per sequence over a paged cache (include/poss.h: poss_kv_attend).
+//
+// Online softmax in the log2 domain: a wave keeps, per query head, the maximum m of its scores z = scale * log2(e) * q.k, l = sum 2^(z-m) and
+// O = sum 2^(z-m) v; two such triples join as m = max, l and O scaled by 2^(m_i - m) and added.  out = O / l, lse = (m + log2 l) * ln 2.
+// What bounds it: keys and values are read once; the matrix instructions, of whose 16 columns the heads that share a key head use theirs, have ten times the rate that
+// is wanted.
+//
+// Work is cut along the batch's slots laid end to end, in blocks of 32: workgroup w of a key head takes blocks [w T / W, (w + 1) T / W) of all T, so
+// that ragged batches are even without the host knowing a length.  A row that lies in one workgroup is written there; pieces of others
+// go to scratch (at most two a workgroup: the end of a row that began before, the beginning of one that goes on) and are joined in order by a second launch.
 #include "kv.h"
 
 namespace poss {
 
+typedef float  f32x4 __attribute__((ext_vector_type(4)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16_t  f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int ATT_BLOCK = 32;                 // slots of a block: never across pages
+constexpr int ATT_WAVES = 4;
+constexpr int ATT_LEAST = 8;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
 struct AttendArgs {
-    int hq;
+    int hq, tiles;        // tiles: groups of 16 query heads of a key head
     const void *q; int64_t q_row; void *out; int64_t out_row;
     const int32_t *lengths; int max_len; float scale;
     float *lse; const float *weights; float *weights_out;
-    float *scores;        // [n_seq][hq][max_len]
-    float *row_lse;       // [n_seq][hq]
+    int W;                // workgroups along the batch's slots
+    float *part;          // [2 W][hkv * tiles][16][dh]
+    float2 *part_ml;      // [2 W][hkv * tiles][16]
+    float *scores; int64_t score_row;   // [n_seq][hq][score_row], log2 domain
+    float *row_lse;       // [n_seq][hq], log2 domain
 };
 
-// A workgroup per sequence and query head: scores of 256 slots at a time, the running maximum and sum, then the values.
-template <typename T>
-__global__ void __launch_bounds__(256) attend_kernel(KvView c, AttendArgs a) {
-    __shared__ float qs[256], ps[256], red_v[17];
-    __shared__ int red_i[17];
-    __shared__ int pages[256];
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, g = a.hq / c.hkv, hk = h / g, dh = c.dh;
-    if (tid < dh) qs[tid] = to_f(static_cast<const T *>(a.q)[b * a.q_row + (int64_t)h * dh + tid]);
-    __syncthreads();
-    int len = a.lengths[b];
-    const bool bad = len > a.max_len;
-    len = len < 0 ? 0 : bad ? 0 : len;
-    const T *k = static_cast<const T *>(c.k), *v = static_cast<const T *>(c.v);
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int s0 = 0; s0 < len; s0 += 256) {
-        const int s = s0 + tid;
-        float z = -INFINITY;
-        int page = -1;
-        if (s < len) {
-            page = kv_page(c, b, s);
-            z = NAN;
-            if (page >= 0) {
-                z = 0.f;
-                const T *key = k + kv_key_at(c, page, hk, s);
-                for (int d = 0; d < dh; ++d) z += qs[d] * to_f(key[d]);
-                z *= a.scale;
-            }
-            if (a.scores) a.scores[((int64_t)b * a.hq + h) * a.max_len + s] = z;
-        }
-        float top = z; int id = tid;
-        block_argmax(top, id, red_v, red_i);
-        const float now = fmaxf(m, top), ref = now == -INFINITY ? 0.f : now, back = m == -INFINITY ? 0.f : expf(m - ref);
-        const float p = expf(z - ref);
-        l = l * back + block_sum(p, red_v);
-        ps[tid] = p; pages[tid] = page;
-        __syncthreads();
-        if (tid < dh) {
-            o *= back;
-            const int n = min(256, len - s0);
-            for (int j = 0; j < n; ++j) o += pages[j] >= 0 ? ps[j] * to_f(v[kv_value_at(c, pages[j], hk, tid, s0 + j)]) : NAN;
-        }
-        m = now;
-        __syncthreads();
+// Blocks of a row; one whose length is beyond the bound has none and is NaN.
+__device__ __forceinline__ int row_blocks(int len, int max_len) { return len <= 0 || len > max_len ? 0 : (len + ATT_BLOCK - 1) / ATT_BLOCK; }
+
+// Workgroups that the slots are cut among: no more than W, and none with less than ATT_LEAST blocks' worth.
+__device__ __forceinline__ int64_t attend_parts(int64_t all, int W) {
+    const int64_t p = (all + ATT_LEAST - 1) / ATT_LEAST;
+    return p < W ? p : W;
+}
+
+// Sum over the wave's lanes up to this one.
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {
+    for (int o = 1; o < 64; o <<= 1) { const int64_t y = __shfl_up(x, o); if ((int)(threadIdx.x & 63) >= o) x += y; }
+    return x;
+}
+// Blocks of all rows, and of those before row `upto`; by every wave for itself.
+__device__ __forceinline__ void count_blocks(const int32_t *lengths, int n, int max_len, int upto, int64_t &all, int64_t &before) {
+    int64_t a = 0, b = 0;
+    for (int i = threadIdx.x & 63; i < n; i += 64) {
+        const int x = row_blocks(lengths[i], max_len);
+        a += x;
+        if (i < upto) b += x;
     }
-    const float sum = m + logf(l);
-    if (tid < dh) static_cast<T *>(a.out)[b * a.out_row + (int64_t)h * dh + tid] = from_f<T>(bad ? NAN : len ? o / l : 0.f);
-    if (tid == 0) {
-        const float lse = bad ? NAN : len ? sum : -INFINITY;
-        if (a.lse) a.lse[(int64_t)b * a.hq + h] = lse;
-        if (a.row_lse) a.row_lse[(int64_t)b * a.hq + h] = lse;
+    for (int o = 32; o; o >>= 1) { a += __shfl_xor(a, o); b += __shfl_xor(b, o); }
+    all = a; before = b;
+}
+// The row that holds block `at` (0 <= at < all) and its first block.
+__device__ __forceinline__ void find_row(const int32_t *lengths, int n, int max_len, int64_t at, int &row, int64_t &first) {
+    int64_t base = 0;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        const int i = i0 + (int)(threadIdx.x & 63);
+        const int x = i < n ? row_blocks(lengths[i], max_len) : 0;
+        const int64_t end = base + wave_scan(x);
+        const unsigned long long past = __ballot(end > at);
+        if (past) {
+            const int lane = __ffsll(past) - 1;
+            row = i0 + lane;
+            first = __shfl(end - x, lane);
+            return;
+        }
+        base = __shfl(end, 63);
+    }
+}
+
+// What a wave does with a block of 32 slots, 16-bit types.  Scores: K as the A operand, its rows ordered so that the lane of group g = lane / 16 gets the scores of slots
+// 8g .. 8g + 7 for head lane % 16 - the B operand of O^T = V^T P^T as it stands.
+template <typename T, int DH> struct Tile {
+    typedef T x8 __attribute__((ext_vector_type(8)));
+    x8 q[DH / 32], k[2][DH / 32], v[DH / 16];
+    static __device__ __forceinline__ int slot_of(int j) { return 8 * ((threadIdx.x & 63) >> 4) + j; }
+    __device__ __forceinline__ void load_q(const T *row, bool there) {
+        const int g = (threadIdx.x & 63) >> 4;
+        for (int s = 0; s < DH / 32; ++s) q[s] = there ? *reinterpret_cast<const x8 *>(row + 32 * s + 8 * g) : x8{};
+    }
+    __device__ __forceinline__ void load(const T *kb, const T *vb, int P) {
+        const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const T *row = kb + (8 * (i >> 2) + 4 * t + (i & 3)) * DH + 8 * g;
+#pragma unroll
+            for (int s = 0; s < DH / 32; ++s) k[t][s] = *reinterpret_cast<const x8 *>(row + 32 * s);
+        }
+#pragma unroll
+        for (int d = 0; d < DH / 16; ++d) v[d] = *reinterpret_cast<const x8 *>(vb + (16 * d + i) * P + 8 * g);
+    }
+    static __device__ __forceinline__ f32x4 mfma(x8 a, x8 b, f32x4 c) {
+        if constexpr (sizeof(T) == 2 && __is_same(T, bf16_t)) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+    __device__ __forceinline__ void scores(float *z) const {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < DH / 32; ++s) c = mfma(k[t][s], q[s], c);
+            for (int r = 0; r < 4; ++r) z[4 * t + r] = c[r];
+        }
+    }
+    __device__ __forceinline__ void clear_beyond(int n) {        // what lies behind the length may be anything
+#pragma unroll
+        for (int d = 0; d < DH / 16; ++d)
+            for (int j = 0; j < 8; ++j) if (slot_of(j) >= n) v[d][j] = (T)0.f;
+    }
+    // A probability enters as the sum of two 16-bit numbers: rounded once to 8 bits (bf16) it alone would be off by more than the result's half step.
+    __device__ __forceinline__ void add_values(const float *p, f32x4 *o) const {
+        x8 hi, lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { hi[j] = (T)p[j]; lo[j] = (T)(p[j] - (float)hi[j]); }
+#pragma unroll
+        for (int d = 0; d < DH / 16; ++d) { o[d] = mfma(v[d], hi, o[d]); o[d] = mfma(v[d], lo, o[d]); }
+    }
+};
+// float32: the instruction of four products deep; slot 4g + r (r < 4) and 16 + 4g + r.
+template <int DH> struct Tile<float, DH> {
+    f32x4 q[DH / 16], k[2][DH / 16], v[2][DH / 16];
+    static __device__ __forceinline__ int slot_of(int j) { return 16 * (j >> 2) + 4 * ((threadIdx.x & 63) >> 4) + (j & 3); }
+    __device__ __forceinline__ void load_q(const float *row, bool there) {
+        const int g = (threadIdx.x & 63) >> 4;
+        for (int s = 0; s < DH / 16; ++s) q[s] = there ? *reinterpret_cast<const f32x4 *>(row + 16 * s + 4 * g) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ void load(const float *kb, const float *vb, int P) {
+        const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int s = 0; s < DH / 16; ++s) k[t][s] = *reinterpret_cast<const f32x4 *>(kb + (16 * t + i) * DH + 16 * s + 4 * g);
+#pragma unroll
+            for (int d = 0; d < DH / 16; ++d) v[t][d] = *reinterpret_cast<const f32x4 *>(vb + (16 * d + i) * P + 16 * t + 4 * g);
+        }
+    }
+    __device__ __forceinline__ void scores(float *z) const {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < DH / 16; ++s)
+                for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][s][j], q[s][j], c, 0, 0, 0);
+            for (int r = 0; r < 4; ++r) z[4 * t + r] = c[r];
+        }
+    }
+    __device__ __forceinline__ void clear_beyond(int n) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            for (int d = 0; d < DH / 16; ++d)
+                for (int r = 0; r < 4; ++r) if (slot_of(4 * t + r) >= n) v[t][d][r] = 0.f;
+    }
+    __device__ __forceinline__ void add_values(const float *p, f32x4 *o) const {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int d = 0; d < DH / 16; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][d][r], p[4 * t + r], o[d], 0, 0, 0);
+    }
+};
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+// 2^(m - to) for a running maximum that may be -infinity (nothing yet: 0).
+__device__ __forceinline__ float back_by(float m, float to) { return m == -INFINITY ? 0.f : exp2_of(m - to); }
+
+template <typename T, int DH, bool WEIGHED>
+__global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, AttendArgs a) {
+    constexpr int ROW = DH + 4;
+    __shared__ float lds_o[ATT_WAVES * 16 * ROW];
+    __shared__ float2 lds_ml[ATT_WAVES][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g4 = lane >> 4;
+    const int w = blockIdx.x, hk = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles;
+    const int group = a.hq / c.hkv, head0 = hk * group + tile * 16, heads = min(16, group - tile * 16);
+    const T *ks = static_cast<const T *>(c.k), *vs = static_cast<const T *>(c.v), *qs = static_cast<const T *>(a.q);
+    T *out = static_cast<T *>(a.out);
+    const int P = 1 << c.shift;
+    // rows without a block are nobody's: workgroup b % W writes row b
+    for (int b = w; b < c.n_seq; b += a.W) {
+        const int len = a.lengths[b];
+        if (row_blocks(len, a.max_len)) continue;
+        for (int i = threadIdx.x; i < heads * DH; i += 64 * ATT_WAVES) out[b * a.out_row + (int64_t)head0 * DH + i] = from_f<T>(len > 0 ? NAN : 0.f);
+        if ((int)threadIdx.x < heads && a.lse) a.lse[(int64_t)b * a.hq + head0 + threadIdx.x] = len > 0 ? NAN : -INFINITY;
+    }
+    int64_t all, none;
+    count_blocks(a.lengths, c.n_seq, a.max_len, 0, all, none);
+    const int64_t parts = attend_parts(all, a.W);
+    if (w >= parts) return;
+    int64_t at = all * w / parts;
+    const int64_t end = all * (w + 1) / parts;
+    int b; int64_t first;
+    find_row(a.lengths, c.n_seq, a.max_len, at, b, first);
+    const float scale = a.scale * LOG2E;
+    Tile<T, DH> t;
+    while (at < end) {
+        const int len = a.lengths[b], blocks = row_blocks(len, a.max_len);
+        if (at >= first + blocks) { first += blocks; ++b; continue; }          // (an empty row)
+        const int i0 = (int)(at - first), i1 = (int)(first + blocks < end ? blocks : end - first);
+        t.load_q(qs + b * a.q_row + (int64_t)(head0 + col) * DH, col < heads);
+        float m = -INFINITY, l = 0.f;
+        f32x4 o[DH / 16];
+        for (int d = 0; d < DH / 16; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int32_t *table = c.table + (int64_t)b * c.table_stride;
+        float *score = WEIGHED ? a.scores + ((int64_t)b * a.hq + head0 + col) * a.score_row : nullptr;
+        // this wave's blocks: every fourth; the pages of 64 of them are looked up at once
+        for (int i64 = i0 + wave; i64 < i1; i64 += 64 * ATT_WAVES) {
+            const int mine = i64 + lane * ATT_WAVES;
+            const int looked = mine < i1 ? table[(mine * ATT_BLOCK) >> c.shift] : 0;
+            for (int j = 0; j < 64 && i64 + j * ATT_WAVES < i1; ++j) {
+                const int i = i64 + j * ATT_WAVES, s0 = i * ATT_BLOCK;
+                int page = __builtin_amdgcn_readlane(looked, j);
+                const bool there = (unsigned)page < (unsigned)c.n_pages;
+                page = there ? page : 0;
+                const int off = s0 & (P - 1);
+                t.load(ks + page * c.k_page + ((int64_t)(hk << c.shift) + off) * DH, vs + page * c.v_page + ((int64_t)(hk * DH) << c.shift) + off, P);
+                float z[8];
+                t.scores(z);
+                const int live = len - s0;
+                float top = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    z[x] = !there ? NAN : t.slot_of(x) < live ? z[x] * scale : -INFINITY;
+                    top = fmaxf(top, z[x]);
+                }
+                if (live < ATT_BLOCK) t.clear_beyond(live);
+                if constexpr (WEIGHED) {
+                    if (col < heads)
+#pragma unroll
+                        for (int x = 0; x < 8; x += 4) *reinterpret_cast<f32x4 *>(score + s0 + t.slot_of(x)) = f32x4{z[x], z[x + 1], z[x + 2], z[x + 3]};
+                }
+                top = rows_max(top);
+                if (__any(top > m)) {
+                    const float now = fmaxf(m, top), back = back_by(m, now);
+                    m = now;
+                    l *= back;
+#pragma unroll
+                    for (int d = 0; d < DH / 16; ++d) o[d] *= back;
+                }
+                const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) { z[x] = exp2_of(z[x] - ref); l += z[x]; }
+                t.add_values(z, o);
+            }
+        }
+        // the four waves' triples become one
+        {
+            float x, y;
+            swap16(l, x, y); l = x + y;
+            swap32(l, x, y); l = x + y;
+        }
+        __syncthreads();
+        if (g4 == 0) lds_ml[wave][col] = make_float2(m, l);
+        if (col < heads)
+#pragma unroll
+            for (int d = 0; d < DH / 16; ++d) *reinterpret_cast<f32x4 *>(&lds_o[(wave * 16 + col) * ROW + 16 * d + 4 * g4]) = o[d];
+        __syncthreads();
+        const bool starts = i0 == 0, ends = i1 == blocks;
+        const int64_t slot = (int64_t)(2 * w + (starts ? 1 : 0)) * c.hkv * a.tiles + blockIdx.y;
+        for (int x = threadIdx.x; x < heads * (DH / 4); x += 64 * ATT_WAVES) {
+            const int h = x / (DH / 4), d = x % (DH / 4) * 4;
+            float top = -INFINITY;
+            for (int v = 0; v < ATT_WAVES; ++v) top = fmaxf(top, lds_ml[v][h].x);
+            float sum = 0.f;
+            f32x4 r = {0.f, 0.f, 0.f, 0.f};
+            for (int v = 0; v < ATT_WAVES; ++v) {
+                const float f = back_by(lds_ml[v][h].x, top);
+                const f32x4 ov = *reinterpret_cast<const f32x4 *>(&lds_o[(v * 16 + h) * ROW + d]);
+                sum += lds_ml[v][h].y * f;                 // (a wave that saw nothing adds 0, one that saw only NaN shows it: 0 * NaN)
+                r += ov * f;
+            }
+            if (starts && ends) {
+                const float inv = 1.f / sum;
+                T *to = out + b * a.out_row + (int64_t)(head0 + h) * DH + d;
+                for (int e = 0; e < 4; ++e) to[e] = from_f<T>(r[e] * inv);
+                if (d == 0) {
+                    const float lse2 = top + __builtin_amdgcn_logf(sum);
+                    if (a.lse) a.lse[(int64_t)b * a.hq + head0 + h] = lse2 * LN2;
+                    if (WEIGHED) a.row_lse[(int64_t)b * a.hq + head0 + h] = lse2;
+                }
+            } else {
+                *reinterpret_cast<f32x4 *>(a.part + (slot * 16 + h) * DH + d) = r;
+                if (d == 0) a.part_ml[slot * 16 + h] = make_float2(top, sum);
+            }
+        }
+        at = first + i1;
+    }
+}
+
+// Joins the pieces of the rows that lie in several workgroups: a workgroup per row and query head.
+template <typename T>
+__global__ void __launch_bounds__(256) attend_join_kernel(KvView c, AttendArgs a, int dh) {
+    const int h = blockIdx.x, b = blockIdx.y, group = a.hq / c.hkv, hk = h / group, tile = h % group / 16, in_tile = h % group % 16;
+    const int blocks = row_blocks(a.lengths[b], a.max_len);
+    if (!blocks) return;
+    int64_t all, first;
+    count_blocks(a.lengths, c.n_seq, a.max_len, b, all, first);
+    const int64_t parts = attend_parts(all, a.W);
+    const int w0 = (int)(((first + 1) * parts - 1) / all), w1 = (int)(((first + blocks) * parts - 1) / all);
+    if (w0 == w1) return;
+    const int64_t per = (int64_t)c.hkv * a.tiles, at = (int64_t)hk * a.tiles + tile;
+    auto slot = [&](int w) { return ((2 * w + (w == w0 ? 1 : 0)) * per + at) * 16 + in_tile; };
+    float top = -INFINITY;
+    for (int w = w0; w <= w1; ++w) top = fmaxf(top, a.part_ml[slot(w)].x);
+    const int d = threadIdx.x;
+    float sum = 0.f, r = 0.f;
+    for (int w = w0; w <= w1; ++w) {
+        const float2 ml = a.part_ml[slot(w)];
+        const float f = back_by(ml.x, top);
+        sum += ml.y * f;
+        if (d < dh) r += a.part[slot(w) * dh + d] * f;
+    }
+    if (d < dh) static_cast<T *>(a.out)[b * a.out_row + (int64_t)h * dh + d] = from_f<T>(r / sum);
+    if (d == 0) {
+        const float lse2 = top + __builtin_amdgcn_logf(sum);
+        if (a.lse) a.lse[(int64_t)b * a.hq + h] = lse2 * LN2;
+        if (a.row_lse) a.row_lse[(int64_t)b * a.hq + h] = lse2;
     }
 }
 
 __global__ void __launch_bounds__(256) attend_weights_kernel(KvView c, AttendArgs a) {
     const int hk = blockIdx.y, b = blockIdx.z, s = blockIdx.x * 256 + threadIdx.x, g = a.hq / c.hkv;
-    const int len = min(a.lengths[b], a.max_len);
+    const int len = a.lengths[b] > a.max_len ? 0 : a.lengths[b];
     if (s >= len) return;
     const int64_t at = ((int64_t)b * c.hkv + hk) * c.slots + s;
     float w = 0.f;
     for (int j = 0; j < g; ++j) {
         const int64_t row = (int64_t)b * a.hq + hk * g + j;
-        w += expf(a.scores[row * a.max_len + s] - a.row_lse[row]);
+        w += exp2_of(a.scores[row * a.score_row + s] - a.row_lse[row]);
     }
     a.weights_out[at] = (a.weights ? a.weights[at] : 0.f) + w;
 }
 
-static size_t attend_scores_bytes(const KvView &c, int hq, int max_len) { return (size_t)c.n_seq * hq * max_len * 4; }
+// How a call runs: workgroups along the slots, and its scratch.
+struct AttendPlan { int tiles, W; int64_t score_row; size_t part, part_ml, row_lse, scores, bytes; };
+static AttendPlan attend_plan(const KvView &c, int hq, int max_len, bool weighed) {
+    AttendPlan p{};
+    p.tiles = (hq / c.hkv + 15) / 16;
+    const int64_t per = (int64_t)c.hkv * p.tiles, blocks = (int64_t)c.n_seq * ((max_len + ATT_BLOCK - 1) / ATT_BLOCK);
+    int64_t W = (512 + per - 1) / per;
+    if (W > (blocks + ATT_LEAST - 1) / ATT_LEAST) W = (blocks + ATT_LEAST - 1) / ATT_LEAST;
+    p.W = W < 1 ? 1 : (int)W;
+    p.score_row = (max_len + ATT_BLOCK - 1) / ATT_BLOCK * ATT_BLOCK;
+    auto take = [&](size_t n) { const size_t at = p.bytes; p.bytes += (n + 255) / 256 * 256; return at; };
+    if (p.W > 1) {
+        p.part = take((size_t)2 * p.W * per * 16 * c.dh * 4);
+        p.part_ml = take((size_t)2 * p.W * per * 16 * 8);
+    }
+    if (weighed) {
+        p.row_lse = take((size_t)c.n_seq * hq * 4);
+        p.scores = take((size_t)c.n_seq * hq * p.score_row * 4);
+    }
+    if (p.bytes == 0) p.bytes = 256;
+    return p;
+}
+
+template <typename T, int DH>
+static void launch_attend(const KvView &c, const AttendArgs &a, bool weighed, hipStream_t st) {
+    const dim3 grid(a.W, c.hkv * a.tiles);
+    if (weighed) attend_kernel<T, DH, true><<<grid, 64 * ATT_WAVES, 0, st>>>(c, a);
+    else attend_kernel<T, DH, false><<<grid, 64 * ATT_WAVES, 0, st>>>(c, a);
+}
+template <typename T>
+static void launch_attend_t(const KvView &c, const AttendArgs &a, bool weighed, hipStream_t st) {
+    switch (c.dh) {
+        case 32: launch_attend<T, 32>(c, a, weighed, st); break;
+        case 64: launch_attend<T, 64>(c, a, weighed, st); break;
+        case 96: launch_attend<T, 96>(c, a, weighed, st); break;
+        case 128: launch_attend<T, 128>(c, a, weighed, st); break;
+        case 160: launch_attend<T, 160>(c, a, weighed, st); break;
+        case 192: launch_attend<T, 192>(c, a, weighed, st); break;
+        case 224: launch_attend<T, 224>(c, a, weighed, st); break;
+        default: launch_attend<T, 256>(c, a, weighed, st); break;
+    }
+    if (a.W > 1) attend_join_kernel<T><<<dim3(a.hq, c.n_seq), 256, 0, st>>>(c, a, c.dh);
+    if (weighed) attend_weights_kernel<<<dim3((a.max_len + 255) / 256, c.hkv, c.n_seq), 256, 0, st>>>(c, a);
+}
 
 }  // namespace poss
 
@@ -97,15 +400,12 @@ const char *attend_bad(const poss_kv_cache *c, int32_t hq, int32_t max_len) {
     if (attend_max_len(*c, max_len) < 0) return "max_len is more than the slots";
     return nullptr;
 }
-size_t attend_scratch(const poss_kv_cache &c, int32_t hq, int max_len, bool weighed) {
-    return 256 + (weighed ? attend_scores_bytes(kv_view(c), hq, max_len) + (size_t)c.n_seq * hq * 4 : 0);
-}
 }  // namespace
 
 extern "C" {
 
 size_t poss_kv_attend_scratch_bytes(const poss_kv_cache *cache, int32_t n_q_heads, int32_t max_len, int32_t weighed) {
-    return attend_bad(cache, n_q_heads, max_len) ? 0 : attend_scratch(*cache, n_q_heads, attend_max_len(*cache, max_len), weighed != 0);
+    return attend_bad(cache, n_q_heads, max_len) ? 0 : attend_plan(kv_view(*cache), n_q_heads, attend_max_len(*cache, max_len), weighed != 0).bytes;
 }
 
 int poss_kv_attend(const poss_kv_cache *cache, int32_t n_q_heads, const void *q, int64_t q_row, void *out, int64_t out_row, const int32_t *lengths, int32_t max_len, float scale,
@@ -121,21 +421,19 @@ int poss_kv_attend(const poss_kv_cache *cache, int32_t n_q_heads, const void *q,
     if (cache->n_seq > 1 && (q_row < row || out_row < row)) return set_error(POSS_E_INVALID_ARG, "%s: rows overlap", who);
     if (!kv_aligned(lengths, 4) || !kv_aligned(lse, 4) || !kv_aligned(weights, 4) || !kv_aligned(weights_out, 4)) return set_error(POSS_E_INVALID_ARG, "%s: an array is not aligned to its type", who);
     if (!kv_aligned(scratch, 256)) return set_error(POSS_E_INVALID_ARG, "%s: scratch must be aligned to 256 bytes", who);
-    const int most = attend_max_len(*cache, max_len);
-    const size_t need = attend_scratch(*cache, n_q_heads, most, weights_out != nullptr);
-    if (scratch_bytes < need) return set_error(POSS_E_CAPACITY, "%s: needs %zu bytes of scratch, got %zu", who, need, scratch_bytes);
-    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const KvView c = kv_view(*cache);
-    AttendArgs a{n_q_heads, q, q_row, out, out_row, lengths, most, scale, lse, weights, weights_out, nullptr, nullptr};
-    if (weights_out) {
-        a.row_lse = static_cast<float *>(scratch);
-        a.scores = a.row_lse + (size_t)c.n_seq * n_q_heads;
-    }
-    const dim3 grid(n_q_heads, c.n_seq);
-    if (cache->dtype == DT_F32) attend_kernel<float><<<grid, 256, 0, st>>>(c, a);
-    else if (cache->dtype == DT_BF16) attend_kernel<bf16_t><<<grid, 256, 0, st>>>(c, a);
-    else attend_kernel<f16_t><<<grid, 256, 0, st>>>(c, a);
-    if (weights_out) attend_weights_kernel<<<dim3((most + 255) / 256, c.hkv, c.n_seq), 256, 0, st>>>(c, a);
+    const int most = attend_max_len(*cache, max_len);
+    const bool weighed = weights_out != nullptr;
+    const AttendPlan p = attend_plan(c, n_q_heads, most, weighed);
+    if (scratch_bytes < p.bytes) return set_error(POSS_E_CAPACITY, "%s: needs %zu bytes of scratch, got %zu", who, p.bytes, scratch_bytes);
+    char *base = static_cast<char *>(scratch);
+    AttendArgs a{n_q_heads, p.tiles, q, q_row, out, out_row, lengths, most, scale, lse, weights, weights_out, p.W, reinterpret_cast<float *>(base + p.part),
+                 reinterpret_cast<float2 *>(base + p.part_ml), weighed ? reinterpret_cast<float *>(base + p.scores) : nullptr, p.score_row,
+                 weighed ? reinterpret_cast<float *>(base + p.row_lse) : nullptr};
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (cache->dtype == DT_F32) launch_attend_t<float>(c, a, weighed, st);
+    else if (cache->dtype == DT_BF16) launch_attend_t<bf16_t>(c, a, weighed, st);
+    else launch_attend_t<f16_t>(c, a, weighed, st);
     return kv_launched(who);
 }
 
