@@ -18,7 +18,7 @@ typedef f16_t  f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int ATT_BLOCK = 32;                 // slots of a block: never across pages
 constexpr int ATT_WAVES = 4;
-constexpr int ATT_LEAST = 8;
+constexpr int ATT_LEAST = 8, ATT_MOST = 512;   // blocks of a workgroup, workgroups along the slots
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct AttendArgs {
@@ -30,7 +30,7 @@ struct AttendArgs {
     float *part;          // [2 W][hkv * tiles][16][dh]
     float2 *part_ml;      // [2 W][hkv * tiles][16]
     float *scores; int64_t score_row;   // [n_seq][hq][score_row], log2 domain
-    float *row_lse;       // [n_seq][hq], log2 domain
+    float *row_lse;       // [n_seq][hq], log2 domain: of rows that lie in one workgroup
 };
 
 // Blocks of a row; one whose length is beyond the bound has none and is NaN.
@@ -294,48 +294,95 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, Attend
     }
 }
 
-// Joins the pieces of the rows that lie in several workgroups: a workgroup per row and query head.
+// What is left once every piece of every row is there.  A row's pieces lie in workgroups w0 .. w1; a workgroup per row and query head joins them, and one per 1024 slots
+// of a row and key head gives the slots their weights: 2^(score - lse), summed over the heads that share the key head.  The latter form a head's lse
+// from its pieces' maxima and sums by themselves, so that one launch does both (131072 slots in 64 pieces a head: 62 us with a thread
+// per value that walks the pieces one after the other, 5 with all of them asked for at once).
+constexpr int FINISH_SLOTS = 1024, FINISH_HEADS = 64;
+
 template <typename T>
-__global__ void __launch_bounds__(256) attend_join_kernel(KvView c, AttendArgs a, int dh) {
-    const int h = blockIdx.x, b = blockIdx.y, group = a.hq / c.hkv, hk = h / group, tile = h % group / 16, in_tile = h % group % 16;
-    const int blocks = row_blocks(a.lengths[b], a.max_len);
+__global__ void __launch_bounds__(256) attend_finish_kernel(KvView c, AttendArgs a, int joins) {
+    __shared__ float factor[ATT_MOST];
+    __shared__ f32x4 sums[256];
+    __shared__ float red[17];
+    const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x, group = a.hq / c.hkv, dh = c.dh;
+    const int len = a.lengths[b], blocks = row_blocks(len, a.max_len);
     if (!blocks) return;
+    const int chunk = (int)blockIdx.x - joins;
+    if (chunk >= 0 && chunk * FINISH_SLOTS >= len) return;
     int64_t all, first;
     count_blocks(a.lengths, c.n_seq, a.max_len, b, all, first);
     const int64_t parts = attend_parts(all, a.W);
-    const int w0 = (int)(((first + 1) * parts - 1) / all), w1 = (int)(((first + blocks) * parts - 1) / all);
-    if (w0 == w1) return;
-    const int64_t per = (int64_t)c.hkv * a.tiles, at = (int64_t)hk * a.tiles + tile;
-    auto slot = [&](int w) { return ((2 * w + (w == w0 ? 1 : 0)) * per + at) * 16 + in_tile; };
-    float top = -INFINITY;
-    for (int w = w0; w <= w1; ++w) top = fmaxf(top, a.part_ml[slot(w)].x);
-    const int d = threadIdx.x;
-    float sum = 0.f, r = 0.f;
-    for (int w = w0; w <= w1; ++w) {
-        const float2 ml = a.part_ml[slot(w)];
-        const float f = back_by(ml.x, top);
-        sum += ml.y * f;
-        if (d < dh) r += a.part[slot(w) * dh + d] * f;
+    const int w0 = (int)(((first + 1) * parts - 1) / all), n = (int)(((first + blocks) * parts - 1) / all) - w0 + 1;
+    // piece p of the head of this group's index j
+    auto slot = [&](int p, int j) { return ((int64_t)(2 * (w0 + p) + (p == 0 ? 1 : 0)) * c.hkv * a.tiles + hk * a.tiles + j / 16) * 16 + j % 16; };
+    if (chunk < 0) {
+        if (n == 1) return;
+        const int j = blockIdx.x;
+        float2 ml = make_float2(-INFINITY, 0.f), other = ml;
+        if (tid < n) ml = a.part_ml[slot(tid, j)];
+        if (tid + 256 < n) other = a.part_ml[slot(tid + 256, j)];
+        float top = wave_max(fmaxf(ml.x, other.x));
+        if ((tid & 63) == 0) red[tid >> 6] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        const float f = back_by(ml.x, top), fo = back_by(other.x, top);
+        factor[tid] = f;
+        if (tid + 256 < ATT_MOST) factor[tid + 256] = fo;
+        const float sum = block_sum(ml.y * f + other.y * fo, red);      // (its barriers stand between the factors' writes and reads)
+        // a thread adds four values of every (256 / quads)-th piece
+        const int quads = dh / 4, ways = 256 / quads, way = tid / quads, d = tid % quads * 4;
+        f32x4 r = {0.f, 0.f, 0.f, 0.f};
+        if (way < ways) {
+#pragma unroll 8
+            for (int p = way; p < n; p += ways) r += *reinterpret_cast<const f32x4 *>(a.part + slot(p, j) * dh + d) * factor[p];
+        }
+        sums[tid] = r;
+        __syncthreads();
+        if (way == 0) {
+            for (int v = 1; v < ways; ++v) r += sums[v * quads + tid];
+            const float inv = 1.f / sum;
+            T *to = static_cast<T *>(a.out) + b * a.out_row + (int64_t)(hk * group + j) * dh + d;
+            for (int e = 0; e < 4; ++e) to[e] = from_f<T>(r[e] * inv);
+        }
+        if (tid == 0 && a.lse) a.lse[(int64_t)b * a.hq + hk * group + j] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+        return;
     }
-    if (d < dh) static_cast<T *>(a.out)[b * a.out_row + (int64_t)h * dh + d] = from_f<T>(r / sum);
-    if (d == 0) {
-        const float lse2 = top + __builtin_amdgcn_logf(sum);
-        if (a.lse) a.lse[(int64_t)b * a.hq + h] = lse2 * LN2;
-        if (a.row_lse) a.row_lse[(int64_t)b * a.hq + h] = lse2;
+    const int s = chunk * FINISH_SLOTS + tid * 4, live = len - s;
+    f32x4 w = {0.f, 0.f, 0.f, 0.f};
+    for (int j0 = 0; j0 < group; j0 += FINISH_HEADS) {
+        const int heads = min(FINISH_HEADS, group - j0);
+        __syncthreads();
+        for (int j = tid >> 6; j < heads; j += 4) {        // a wave per head: its lse in `factor`
+            float lse;
+            if (n == 1) lse = a.row_lse[(int64_t)b * a.hq + hk * group + j0 + j];
+            else {
+                float top = -INFINITY, sum = 0.f;
+                for (int p = tid & 63; p < n; p += 64) top = fmaxf(top, a.part_ml[slot(p, j0 + j)].x);
+                top = wave_max(top);
+                for (int p = tid & 63; p < n; p += 64) { const float2 ml = a.part_ml[slot(p, j0 + j)]; sum += ml.y * back_by(ml.x, top); }
+                lse = top + __builtin_amdgcn_logf(wave_sum(sum));
+            }
+            if ((tid & 63) == 0) factor[j] = lse;
+        }
+        __syncthreads();
+        if (live > 0) {
+            const float *row = a.scores + ((int64_t)b * a.hq + hk * group + j0) * a.score_row + s;
+#pragma unroll 4
+            for (int j = 0; j < heads; ++j) {
+                const f32x4 z = *reinterpret_cast<const f32x4 *>(row + j * a.score_row);
+                for (int e = 0; e < 4; ++e) w[e] += exp2_of(z[e] - factor[j]);
+            }
+        }
     }
-}
-
-__global__ void __launch_bounds__(256) attend_weights_kernel(KvView c, AttendArgs a) {
-    const int hk = blockIdx.y, b = blockIdx.z, s = blockIdx.x * 256 + threadIdx.x, g = a.hq / c.hkv;
-    const int len = a.lengths[b] > a.max_len ? 0 : a.lengths[b];
-    if (s >= len) return;
+    if (live <= 0) return;
     const int64_t at = ((int64_t)b * c.hkv + hk) * c.slots + s;
-    float w = 0.f;
-    for (int j = 0; j < g; ++j) {
-        const int64_t row = (int64_t)b * a.hq + hk * g + j;
-        w += exp2_of(a.scores[row * a.score_row + s] - a.row_lse[row]);
+    if (live >= 4 && (reinterpret_cast<uintptr_t>(a.weights) | reinterpret_cast<uintptr_t>(a.weights_out)) % 16 == 0) {
+        if (a.weights) w += *reinterpret_cast<const f32x4 *>(a.weights + at);
+        *reinterpret_cast<f32x4 *>(a.weights_out + at) = w;
+        return;
     }
-    a.weights_out[at] = (a.weights ? a.weights[at] : 0.f) + w;
+    for (int e = 0; e < min(4, live); ++e) a.weights_out[at + e] = (a.weights ? a.weights[at + e] : 0.f) + w[e];
 }
 
 // How a call runs: workgroups along the slots, and its scratch.
@@ -344,7 +391,9 @@ static AttendPlan attend_plan(const KvView &c, int hq, int max_len, bool weighed
     AttendPlan p{};
     p.tiles = (hq / c.hkv + 15) / 16;
     const int64_t per = (int64_t)c.hkv * p.tiles, blocks = (int64_t)c.n_seq * ((max_len + ATT_BLOCK - 1) / ATT_BLOCK);
-    int64_t W = (512 + per - 1) / per;
+    // Two workgroups a CU, the registers' limit, and never more: a third round of a few costs as much as a whole one (40 key heads, 16 rows: 94 us with 13 x 40
+    // workgroups, 74 with 12 x 40).
+    int64_t W = ATT_MOST / per;
     if (W > (blocks + ATT_LEAST - 1) / ATT_LEAST) W = (blocks + ATT_LEAST - 1) / ATT_LEAST;
     p.W = W < 1 ? 1 : (int)W;
     p.score_row = (max_len + ATT_BLOCK - 1) / ATT_BLOCK * ATT_BLOCK;
@@ -379,8 +428,8 @@ static void launch_attend_t(const KvView &c, const AttendArgs &a, bool weighed, 
         case 224: launch_attend<T, 224>(c, a, weighed, st); break;
         default: launch_attend<T, 256>(c, a, weighed, st); break;
     }
-    if (a.W > 1) attend_join_kernel<T><<<dim3(a.hq, c.n_seq), 256, 0, st>>>(c, a, c.dh);
-    if (weighed) attend_weights_kernel<<<dim3((a.max_len + 255) / 256, c.hkv, c.n_seq), 256, 0, st>>>(c, a);
+    const int joins = a.W > 1 ? a.hq / c.hkv : 0, chunks = weighed ? (a.max_len + FINISH_SLOTS - 1) / FINISH_SLOTS : 0;
+    if (joins + chunks) attend_finish_kernel<T><<<dim3(joins + chunks, c.hkv, c.n_seq), 256, 0, st>>>(c, a, joins);
 }
 
 }  // namespace poss
