@@ -451,7 +451,7 @@ int poss_kv_evict(const poss_kv_cache *cache, const float *weights, const int32_
 
 /* Log-probabilities under softmax(x / temperature) for x[rows][vocab] of `dtype`, rows ldx values apart: logp[rows][n_tokens] of tokens[rows][n_tokens] (int32; one
  * outside the vocabulary gets NaN), entropy[rows] (may be NULL), and of the n_top largest logits of a row, equal ones by the lowest id,
- * ids and log-probabilities, top_ids and top_logp [rows][n_top].  n_tokens may be 0, n_top is at most POSS_LOGPROBS_TOP and vocab.  Logits of -infinity have
+ * ids and log-probabilities, top_ids and top_logp [rows][n_top].  At most 2^23 rows and 2^30 ids; n_tokens may be 0, n_top is at most POSS_LOGPROBS_TOP and vocab.  Logits of -infinity have
  * no probability; a row with a NaN or +infinity, or nothing above -infinity, has NaN for all but its ids, among which NaN come last.
  * Outputs float32, all arrays DEVICE.  scratch: as for poss_kv_attend (0 bytes needed: a bad shape). */
 #define POSS_LOGPROBS_TOP 32

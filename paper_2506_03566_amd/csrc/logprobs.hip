@@ -6,55 +6,262 @@
 
 namespace poss {
 
-// One workgroup per row: a pass for the maximum, one for the sums, one for each alternative.
+constexpr float LOG2_E = 1.4426950408889634f;
+
+// A row is read once, by one workgroup or by several that share it; each thread keeps the maximum of what it has seen, S and sum(e^d d) relative to it.
+//
+// The best n of a row as 64-bit numbers, larger is better: the value, mapped so that unsigned order is the order of the numbers (NaN 0, -0 as 0), above the
+// complement of its id.  A tile's values that can still be among them go to a list in LDS: those above the n-th best so far (tiles ascend, so an equal value loses by its
+// id); at first, those from the n-th largest of the threads' maxima on, which is no more than the n-th best.  A list too long for another tile is
+// cut to its n best.  Random rows put a few dozen values there, a rising row every one of them.
+typedef unsigned long long Best;
+
+__device__ __forceinline__ Best best_of(float v, int id) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.f), key = v != v ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
+    return (Best)key << 32 | (uint32_t)~id;
+}
+__device__ __forceinline__ int best_id(Best b) { return (int)~(uint32_t)b; }
+__device__ __forceinline__ float best_value(Best b) {
+    const uint32_t key = (uint32_t)(b >> 32);
+    return key == 0 ? NAN : __builtin_bit_cast(float, key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
+
+// m: the largest logit seen (-infinity: none), s: sum 2^((x - m) c), t: sum of the same times (x - m) c;  c = log2(e) / temperature.
+struct Sums { float m, s, t; };
+
+__device__ __forceinline__ Sums add_sums(Sums a, Sums b, float c) {
+    const float m = fmaxf(a.m, b.m);
+    Sums r = {m, 0.f, 0.f};
+    if (a.m != -INFINITY || a.s != a.s) { const float d = fmaxf((a.m - m) * c, -1e4f), f = __builtin_amdgcn_exp2f((a.m - m) * c); r.s += a.s * f; r.t += (a.t + a.s * d) * f; }
+    if (b.m != -INFINITY || b.s != b.s) { const float d = fmaxf((b.m - m) * c, -1e4f), f = __builtin_amdgcn_exp2f((b.m - m) * c); r.s += b.s * f; r.t += (b.t + b.s * d) * f; }
+    return r;
+}
+__device__ __forceinline__ Sums wave_sums(Sums a, float c) {
+    for (int o = 32; o; o >>= 1) a = add_sums(a, Sums{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)}, c);
+    return a;
+}
+
+constexpr int LP_THREADS = 256, LP_PER = 16, LP_TILE = LP_THREADS * LP_PER, LP_SPARE = 512, LP_MOST_PARTS = 64;
+
+// The n best of list[0 .. count) to the front, in order; the rest of the first n are 0.  All threads; barriers on both sides.
+__device__ __forceinline__ void keep_best(Best *list, int count, int n, Best *room /* POSS_LOGPROBS_TOP + 8 */) {
+    const int tid = threadIdx.x;
+    __syncthreads();
+    if (count <= LP_THREADS) {                             // a thread per number: how many are better
+        const Best mine = tid < count ? list[tid] : 0;
+        int rank = 0;
+        for (int i = 0; i < count; ++i) rank += list[i] > mine;
+        if (tid < n) room[tid] = 0;
+        __syncthreads();
+        if (tid < count && rank < n) room[rank] = mine;
+    } else {
+        Best last = ~0ull;
+        for (int j = 0; j < n; ++j) {
+            Best top = 0;
+            for (int i = tid; i < count; i += LP_THREADS) { const Best b = list[i]; if (b < last && b > top) top = b; }
+            for (int o = 32; o; o >>= 1) { const Best b = __shfl_xor(top, o); if (b > top) top = b; }
+            if ((tid & 63) == 0) room[POSS_LOGPROBS_TOP + (j & 1) * 4 + (tid >> 6)] = top;
+            __syncthreads();
+            for (int v = 0; v < 4; ++v) { const Best b = room[POSS_LOGPROBS_TOP + (j & 1) * 4 + v]; if (b > top) top = b; }
+            last = top;
+            if (tid == 0) room[j] = top;
+        }
+    }
+    __syncthreads();
+    if (tid < n) list[tid] = room[tid];
+    __syncthreads();
+}
+// The n-th largest of the threads' numbers (n <= 256), in every thread.
+__device__ __forceinline__ float nth_of_threads(float v, int n, float *all /* LP_THREADS + 1 */) {
+    __syncthreads();
+    all[threadIdx.x] = v;
+    __syncthreads();
+    int above = 0, before = 0;
+    for (int i = 0; i < LP_THREADS; ++i) { above += all[i] > v; before += all[i] == v && i < (int)threadIdx.x; }
+    if (above + before == n - 1) all[LP_THREADS] = v;
+    __syncthreads();
+    return all[LP_THREADS];
+}
+
+struct LogprobsArgs {
+    const void *x; int64_t ldx; int vocab, parts; float temperature;
+    const int32_t *tokens; int n_tokens; float *logp, *entropy;
+    int n_top; int32_t *top_ids; float *top_logp;
+    Sums *part_sums; Best *part_best;           // [rows][parts], [rows][parts][n_top]
+};
+
+// What a row's sums and best ids give.
 template <typename T>
-__global__ void __launch_bounds__(1024) logprobs_kernel(const T *x, int64_t ldx, int vocab, float temperature, const int32_t *__restrict__ tokens, int n_tokens,
-                                                        float *__restrict__ logp, float *__restrict__ entropy, int n_top, int32_t *__restrict__ top_ids, float *__restrict__ top_logp) {
-    __shared__ float red[17], red_v[17];
-    __shared__ int red_i[17];
-    const int64_t r = blockIdx.x;
-    const T *row = x + r * ldx;
-    float m = -INFINITY;
-    for (int i = threadIdx.x; i < vocab; i += 1024) m = fmaxf(m, to_f(row[i]));
-    int dummy = threadIdx.x;
-    block_argmax(m, dummy, red_v, red_i);
-    float s = 0.f, t = 0.f;
-    for (int i = threadIdx.x; i < vocab; i += 1024) {
-        const float d = (to_f(row[i]) - m) / temperature, e = expf(d);
-        s += e;
-        t += e * fmaxf(d, -1e4f);
+__device__ __forceinline__ void write_row(const LogprobsArgs &a, int64_t r, Sums q, const Best *best) {
+    const T *row = static_cast<const T *>(a.x) + r * a.ldx;
+    const float log_s = logf(q.s);                         // NaN where a logit is NaN or +infinity; -infinity, and x - m NaN, where none is above -infinity
+    if (threadIdx.x == 0 && a.entropy) a.entropy[r] = log_s - q.t * 0.6931471805599453f / q.s;
+    for (int j = threadIdx.x; j < a.n_tokens; j += LP_THREADS) {
+        const int id = a.tokens[r * a.n_tokens + j];
+        a.logp[r * a.n_tokens + j] = (unsigned)id < (unsigned)a.vocab ? (to_f(row[id]) - q.m) / a.temperature - log_s : NAN;
     }
-    s = block_sum(s, red);
-    t = block_sum(t, red);
-    const float log_s = logf(s);                           // NaN where a logit is NaN or +infinity, or none is above -infinity
-    if (entropy && threadIdx.x == 0) entropy[r] = log_s - t / s;
-    for (int j = threadIdx.x; j < n_tokens; j += 1024) {
-        const int id = tokens[r * n_tokens + j];
-        logp[r * n_tokens + j] = (unsigned)id < (unsigned)vocab ? (to_f(row[id]) - m) / temperature - log_s : NAN;
+    if ((int)threadIdx.x < a.n_top) {
+        const Best b = best[threadIdx.x];
+        a.top_ids[r * a.n_top + threadIdx.x] = best_id(b);
+        a.top_logp[r * a.n_top + threadIdx.x] = (best_value(b) - q.m) / a.temperature - log_s;
     }
-    // numbers by (value, id), then NaN by id: NaN stands as the value below -infinity, told apart by `nan`
-    float last = INFINITY; int last_id = -1; bool nans = false;
-    for (int j = 0; j < n_top; ++j) {
-        float v = -INFINITY; int id = 0x7fffffff;
-        if (!nans)
-            for (int i = threadIdx.x; i < vocab; i += 1024) {
-                const float z = to_f(row[i]);
-                if (z == z && (z < last || (z == last && i > last_id)) && better(z, i, v, id)) { v = z; id = i; }
+}
+
+// A workgroup per row and part of it.  TOP: 0 no alternatives, 1 one (each thread keeps its best), 2 up to POSS_LOGPROBS_TOP.
+template <typename T, int TOP>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
+    constexpr int E = 16 / sizeof(T), VECS = LP_PER / E;
+    typedef T vec __attribute__((ext_vector_type(E)));
+    __shared__ Best list[TOP == 2 ? LP_TILE + LP_SPARE : 1], room[POSS_LOGPROBS_TOP + 8];
+    __shared__ float all[LP_THREADS + 1];
+    __shared__ Sums waves[4];
+    __shared__ int count;
+    const int tid = threadIdx.x, part = blockIdx.x % a.parts;
+    const int64_t r = blockIdx.x / a.parts;
+    const float c = LOG2_E / a.temperature;
+    // this part's ids [lo, hi); counted from the 16-byte boundary at or before the row, so that whole pieces are aligned loads
+    const T *row = static_cast<const T *>(a.x) + r * a.ldx;
+    const int shift = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
+    const int lo = (int)((int64_t)a.vocab * part / a.parts), hi = (int)((int64_t)a.vocab * (part + 1) / a.parts);
+    const int u0 = (lo + shift) / E * E;
+    auto load = [&](int u, float *x) {                     // ids u - shift .. of this thread's pieces in the tile at u
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) {
+            const int i = u + (v * LP_THREADS + tid) * E - shift;
+            if (i >= lo && i + E <= hi) {
+                const vec p = *reinterpret_cast<const vec *>(row + i);
+                for (int e = 0; e < E; ++e) x[v * E + e] = to_f(p[e]);
+            } else
+                for (int e = 0; e < E; ++e) x[v * E + e] = i + e >= lo && i + e < hi ? to_f(row[i + e]) : -INFINITY;
+        }
+    };
+    if (tid == 0) count = 0;
+    Sums q = {-INFINITY, 0.f, 0.f};
+    float border = -INFINITY;                              // TOP 2: what a value has to exceed; NaN: any value may pass
+    Best mine = 0;                                         // TOP 1
+    float x[LP_PER];
+    for (int u = u0; u < hi + shift; u += LP_TILE) {
+        load(u, x);
+        float top = -INFINITY;                             // (of what is a number)
+#pragma unroll
+        for (int e = 0; e < LP_PER; ++e) top = fmaxf(top, x[e]);
+        const float m = fmaxf(q.m, top), ref = m == -INFINITY ? 0.f : m;
+        if (m > q.m) {
+            const Sums moved = add_sums(q, Sums{m, 0.f, 0.f}, c);
+            q = moved;
+        }
+#pragma unroll
+        for (int e = 0; e < LP_PER; ++e) {
+            const float d = (x[e] - ref) * c, p = __builtin_amdgcn_exp2f(d);
+            q.s += p;
+            q.t += p * fmaxf(d, -1e4f);
+        }
+        if constexpr (TOP == 1) {
+            if (top > best_value(mine) || mine < ((Best)0x00800000u << 32)) {
+#pragma unroll
+                for (int e = 0; e < LP_PER; ++e) {
+                    const int i = u + (e / E * LP_THREADS + tid) * E + e % E - shift;
+                    const Best b = best_of(x[e], i);
+                    if (i >= lo && i < hi && b > mine) mine = b;
+                }
             }
-        block_argmax(v, id, red_v, red_i);
-        if (id == 0x7fffffff) {
-            if (!nans) { nans = true; last_id = -1; }
-            v = 0.f;
-            for (int i = threadIdx.x; i < vocab; i += 1024)
-                if (row[i] != row[i] && i > last_id) { id = i; break; }
-            block_argmax(v, id, red_v, red_i);
         }
-        last = v; last_id = id;
-        if (threadIdx.x == 0) {
-            top_ids[r * n_top + j] = id;
-            top_logp[r * n_top + j] = (to_f(row[id]) - m) / temperature - log_s;
+        if constexpr (TOP == 2) {
+            const bool first = u == u0;
+            float from = border;
+            if (first) from = nth_of_threads(top, a.n_top, all);
+            const bool any = first ? from == -INFINITY : border != border;
+            if (any || (first ? top >= from : top > from)) {
+#pragma unroll
+                for (int e = 0; e < LP_PER; ++e) {
+                    const int i = u + (e / E * LP_THREADS + tid) * E + e % E - shift;
+                    if (i >= lo && i < hi && (any || (first ? x[e] >= from : x[e] > from))) list[atomicAdd(&count, 1)] = best_of(x[e], i);
+                }
+            }
+            __syncthreads();
+            const int n = count;
+            if (first || n > LP_SPARE || u + LP_TILE >= hi + shift) {
+                keep_best(list, n, a.n_top, room);
+                border = best_value(list[a.n_top - 1]);
+                if (tid == 0) count = a.n_top;
+            }
+            __syncthreads();
         }
     }
+    q = wave_sums(q, c);
+    if (TOP == 1) {
+        for (int o = 32; o; o >>= 1) { const Best b = __shfl_xor(mine, o); if (b > mine) mine = b; }
+        if ((tid & 63) == 0) room[tid >> 6] = mine;
+    }
+    if ((tid & 63) == 0) waves[tid >> 6] = q;
+    __syncthreads();
+    q = add_sums(add_sums(waves[0], waves[1], c), add_sums(waves[2], waves[3], c), c);
+    const Best *best = list;
+    if (TOP == 1) {
+        if (tid == 0) for (int v = 1; v < 4; ++v) if (room[v] > room[0]) room[0] = room[v];
+        best = room;
+        __syncthreads();
+    }
+    if (a.parts == 1) return write_row<T>(a, r, q, best);
+    if (tid == 0) a.part_sums[blockIdx.x] = q;
+    if (tid < a.n_top) a.part_best[(int64_t)blockIdx.x * a.n_top + tid] = best[tid];
+}
+
+// Joins a row's parts: a workgroup per row.  Of their best, those from the n-th largest of the parts' first on can be among the n best.
+template <typename T>
+__global__ void __launch_bounds__(LP_THREADS) logprobs_join_kernel(LogprobsArgs a) {
+    __shared__ Best list[LP_MOST_PARTS * POSS_LOGPROBS_TOP], room[POSS_LOGPROBS_TOP + 8];
+    __shared__ Sums joined;
+    __shared__ int count;
+    const int64_t r = blockIdx.x;
+    const int tid = threadIdx.x, n = a.n_top;
+    const float c = LOG2_E / a.temperature;
+    if (tid == 0) count = 0;
+    if (tid < 64) {
+        const Sums q = wave_sums(tid < a.parts ? a.part_sums[r * a.parts + tid] : Sums{-INFINITY, 0.f, 0.f}, c);
+        if (tid == 0) joined = q;
+    }
+    __syncthreads();
+    if (n) {
+        const Best *best = a.part_best + r * a.parts * n;
+        Best from = 0;
+        if (n <= a.parts) {
+            Best first = 0;
+            if (tid < a.parts) first = best[tid * n];
+            if (tid < a.parts) list[tid] = first;
+            __syncthreads();
+            int rank = 0;
+            for (int i = 0; i < a.parts; ++i) rank += list[i] > first || (list[i] == first && i < tid);
+            if (tid < a.parts && rank == n - 1) room[0] = first;
+            __syncthreads();
+            from = room[0];
+            __syncthreads();
+        }
+        for (int i = tid; i < a.parts * n; i += LP_THREADS) {
+            const Best b = best[i];
+            if (b >= from) list[atomicAdd(&count, 1)] = b;
+        }
+        __syncthreads();
+        keep_best(list, count, n, room);
+    }
+    write_row<T>(a, r, joined, list);
+}
+
+// Parts of a row: as many as give the chip two thousand workgroups, none of less than a tile.
+static int logprobs_parts(int rows, int vocab) {
+    int p = rows ? 2048 / rows : 1;
+    const int most = (vocab + LP_TILE - 1) / LP_TILE;
+    p = p < most ? p : most;
+    return p < 1 ? 1 : p > LP_MOST_PARTS ? LP_MOST_PARTS : p;
+}
+
+template <typename T>
+static void launch_logprobs(const LogprobsArgs &a, int rows, hipStream_t st) {
+    const unsigned grid = (unsigned)((int64_t)rows * a.parts);
+    if (a.n_top == 0) logprobs_kernel<T, 0><<<grid, LP_THREADS, 0, st>>>(a);
+    else if (a.n_top == 1) logprobs_kernel<T, 1><<<grid, LP_THREADS, 0, st>>>(a);
+    else logprobs_kernel<T, 2><<<grid, LP_THREADS, 0, st>>>(a);
+    if (a.parts > 1) logprobs_join_kernel<T><<<rows, LP_THREADS, 0, st>>>(a);
 }
 
 }  // namespace poss
@@ -63,12 +270,17 @@ __global__ void __launch_bounds__(1024) logprobs_kernel(const T *x, int64_t ldx,
 using namespace poss;
 
 namespace {
-bool logprobs_ok(int32_t rows, int32_t vocab, int32_t n_top) { return rows >= 0 && vocab >= 1 && vocab <= 1 << 30 && n_top >= 0 && n_top <= POSS_LOGPROBS_TOP && n_top <= vocab; }
+bool logprobs_ok(int32_t rows, int32_t vocab, int32_t n_top) { return rows >= 0 && rows <= 1 << 23 && vocab >= 1 && vocab <= 1 << 30 && n_top >= 0 && n_top <= POSS_LOGPROBS_TOP && n_top <= vocab; }
+size_t sums_bytes(int32_t rows, int parts) { return ((size_t)rows * parts * sizeof(Sums) + 255) / 256 * 256; }
 }  // namespace
 
 extern "C" {
 
-size_t poss_logprobs_scratch_bytes(int32_t rows, int32_t vocab, int32_t n_top) { return logprobs_ok(rows, vocab, n_top) ? 256 : 0; }
+size_t poss_logprobs_scratch_bytes(int32_t rows, int32_t vocab, int32_t n_top) {
+    if (!logprobs_ok(rows, vocab, n_top)) return 0;
+    const int parts = logprobs_parts(rows, vocab);
+    return parts == 1 ? 256 : 256 + sums_bytes(rows, parts) + (size_t)rows * parts * n_top * sizeof(Best);
+}
 
 int poss_logprobs(int32_t dtype, const void *x, int64_t ldx, int32_t rows, int32_t vocab, float temperature, const int32_t *tokens, int32_t n_tokens, float *logp, float *entropy,
                   int32_t n_top, int32_t *top_ids, float *top_logp, void *scratch, size_t scratch_bytes, void *hip_stream) {
@@ -83,9 +295,13 @@ int poss_logprobs(int32_t dtype, const void *x, int64_t ldx, int32_t rows, int32
     const size_t need = poss_logprobs_scratch_bytes(rows, vocab, n_top);
     if (scratch_bytes < need) return set_error(POSS_E_CAPACITY, "%s: rows=%d vocab=%d n_top=%d needs %zu bytes of scratch, got %zu", who, rows, vocab, n_top, need, scratch_bytes);
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-#define POSS_LOGPROBS(T) logprobs_kernel<T><<<rows, 1024, 0, st>>>(static_cast<const T *>(x), ldx, vocab, temperature, tokens, n_tokens, logp, entropy, n_top, top_ids, top_logp)
-    if (dtype == DT_F32) POSS_LOGPROBS(float); else if (dtype == DT_BF16) POSS_LOGPROBS(bf16_t); else POSS_LOGPROBS(f16_t);
-#undef POSS_LOGPROBS
+    const int parts = logprobs_parts(rows, vocab);
+    char *base = static_cast<char *>(scratch);
+    const LogprobsArgs a{x, ldx, vocab, parts, temperature, tokens, n_tokens, logp, entropy, n_top, top_ids, top_logp, reinterpret_cast<Sums *>(base),
+                         reinterpret_cast<Best *>(base + sums_bytes(rows, parts))};
+    if (dtype == DT_F32) launch_logprobs<float>(a, rows, st);
+    else if (dtype == DT_BF16) launch_logprobs<bf16_t>(a, rows, st);
+    else launch_logprobs<f16_t>(a, rows, st);
     return kv_launched(who);
 }
 
