@@ -36,12 +36,26 @@ __device__ __forceinline__ Sums add_sums(Sums a, Sums b, float c) {
     if (b.m != -INFINITY || b.s != b.s) { const float d = fmaxf((b.m - m) * c, -1e4f), f = __builtin_amdgcn_exp2f((b.m - m) * c); r.s += b.s * f; r.t += (b.t + b.s * d) * f; }
     return r;
 }
-__device__ __forceinline__ Sums wave_sums(Sums a, float c) {
-    for (int o = 32; o; o >>= 1) a = add_sums(a, Sums{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)}, c);
-    return a;
+// The sums of all threads (first WAVES waves of a workgroup), to every thread: all brought to the largest maximum, then added.
+template <int WAVES>
+__device__ __forceinline__ Sums block_sums(Sums q, float c, float *red /* 3 * WAVES */) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto all = [&](float v, float *at, bool largest) {
+        v = largest ? wave_max(v) : wave_sum(v);
+        if constexpr (WAVES > 1) {
+            if (lane == 0) at[wave] = v;
+            __syncthreads();
+            v = at[0];
+            for (int w = 1; w < WAVES; ++w) v = largest ? fmaxf(v, at[w]) : v + at[w];
+        }
+        return v;
+    };
+    const float m = all(q.m, red, true);
+    const Sums r = add_sums(q, Sums{m, 0.f, 0.f}, c);
+    return Sums{m, all(r.s, red + WAVES, false), all(r.t, red + 2 * WAVES, false)};
 }
 
-constexpr int LP_THREADS = 256, LP_PER = 16, LP_TILE = LP_THREADS * LP_PER, LP_SPARE = 512, LP_MOST_PARTS = 64;
+constexpr int LP_THREADS = 256, LP_PER = 16, LP_TILE = LP_THREADS * LP_PER, LP_LIST = 768, LP_MOST_PARTS = 64;
 
 // The n best of list[0 .. count) to the front, in order; the rest of the first n are 0.  All threads; barriers on both sides.
 __device__ __forceinline__ void keep_best(Best *list, int count, int n, Best *room /* POSS_LOGPROBS_TOP + 8 */) {
@@ -71,20 +85,24 @@ __device__ __forceinline__ void keep_best(Best *list, int count, int n, Best *ro
     if (tid < n) list[tid] = room[tid];
     __syncthreads();
 }
-// The n-th largest of the threads' numbers (n <= 256), in every thread.
-__device__ __forceinline__ float nth_of_threads(float v, int n, float *all /* LP_THREADS + 1 */) {
+// The n-th largest of 64 numbers, the largest of four neighbouring threads' each (n <= 64), in every thread: no more than the n-th largest of what they stand for.
+__device__ __forceinline__ float nth_of_threads(float v, int n, float *all /* 65 */) {
+    v = fmaxf(v, xor1(v));
+    v = fmaxf(v, xor2(v));
+    if ((threadIdx.x & 3) == 0) all[threadIdx.x >> 2] = v;
     __syncthreads();
-    all[threadIdx.x] = v;
+    if (threadIdx.x < 64) {
+        v = all[threadIdx.x];
+        int above = 0, least = 0;
+        for (int i = 0; i < 64; ++i) { const float o = lane_value(v, i); above += o > v; least += o >= v; }
+        if (above < n && least >= n) all[64] = v;          // (equal ones write the same)
+    }
     __syncthreads();
-    int above = 0, before = 0;
-    for (int i = 0; i < LP_THREADS; ++i) { above += all[i] > v; before += all[i] == v && i < (int)threadIdx.x; }
-    if (above + before == n - 1) all[LP_THREADS] = v;
-    __syncthreads();
-    return all[LP_THREADS];
+    return all[64];
 }
 
 struct LogprobsArgs {
-    const void *x; int64_t ldx; int vocab, parts; float temperature;
+    const void *x; int64_t ldx; int vocab, parts, per; float temperature;      // per: ids of a part
     const int32_t *tokens; int n_tokens; float *logp, *entropy;
     int n_top; int32_t *top_ids; float *top_logp;
     Sums *part_sums; Best *part_best;           // [rows][parts], [rows][parts][n_top]
@@ -112,44 +130,48 @@ template <typename T, int TOP>
 __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
     constexpr int E = 16 / sizeof(T), VECS = LP_PER / E;
     typedef T vec __attribute__((ext_vector_type(E)));
-    __shared__ Best list[TOP == 2 ? LP_TILE + LP_SPARE : 1], room[POSS_LOGPROBS_TOP + 8];
-    __shared__ float all[LP_THREADS + 1];
-    __shared__ Sums waves[4];
+    __shared__ Best list[TOP == 2 ? LP_LIST : 1], room[POSS_LOGPROBS_TOP + 8];
+    __shared__ float all[65], red[12];
     __shared__ int count;
-    const int tid = threadIdx.x, part = blockIdx.x % a.parts;
-    const int64_t r = blockIdx.x / a.parts;
+    const int tid = threadIdx.x;
+    const int64_t r = blockIdx.x;
     const float c = LOG2_E / a.temperature;
-    // this part's ids [lo, hi); counted from the 16-byte boundary at or before the row, so that whole pieces are aligned loads
+    // this part's ids [lo, hi); tiles are counted from the 16-byte boundary at or before lo, so that whole pieces are aligned loads
     const T *row = static_cast<const T *>(a.x) + r * a.ldx;
-    const int shift = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
-    const int lo = (int)((int64_t)a.vocab * part / a.parts), hi = (int)((int64_t)a.vocab * (part + 1) / a.parts);
-    const int u0 = (lo + shift) / E * E;
-    auto load = [&](int u, float *x) {                     // ids u - shift .. of this thread's pieces in the tile at u
+    const int lo = (int)blockIdx.y * a.per, hi = min(a.vocab, lo + a.per);
+    const int start = lo - (int)(reinterpret_cast<uintptr_t>(row + lo) % 16 / sizeof(T));
+    vec raw[VECS];
+    auto load = [&](int i0) {                              // the pieces of this thread in the tile at id i0
+        if (i0 >= lo && i0 + LP_TILE <= hi) {
 #pragma unroll
-        for (int v = 0; v < VECS; ++v) {
-            const int i = u + (v * LP_THREADS + tid) * E - shift;
-            if (i >= lo && i + E <= hi) {
-                const vec p = *reinterpret_cast<const vec *>(row + i);
-                for (int e = 0; e < E; ++e) x[v * E + e] = to_f(p[e]);
-            } else
-                for (int e = 0; e < E; ++e) x[v * E + e] = i + e >= lo && i + e < hi ? to_f(row[i + e]) : -INFINITY;
+            for (int v = 0; v < VECS; ++v) raw[v] = *reinterpret_cast<const vec *>(row + i0 + (v * LP_THREADS + tid) * E);
+        } else {
+#pragma unroll
+            for (int v = 0; v < VECS; ++v) {
+                const int i = i0 + (v * LP_THREADS + tid) * E;
+                if (i >= lo && i + E <= hi) raw[v] = *reinterpret_cast<const vec *>(row + i);
+                else
+#pragma unroll
+                    for (int e = 0; e < E; ++e) raw[v][e] = i + e >= lo && i + e < hi ? row[i + e] : (T)-INFINITY;
+            }
         }
     };
+    auto id_of = [&](int i0, int e) { return i0 + (e / E * LP_THREADS + tid) * E + e % E; };
     if (tid == 0) count = 0;
     Sums q = {-INFINITY, 0.f, 0.f};
     float border = -INFINITY;                              // TOP 2: what a value has to exceed; NaN: any value may pass
     Best mine = 0;                                         // TOP 1
-    float x[LP_PER];
-    for (int u = u0; u < hi + shift; u += LP_TILE) {
-        load(u, x);
+    load(start);
+    for (int i0 = start; i0 < hi; i0 += LP_TILE) {
+        float x[LP_PER];
+#pragma unroll
+        for (int e = 0; e < LP_PER; ++e) x[e] = to_f(raw[e / E][e % E]);
+        if (i0 + LP_TILE < hi) load(i0 + LP_TILE);         // under way while this tile is summed
         float top = -INFINITY;                             // (of what is a number)
 #pragma unroll
         for (int e = 0; e < LP_PER; ++e) top = fmaxf(top, x[e]);
-        const float m = fmaxf(q.m, top), ref = m == -INFINITY ? 0.f : m;
-        if (m > q.m) {
-            const Sums moved = add_sums(q, Sums{m, 0.f, 0.f}, c);
-            q = moved;
-        }
+        if (top > q.m) q = add_sums(q, Sums{top, 0.f, 0.f}, c);
+        const float ref = q.m == -INFINITY ? 0.f : q.m;
 #pragma unroll
         for (int e = 0; e < LP_PER; ++e) {
             const float d = (x[e] - ref) * c, p = __builtin_amdgcn_exp2f(d);
@@ -157,30 +179,57 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
             q.t += p * fmaxf(d, -1e4f);
         }
         if constexpr (TOP == 1) {
-            if (top > best_value(mine) || mine < ((Best)0x00800000u << 32)) {
+            if (top > best_value(mine) || mine < ((Best)0x00800000u << 32)) {      // (nothing yet, NaN or -infinity: looked at anew)
 #pragma unroll
                 for (int e = 0; e < LP_PER; ++e) {
-                    const int i = u + (e / E * LP_THREADS + tid) * E + e % E - shift;
+                    const int i = id_of(i0, e);
                     const Best b = best_of(x[e], i);
                     if (i >= lo && i < hi && b > mine) mine = b;
                 }
             }
         }
         if constexpr (TOP == 2) {
-            const bool first = u == u0;
+            const bool first = i0 == start;
             float from = border;
             if (first) from = nth_of_threads(top, a.n_top, all);
             const bool any = first ? from == -INFINITY : border != border;
+            uint32_t passes = 0;
             if (any || (first ? top >= from : top > from)) {
 #pragma unroll
                 for (int e = 0; e < LP_PER; ++e) {
-                    const int i = u + (e / E * LP_THREADS + tid) * E + e % E - shift;
-                    if (i >= lo && i < hi && (any || (first ? x[e] >= from : x[e] > from))) list[atomicAdd(&count, 1)] = best_of(x[e], i);
+                    const int i = id_of(i0, e);
+                    if (i >= lo && i < hi && (any || (first ? x[e] >= from : x[e] > from))) passes |= 1u << e;
                 }
             }
+            const int have = count;                        // (nobody adds before the barrier below)
             __syncthreads();
-            const int n = count;
-            if (first || n > LP_SPARE || u + LP_TILE >= hi + shift) {
+            int at = passes ? atomicAdd(&count, __builtin_popcount(passes)) : 0;
+            __syncthreads();
+            int n = count;
+            if (n <= LP_LIST) {
+                if (passes)
+#pragma unroll
+                    for (int e = 0; e < LP_PER; ++e) if (passes >> e & 1) list[at++] = best_of(x[e], id_of(i0, e));
+            } else {                                       // too many at once: one of each thread at a time
+                __syncthreads();
+                if (tid == 0) count = have;
+                __syncthreads();
+#pragma unroll 1
+                for (int e = 0; e < LP_PER; ++e) {
+                    if (count > LP_LIST - LP_THREADS) {
+                        keep_best(list, count, a.n_top, room);
+                        if (tid == 0) count = a.n_top;
+                    }
+                    __syncthreads();
+                    float xe = x[0];
+#pragma unroll
+                    for (int k = 1; k < LP_PER; ++k) xe = e == k ? x[k] : xe;
+                    if (passes >> e & 1) list[atomicAdd(&count, 1)] = best_of(xe, id_of(i0, e));
+                    __syncthreads();
+                }
+                n = count;
+            }
+            if (first || n > LP_LIST / 2 || i0 + LP_TILE >= hi) {
                 keep_best(list, n, a.n_top, room);
                 border = best_value(list[a.n_top - 1]);
                 if (tid == 0) count = a.n_top;
@@ -188,23 +237,19 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
             __syncthreads();
         }
     }
-    q = wave_sums(q, c);
-    if (TOP == 1) {
-        for (int o = 32; o; o >>= 1) { const Best b = __shfl_xor(mine, o); if (b > mine) mine = b; }
-        if ((tid & 63) == 0) room[tid >> 6] = mine;
-    }
-    if ((tid & 63) == 0) waves[tid >> 6] = q;
-    __syncthreads();
-    q = add_sums(add_sums(waves[0], waves[1], c), add_sums(waves[2], waves[3], c), c);
+    q = block_sums<LP_THREADS / 64>(q, c, red);
     const Best *best = list;
-    if (TOP == 1) {
-        if (tid == 0) for (int v = 1; v < 4; ++v) if (room[v] > room[0]) room[0] = room[v];
-        best = room;
+    if constexpr (TOP == 1) {
+        for (int o = 32; o; o >>= 1) { const Best b = __shfl_xor(mine, o); if (b > mine) mine = b; }
+        if ((tid & 63) == 0) room[4 + (tid >> 6)] = mine;
         __syncthreads();
+        if (tid == 0) { for (int v = 0; v < 4; ++v) if (room[4 + v] > mine) mine = room[4 + v]; room[0] = mine; }      // (thread 0 alone reads it)
+        best = room;
     }
     if (a.parts == 1) return write_row<T>(a, r, q, best);
-    if (tid == 0) a.part_sums[blockIdx.x] = q;
-    if (tid < a.n_top) a.part_best[(int64_t)blockIdx.x * a.n_top + tid] = best[tid];
+    const int64_t at = r * a.parts + blockIdx.y;
+    if (tid == 0) a.part_sums[at] = q;
+    if (tid < a.n_top) a.part_best[at * a.n_top + tid] = best[tid];
 }
 
 // Joins a row's parts: a workgroup per row.  Of their best, those from the n-th largest of the parts' first on can be among the n best.
@@ -218,7 +263,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_join_kernel(LogprobsArgs 
     const float c = LOG2_E / a.temperature;
     if (tid == 0) count = 0;
     if (tid < 64) {
-        const Sums q = wave_sums(tid < a.parts ? a.part_sums[r * a.parts + tid] : Sums{-INFINITY, 0.f, 0.f}, c);
+        const Sums q = block_sums<1>(tid < a.parts ? a.part_sums[r * a.parts + tid] : Sums{-INFINITY, 0.f, 0.f}, c, nullptr);
         if (tid == 0) joined = q;
     }
     __syncthreads();
@@ -247,17 +292,20 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_join_kernel(LogprobsArgs 
     write_row<T>(a, r, joined, list);
 }
 
-// Parts of a row: as many as give the chip two thousand workgroups, none of less than a tile.
-static int logprobs_parts(int rows, int vocab) {
+// Parts of a row: as many as give the chip two thousand workgroups, none of less than a tile.  per: ids of each, whole pieces of 16 bytes.
+static int logprobs_parts(int rows, int vocab, int *per = nullptr) {
     int p = rows ? 2048 / rows : 1;
     const int most = (vocab + LP_TILE - 1) / LP_TILE;
     p = p < most ? p : most;
-    return p < 1 ? 1 : p > LP_MOST_PARTS ? LP_MOST_PARTS : p;
+    p = p < 1 ? 1 : p > LP_MOST_PARTS ? LP_MOST_PARTS : p;
+    const int ids = ((vocab + p - 1) / p + 7) / 8 * 8;
+    if (per) *per = ids;
+    return (vocab + ids - 1) / ids;
 }
 
 template <typename T>
 static void launch_logprobs(const LogprobsArgs &a, int rows, hipStream_t st) {
-    const unsigned grid = (unsigned)((int64_t)rows * a.parts);
+    const dim3 grid(rows, a.parts);
     if (a.n_top == 0) logprobs_kernel<T, 0><<<grid, LP_THREADS, 0, st>>>(a);
     else if (a.n_top == 1) logprobs_kernel<T, 1><<<grid, LP_THREADS, 0, st>>>(a);
     else logprobs_kernel<T, 2><<<grid, LP_THREADS, 0, st>>>(a);
@@ -295,9 +343,10 @@ int poss_logprobs(int32_t dtype, const void *x, int64_t ldx, int32_t rows, int32
     const size_t need = poss_logprobs_scratch_bytes(rows, vocab, n_top);
     if (scratch_bytes < need) return set_error(POSS_E_CAPACITY, "%s: rows=%d vocab=%d n_top=%d needs %zu bytes of scratch, got %zu", who, rows, vocab, n_top, need, scratch_bytes);
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const int parts = logprobs_parts(rows, vocab);
+    int per;
+    const int parts = logprobs_parts(rows, vocab, &per);
     char *base = static_cast<char *>(scratch);
-    const LogprobsArgs a{x, ldx, vocab, parts, temperature, tokens, n_tokens, logp, entropy, n_top, top_ids, top_logp, reinterpret_cast<Sums *>(base),
+    const LogprobsArgs a{x, ldx, vocab, parts, per, temperature, tokens, n_tokens, logp, entropy, n_top, top_ids, top_logp, reinterpret_cast<Sums *>(base),
                          reinterpret_cast<Best *>(base + sums_bytes(rows, parts))};
     if (dtype == DT_F32) launch_logprobs<float>(a, rows, st);
     else if (dtype == DT_BF16) launch_logprobs<bf16_t>(a, rows, st);
