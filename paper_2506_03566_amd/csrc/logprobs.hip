@@ -8,7 +8,7 @@ namespace poss {
 
 constexpr float LOG2_E = 1.4426950408889634f;
 
-// A row is read once, by one workgroup or by several that share it; each thread keeps the maximum of what it has seen, S and sum(e^d d) relative to it.
+// A row is read once, by one workgroup or by several that share it; each thread keeps S and sum(e^d d) relative to the maximum that its wave has seen.
 //
 // The best n of a row as 64-bit numbers, larger is better: the value, mapped so that unsigned order is the order of the numbers (NaN 0, -0 as 0), above the
 // complement of its id.  A tile's values that can still be among them go to a list in LDS: those above the n-th best so far (tiles ascend, so an equal value loses by its
@@ -125,7 +125,7 @@ __device__ __forceinline__ void write_row(const LogprobsArgs &a, int64_t r, Sums
     }
 }
 
-// A workgroup per row and part of it.  TOP: 0 no alternatives, 1 one (each thread keeps its best), 2 up to POSS_LOGPROBS_TOP.
+// A workgroup per row and part of it.  TOP: 0 no alternatives, 1 one (each wave keeps its best), 2 up to POSS_LOGPROBS_TOP.
 template <typename T, int TOP>
 __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
     constexpr int E = 16 / sizeof(T), VECS = LP_PER / E;
@@ -140,19 +140,22 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
     const T *row = static_cast<const T *>(a.x) + r * a.ldx;
     const int lo = (int)blockIdx.y * a.per, hi = min(a.vocab, lo + a.per);
     const int start = lo - (int)(reinterpret_cast<uintptr_t>(row + lo) % 16 / sizeof(T));
-    vec raw[VECS];
-    auto load = [&](int i0) {                              // the pieces of this thread in the tile at id i0
-        if (i0 >= lo && i0 + LP_TILE <= hi) {
+    auto whole = [&](int i0) { return i0 >= lo && i0 + LP_TILE <= hi; };
+    auto fetch = [&](int i0, vec *raw) {                   // the pieces of this thread in the whole tile at id i0
 #pragma unroll
-            for (int v = 0; v < VECS; ++v) raw[v] = *reinterpret_cast<const vec *>(row + i0 + (v * LP_THREADS + tid) * E);
-        } else {
+        for (int v = 0; v < VECS; ++v) raw[v] = *reinterpret_cast<const vec *>(row + i0 + (v * LP_THREADS + tid) * E);
+    };
+    auto fetch_guarded = [&](int i0, vec *raw) {           // a tile that begins before lo or ends behind hi
 #pragma unroll
-            for (int v = 0; v < VECS; ++v) {
-                const int i = i0 + (v * LP_THREADS + tid) * E;
-                if (i >= lo && i + E <= hi) raw[v] = *reinterpret_cast<const vec *>(row + i);
-                else
+        for (int v = 0; v < VECS; ++v) {
+            const int i = i0 + (v * LP_THREADS + tid) * E;
+            if (i >= lo && i + E <= hi) raw[v] = *reinterpret_cast<const vec *>(row + i);
+            else {                                         // its values one by one, all asked for before the first is waited for
+                T at[E];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) raw[v][e] = i + e >= lo && i + e < hi ? row[i + e] : (T)-INFINITY;
+                for (int e = 0; e < E; ++e) at[e] = row[min(max(i + e, lo), hi - 1)];
+#pragma unroll
+                for (int e = 0; e < E; ++e) raw[v][e] = i + e >= lo && i + e < hi ? at[e] : (T)-INFINITY;
             }
         }
     };
@@ -160,33 +163,31 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
     if (tid == 0) count = 0;
     Sums q = {-INFINITY, 0.f, 0.f};
     float border = -INFINITY;                              // TOP 2: what a value has to exceed; NaN: any value may pass
-    Best mine = 0;                                         // TOP 1
-    load(start);
-    for (int i0 = start; i0 < hi; i0 += LP_TILE) {
+    int best_at = 0;                                       // TOP 1: the lowest id with the wave's maximum
+    auto take = [&](int i0, const vec *raw) {
         float x[LP_PER];
 #pragma unroll
         for (int e = 0; e < LP_PER; ++e) x[e] = to_f(raw[e / E][e % E]);
-        if (i0 + LP_TILE < hi) load(i0 + LP_TILE);         // under way while this tile is summed
         float top = -INFINITY;                             // (of what is a number)
 #pragma unroll
         for (int e = 0; e < LP_PER; ++e) top = fmaxf(top, x[e]);
-        if (top > q.m) q = add_sums(q, Sums{top, 0.f, 0.f}, c);
+        // the reference is the wave's maximum: few tiles of a row have a new one, where nearly every tile has a new one for some thread of 64
+        if (__any(top > q.m)) {
+            const float m = wave_max(top);
+            q = add_sums(q, Sums{m, 0.f, 0.f}, c);
+            if constexpr (TOP == 1) {
+                best_at = INT32_MAX;
+#pragma unroll
+                for (int e = LP_PER - 1; e >= 0; --e) best_at = x[e] == m ? id_of(i0, e) : best_at;
+                for (int o = 32; o; o >>= 1) best_at = min(best_at, __shfl_xor(best_at, o));
+            }
+        }
         const float ref = q.m == -INFINITY ? 0.f : q.m;
 #pragma unroll
         for (int e = 0; e < LP_PER; ++e) {
             const float d = (x[e] - ref) * c, p = __builtin_amdgcn_exp2f(d);
             q.s += p;
             q.t += p * fmaxf(d, -1e4f);
-        }
-        if constexpr (TOP == 1) {
-            if (top > best_value(mine) || mine < ((Best)0x00800000u << 32)) {      // (nothing yet, NaN or -infinity: looked at anew)
-#pragma unroll
-                for (int e = 0; e < LP_PER; ++e) {
-                    const int i = id_of(i0, e);
-                    const Best b = best_of(x[e], i);
-                    if (i >= lo && i < hi && b > mine) mine = b;
-                }
-            }
         }
         if constexpr (TOP == 2) {
             const bool first = i0 == start;
@@ -236,10 +237,32 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
             }
             __syncthreads();
         }
+    };
+    for (int i0 = start; i0 < hi;) {
+        vec raw[VECS];
+        if (!whole(i0)) {
+            fetch_guarded(i0, raw);
+            take(i0, raw);
+            i0 += LP_TILE;
+            continue;
+        }
+        fetch(i0, raw);
+        for (bool more = true; more; i0 += LP_TILE) {      // the next whole tile is under way while one is summed
+            vec next[VECS];
+            more = whole(i0 + LP_TILE);
+            fetch(more ? i0 + LP_TILE : i0, next);
+            take(i0, raw);
+#pragma unroll
+            for (int v = 0; v < VECS; ++v) raw[v] = next[v];
+        }
     }
+    const float own_m = q.m;
     q = block_sums<LP_THREADS / 64>(q, c, red);
     const Best *best = list;
     if constexpr (TOP == 1) {
+        Best mine = own_m > -INFINITY ? best_of(own_m, best_at) : 0;
+        if (q.m == -INFINITY)                              // nothing but -infinity and NaN
+            for (int i = lo + tid; i < hi; i += LP_THREADS) { const Best b = best_of(to_f(row[i]), i); if (b > mine) mine = b; }
         for (int o = 32; o; o >>= 1) { const Best b = __shfl_xor(mine, o); if (b > mine) mine = b; }
         if ((tid & 63) == 0) room[4 + (tid >> 6)] = mine;
         __syncthreads();
