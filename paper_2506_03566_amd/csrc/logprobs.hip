@@ -11,15 +11,19 @@ constexpr float LOG2_E = 1.4426950408889634f;
 // A row is read once, by one workgroup or by several that share it; each thread keeps S and sum(e^d d) relative to the maximum that its wave has seen.
 //
 // The best n of a row as 64-bit numbers, larger is better: the value, mapped so that unsigned order is the order of the numbers (NaN 0, -0 as 0), above the
-// complement of its id.  A tile's values that can still be among them go to a list in LDS: those above the n-th best so far (tiles ascend, so an equal value loses by its
-// id); at first, those from the n-th largest of the threads' maxima on, which is no more than the n-th best.  A list too long for another tile is
-// cut to its n best.  Random rows put a few dozen values there, a rising row every one of them.
+// complement of its id.  Each wave keeps a list of its own in LDS: of its first tile the values from about the n-th largest of its lanes' maxima on (never
+// above it), then what exceeds that (tiles ascend, so an equal value loses by its id).  A list too long for another 64 is cut to its n best, whose last is the
+// border from then on.  Nothing waits for other waves until the end.  Random rows put a few dozen values there, a rising row every one of them.
+// -infinity and NaN are looked for at the end, where fewer than n others are there.
 typedef unsigned long long Best;
 
 __device__ __forceinline__ Best best_of(float v, int id) {
     const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.f), key = v != v ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
     return (Best)key << 32 | (uint32_t)~id;
 }
+// A number on a wave's list: the value as it is above its id, made comparable when the list is looked at.
+__device__ __forceinline__ Best listed(float v, int id) { return (Best)__builtin_bit_cast(uint32_t, v) << 32 | (uint32_t)id; }
+__device__ __forceinline__ Best best_of_listed(Best b) { return best_of(__builtin_bit_cast(float, (uint32_t)(b >> 32)), (int)(uint32_t)b); }
 __device__ __forceinline__ int best_id(Best b) { return (int)~(uint32_t)b; }
 __device__ __forceinline__ float best_value(Best b) {
     const uint32_t key = (uint32_t)(b >> 32);
@@ -55,50 +59,67 @@ __device__ __forceinline__ Sums block_sums(Sums q, float c, float *red /* 3 * WA
     return Sums{m, all(r.s, red + WAVES, false), all(r.t, red + 2 * WAVES, false)};
 }
 
-constexpr int LP_THREADS = 256, LP_PER = 16, LP_TILE = LP_THREADS * LP_PER, LP_LIST = 768, LP_MOST_PARTS = 64;
+constexpr int LP_THREADS = 256, LP_PER = 16, LP_TILE = LP_THREADS * LP_PER, LP_LIST = 192, LP_MOST_PARTS = 64;
 
-// The n best of list[0 .. count) to the front, in order; the rest of the first n are 0.  All threads; barriers on both sides.
-__device__ __forceinline__ void keep_best(Best *list, int count, int n, Best *room /* POSS_LOGPROBS_TOP + 8 */) {
-    const int tid = threadIdx.x;
-    __syncthreads();
-    if (count <= LP_THREADS) {                             // a thread per number: how many are better
-        const Best mine = tid < count ? list[tid] : 0;
-        int rank = 0;
-        for (int i = 0; i < count; ++i) rank += list[i] > mine;
-        if (tid < n) room[tid] = 0;
-        __syncthreads();
-        if (tid < count && rank < n) room[rank] = mine;
-    } else {
-        Best last = ~0ull;
-        for (int j = 0; j < n; ++j) {
-            Best top = 0;
-            for (int i = tid; i < count; i += LP_THREADS) { const Best b = list[i]; if (b < last && b > top) top = b; }
-            for (int o = 32; o; o >>= 1) { const Best b = __shfl_xor(top, o); if (b > top) top = b; }
-            if ((tid & 63) == 0) room[POSS_LOGPROBS_TOP + (j & 1) * 4 + (tid >> 6)] = top;
-            __syncthreads();
-            for (int v = 0; v < 4; ++v) { const Best b = room[POSS_LOGPROBS_TOP + (j & 1) * 4 + v]; if (b > top) top = b; }
-            last = top;
-            if (tid == 0) room[j] = top;
-        }
+// A lower bound of the n-th largest of the wave's 64 values, near it (its upper 16 bits as a key); -infinity where fewer than n are above that.
+__device__ __forceinline__ float near_nth(float v, int n) {
+    const uint32_t key = (uint32_t)(best_of(v, 0) >> 48);
+    uint32_t found = 0;
+#pragma unroll
+    for (int bit = 15; bit >= 0; --bit) {
+        const uint32_t more = found | 1u << bit;
+        if (__popcll(__ballot(key >= more)) >= n) found = more;
     }
-    __syncthreads();
-    if (tid < n) list[tid] = room[tid];
-    __syncthreads();
+    return found < 0x80u ? -INFINITY : best_value((Best)found << 48);
 }
-// The n-th largest of 64 numbers, the largest of four neighbouring threads' each (n <= 64), in every thread: no more than the n-th largest of what they stand for.
-__device__ __forceinline__ float nth_of_threads(float v, int n, float *all /* 65 */) {
-    v = fmaxf(v, xor1(v));
-    v = fmaxf(v, xor2(v));
-    if ((threadIdx.x & 3) == 0) all[threadIdx.x >> 2] = v;
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        v = all[threadIdx.x];
-        int above = 0, least = 0;
-        for (int i = 0; i < 64; ++i) { const float o = lane_value(v, i); above += o > v; least += o >= v; }
-        if (above < n && least >= n) all[64] = v;          // (equal ones write the same)
+// A wave's list of `count` numbers (at most LP_LIST), its n best to the front.  All lanes.
+__device__ __forceinline__ void cut_list(Best *list, int count, int n) {      // (its numbers as `listed` leaves them)
+    const int lane = threadIdx.x & 63;
+    Best mine[LP_LIST / 64];
+    int rank[LP_LIST / 64];
+    wave_lds_sync();
+#pragma unroll
+    for (int k = 0; k < LP_LIST / 64; ++k) { mine[k] = k * 64 + lane < count ? best_of_listed(list[k * 64 + lane]) : 0; rank[k] = 0; }
+    for (int i = 0; i < count; ++i) {
+        const Best o = best_of_listed(list[i]);
+#pragma unroll
+        for (int k = 0; k < LP_LIST / 64; ++k) rank[k] += o > mine[k];
+    }
+    wave_lds_sync();
+#pragma unroll
+    for (int k = 0; k < LP_LIST / 64; ++k) if (k * 64 + lane < count && rank[k] < n) list[rank[k]] = listed(best_value(mine[k]), best_id(mine[k]));
+    wave_lds_sync();
+}
+// The n best of list[0 .. count), in order, to room[0 .. n); returns how many there are.  The workgroup, behind a barrier; a barrier at the end.
+__device__ __forceinline__ int rank_list(const Best *list, int count, int n, Best *room) {
+    for (int at = threadIdx.x; at < count; at += LP_THREADS) {
+        const Best mine = list[at];
+        int rank = 0;
+        for (int j = 0; j < count; ++j) rank += list[j] > mine;
+        if (rank < n) room[rank] = mine;
     }
     __syncthreads();
-    return all[64];
+    return count < n ? count : n;
+}
+// room[have .. n) from the ids [lo, hi): -infinity by id, then NaN by id, then 0.  The workgroup.
+template <typename T>
+__device__ __forceinline__ void fill_rest(const T *row, int lo, int hi, int have, int n, Best *room, int *red /* 4 */) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int what = 0; what < 2; ++what)
+        for (int i0 = lo; i0 < hi && have < n; i0 += LP_THREADS) {
+            const int i = i0 + (int)threadIdx.x;
+            const float v = i < hi ? to_f(row[i]) : 0.f;
+            const bool it = what ? v != v : v == -INFINITY;
+            const unsigned long long them = __ballot(it);
+            __syncthreads();
+            if (lane == 0) red[wave] = __popcll(them);
+            __syncthreads();
+            int at = have + __popcll(them & ((1ull << lane) - 1));
+            for (int w = 0; w < LP_THREADS / 64; ++w) { if (w < wave) at += red[w]; have += red[w]; }
+            if (it && at < n) room[at] = best_of(v, i);
+        }
+    if ((int)threadIdx.x < n && (int)threadIdx.x >= have) room[threadIdx.x] = 0;
+    __syncthreads();
 }
 
 struct LogprobsArgs {
@@ -130,9 +151,10 @@ template <typename T, int TOP>
 __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
     constexpr int E = 16 / sizeof(T), VECS = LP_PER / E;
     typedef T vec __attribute__((ext_vector_type(E)));
-    __shared__ Best list[TOP == 2 ? LP_LIST : 1], room[POSS_LOGPROBS_TOP + 8];
-    __shared__ float all[65], red[12];
-    __shared__ int count;
+    constexpr int WAVES = LP_THREADS / 64;
+    __shared__ Best lists[TOP == 2 ? WAVES : 1][LP_LIST], joint[TOP == 2 ? WAVES * LP_LIST : WAVES], room[POSS_LOGPROBS_TOP];
+    __shared__ float red[3 * WAVES], borders[WAVES];
+    __shared__ int joined, found[WAVES];
     const int tid = threadIdx.x;
     const int64_t r = blockIdx.x;
     const float c = LOG2_E / a.temperature;
@@ -150,6 +172,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
         for (int v = 0; v < VECS; ++v) {
             const int i = i0 + (v * LP_THREADS + tid) * E;
             if (i >= lo && i + E <= hi) raw[v] = *reinterpret_cast<const vec *>(row + i);
+            else if (i + E <= lo || i >= hi) raw[v] = (vec)((T)-INFINITY);
             else {                                         // its values one by one, all asked for before the first is waited for
                 T at[E];
 #pragma unroll
@@ -160,9 +183,11 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
         }
     };
     auto id_of = [&](int i0, int e) { return i0 + (e / E * LP_THREADS + tid) * E + e % E; };
-    if (tid == 0) count = 0;
     Sums q = {-INFINITY, 0.f, 0.f};
-    float border = -INFINITY;                              // TOP 2: what a value has to exceed; NaN: any value may pass
+    Best *const list = lists[TOP == 2 ? tid >> 6 : 0];     // TOP 2: the wave's list, how long it is, what a value has to exceed
+    int count = 0;
+    float border = -INFINITY, tops = -INFINITY;            // tops: this lane's maximum
+    int tile = 0;
     int best_at = 0;                                       // TOP 1: the lowest id with the wave's maximum
     auto take = [&](int i0, const vec *raw) {
         float x[LP_PER];
@@ -190,52 +215,31 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
             q.t += p * fmaxf(d, -1e4f);
         }
         if constexpr (TOP == 2) {
-            const bool first = i0 == start;
-            float from = border;
-            if (first) from = nth_of_threads(top, a.n_top, all);
-            const bool any = first ? from == -INFINITY : border != border;
-            uint32_t passes = 0;
-            if (any || (first ? top >= from : top > from)) {
+            bool equal = false;                            // whether a value may equal the border
+            if (i0 == start) { border = near_nth(top, a.n_top); equal = border > -INFINITY; }
+            else if ((tile & (tile - 1)) == 0) border = fmaxf(border, near_nth(tops, a.n_top));      // of the tiles before, at the 2nd, 4th, 8th ..: a tile puts fewer on the list
+            tops = fmaxf(tops, top);
+            ++tile;
+            if (__any(equal ? top >= border : top > border)) {
 #pragma unroll
                 for (int e = 0; e < LP_PER; ++e) {
-                    const int i = id_of(i0, e);
-                    if (i >= lo && i < hi && (any || (first ? x[e] >= from : x[e] > from))) passes |= 1u << e;
-                }
-            }
-            const int have = count;                        // (nobody adds before the barrier below)
-            __syncthreads();
-            int at = passes ? atomicAdd(&count, __builtin_popcount(passes)) : 0;
-            __syncthreads();
-            int n = count;
-            if (n <= LP_LIST) {
-                if (passes)
-#pragma unroll
-                    for (int e = 0; e < LP_PER; ++e) if (passes >> e & 1) list[at++] = best_of(x[e], id_of(i0, e));
-            } else {                                       // too many at once: one of each thread at a time
-                __syncthreads();
-                if (tid == 0) count = have;
-                __syncthreads();
-#pragma unroll 1
-                for (int e = 0; e < LP_PER; ++e) {
-                    if (count > LP_LIST - LP_THREADS) {
-                        keep_best(list, count, a.n_top, room);
-                        if (tid == 0) count = a.n_top;
+                    const unsigned long long them = __ballot(equal ? x[e] >= border : x[e] > border);      // (ids outside the part stand as -infinity)
+                    if (!them) continue;
+                    if (count > LP_LIST - 64) {
+                        // its n best, a border that may rise: an equal value of this tile with a lower id can still be to come, so the border of this tile stays
+                        cut_list(list, count, a.n_top);
+                        count = a.n_top;
                     }
-                    __syncthreads();
-                    float xe = x[0];
-#pragma unroll
-                    for (int k = 1; k < LP_PER; ++k) xe = e == k ? x[k] : xe;
-                    if (passes >> e & 1) list[atomicAdd(&count, 1)] = best_of(xe, id_of(i0, e));
-                    __syncthreads();
+                    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(them >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)them, 0));
+                    if (equal ? x[e] >= border : x[e] > border) list[count + before] = listed(x[e], id_of(i0, e));
+                    count += __popcll(them);
                 }
-                n = count;
+                if (count > LP_LIST / 2) {
+                    cut_list(list, count, a.n_top);
+                    count = a.n_top;
+                    border = __builtin_bit_cast(float, (uint32_t)(list[a.n_top - 1] >> 32));
+                }
             }
-            if (first || n > LP_LIST / 2 || i0 + LP_TILE >= hi) {
-                keep_best(list, n, a.n_top, room);
-                border = best_value(list[a.n_top - 1]);
-                if (tid == 0) count = a.n_top;
-            }
-            __syncthreads();
         }
     };
     for (int i0 = start; i0 < hi;) {
@@ -257,67 +261,76 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
         }
     }
     const float own_m = q.m;
-    q = block_sums<LP_THREADS / 64>(q, c, red);
-    const Best *best = list;
-    if constexpr (TOP == 1) {
-        Best mine = own_m > -INFINITY ? best_of(own_m, best_at) : 0;
-        if (q.m == -INFINITY)                              // nothing but -infinity and NaN
-            for (int i = lo + tid; i < hi; i += LP_THREADS) { const Best b = best_of(to_f(row[i]), i); if (b > mine) mine = b; }
-        for (int o = 32; o; o >>= 1) { const Best b = __shfl_xor(mine, o); if (b > mine) mine = b; }
-        if ((tid & 63) == 0) room[4 + (tid >> 6)] = mine;
-        __syncthreads();
-        if (tid == 0) { for (int v = 0; v < 4; ++v) if (room[4 + v] > mine) mine = room[4 + v]; room[0] = mine; }      // (thread 0 alone reads it)
-        best = room;
+    q = block_sums<WAVES>(q, c, red);
+    if constexpr (TOP > 0) {
+        if (TOP == 1) {
+            if ((tid & 63) == 0) joint[tid >> 6] = best_of(own_m, best_at);
+            __syncthreads();
+        } else {
+            // each wave has n / WAVES numbers from its border here on, so the lowest of the borders is no more than the part's n-th best
+            const float b = near_nth(tops, (a.n_top + WAVES - 1) / WAVES);
+            if ((tid & 63) == 0) borders[tid >> 6] = b;
+            if (tid == 0) joined = 0;
+            __syncthreads();
+            float from = borders[0];
+            for (int w = 1; w < WAVES; ++w) from = fminf(from, borders[w]);
+            for (int i = tid & 63; i < count; i += 64) {
+                const Best o = list[i];
+                if (__builtin_bit_cast(float, (uint32_t)(o >> 32)) >= from) joint[atomicAdd(&joined, 1)] = best_of_listed(o);
+            }
+            __syncthreads();
+        }
+        int have = rank_list(joint, TOP == 1 ? WAVES : joined, a.n_top, room);
+        if (TOP == 1 && q.m == -INFINITY) have = 0;
+        if (have < a.n_top) fill_rest(row, lo, hi, have, a.n_top, room, found);
     }
+    const Best *best = room;
     if (a.parts == 1) return write_row<T>(a, r, q, best);
     const int64_t at = r * a.parts + blockIdx.y;
     if (tid == 0) a.part_sums[at] = q;
     if (tid < a.n_top) a.part_best[at * a.n_top + tid] = best[tid];
 }
 
-// Joins a row's parts: a workgroup per row.  Of their best, those from the n-th largest of the parts' first on can be among the n best.
+// Joins a row's parts: a workgroup per row.  Of their best, those from about the n-th largest of the parts' first on can be among the n best.
 template <typename T>
 __global__ void __launch_bounds__(LP_THREADS) logprobs_join_kernel(LogprobsArgs a) {
-    __shared__ Best list[LP_MOST_PARTS * POSS_LOGPROBS_TOP], room[POSS_LOGPROBS_TOP + 8];
+    constexpr int EACH = LP_MOST_PARTS * POSS_LOGPROBS_TOP / LP_THREADS;
+    __shared__ Best list[LP_MOST_PARTS * POSS_LOGPROBS_TOP], room[POSS_LOGPROBS_TOP];
     __shared__ Sums joined;
+    __shared__ uint32_t from;
     __shared__ int count;
     const int64_t r = blockIdx.x;
     const int tid = threadIdx.x, n = a.n_top;
     const float c = LOG2_E / a.temperature;
-    if (tid == 0) count = 0;
+    const Best *best = a.part_best + r * a.parts * n;
+    Best mine[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) mine[k] = tid + k * LP_THREADS < a.parts * n ? best[tid + k * LP_THREADS] : 0;
     if (tid < 64) {
-        const Sums q = block_sums<1>(tid < a.parts ? a.part_sums[r * a.parts + tid] : Sums{-INFINITY, 0.f, 0.f}, c, nullptr);
-        if (tid == 0) joined = q;
+        const Sums part = tid < a.parts ? a.part_sums[r * a.parts + tid] : Sums{-INFINITY, 0.f, 0.f};
+        uint32_t key = 0, found = 0;
+        if (n) {
+            key = tid < a.parts ? (uint32_t)(best[tid * n] >> 48) : 0;
+            for (int bit = 15; bit >= 0; --bit)
+                if (__popcll(__ballot(key >= (found | 1u << bit))) >= n) found |= 1u << bit;
+        }
+        const Sums q = block_sums<1>(part, c, nullptr);
+        if (tid == 0) { joined = q; from = found; count = 0; }
     }
     __syncthreads();
     if (n) {
-        const Best *best = a.part_best + r * a.parts * n;
-        Best from = 0;
-        if (n <= a.parts) {
-            Best first = 0;
-            if (tid < a.parts) first = best[tid * n];
-            if (tid < a.parts) list[tid] = first;
-            __syncthreads();
-            int rank = 0;
-            for (int i = 0; i < a.parts; ++i) rank += list[i] > first || (list[i] == first && i < tid);
-            if (tid < a.parts && rank == n - 1) room[0] = first;
-            __syncthreads();
-            from = room[0];
-            __syncthreads();
-        }
-        for (int i = tid; i < a.parts * n; i += LP_THREADS) {
-            const Best b = best[i];
-            if (b >= from) list[atomicAdd(&count, 1)] = b;
-        }
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+            if (tid + k * LP_THREADS < a.parts * n && (uint32_t)(mine[k] >> 48) >= from && mine[k]) list[atomicAdd(&count, 1)] = mine[k];
         __syncthreads();
-        keep_best(list, count, n, room);
+        rank_list(list, count, n, room);
     }
-    write_row<T>(a, r, joined, list);
+    write_row<T>(a, r, joined, room);
 }
 
-// Parts of a row: as many as give the chip two thousand workgroups, none of less than a tile.  per: ids of each, whole pieces of 16 bytes.
+// Parts of a row: as many as give the chip four workgroups a CU, none of less than a tile.  per: ids of each, whole pieces of 16 bytes.
 static int logprobs_parts(int rows, int vocab, int *per = nullptr) {
-    int p = rows ? 2048 / rows : 1;
+    int p = rows ? 1024 / rows : 1;
     const int most = (vocab + LP_TILE - 1) / LP_TILE;
     p = p < most ? p : most;
     p = p < 1 ? 1 : p > LP_MOST_PARTS ? LP_MOST_PARTS : p;
