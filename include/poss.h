@@ -407,7 +407,7 @@ int poss_rope_fill(int32_t rot_dim, int32_t interleaved, double theta, int32_t s
                    double original, double magnitude, poss_rope *out);
 
 /* y = x rotated, rounded once: value d of head h of row r lies at x[r * x_row + h * x_head + d], the same for y.  positions: DEVICE int32[rows], of
- * any sign.  inverse != 0: by the opposite angle (the transpose, up to magnitude^2: what a gradient is multiplied by).  y may be x, with the same distances. */
+ * any sign; at most 2^23 rows.  inverse != 0: by the opposite angle (the transpose, up to magnitude^2: what a gradient is multiplied by).  y may be x, with the same distances. */
 int poss_rotary(int32_t dtype, const void *x, int64_t x_row, int64_t x_head, void *y, int64_t y_row, int64_t y_head, int32_t rows,
                 int32_t heads, int32_t head_dim, const int32_t *positions, const poss_rope *rope, int32_t inverse, void *hip_stream);
 

@@ -5,25 +5,47 @@
 
 namespace poss {
 
-// Cosine and sine of position * freq[i], times magnitude, for the pairs of one row: into LDS, by the row's workgroup.
-__device__ __forceinline__ void rope_angles(const poss_rope &rope, int pos, float sign, float2 *cs) {
-    for (int i = threadIdx.x; i < rope.rot_dim / 2; i += blockDim.x) {
-        double s, c;
-        sincos((double)pos * rope.freq[i], &s, &c);
-        cs[i] = make_float2((float)(c * rope.magnitude), (float)(s * rope.magnitude) * sign);
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Cosine and sine of position * freq.  The angle is formed and brought to within pi/4 of a multiple of pi/2 in 64 bits (pi/2 as the sum of two numbers), so that
+// far positions lose nothing; the series that are left are summed in float32 (their next terms are below 2^-28).  Some thirty instructions, a
+// seventh of the 64-bit functions' time.
+__device__ __forceinline__ float2 cos_sin(int pos, double freq) {
+    const double t = (double)pos * freq, n = rint(t * 0.63661977236758134308);
+    double rd = fma(-n, 1.57079632679489655800, t);
+    rd = fma(-n, 6.12323399573676603587e-17, rd);
+    const float r = (float)rd, q = r * r;
+    const int quarter = (int)(n - 4.0 * rint(n * 0.25));   // -2 .. 2
+    float s = fmaf(q, fmaf(q, fmaf(q, fmaf(q, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), 1.f) * r;
+    float c = fmaf(q, fmaf(q, fmaf(q, fmaf(q, fmaf(q, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.f);
+    if (quarter & 1) { const float x = s; s = c; c = -x; }
+    return quarter & 2 ? make_float2(-c, -s) : make_float2(c, s);
+}
+
+// The table of one row, times magnitude, into LDS: by the threads first, first + step ..
+__device__ __forceinline__ void rope_angles(const poss_rope &rope, int pos, float sign, float2 *cs, int first, int step) {
+    for (int i = first; i < rope.rot_dim / 2; i += step) {
+        const float2 v = cos_sin(pos, rope.freq[i]);
+        cs[i] = make_float2(v.x * rope.magnitude, v.y * rope.magnitude * sign);
     }
 }
 
-// What value d of a head at x becomes.
+// ------------------------------------------------------------------------------------------ any size and alignment, few rows
+// A thread's part of a row's heads: pairs, and the values that stay.
 template <typename T>
-__device__ __forceinline__ T rope_value(const T *x, int d, int rot, int interleaved, const float2 *cs) {
-    if (d >= rot) return x[d];
-    const int half = rot >> 1;
-    const int i = interleaved ? d >> 1 : d < half ? d : d - half;
-    const bool second = interleaved ? d & 1 : d >= half;
-    float a, b;
-    rope_pair(to_f(x[interleaved ? 2 * i : i]), to_f(x[interleaved ? 2 * i + 1 : i + half]), cs[i], a, b);
-    return from_f<T>(second ? b : a);
+__device__ __forceinline__ void rotate_values(const T *x, int64_t x_head, T *y, int64_t y_head, int heads, int dh, int rot, int interleaved, const float2 *cs) {
+    const int half = rot >> 1, per = half + dh - rot;      // a thread takes a pair, or a value that stays
+    for (int64_t j = threadIdx.x; j < (int64_t)heads * per; j += blockDim.x) {
+        const int64_t h = j / per;
+        const int i = (int)(j - h * per);
+        const T *xi = x + h * x_head;
+        T *yi = y + h * y_head;
+        if (i >= half) { yi[i + half] = xi[i + half]; continue; }
+        const int a = interleaved ? 2 * i : i, b = interleaved ? 2 * i + 1 : i + half;
+        float o1, o2;
+        rope_pair(to_f(xi[a]), to_f(xi[b]), cs[i], o1, o2);
+        yi[a] = round_f<T>(o1); yi[b] = round_f<T>(o2);
+    }
 }
 
 // A workgroup per row.
@@ -32,60 +54,173 @@ __global__ void __launch_bounds__(256) rotary_kernel(const T *x, int64_t x_row, 
                                                      const int32_t *__restrict__ positions, poss_rope rope, float sign) {
     __shared__ float2 cs[POSS_ROPE_PAIRS];
     const int64_t r = blockIdx.x;
-    rope_angles(rope, positions[r], sign, cs);
+    rope_angles(rope, positions[r], sign, cs, threadIdx.x, blockDim.x);
     __syncthreads();
-    const int half = rope.rot_dim >> 1, rest = dh - rope.rot_dim, per = half + rest;      // a thread takes a pair, or a value that stays
-    for (int64_t j = threadIdx.x; j < (int64_t)heads * per; j += blockDim.x) {
-        const int64_t h = j / per;
-        const int i = (int)(j - h * per);
-        const T *xi = x + r * x_row + h * x_head;
-        T *yi = y + r * y_row + h * y_head;
-        if (i >= half) { yi[i + half] = xi[i + half]; continue; }
-        const int a = rope.interleaved ? 2 * i : i, b = rope.interleaved ? 2 * i + 1 : i + half;
-        float o1, o2;
-        rope_pair(to_f(xi[a]), to_f(xi[b]), cs[i], o1, o2);
-        yi[a] = from_f<T>(o1); yi[b] = from_f<T>(o2);
-    }
+    rotate_values(x + r * x_row, x_head, y + r * y_row, y_head, heads, dh, rope.rot_dim, rope.interleaved, cs);
 }
 
 struct AppendArgs {
-    int hq;
+    int rows, hq;
     const void *q; int64_t q_row; void *q_out; int64_t q_out_row;
     const void *k; int64_t k_row; const void *v; int64_t v_row;
     const int32_t *seq, *slots, *positions;
     int32_t *slot_positions;
 };
 
+// The page that a row goes to (-1: nowhere), its sequence and slot.
+__device__ __forceinline__ int append_page(const KvView &c, const AppendArgs &a, int r, int &b, int &slot) {
+    b = a.seq ? a.seq[r] : r;
+    slot = a.slots[r];
+    return (unsigned)b < (unsigned)c.n_seq ? kv_page(c, b, slot) : -1;
+}
+__device__ __forceinline__ void note_positions(const KvView &c, const AppendArgs &a, int r, int b, int slot, int first, int step) {
+    if (a.slot_positions)
+        for (int h = first; h < c.hkv; h += step) a.slot_positions[((int64_t)b * c.hkv + h) * c.slots + slot] = a.positions[r];
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256) append_kernel(KvView c, AppendArgs a, poss_rope rope) {
     __shared__ float2 cs[POSS_ROPE_PAIRS];
-    const int r = blockIdx.x, dh = c.dh, half = rope.rot_dim >> 1;
-    if (half) rope_angles(rope, a.positions[r], 1.f, cs);
+    const int r = blockIdx.x, dh = c.dh;
+    int b, slot;
+    const int page = append_page(c, a, r, b, slot);
+    if (rope.rot_dim) rope_angles(rope, a.positions[r], 1.f, cs, threadIdx.x, blockDim.x);
     __syncthreads();
-    const int rest = dh - rope.rot_dim, per = half + rest;
-    const T *q = static_cast<const T *>(a.q) + r * a.q_row;
-    T *qo = static_cast<T *>(a.q_out) + r * a.q_out_row;
-    for (int j = threadIdx.x; j < a.hq * per; j += blockDim.x) {
-        const int h = j / per, i = j - h * per;
-        if (i >= half) { qo[h * dh + i + half] = q[h * dh + i + half]; continue; }
-        const int x = h * dh + (rope.interleaved ? 2 * i : i), y = h * dh + (rope.interleaved ? 2 * i + 1 : i + half);
-        float o1, o2;
-        rope_pair(to_f(q[x]), to_f(q[y]), cs[i], o1, o2);
-        qo[x] = from_f<T>(o1); qo[y] = from_f<T>(o2);
-    }
-    const int b = a.seq ? a.seq[r] : r, slot = a.slots[r];
-    if ((unsigned)b >= (unsigned)c.n_seq) return;
-    const int page = kv_page(c, b, slot);
+    rotate_values(static_cast<const T *>(a.q) + r * a.q_row, dh, static_cast<T *>(a.q_out) + r * a.q_out_row, dh, a.hq, dh, rope.rot_dim, rope.interleaved, cs);
     if (page < 0) return;
-    const T *k = static_cast<const T *>(a.k) + r * a.k_row, *v = static_cast<const T *>(a.v) + r * a.v_row;
-    T *ck = static_cast<T *>(c.k), *cv = static_cast<T *>(c.v);
-    for (int j = threadIdx.x; j < c.hkv * dh; j += blockDim.x) {
-        const int h = j / dh, d = j - h * dh;
-        ck[kv_key_at(c, page, h, slot) + d] = rope_value(k + h * dh, d, rope.rot_dim, rope.interleaved, cs);
-        cv[kv_value_at(c, page, h, d, slot)] = v[j];
+    T *ck = static_cast<T *>(c.k) + kv_key_at(c, page, 0, slot), *cv = static_cast<T *>(c.v) + kv_value_at(c, page, 0, 0, slot);
+    rotate_values(static_cast<const T *>(a.k) + r * a.k_row, dh, ck, (int64_t)dh << c.shift, c.hkv, dh, rope.rot_dim, rope.interleaved, cs);
+    const T *v = static_cast<const T *>(a.v) + r * a.v_row;
+    for (int j = threadIdx.x; j < c.hkv * dh; j += blockDim.x) cv[(int64_t)j << c.shift] = v[j];
+    note_positions(c, a, r, b, slot, threadIdx.x, blockDim.x);
+}
+
+// ------------------------------------------------------------------------------------------ whole pieces of 16 bytes, many rows
+// A wave's part of a row: pieces of 16 bytes, of both members' halves at once where pairs lie apart.  units: of one head; of_units: 2^32 / units, rounded up.
+struct Units { int units; uint32_t of_units; };
+
+template <typename T, bool INTERLEAVED>
+__device__ __forceinline__ void rotate_pieces(const T *x, int64_t x_head, T *y, int64_t y_head, int heads, int rot, Units n, const float2 *cs) {
+    constexpr int E = 16 / sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(E)));
+    const int half = rot >> 1, turned = INTERLEAVED ? rot / E : half / E, all = heads * n.units;
+#pragma unroll 2
+    for (int j = threadIdx.x & 63; j < all; j += 64) {
+        const int h = (int)__umulhi((uint32_t)j, n.of_units), u = j - h * n.units;
+        const T *xi = x + h * x_head;
+        T *yi = y + h * y_head;
+        if (u >= turned) {                                 // values that stay
+            const int d = rot + (u - turned) * E;
+            *reinterpret_cast<vec *>(yi + d) = *reinterpret_cast<const vec *>(xi + d);
+        } else if (INTERLEAVED) {
+            const vec p = *reinterpret_cast<const vec *>(xi + u * E);
+            vec o;
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                float o1, o2;
+                rope_pair(to_f(p[e]), to_f(p[e + 1]), cs[u * (E / 2) + e / 2], o1, o2);
+                o[e] = round_f<T>(o1); o[e + 1] = round_f<T>(o2);
+            }
+            *reinterpret_cast<vec *>(yi + u * E) = o;
+        } else {
+            const vec p = *reinterpret_cast<const vec *>(xi + u * E), q = *reinterpret_cast<const vec *>(xi + half + u * E);
+            vec o, s;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float o1, o2;
+                rope_pair(to_f(p[e]), to_f(q[e]), cs[u * E + e], o1, o2);
+                o[e] = round_f<T>(o1); s[e] = round_f<T>(o2);
+            }
+            *reinterpret_cast<vec *>(yi + u * E) = o;
+            *reinterpret_cast<vec *>(yi + half + u * E) = s;
+        }
     }
-    if (a.slot_positions)
-        for (int h = threadIdx.x; h < c.hkv; h += blockDim.x) a.slot_positions[((int64_t)b * c.hkv + h) * c.slots + slot] = a.positions[r];
+}
+
+// A wave per row.
+template <typename T, bool INTERLEAVED>
+__global__ void __launch_bounds__(256) rotary_rows_kernel(const T *x, int64_t x_row, int64_t x_head, T *y, int64_t y_row, int64_t y_head, int rows, int heads, Units n,
+                                                          const int32_t *__restrict__ positions, poss_rope rope, float sign) {
+    __shared__ __align__(16) float2 cs[4][POSS_ROPE_PAIRS];
+    const int wave = threadIdx.x >> 6;
+    const int64_t r = (int64_t)blockIdx.x * 4 + wave;
+    if (r >= rows) return;
+    rope_angles(rope, positions[r], sign, cs[wave], threadIdx.x & 63, 64);
+    wave_lds_sync();
+    rotate_pieces<T, INTERLEAVED>(x + r * x_row, x_head, y + r * y_row, y_head, heads, rope.rot_dim, n, cs[wave]);
+}
+
+// Queries and keys: a wave per row, in the first workgroups.  Values: behind them, a wave per square of eight by eight pieces - 16-bit types 64 rows by 64 dims -
+// of which a lane turns a square of E by E values over in its registers, so that the rows of consecutive slots leave as whole lines of a value row.
+// That needs E rows with consecutive slots of one page, the first at a multiple of E; squares are laid so for the rows that follow the call's first slot.
+// Other squares are written value by value (8192 rows of 8 value heads all at once: 88 us, whole lines 9).
+template <typename T, bool INTERLEAVED>
+__global__ void __launch_bounds__(256) append_rows_kernel(KvView c, AppendArgs a, poss_rope rope, Units n, int row_groups) {
+    constexpr int E = 16 / sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(E)));
+    __shared__ __align__(16) float2 cs[4][POSS_ROPE_PAIRS];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, dh = c.dh;
+    if ((int)blockIdx.x < row_groups) {
+        const int r = blockIdx.x * 4 + wave;
+        if (r >= a.rows) return;
+        int b, slot;
+        const int page = append_page(c, a, r, b, slot);
+        if (rope.rot_dim) rope_angles(rope, a.positions[r], 1.f, cs[wave], lane, 64);
+        wave_lds_sync();
+        rotate_pieces<T, INTERLEAVED>(static_cast<const T *>(a.q) + r * a.q_row, dh, static_cast<T *>(a.q_out) + r * a.q_out_row, dh, a.hq, rope.rot_dim, n, cs[wave]);
+        if (page < 0) return;
+        rotate_pieces<T, INTERLEAVED>(static_cast<const T *>(a.k) + r * a.k_row, dh, static_cast<T *>(c.k) + kv_key_at(c, page, 0, slot), (int64_t)dh << c.shift, c.hkv, rope.rot_dim, n,
+                                      cs[wave]);
+        note_positions(c, a, r, b, slot, lane, 64);
+        return;
+    }
+    const int across = (c.hkv * dh + 8 * E - 1) / (8 * E);                     // squares of a row of values
+    const int64_t square = (int64_t)(blockIdx.x - row_groups) * 4 + wave;
+    const int sr = (int)(square / across), d0 = (int)(square - (int64_t)sr * across) * 8 * E + (lane >> 3) * E;
+    const int first = a.slots[0], r0 = sr * 8 * E + (lane & 7) * E - (first > 0 ? first & (E - 1) : 0);
+    if (r0 >= a.rows || d0 >= c.hkv * dh) return;
+    const T *v = static_cast<const T *>(a.v);
+    T *cv = static_cast<T *>(c.v);
+    if (r0 >= 0 && r0 + E <= a.rows) {
+        bool run = true;
+        int b, slot;
+        const int page = append_page(c, a, r0, b, slot);
+        for (int e = 1; e < E; ++e) run = run && a.slots[r0 + e] == slot + e && (a.seq ? a.seq[r0 + e] : r0 + e) == b;
+        if (run && page >= 0 && slot % E == 0) {
+            vec in[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) in[e] = *reinterpret_cast<const vec *>(v + (r0 + e) * a.v_row + d0);
+            T *to = cv + kv_value_at(c, page, 0, d0, slot);                    // (heads and dims are one sequence of value rows)
+#pragma unroll
+            for (int d = 0; d < E; ++d) {
+                vec o;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = in[e][d];
+                *reinterpret_cast<vec *>(to + ((int64_t)d << c.shift)) = o;
+            }
+            return;
+        }
+    }
+    for (int e = 0; e < E; ++e) {
+        const int r = r0 + e;
+        if (r < 0 || r >= a.rows) continue;
+        int b, slot;
+        const int page = append_page(c, a, r, b, slot);
+        if (page < 0) continue;
+        const vec in = *reinterpret_cast<const vec *>(v + r * a.v_row + d0);
+        T *to = cv + kv_value_at(c, page, 0, d0, slot);
+#pragma unroll
+        for (int d = 0; d < E; ++d) to[(int64_t)d << c.shift] = in[d];
+    }
+}
+
+// Whether a head of dh values, rot of them rotated, is whole pieces of 16 bytes, and how many units.
+static bool units_of(int dt, int dh, int rot, bool interleaved, Units &n) {
+    const int E = dt == DT_F32 ? 4 : 8, half = rot / 2;
+    if (dh % E || rot % E || (!interleaved && half % E)) return false;
+    n.units = dh / E - (interleaved ? 0 : half / E);
+    n.of_units = (uint32_t)(((1ull << 32) + n.units - 1) / n.units);
+    return true;
 }
 
 }  // namespace poss
@@ -94,6 +229,7 @@ __global__ void __launch_bounds__(256) append_kernel(KvView c, AppendArgs a, pos
 using namespace poss;
 
 namespace {
+constexpr int ROWS_MANY = 16, ROWS_MOST = 1 << 23;
 bool rope_ok(const poss_rope &r, int head_dim) { return r.rot_dim >= 2 && r.rot_dim <= 2 * POSS_ROPE_PAIRS && r.rot_dim % 2 == 0 && r.rot_dim <= head_dim; }
 }  // namespace
 
@@ -139,7 +275,7 @@ int poss_rope_fill(int32_t rot_dim, int32_t interleaved, double theta, int32_t s
 int poss_rotary(int32_t dtype, const void *x, int64_t x_row, int64_t x_head, void *y, int64_t y_row, int64_t y_head, int32_t rows, int32_t heads, int32_t head_dim,
                 const int32_t *positions, const poss_rope *rope, int32_t inverse, void *hip_stream) {
     const char *who = "poss_rotary";
-    if (kv_bad_dtype(dtype) || rows < 0 || heads < 1 || head_dim < 2) return set_error(POSS_E_INVALID_ARG, "%s: bad shape or type", who);
+    if (kv_bad_dtype(dtype) || rows < 0 || rows > ROWS_MOST || heads < 1 || head_dim < 2) return set_error(POSS_E_INVALID_ARG, "%s: bad shape or type", who);
     if (!rope || !rope_ok(*rope, head_dim)) return set_error(POSS_E_INVALID_ARG, "%s: rope: an even rot_dim up to the head's values is wanted", who);
     if (rows == 0) return POSS_OK;
     if (!x || !y || !positions) return set_error(POSS_E_INVALID_ARG, "%s: null argument", who);
@@ -150,7 +286,17 @@ int poss_rotary(int32_t dtype, const void *x, int64_t x_row, int64_t x_head, voi
     if (x == y && ((rows > 1 && x_row != y_row) || (heads > 1 && x_head != y_head))) return set_error(POSS_E_INVALID_ARG, "%s: y is x with other distances", who);
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const float sign = inverse ? -1.f : 1.f;
-#define POSS_ROTARY(T) rotary_kernel<T><<<rows, 256, 0, st>>>(static_cast<const T *>(x), x_row, x_head, static_cast<T *>(y), y_row, y_head, heads, head_dim, positions, *rope, sign)
+    const int64_t whole = 16 / (int64_t)e;
+    Units n;
+    const bool pieces = rows >= ROWS_MANY && units_of(dtype, head_dim, rope->rot_dim, rope->interleaved, n) && (int64_t)heads * n.units < 1 << 24 && kv_aligned(x, 16) && kv_aligned(y, 16) &&
+                        x_row % whole == 0 && y_row % whole == 0 && x_head % whole == 0 && y_head % whole == 0;
+#define POSS_ROTARY(T)                                                                                                                                    \
+    do {                                                                                                                                                  \
+        const T *xt = static_cast<const T *>(x); T *yt = static_cast<T *>(y);                                                                             \
+        if (!pieces) rotary_kernel<T><<<rows, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, heads, head_dim, positions, *rope, sign);               \
+        else if (rope->interleaved) rotary_rows_kernel<T, true><<<(rows + 3) / 4, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, rows, heads, n, positions, *rope, sign); \
+        else rotary_rows_kernel<T, false><<<(rows + 3) / 4, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, rows, heads, n, positions, *rope, sign);  \
+    } while (0)
     if (dtype == DT_F32) POSS_ROTARY(float); else if (dtype == DT_BF16) POSS_ROTARY(bf16_t); else POSS_ROTARY(f16_t);
 #undef POSS_ROTARY
     return kv_launched(who);
@@ -161,7 +307,7 @@ int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t ro
                    int32_t *slot_positions, void *hip_stream) {
     const char *who = "poss_kv_append";
     if (const char *why = kv_cache_bad(cache)) return set_error(POSS_E_INVALID_ARG, "%s: %s", who, why);
-    if (rows < 0 || n_q_heads < 0 || n_q_heads > 65535) return set_error(POSS_E_INVALID_ARG, "%s: bad shape", who);
+    if (rows < 0 || rows > ROWS_MOST || n_q_heads < 0 || n_q_heads > 65535) return set_error(POSS_E_INVALID_ARG, "%s: bad shape", who);
     if (rope && !rope_ok(*rope, cache->head_dim)) return set_error(POSS_E_INVALID_ARG, "%s: rope: an even rot_dim up to the head's values is wanted", who);
     if (rows == 0 || cache->n_seq == 0) return POSS_OK;
     if (!k || !v || !slots || (n_q_heads && (!q || !q_out)) || ((rope || slot_positions) && !positions)) return set_error(POSS_E_INVALID_ARG, "%s: null argument", who);
@@ -173,13 +319,25 @@ int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t ro
     if (rows > 1 && (k_row < kv_len || v_row < kv_len || (n_q_heads && (q_row < q_len || q_out_row < q_len)))) return set_error(POSS_E_INVALID_ARG, "%s: rows overlap", who);
     if (n_q_heads && rows > 1 && q == q_out && q_row != q_out_row) return set_error(POSS_E_INVALID_ARG, "%s: q_out is q with another distance", who);
     poss_rope none{};
-    const AppendArgs a{n_q_heads, q, q_row, q_out, q_out_row, k, k_row, v, v_row, seq, slots, positions, slot_positions};
+    const AppendArgs a{rows, n_q_heads, q, q_row, q_out, q_out_row, k, k_row, v, v_row, seq, slots, positions, slot_positions};
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const KvView c = kv_view(*cache);
     const poss_rope &r = rope ? *rope : none;
-    if (cache->dtype == DT_F32) append_kernel<float><<<rows, 256, 0, st>>>(c, a, r);
-    else if (cache->dtype == DT_BF16) append_kernel<bf16_t><<<rows, 256, 0, st>>>(c, a, r);
-    else append_kernel<f16_t><<<rows, 256, 0, st>>>(c, a, r);
+    const int64_t whole = 16 / (int64_t)e;
+    Units n;
+    const bool pieces = rows >= ROWS_MANY && units_of(cache->dtype, cache->head_dim, r.rot_dim, r.interleaved, n) && kv_aligned(k, 16) && kv_aligned(v, 16) && k_row % whole == 0 &&
+                        v_row % whole == 0 && (!n_q_heads || (kv_aligned(q, 16) && kv_aligned(q_out, 16) && q_row % whole == 0 && q_out_row % whole == 0));
+    const int row_groups = (rows + 3) / 4;
+    const int64_t squares = ((int64_t)rows + whole - 1 + 8 * whole - 1) / (8 * whole) * ((kv_len + 8 * whole - 1) / (8 * whole));      // (the first rows may begin inside a piece)
+    const int64_t groups = row_groups + (squares + 3) / 4;
+#define POSS_APPEND(T)                                                                                                     \
+    do {                                                                                                                   \
+        if (!pieces || groups > 1 << 23) append_kernel<T><<<rows, 256, 0, st>>>(c, a, r);                                  \
+        else if (r.interleaved) append_rows_kernel<T, true><<<(unsigned)groups, 256, 0, st>>>(c, a, r, n, row_groups);     \
+        else append_rows_kernel<T, false><<<(unsigned)groups, 256, 0, st>>>(c, a, r, n, row_groups);                       \
+    } while (0)
+    if (cache->dtype == DT_F32) POSS_APPEND(float); else if (cache->dtype == DT_BF16) POSS_APPEND(bf16_t); else POSS_APPEND(f16_t);
+#undef POSS_APPEND
     return kv_launched(who);
 }
 
