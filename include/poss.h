@@ -407,11 +407,11 @@ int poss_rope_fill(int32_t rot_dim, int32_t interleaved, double theta, int32_t s
                    double original, double magnitude, poss_rope *out);
 
 /* y = x rotated, rounded once: value d of head h of row r lies at x[r * x_row + h * x_head + d], the same for y.  positions: DEVICE int32[rows], of
- * any sign; at most 2^23 rows.  inverse != 0: by the opposite angle (the transpose, up to magnitude^2: what a gradient is multiplied by).  y may be x, with the same distances. */
+ * any sign; at most 2^21 rows.  inverse != 0: by the opposite angle (the transpose, up to magnitude^2: what a gradient is multiplied by).  y may be x, with the same distances. */
 int poss_rotary(int32_t dtype, const void *x, int64_t x_row, int64_t x_head, void *y, int64_t y_row, int64_t y_head, int32_t rows,
                 int32_t heads, int32_t head_dim, const int32_t *positions, const poss_rope *rope, int32_t inverse, void *hip_stream);
 
-/* New rows on their way into the cache: k and v [rows][n_kv_heads][head_dim] (heads contiguous, rows k_row and v_row values apart) are written to
+/* New rows (at most 2^21) on their way into the cache: k and v [rows][n_kv_heads][head_dim] (heads contiguous, rows k_row and v_row values apart) are written to
  * slot slots[r] of sequence seq[r] (seq NULL: row r is sequence r), keys rotated; q [rows][n_q_heads][head_dim] is rotated into q_out, which may be q
  * (n_q_heads 0: no queries).  rope NULL: nothing is rotated (positions may then be NULL).  A row whose slot, sequence or page is not there has
  * its queries rotated and nothing written: slot -1 marks padding.  Two rows with the same slot leave either's values, value by value.

@@ -31,32 +31,29 @@ __device__ __forceinline__ void rope_angles(const poss_rope &rope, int pos, floa
 }
 
 // ------------------------------------------------------------------------------------------ any size and alignment, few rows
-// A thread's part of a row's heads: pairs, and the values that stay.
+// One head: a lane takes pairs, and the values that stay.
 template <typename T>
-__device__ __forceinline__ void rotate_values(const T *x, int64_t x_head, T *y, int64_t y_head, int heads, int dh, int rot, int interleaved, const float2 *cs) {
-    const int half = rot >> 1, per = half + dh - rot;      // a thread takes a pair, or a value that stays
-    for (int64_t j = threadIdx.x; j < (int64_t)heads * per; j += blockDim.x) {
-        const int64_t h = j / per;
-        const int i = (int)(j - h * per);
-        const T *xi = x + h * x_head;
-        T *yi = y + h * y_head;
-        if (i >= half) { yi[i + half] = xi[i + half]; continue; }
+__device__ __forceinline__ void rotate_head(const T *x, T *y, int dh, int rot, int interleaved, const float2 *cs) {
+    const int half = rot >> 1;
+    for (int i = threadIdx.x & 63; i < half + dh - rot; i += 64) {
+        if (i >= half) { y[i + half] = x[i + half]; continue; }
         const int a = interleaved ? 2 * i : i, b = interleaved ? 2 * i + 1 : i + half;
         float o1, o2;
-        rope_pair(to_f(xi[a]), to_f(xi[b]), cs[i], o1, o2);
-        yi[a] = round_f<T>(o1); yi[b] = round_f<T>(o2);
+        rope_pair(to_f(x[a]), to_f(x[b]), cs[i], o1, o2);
+        y[a] = round_f<T>(o1); y[b] = round_f<T>(o2);
     }
 }
 
-// A workgroup per row.
+// A workgroup per row, a wave per head.
 template <typename T>
-__global__ void __launch_bounds__(256) rotary_kernel(const T *x, int64_t x_row, int64_t x_head, T *y, int64_t y_row, int64_t y_head, int heads, int dh,
+__global__ void __launch_bounds__(1024) rotary_kernel(const T *x, int64_t x_row, int64_t x_head, T *y, int64_t y_row, int64_t y_head, int heads, int dh,
                                                      const int32_t *__restrict__ positions, poss_rope rope, float sign) {
     __shared__ float2 cs[POSS_ROPE_PAIRS];
     const int64_t r = blockIdx.x;
     rope_angles(rope, positions[r], sign, cs, threadIdx.x, blockDim.x);
     __syncthreads();
-    rotate_values(x + r * x_row, x_head, y + r * y_row, y_head, heads, dh, rope.rot_dim, rope.interleaved, cs);
+    for (int64_t h = threadIdx.x >> 6; h < heads; h += blockDim.x >> 6)
+        rotate_head(x + r * x_row + h * x_head, y + r * y_row + h * y_head, dh, rope.rot_dim, rope.interleaved, cs);
 }
 
 struct AppendArgs {
@@ -79,19 +76,23 @@ __device__ __forceinline__ void note_positions(const KvView &c, const AppendArgs
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) append_kernel(KvView c, AppendArgs a, poss_rope rope) {
+__global__ void __launch_bounds__(1024) append_kernel(KvView c, AppendArgs a, poss_rope rope) {
     __shared__ float2 cs[POSS_ROPE_PAIRS];
     const int r = blockIdx.x, dh = c.dh;
     int b, slot;
     const int page = append_page(c, a, r, b, slot);
     if (rope.rot_dim) rope_angles(rope, a.positions[r], 1.f, cs, threadIdx.x, blockDim.x);
     __syncthreads();
-    rotate_values(static_cast<const T *>(a.q) + r * a.q_row, dh, static_cast<T *>(a.q_out) + r * a.q_out_row, dh, a.hq, dh, rope.rot_dim, rope.interleaved, cs);
+    const T *q = static_cast<const T *>(a.q) + r * a.q_row, *k = static_cast<const T *>(a.k) + r * a.k_row, *v = static_cast<const T *>(a.v) + r * a.v_row;
+    T *qo = static_cast<T *>(a.q_out) + r * a.q_out_row, *ck = static_cast<T *>(c.k), *cv = static_cast<T *>(c.v);
+    const int heads = page < 0 ? a.hq : a.hq + 2 * c.hkv;
+    for (int h = threadIdx.x >> 6; h < heads; h += blockDim.x >> 6) {          // heads of queries, keys, values
+        const int hk = h - a.hq, hv = hk - c.hkv;
+        if (hv >= 0)
+            for (int d = threadIdx.x & 63; d < dh; d += 64) cv[kv_value_at(c, page, hv, d, slot)] = v[hv * dh + d];
+        else rotate_head(hk < 0 ? q + h * dh : k + hk * dh, hk < 0 ? qo + h * dh : ck + kv_key_at(c, page, hk, slot), dh, rope.rot_dim, rope.interleaved, cs);
+    }
     if (page < 0) return;
-    T *ck = static_cast<T *>(c.k) + kv_key_at(c, page, 0, slot), *cv = static_cast<T *>(c.v) + kv_value_at(c, page, 0, 0, slot);
-    rotate_values(static_cast<const T *>(a.k) + r * a.k_row, dh, ck, (int64_t)dh << c.shift, c.hkv, dh, rope.rot_dim, rope.interleaved, cs);
-    const T *v = static_cast<const T *>(a.v) + r * a.v_row;
-    for (int j = threadIdx.x; j < c.hkv * dh; j += blockDim.x) cv[(int64_t)j << c.shift] = v[j];
     note_positions(c, a, r, b, slot, threadIdx.x, blockDim.x);
 }
 
@@ -152,8 +153,8 @@ __global__ void __launch_bounds__(256) rotary_rows_kernel(const T *x, int64_t x_
 
 // Queries and keys: a wave per row, in the first workgroups.  Values: behind them, a wave per square of eight by eight pieces - 16-bit types 64 rows by 64 dims -
 // of which a lane turns a square of E by E values over in its registers, so that the rows of consecutive slots leave as whole lines of a value row.
-// That needs E rows with consecutive slots of one page, the first at a multiple of E; squares are laid so for the rows that follow the call's first slot.
-// Other squares are written value by value (8192 rows of 8 value heads all at once: 88 us, whole lines 9).
+// That needs E rows with consecutive slots, the first at a multiple of E; squares are laid so for the rows that follow the call's first slot.
+// In other squares a lane takes a row and writes value by value: of consecutive slots 64 stand side by side.
 template <typename T, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) append_rows_kernel(KvView c, AppendArgs a, poss_rope rope, Units n, int row_groups) {
     constexpr int E = 16 / sizeof(T);
@@ -176,41 +177,42 @@ __global__ void __launch_bounds__(256) append_rows_kernel(KvView c, AppendArgs a
     }
     const int across = (c.hkv * dh + 8 * E - 1) / (8 * E);                     // squares of a row of values
     const int64_t square = (int64_t)(blockIdx.x - row_groups) * 4 + wave;
-    const int sr = (int)(square / across), d0 = (int)(square - (int64_t)sr * across) * 8 * E + (lane >> 3) * E;
-    const int first = a.slots[0], r0 = sr * 8 * E + (lane & 7) * E - (first > 0 ? first & (E - 1) : 0);
-    if (r0 >= a.rows || d0 >= c.hkv * dh) return;
+    const int sr = (int)(square / across), dims = c.hkv * dh, d_first = (int)(square - (int64_t)sr * across) * 8 * E;
+    const int shift = a.slots[0] > 0 ? a.slots[0] & (E - 1) : 0, r_first = sr * 8 * E - shift;
     const T *v = static_cast<const T *>(a.v);
     T *cv = static_cast<T *>(c.v);
-    if (r0 >= 0 && r0 + E <= a.rows) {
-        bool run = true;
-        int b, slot;
-        const int page = append_page(c, a, r0, b, slot);
-        for (int e = 1; e < E; ++e) run = run && a.slots[r0 + e] == slot + e && (a.seq ? a.seq[r0 + e] : r0 + e) == b;
-        if (run && page >= 0 && slot % E == 0) {
-            vec in[E];
+    // lane i looks up row i of the square's 8 E
+    const int mine = r_first + lane;
+    int b = -1, slot = -1;
+    const int page = lane < 8 * E && mine >= 0 && mine < a.rows ? append_page(c, a, mine, b, slot) : -1;
+    const int place = lane & (E - 1), head_slot = __shfl(slot, lane - place), head_b = __shfl(b, lane - place);
+    const bool run = page >= 0 && head_slot % E == 0 && slot == head_slot + place && b == head_b;
+    if (__all(run || (lane >= 8 * E))) {
+        const int g = lane & 7, d0 = d_first + (lane >> 3) * E, r0 = r_first + g * E;
+        const int page0 = __shfl(page, g * E), slot0 = __shfl(slot, g * E);
+        if (d0 >= dims) return;
+        vec in[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) in[e] = *reinterpret_cast<const vec *>(v + (r0 + e) * a.v_row + d0);
-            T *to = cv + kv_value_at(c, page, 0, d0, slot);                    // (heads and dims are one sequence of value rows)
+        for (int e = 0; e < E; ++e) in[e] = *reinterpret_cast<const vec *>(v + (int64_t)(r0 + e) * a.v_row + d0);
+        T *to = cv + kv_value_at(c, page0, 0, d0, slot0);                      // (heads and dims are one sequence of value rows)
 #pragma unroll
-            for (int d = 0; d < E; ++d) {
-                vec o;
+        for (int d = 0; d < E; ++d) {
+            vec o;
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = in[e][d];
-                *reinterpret_cast<vec *>(to + ((int64_t)d << c.shift)) = o;
-            }
-            return;
+            for (int e = 0; e < E; ++e) o[e] = in[e][d];
+            *reinterpret_cast<vec *>(to + ((int64_t)d << c.shift)) = o;
         }
+        return;
     }
-    for (int e = 0; e < E; ++e) {
-        const int r = r0 + e;
-        if (r < 0 || r >= a.rows) continue;
-        int b, slot;
-        const int page = append_page(c, a, r, b, slot);
-        if (page < 0) continue;
-        const vec in = *reinterpret_cast<const vec *>(v + r * a.v_row + d0);
-        T *to = cv + kv_value_at(c, page, 0, d0, slot);
+    // any rows: a lane per row, so that what lies side by side in a value row leaves side by side
+    if (page < 0) return;
+    T *to = cv + kv_value_at(c, page, 0, d_first, slot);
+    const int across_d = min(8 * E, dims - d_first);
+#pragma unroll 2
+    for (int d = 0; d < across_d; d += E) {
+        const vec in = *reinterpret_cast<const vec *>(v + mine * a.v_row + d_first + d);
 #pragma unroll
-        for (int d = 0; d < E; ++d) to[(int64_t)d << c.shift] = in[d];
+        for (int e = 0; e < E; ++e) to[(int64_t)(d + e) << c.shift] = in[e];
     }
 }
 
@@ -229,7 +231,8 @@ static bool units_of(int dt, int dh, int rot, bool interleaved, Units &n) {
 using namespace poss;
 
 namespace {
-constexpr int ROWS_MANY = 16, ROWS_MOST = 1 << 23;
+constexpr int ROWS_MANY = 200, ROWS_MOST = 1 << 21;     // (threads of a launch are counted in 32 bits)
+int row_threads(int heads) { return heads >= 16 ? 1024 : heads > 4 ? 512 : 256; }
 bool rope_ok(const poss_rope &r, int head_dim) { return r.rot_dim >= 2 && r.rot_dim <= 2 * POSS_ROPE_PAIRS && r.rot_dim % 2 == 0 && r.rot_dim <= head_dim; }
 }  // namespace
 
@@ -287,13 +290,14 @@ int poss_rotary(int32_t dtype, const void *x, int64_t x_row, int64_t x_head, voi
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const float sign = inverse ? -1.f : 1.f;
     const int64_t whole = 16 / (int64_t)e;
+    const int threads = row_threads(heads);
     Units n;
     const bool pieces = rows >= ROWS_MANY && units_of(dtype, head_dim, rope->rot_dim, rope->interleaved, n) && (int64_t)heads * n.units < 1 << 24 && kv_aligned(x, 16) && kv_aligned(y, 16) &&
                         x_row % whole == 0 && y_row % whole == 0 && x_head % whole == 0 && y_head % whole == 0;
 #define POSS_ROTARY(T)                                                                                                                                    \
     do {                                                                                                                                                  \
         const T *xt = static_cast<const T *>(x); T *yt = static_cast<T *>(y);                                                                             \
-        if (!pieces) rotary_kernel<T><<<rows, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, heads, head_dim, positions, *rope, sign);               \
+        if (!pieces) rotary_kernel<T><<<rows, threads, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, heads, head_dim, positions, *rope, sign);               \
         else if (rope->interleaved) rotary_rows_kernel<T, true><<<(rows + 3) / 4, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, rows, heads, n, positions, *rope, sign); \
         else rotary_rows_kernel<T, false><<<(rows + 3) / 4, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, rows, heads, n, positions, *rope, sign);  \
     } while (0)
@@ -324,6 +328,7 @@ int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t ro
     const KvView c = kv_view(*cache);
     const poss_rope &r = rope ? *rope : none;
     const int64_t whole = 16 / (int64_t)e;
+    const int threads = row_threads(n_q_heads + 2 * cache->n_kv_heads);
     Units n;
     const bool pieces = rows >= ROWS_MANY && units_of(cache->dtype, cache->head_dim, r.rot_dim, r.interleaved, n) && kv_aligned(k, 16) && kv_aligned(v, 16) && k_row % whole == 0 &&
                         v_row % whole == 0 && (!n_q_heads || (kv_aligned(q, 16) && kv_aligned(q_out, 16) && q_row % whole == 0 && q_out_row % whole == 0));
@@ -332,7 +337,7 @@ int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t ro
     const int64_t groups = row_groups + (squares + 3) / 4;
 #define POSS_APPEND(T)                                                                                                     \
     do {                                                                                                                   \
-        if (!pieces || groups > 1 << 23) append_kernel<T><<<rows, 256, 0, st>>>(c, a, r);                                  \
+        if (!pieces || groups > 1 << 23) append_kernel<T><<<rows, threads, 0, st>>>(c, a, r);                                  \
         else if (r.interleaved) append_rows_kernel<T, true><<<(unsigned)groups, 256, 0, st>>>(c, a, r, n, row_groups);     \
         else append_rows_kernel<T, false><<<(unsigned)groups, 256, 0, st>>>(c, a, r, n, row_groups);                       \
     } while (0)
