@@ -1,8 +1,8 @@
 // Eviction from a paged cache by accumulated attention weight (include/poss.h: poss_kv_evict).
 //
 // Slots are ranked by a 32-bit key: those that always stay above all, NaN below all, the others by their weight, mapped so that unsigned order is
-// the order of the numbers (-0 as 0).  Of the n = min(length, budget) that stay, the n-th largest key is found digit by digit
-// (four counts of 8 bits each); of the slots with that very key the lowest stay.  Holes below n and kept slots from n on are equally many:
+// the order of the numbers (-0 as 0).  Of the n = min(length, budget) that stay the n-th largest key is found; of the slots with that very key the lowest
+// stay.  Holes below n and kept slots from n on are equally many:
 // the j-th hole is filled from the j-th of those.  No source is a destination, so the moves need no order.
 #include "kv.h"
 
@@ -20,9 +20,154 @@ struct EvictArgs {
     int32_t *kept; float *weights_out; int32_t *positions_out, *lengths_out;
 };
 
-constexpr int EVICT_THREADS = 1024;
+constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / 64;
 
-// Sum over the workgroup of the threads before this one, and of all (LDS: 17 ints).
+__device__ __forceinline__ int lanes_below(unsigned long long them) {      // of them, those before this lane
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(them >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)them, 0));
+}
+// Sum of a number per wave over the waves; one barrier.  red: two sets of EVICT_WAVES, used in turn.
+__device__ __forceinline__ int waves_sum(int x, int *red) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
+    int s = 0;
+#pragma unroll
+    for (int w = 0; w < EVICT_WAVES; ++w) s += red[w];
+    return s;
+}
+__device__ __forceinline__ int block_newest(int newest, int *red) {
+    for (int o = 32; o; o >>= 1) newest = max(newest, __shfl_xor(newest, o));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = newest;
+    __syncthreads();
+    for (int w = 0; w < EVICT_WAVES; ++w) newest = max(newest, red[w]);
+    return newest;
+}
+__device__ __forceinline__ uint32_t slot_key(float w, int pos, int first, int64_t border) { return pos < first || pos > border ? 0xffffffffu : weight_key(w); }
+
+// One head's rows of the arrays, and what every kernel does with them first: what lies beyond the new length, and a head that loses nothing.
+struct EvictHead { const float *w; const int32_t *pos; int32_t *kept; float *wo; int32_t *po; int len, n; };
+__device__ __forceinline__ EvictHead evict_head(const KvView &c, const EvictArgs &a) {
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    const int64_t row = (int64_t)b * c.hkv + h, base = row * c.slots;
+    EvictHead e{a.weights + base, a.positions + base, a.kept + row * a.budget, a.weights_out + base, a.positions_out + base, a.lengths[b], 0};
+    e.len = e.len < 0 ? 0 : e.len > c.slots ? c.slots : e.len;
+    e.n = e.len < a.budget ? e.len : a.budget;
+    if (h == 0 && tid == 0) a.lengths_out[b] = e.n;
+    for (int i = e.n + tid; i < a.budget; i += EVICT_THREADS) e.kept[i] = -1;
+    for (int i = e.n + tid; i < c.slots; i += EVICT_THREADS) { e.wo[i] = 0.f; e.po[i] = -1; }
+    if (e.n == e.len)
+        for (int i = tid; i < e.n; i += EVICT_THREADS) { e.kept[i] = i; e.wo[i] = e.w[i]; e.po[i] = e.pos[i]; }
+    return e;
+}
+
+// One workgroup per sequence and key head, up to K * 1024 slots: slot k * 1024 + t is thread t's k-th, its key stays in a register.  The n-th largest key is found from the
+// highest bit down, two bits at a time, by counting the keys from each candidate on: counting is ballots, with no contention for
+// a histogram's few busy bins.  It ends as soon as exactly n keys are counted, for distinct weights long before the last bit.
+template <int K>
+__global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, EvictArgs a) {
+    __shared__ int red[2][3][EVICT_WAVES], before[K][EVICT_WAVES];
+    __shared__ uint16_t movers[K * EVICT_THREADS / 2];       // as many as there are holes, at most half of the slots
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const EvictHead e = evict_head(c, a);
+    const int len = e.len, n = e.n;
+    if (n == len) return;
+    float w[K];
+    int pos[K];
+    int newest = INT32_MIN;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int i = k * EVICT_THREADS + tid;
+        w[k] = i < len ? e.w[i] : 0.f;
+        pos[k] = i < len ? e.pos[i] : INT32_MIN;
+        newest = max(newest, pos[k]);
+    }
+    const int64_t border = (int64_t)block_newest(newest, red[0][0]) - a.recent;
+    uint32_t key[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) key[k] = k * EVICT_THREADS + tid < len ? slot_key(w[k], pos[k], a.first, border) : 0;
+    uint32_t found = 0;                                      // the keys from here on are at least n
+    int above = 0;                                           // the keys beyond it, once it is the n-th
+    bool exact = false;                                      // just n keys from `found` on
+    int turn = 1;
+    for (int shift = 30; shift >= 0 && !exact; shift -= 2, turn ^= 1) {
+        int many[3] = {0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < 3; ++j) many[j] += __popcll(__ballot(key[k] >= (found | (uint32_t)(j + 1) << shift)));
+        if (lane == 0)
+            for (int j = 0; j < 3; ++j) red[turn][j][wave] = many[j];
+        __syncthreads();
+        for (int j = 0; j < 3; ++j) {
+            many[j] = 0;
+#pragma unroll
+            for (int v = 0; v < EVICT_WAVES; ++v) many[j] += red[turn][j][v];
+        }
+        const int step = many[2] >= n ? 3 : many[1] >= n ? 2 : many[0] >= n ? 1 : 0;
+        found |= (uint32_t)step << shift;
+        exact = step && many[step - 1] == n;
+    }
+    // of the keys equal to the n-th the first `want`, in slot order
+    int want = 0;
+    if (!exact) {
+        int more = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) more += __popcll(__ballot(key[k] > found));
+        above = waves_sum(more, red[turn][0]);
+        want = n - above;
+    }
+    uint32_t stays = 0;
+    if (exact) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) if (k * EVICT_THREADS + tid < len && key[k] >= found) stays |= 1u << k;
+    } else {
+        unsigned long long equal[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            equal[k] = __ballot(k * EVICT_THREADS + tid < len && key[k] == found);
+            if (lane == 0) before[k][wave] = __popcll(equal[k]);
+        }
+        __syncthreads();
+        int base = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            int mine = base;
+            for (int v = 0; v < EVICT_WAVES; ++v) { const int x = before[k][v]; base += x; if (v < wave) mine += x; }
+            const bool eq = equal[k] >> lane & 1;
+            if (k * EVICT_THREADS + tid < len && (key[k] > found || (eq && mine + lanes_below(equal[k]) < want))) stays |= 1u << k;
+        }
+        __syncthreads();
+    }
+    // holes below n and movers from n on, counted off in slot order in the two halves of a number
+    unsigned long long holes[K], moves[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int i = k * EVICT_THREADS + tid;
+        holes[k] = __ballot(i < n && !(stays >> k & 1));
+        moves[k] = __ballot(i >= n && (stays >> k & 1));
+        if (lane == 0) before[k][wave] = __popcll(holes[k]) | __popcll(moves[k]) << 16;
+    }
+    __syncthreads();
+    int hole_at[K], base = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        int mine = base;
+        for (int v = 0; v < EVICT_WAVES; ++v) { const int x = before[k][v]; base += x; if (v < wave) mine += x; }
+        hole_at[k] = holes[k] >> lane & 1 ? (mine & 0xffff) + lanes_below(holes[k]) : -1;
+        if (moves[k] >> lane & 1) movers[(mine >> 16) + lanes_below(moves[k])] = (uint16_t)(k * EVICT_THREADS + tid);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int i = k * EVICT_THREADS + tid;
+        if (i >= n) continue;
+        int from = i;
+        if (hole_at[k] >= 0) { from = movers[hole_at[k]]; w[k] = e.w[from]; pos[k] = e.pos[from]; }
+        e.kept[i] = from; e.wo[i] = w[k]; e.po[i] = pos[k];
+    }
+}
+
+// The same for any number of slots: keys are read again for every pass, the n-th largest is found in digits of 12, 12 and 8 bits (the first holds sign,
+// exponent and three bits of mantissa: weights spread over its bins).
 __device__ __forceinline__ int block_scan(int x, int *red, int &all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int s = x;
@@ -31,107 +176,120 @@ __device__ __forceinline__ int block_scan(int x, int *red, int &all) {
     if (lane == 63) red[wave] = s;
     __syncthreads();
     int before = 0; all = 0;
-    for (int w = 0; w < EVICT_THREADS / 64; ++w) { if (w < wave) before += red[w]; all += red[w]; }
+    for (int w = 0; w < EVICT_WAVES; ++w) { if (w < wave) before += red[w]; all += red[w]; }
     return before + s - x;
 }
-
-// One workgroup per sequence and key head.
-__global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, EvictArgs a) {
-    __shared__ int hist[256], red[17], pick[2];
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-    const int64_t row = (int64_t)b * c.hkv + h, base = row * c.slots;
-    const float *w = a.weights + base;
-    const int32_t *pos = a.positions + base;
-    int32_t *kept = a.kept + row * a.budget;
-    float *wo = a.weights_out + base;
-    int32_t *po = a.positions_out + base;
-    int len = a.lengths[b];
-    len = len < 0 ? 0 : len > c.slots ? c.slots : len;
-    const int n = len < a.budget ? len : a.budget;
-    if (h == 0 && tid == 0) a.lengths_out[b] = n;
-    for (int i = n + tid; i < a.budget; i += EVICT_THREADS) kept[i] = -1;
-    for (int i = n + tid; i < c.slots; i += EVICT_THREADS) { wo[i] = 0.f; po[i] = -1; }
-    if (n == len) {
-        for (int i = tid; i < n; i += EVICT_THREADS) { kept[i] = i; wo[i] = w[i]; po[i] = pos[i]; }
-        return;
-    }
-    // the newest position
+__global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView c, EvictArgs a) {
+    constexpr int BINS = 4096, EACH = BINS / EVICT_THREADS;
+    __shared__ int hist[BINS], red[EVICT_WAVES], pick[2];
+    const int tid = threadIdx.x;
+    const EvictHead e = evict_head(c, a);
+    const int len = e.len, n = e.n;
+    if (n == len) return;
     int newest = INT32_MIN;
-    for (int i = tid; i < len; i += EVICT_THREADS) newest = max(newest, pos[i]);
-    for (int o = 32; o; o >>= 1) newest = max(newest, __shfl_xor(newest, o));
-    if ((tid & 63) == 0) red[tid >> 6] = newest;
-    __syncthreads();
-    for (int i = 0; i < EVICT_THREADS / 64; ++i) newest = max(newest, red[i]);
-    const int64_t border = (int64_t)newest - a.recent;
-    auto key_of = [&](int i) { const int p = pos[i]; return p < a.first || p > border ? 0xffffffffu : weight_key(w[i]); };
-    // the n-th largest key
+    for (int i = tid; i < len; i += EVICT_THREADS) newest = max(newest, e.pos[i]);
+    const int64_t border = (int64_t)block_newest(newest, red) - a.recent;
+    auto key_of = [&](int i) { return slot_key(e.w[i], e.pos[i], a.first, border); };
     uint32_t prefix = 0;
     int want = n;                                    // which one of the keys that share the digits found so far
-    for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int digit = 0; digit < 3; ++digit) {
+        const int shift = digit == 0 ? 20 : digit == 1 ? 8 : 0, bits = digit == 2 ? 8 : 12;
         __syncthreads();
-        for (int i = tid; i < 256; i += EVICT_THREADS) hist[i] = 0;
+        for (int i = tid; i < BINS; i += EVICT_THREADS) hist[i] = 0;
         __syncthreads();
+#pragma unroll 4
         for (int i = tid; i < len; i += EVICT_THREADS) {
             const uint32_t k = key_of(i);
-            if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
+            if (digit == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[(k >> shift) & ((1 << bits) - 1)], 1);
         }
         __syncthreads();
-        if (tid == 0) {
-            int d = 255;
-            while (want > hist[d]) want -= hist[d--];
-            pick[0] = d; pick[1] = want;
+        // thread t looks at bins from the top: EACH t .. EACH t + EACH - 1 counted from the last
+        int mine[EACH], sum = 0, all;
+        for (int j = 0; j < EACH; ++j) sum += mine[j] = hist[BINS - 1 - (tid * EACH + j)];
+        int at = block_scan(sum, red, all);
+        for (int j = 0; j < EACH; ++j) {
+            if (at < want && want <= at + mine[j]) { pick[0] = BINS - 1 - (tid * EACH + j); pick[1] = want - at; }
+            at += mine[j];
         }
         __syncthreads();
-        prefix = prefix << 8 | (uint32_t)pick[0];
+        prefix = prefix << bits | (uint32_t)pick[0];
         want = pick[1];
     }
     // kept: keys above the prefix, and the first `want` with it.  First the holes and movers are counted off in index order.
     int equal_before = 0, holes_before = 0, movers_before = 0;
     for (int i0 = 0; i0 < len; i0 += EVICT_THREADS) {
         const int i = i0 + tid;
-        const uint32_t k = i < len ? key_of(i) : 0;
-        const bool in = i < len, eq = in && k == prefix;
+        const bool in = i < len;
+        const uint32_t k = in ? key_of(i) : 0;
+        const bool eq = in && k == prefix;
         int all;
         const int rank = equal_before + block_scan(eq, red, all);
         equal_before += all;
         const bool stays = in && (k > prefix || (eq && rank < want));
         const bool mover = stays && i >= n, hole = in && i < n && !stays;
-        int holes, movers;
-        const int hr = holes_before + block_scan(hole, red, holes), mr = movers_before + block_scan(mover, red, movers);
-        holes_before += holes; movers_before += movers;
-        // the lists meet in `kept`: a hole notes its rank as -2 - rank, and po[n ..] lends its room to the movers
-        if (hole) kept[i] = -2 - hr;
-        else if (in && i < n) { kept[i] = i; wo[i] = w[i]; po[i] = pos[i]; }
-        if (mover) po[n + mr] = i;
+        const int at = block_scan((int)hole | (int)mover << 16, red, all);
+        // the lists meet in the outputs: a hole notes its rank as -2 - rank, and po[n ..] lends its room to the movers
+        if (hole) e.kept[i] = -2 - (holes_before + (at & 0xffff));
+        else if (in && i < n) { e.kept[i] = i; e.wo[i] = e.w[i]; e.po[i] = e.pos[i]; }
+        if (mover) e.po[n + movers_before + (at >> 16)] = i;
+        holes_before += all & 0xffff; movers_before += all >> 16;
     }
     __syncthreads();
-    __threadfence_block();
     for (int i = tid; i < n; i += EVICT_THREADS) {
-        const int k = kept[i];
+        const int k = e.kept[i];
         if (k >= 0) continue;
-        const int s = po[n + (-2 - k)];
-        kept[i] = s; wo[i] = w[s]; po[i] = pos[s];
+        const int s = e.po[n + (-2 - k)];
+        e.kept[i] = s; e.wo[i] = e.w[s]; e.po[i] = e.pos[s];
     }
     __syncthreads();
-    for (int i = n + tid; i < n + movers_before; i += EVICT_THREADS) po[i] = -1;
+    for (int i = n + tid; i < n + movers_before; i += EVICT_THREADS) e.po[i] = -1;
 }
 
-// 64 slots below the budget of one sequence and head per workgroup: those whose source is another take its key and value.
+// The slots 256 x .. below the budget of one sequence and head whose source is another: listed, then moved, keys in pieces of 16 bytes, values with a lane per
+// slot: sources ascend with destinations, so that the values of 64 of them lie in a few lines of each value row.
+constexpr int MOVE_SLOTS = 256;
 template <typename T>
 __global__ void __launch_bounds__(256) evict_move_kernel(KvView c, const int32_t *__restrict__ kept, int budget) {
-    const int h = blockIdx.y, b = blockIdx.z, d0 = threadIdx.x & 31;
-    const int32_t *list = kept + ((int64_t)b * c.hkv + h) * budget;
+    constexpr int E = 16 / sizeof(T), AHEAD = 8;
+    typedef T vec __attribute__((ext_vector_type(E)));
+    __shared__ int64_t key_from[MOVE_SLOTS], key_to[MOVE_SLOTS], value_from[MOVE_SLOTS], value_to[MOVE_SLOTS];
+    __shared__ int count;
+    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, to = blockIdx.x * MOVE_SLOTS + tid;
+    const int from = to < budget ? kept[((int64_t)b * c.hkv + h) * budget + to] : -1;
+    int pf = -1, pt = -1;
+    if (from >= 0 && from != to) { pf = kv_page(c, b, from); pt = kv_page(c, b, to); }
+    const bool moves = pf >= 0 && pt >= 0;
+    if (tid == 0) count = 0;
+    __syncthreads();
+    // (the order between waves does not matter, a wave's own slots stay together)
+    const unsigned long long them = __ballot(moves);
+    int at = 0;
+    if ((tid & 63) == 0 && them) at = atomicAdd(&count, __popcll(them));
+    at = __shfl(at, 0) + lanes_below(them);
+    if (moves) {
+        key_from[at] = kv_key_at(c, pf, h, from); key_to[at] = kv_key_at(c, pt, h, to);
+        value_from[at] = kv_value_at(c, pf, h, 0, from); value_to[at] = kv_value_at(c, pt, h, 0, to);
+    }
+    __syncthreads();
+    const int n = count;
+    if (n == 0) return;
     T *k = static_cast<T *>(c.k), *v = static_cast<T *>(c.v);
-    for (int j = threadIdx.x >> 5; j < 64; j += 8) {
-        const int to = blockIdx.x * 64 + j;
-        if (to >= budget) break;
-        const int from = list[to];
-        if (from < 0 || from == to) continue;
-        const int pf = kv_page(c, b, from), pt = kv_page(c, b, to);
-        if (pf < 0 || pt < 0) continue;
-        for (int d = d0; d < c.dh; d += 32) {
-            k[kv_key_at(c, pt, h, to) + d] = k[kv_key_at(c, pf, h, from) + d];
-            v[kv_value_at(c, pt, h, d, to)] = v[kv_value_at(c, pf, h, d, from)];
+    const int pieces = c.dh / E;
+#pragma unroll 2
+    for (int x = tid; x < n * pieces; x += 256) {
+        const int i = x / pieces, d = (x - i * pieces) * E;
+        *reinterpret_cast<vec *>(k + key_to[i] + d) = *reinterpret_cast<const vec *>(k + key_from[i] + d);
+    }
+    const int each = c.dh / 4, d0 = (tid >> 6) * each;       // a wave takes a quarter of the value rows (a multiple of AHEAD)
+    for (int i = tid & 63; i < n; i += 64) {
+        const T *vf = v + value_from[i];
+        T *vt = v + value_to[i];
+        for (int d = d0; d < d0 + each; d += AHEAD) {
+            T got[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) got[j] = vf[(int64_t)(d + j) << c.shift];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) vt[(int64_t)(d + j) << c.shift] = got[j];
         }
     }
 }
@@ -154,9 +312,14 @@ extern "C" int poss_kv_evict(const poss_kv_cache *cache, const float *weights, c
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const KvView c = kv_view(*cache);
     const EvictArgs a{weights, positions, lengths, budget, first, recent, kept, weights_out, positions_out, lengths_out};
-    evict_select_kernel<<<dim3(c.hkv, c.n_seq), EVICT_THREADS, 0, st>>>(c, a);
+    const dim3 heads(c.hkv, c.n_seq);
+    if (c.slots <= 2 * EVICT_THREADS) evict_select_kernel<2><<<heads, EVICT_THREADS, 0, st>>>(c, a);
+    else if (c.slots <= 4 * EVICT_THREADS) evict_select_kernel<4><<<heads, EVICT_THREADS, 0, st>>>(c, a);
+    else if (c.slots <= 8 * EVICT_THREADS) evict_select_kernel<8><<<heads, EVICT_THREADS, 0, st>>>(c, a);
+    else if (c.slots <= 16 * EVICT_THREADS) evict_select_kernel<16><<<heads, EVICT_THREADS, 0, st>>>(c, a);
+    else evict_select_long_kernel<<<heads, EVICT_THREADS, 0, st>>>(c, a);
     const int most = budget < c.slots ? budget : c.slots;
-    const dim3 grid((most + 63) / 64, c.hkv, c.n_seq);
+    const dim3 grid((most + MOVE_SLOTS - 1) / MOVE_SLOTS, c.hkv, c.n_seq);
     if (cache->dtype == DT_F32) evict_move_kernel<float><<<grid, 256, 0, st>>>(c, kept, budget);
     else if (cache->dtype == DT_BF16) evict_move_kernel<bf16_t><<<grid, 256, 0, st>>>(c, kept, budget);
     else evict_move_kernel<f16_t><<<grid, 256, 0, st>>>(c, kept, budget);
