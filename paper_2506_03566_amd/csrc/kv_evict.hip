@@ -166,83 +166,177 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, E
     }
 }
 
-// The same for any number of slots: keys are read again for every pass, the n-th largest is found in digits of 12, 12 and 8 bits (the first holds sign,
-// exponent and three bits of mantissa: weights spread over its bins).
-__device__ __forceinline__ int block_scan(int x, int *red, int &all) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int s = x;
-    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(s, o); if (lane >= o) s += y; }
-    __syncthreads();
-    if (lane == 63) red[wave] = s;
-    __syncthreads();
-    int before = 0; all = 0;
-    for (int w = 0; w < EVICT_WAVES; ++w) { if (w < wave) before += red[w]; all += red[w]; }
-    return before + s - x;
-}
+// The same for any number of slots: what is read is read again for every pass, by each wave its own stretch of slots, 64 side by side, with a barrier only between passes.  The
+// 12 highest bits of the n-th key (sign, exponent, three bits of mantissa) come from a histogram, the others by counting among the keys that share them, in LDS;
+// where those are too many (equal weights), from two more histograms.
 __global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView c, EvictArgs a) {
-    constexpr int BINS = 4096, EACH = BINS / EVICT_THREADS;
-    __shared__ int hist[BINS], red[EVICT_WAVES], pick[2];
-    const int tid = threadIdx.x;
+    constexpr int BINS = 4096, EACH = BINS / EVICT_THREADS, AHEAD = 16;      // AHEAD: loads of an array on their way at a time
+    __shared__ int hist[BINS], red[2][3][EVICT_WAVES], pick[3];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const EvictHead e = evict_head(c, a);
     const int len = e.len, n = e.n;
     if (n == len) return;
+    const int per = (len + 64 * EVICT_WAVES - 1) / (64 * EVICT_WAVES) * 64, i0 = wave * per + lane, i1 = min(len, (wave + 1) * per);
     int newest = INT32_MIN;
-    for (int i = tid; i < len; i += EVICT_THREADS) newest = max(newest, e.pos[i]);
-    const int64_t border = (int64_t)block_newest(newest, red) - a.recent;
-    auto key_of = [&](int i) { return slot_key(e.w[i], e.pos[i], a.first, border); };
+    for (int i = i0; i < i1; i += 64 * AHEAD) {
+        int pos[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) pos[u] = i + 64 * u < i1 ? e.pos[i + 64 * u] : INT32_MIN;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) newest = max(newest, pos[u]);
+    }
+    const int64_t border = (int64_t)block_newest(newest, red[0][0]) - a.recent;
+    float w[AHEAD];
+    int pos[AHEAD];
+    auto load = [&](int i) {                                   // slots i, i + 64 ..
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) { const bool in = i + 64 * u < i1; w[u] = in ? e.w[i + 64 * u] : 0.f; pos[u] = in ? e.pos[i + 64 * u] : 0; }
+    };
+    auto key_of = [&](int u) { return slot_key(w[u], pos[u], a.first, border); };
+    // the digit of `bits` bits at `shift` of the key that is the want-th largest of those with this prefix: prefix, want, and how many share the new prefix
     uint32_t prefix = 0;
-    int want = n;                                    // which one of the keys that share the digits found so far
-    for (int digit = 0; digit < 3; ++digit) {
-        const int shift = digit == 0 ? 20 : digit == 1 ? 8 : 0, bits = digit == 2 ? 8 : 12;
+    int want = n, share = len;
+    auto digit = [&](int shift, int bits) {
         __syncthreads();
         for (int i = tid; i < BINS; i += EVICT_THREADS) hist[i] = 0;
         __syncthreads();
-#pragma unroll 4
-        for (int i = tid; i < len; i += EVICT_THREADS) {
-            const uint32_t k = key_of(i);
-            if (digit == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[(k >> shift) & ((1 << bits) - 1)], 1);
+        for (int i = i0; i < i1; i += 64 * AHEAD) {
+            load(i);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const uint32_t k = key_of(u);
+                if (i + 64 * u < i1 && (shift + bits == 32 || k >> (shift + bits & 31) == prefix)) atomicAdd(&hist[k >> shift & ((1 << bits) - 1)], 1);
+            }
         }
         __syncthreads();
-        // thread t looks at bins from the top: EACH t .. EACH t + EACH - 1 counted from the last
-        int mine[EACH], sum = 0, all;
+        // thread t looks at bins EACH t .. EACH t + EACH - 1, counted from the last
+        int mine[EACH], sum = 0;
+#pragma unroll
         for (int j = 0; j < EACH; ++j) sum += mine[j] = hist[BINS - 1 - (tid * EACH + j)];
-        int at = block_scan(sum, red, all);
+        int at = sum;
+        for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(at, o); if (lane >= o) at += y; }
+        if (lane == 63) red[1][0][wave] = at;
+        __syncthreads();
+        at -= sum;
+        for (int v = 0; v < wave; ++v) at += red[1][0][v];
+#pragma unroll
         for (int j = 0; j < EACH; ++j) {
-            if (at < want && want <= at + mine[j]) { pick[0] = BINS - 1 - (tid * EACH + j); pick[1] = want - at; }
+            if (at < want && want <= at + mine[j]) { pick[0] = BINS - 1 - (tid * EACH + j); pick[1] = want - at; pick[2] = mine[j]; }
             at += mine[j];
         }
         __syncthreads();
         prefix = prefix << bits | (uint32_t)pick[0];
-        want = pick[1];
+        want = pick[1]; share = pick[2];
+    };
+    digit(20, 12);
+    if (share <= BINS) {
+        if (tid == 0) pick[0] = 0;
+        __syncthreads();
+        for (int i = i0; i < i1; i += 64 * AHEAD) {
+            load(i);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const uint32_t k = key_of(u);
+                if (i + 64 * u < i1 && k >> 20 == prefix) hist[atomicAdd(&pick[0], 1)] = (int)k;      // (in any order: they are counted)
+            }
+        }
+        __syncthreads();
+        uint32_t key[EACH], found = prefix << 20;
+        bool in[EACH];
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) { in[j] = j * EVICT_THREADS + tid < share; key[j] = in[j] ? (uint32_t)hist[j * EVICT_THREADS + tid] : 0; }
+        int turn = 0, beyond = 0, least = share;               // keys above `found`'s stretch, and from it on
+        for (int shift = 18; shift >= 0; shift -= 2, turn ^= 1) {
+            int many[3] = {0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < EACH; ++k)
+#pragma unroll
+                for (int j = 0; j < 3; ++j) many[j] += __popcll(__ballot(in[k] && key[k] >= (found | (uint32_t)(j + 1) << shift)));
+            if (lane == 0)
+                for (int j = 0; j < 3; ++j) red[turn][j][wave] = many[j];
+            __syncthreads();
+            for (int j = 0; j < 3; ++j) {
+                many[j] = 0;
+#pragma unroll
+                for (int v = 0; v < EVICT_WAVES; ++v) many[j] += red[turn][j][v];
+            }
+            const int step = many[2] >= want ? 3 : many[1] >= want ? 2 : many[0] >= want ? 1 : 0;
+            found |= (uint32_t)step << shift;
+            if (step < 3) beyond = many[step];                 // (with step 3 what lies above is as before)
+            if (step) least = many[step - 1];
+        }
+        prefix = found;
+        want -= beyond;
+        share = least - beyond;
+    } else {
+        digit(8, 12);
+        digit(0, 8);
     }
-    // kept: keys above the prefix, and the first `want` with it.  First the holes and movers are counted off in index order.
-    int equal_before = 0, holes_before = 0, movers_before = 0;
-    for (int i0 = 0; i0 < len; i0 += EVICT_THREADS) {
-        const int i = i0 + tid;
-        const bool in = i < len;
-        const uint32_t k = in ? key_of(i) : 0;
-        const bool eq = in && k == prefix;
-        int all;
-        const int rank = equal_before + block_scan(eq, red, all);
-        equal_before += all;
-        const bool stays = in && (k > prefix || (eq && rank < want));
-        const bool mover = stays && i >= n, hole = in && i < n && !stays;
-        const int at = block_scan((int)hole | (int)mover << 16, red, all);
-        // the lists meet in the outputs: a hole notes its rank as -2 - rank, and po[n ..] lends its room to the movers
-        if (hole) e.kept[i] = -2 - (holes_before + (at & 0xffff));
-        else if (in && i < n) { e.kept[i] = i; e.wo[i] = e.w[i]; e.po[i] = e.pos[i]; }
-        if (mover) e.po[n + movers_before + (at >> 16)] = i;
-        holes_before += all & 0xffff; movers_before += all >> 16;
+    // kept: keys above the prefix, and the first `want` of the `share` with it.  Each wave counts its equal ones, then its holes and movers, then writes.
+    __syncthreads();
+    const bool ties = want < share;
+    if (ties) {
+        int many = 0;
+        for (int i = i0; i - lane < i1; i += 64 * AHEAD) {
+            load(i);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) many += __popcll(__ballot(i + 64 * u < i1 && key_of(u) == prefix));
+        }
+        if (lane == 0) red[0][0][wave] = many;
     }
     __syncthreads();
-    for (int i = tid; i < n; i += EVICT_THREADS) {
-        const int k = e.kept[i];
-        if (k >= 0) continue;
-        const int s = e.po[n + (-2 - k)];
-        e.kept[i] = s; e.wo[i] = e.w[s]; e.po[i] = e.pos[s];
+    int equal_first = 0;
+    if (ties) for (int v = 0; v < wave; ++v) equal_first += red[0][0][v];
+    auto stays_at = [&](int i, int u, int &equal) {            // of the 64 slots side by side, the u-th loaded; equal: equal ones before them, brought forward
+        const uint32_t k = key_of(u);
+        const unsigned long long eq = __ballot(i < i1 && k == prefix);
+        const bool stays = i < i1 && (k > prefix || (k == prefix && (!ties || equal + lanes_below(eq) < want)));
+        equal += __popcll(eq);
+        return stays;
+    };
+    int holes = 0, movers = 0, equal = equal_first;
+    for (int j = i0; j - lane < i1; j += 64 * AHEAD) {
+        load(j);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int i = j + 64 * u;
+            const unsigned long long stay = __ballot(stays_at(i, u, equal)), low = __ballot(i < n), in = __ballot(i < i1);
+            holes += __popcll(in & low & ~stay); movers += __popcll(stay & ~low);
+        }
+    }
+    if (lane == 0) { red[0][1][wave] = holes; red[0][2][wave] = movers; }
+    __syncthreads();
+    int hole = 0, mover = 0, all = 0;
+    for (int v = 0; v < EVICT_WAVES; ++v) { if (v < wave) { hole += red[0][1][v]; mover += red[0][2][v]; } all += red[0][2][v]; }
+    equal = equal_first;
+    for (int j = i0; j - lane < i1; j += 64 * AHEAD) {
+        load(j);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int i = j + 64 * u;
+            const bool stays = stays_at(i, u, equal), is_hole = i < i1 && i < n && !stays, is_mover = stays && i >= n;
+            const unsigned long long them = __ballot(is_hole), those = __ballot(is_mover);
+            // the lists meet in the outputs: a hole notes its rank as -2 - rank, and po[n ..] lends its room to the movers
+            if (is_hole) e.kept[i] = -2 - (hole + lanes_below(them));
+            else if (stays && i < n) { e.kept[i] = i; e.wo[i] = w[u]; e.po[i] = pos[u]; }
+            if (is_mover) e.po[n + mover + lanes_below(those)] = i;
+            hole += __popcll(them); mover += __popcll(those);
+        }
     }
     __syncthreads();
-    for (int i = n + tid; i < n + movers_before; i += EVICT_THREADS) e.po[i] = -1;
+    for (int i = tid; i < n; i += EVICT_THREADS * AHEAD) {
+        int from[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) from[u] = i + u * EVICT_THREADS < n ? e.kept[i + u * EVICT_THREADS] : 0;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) from[u] = from[u] < 0 ? e.po[n + (-2 - from[u])] : -1;
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) if (from[u] >= 0) { w[u] = e.w[from[u]]; pos[u] = e.pos[from[u]]; }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) if (from[u] >= 0) { const int to = i + u * EVICT_THREADS; e.kept[to] = from[u]; e.wo[to] = w[u]; e.po[to] = pos[u]; }
+    }
+    __syncthreads();
+    for (int i = n + tid; i < n + all; i += EVICT_THREADS) e.po[i] = -1;
 }
 
 // The slots 256 x .. below the budget of one sequence and head whose source is another: listed, then moved, keys in pieces of 16 bytes, values with a lane per
