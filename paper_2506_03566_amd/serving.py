@@ -218,32 +218,31 @@ def logprobs(logits, tokens=None, n_top=0, temperature=1.0, logp=None, entropy=N
         _mx_refuse("logits must have contiguous rows that do not overlap")
     if n_top < 0 or n_top > min(LOGPROBS_TOP, vocab):
         _mx_refuse("n_top must be at most %d and the vocabulary" % LOGPROBS_TOP)
-    made = []
+    f32, i32 = torch.float32, torch.int32
 
-    def array(given, shape, dtype, what):
-        if given is None:
-            if stream is None:
-                given = torch.empty(shape, dtype=dtype, device=logits.device)
-            else:
-                with torch.cuda.stream(stream):
-                    given = torch.empty(shape, dtype=dtype, device=logits.device)
-        (_ints if dtype is torch.int32 else _floats)(given, shape, what)
-        made.append(given)
-        return given
+    def new(shape, dtype):
+        if stream is None:
+            return logits.new_empty(shape, dtype=dtype)
+        with torch.cuda.stream(stream):
+            return logits.new_empty(shape, dtype=dtype)
     n_tokens = tp = lp = 0
     tensors = [logits]
     if tokens is not None:
         n_tokens = 1 if tokens.dim() == 1 else tokens.shape[1] if tokens.dim() == 2 else _mx_refuse("tokens must be [rows] or [rows, n]")
         tp = _ints(tokens, (rows,) if tokens.dim() == 1 else (rows, n_tokens), "tokens")
-        logp = array(logp, tokens.shape, torch.float32, "logp")
-        lp = logp.data_ptr()
-        tensors.append(tokens)
-    entropy = array(entropy, (rows,), torch.float32, "entropy")
-    top_ids, top_logp = array(top_ids, (rows, n_top), torch.int32, "top_ids"), array(top_logp, (rows, n_top), torch.float32, "top_logp")
+        if logp is None:
+            logp = new(tokens.shape, f32)
+        lp = _floats(logp, tokens.shape, "logp")
+        tensors += (tokens, logp)
+    tops = (rows, n_top)
+    entropy = new((rows,), f32) if entropy is None else entropy
+    top_ids = new(tops, i32) if top_ids is None else top_ids
+    top_logp = new(tops, f32) if top_logp is None else top_logp
+    ep, ip, op = _floats(entropy, (rows,), "entropy"), _ints(top_ids, tops, "top_ids"), _floats(top_logp, tops, "top_logp")
     if scratch is None:
         scratch = logprobs_scratch(rows, vocab, n_top, logits.device, stream)
     elif not scratch.is_contiguous():
         _mx_refuse("scratch must be contiguous")
-    _mx_call(_mx.lib.poss_logprobs, stream, (*tensors, *made, scratch), t, logits.data_ptr(), ld if rows > 1 else vocab, rows, vocab, temperature, tp, n_tokens, lp,
-             entropy.data_ptr(), n_top, top_ids.data_ptr(), top_logp.data_ptr(), scratch.data_ptr(), scratch.nbytes)
+    _mx_call(_mx.lib.poss_logprobs, stream, (*tensors, entropy, top_ids, top_logp, scratch), t, logits.data_ptr(), ld if rows > 1 else vocab, rows, vocab, temperature, tp, n_tokens,
+             lp, ep, n_top, ip, op, scratch.data_ptr(), scratch.nbytes)
     return logp, entropy, top_ids, top_logp
