@@ -42,37 +42,60 @@ __device__ __forceinline__ int64_t attend_parts(int64_t all, int W) {
     return p < W ? p : W;
 }
 
-// Sum over the wave's lanes up to this one.
-__device__ __forceinline__ int64_t wave_scan(int64_t x) {
-    for (int o = 1; o < 64; o <<= 1) { const int64_t y = __shfl_up(x, o); if ((int)(threadIdx.x & 63) >= o) x += y; }
+// a * b / c, rounded down: in 32 bits where they hold it (a 64-bit division takes some hundred instructions).
+__device__ __forceinline__ int64_t times_over(int64_t a, int64_t b, int64_t c) {
+    if (a < 1 << 20 && b <= 1 << 10) return (uint32_t)a * (uint32_t)b / (uint32_t)c;
+    return a * b / c;
+}
+// Sum over the wave's lanes up to this one (64 rows' blocks fit: a row has 2^25 at most).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+    for (int o = 1; o < 64; o <<= 1) { const uint32_t y = __shfl_up(x, o); if ((int)(threadIdx.x & 63) >= o) x += y; }
     return x;
 }
-// Blocks of all rows, and of those before row `upto`; by every wave for itself.
-__device__ __forceinline__ void count_blocks(const int32_t *lengths, int n, int max_len, int upto, int64_t &all, int64_t &before) {
-    int64_t a = 0, b = 0;
-    for (int i = threadIdx.x & 63; i < n; i += 64) {
-        const int x = row_blocks(lengths[i], max_len);
-        a += x;
-        if (i < upto) b += x;
+// The batch's rows as blocks laid end to end, by every wave for itself.  Up to 64 rows are looked at once: x and end are lane i's blocks and those up to it; of more, a
+// pass for the sum comes first.
+struct Batch { int64_t all; uint32_t x, end; };
+__device__ __forceinline__ Batch count_blocks(const int32_t *lengths, int n, int max_len) {
+    const int lane = threadIdx.x & 63;
+    Batch r{0, 0, 0};
+    if (n == 1) { r.x = r.end = row_blocks(lengths[0], max_len); r.all = r.x; return r; }
+    if (n <= 64) {
+        r.x = lane < n ? row_blocks(lengths[lane], max_len) : 0;
+        r.end = wave_scan(r.x);
+        r.all = (uint32_t)__builtin_amdgcn_readlane(r.end, 63);
+        return r;
     }
-    for (int o = 32; o; o >>= 1) { a += __shfl_xor(a, o); b += __shfl_xor(b, o); }
-    all = a; before = b;
+    int64_t a = 0;
+    for (int i = lane; i < n; i += 64) a += row_blocks(lengths[i], max_len);
+    for (int o = 32; o; o >>= 1) a += __shfl_xor(a, o);
+    r.all = a;
+    return r;
+}
+// Blocks before row b.
+__device__ __forceinline__ int64_t blocks_before(const Batch &r, const int32_t *lengths, int n, int max_len, int b) {
+    if (n == 1) return 0;
+    if (n <= 64) return (uint32_t)__builtin_amdgcn_readlane(r.end - r.x, b);
+    int64_t a = 0;
+    for (int i = threadIdx.x & 63; i < b; i += 64) a += row_blocks(lengths[i], max_len);
+    for (int o = 32; o; o >>= 1) a += __shfl_xor(a, o);
+    return a;
 }
 // The row that holds block `at` (0 <= at < all) and its first block.
-__device__ __forceinline__ void find_row(const int32_t *lengths, int n, int max_len, int64_t at, int &row, int64_t &first) {
+__device__ __forceinline__ void find_row(const Batch &r, const int32_t *lengths, int n, int max_len, int64_t at, int &row, int64_t &first) {
+    row = 0; first = 0;
+    if (n == 1) return;
     int64_t base = 0;
     for (int i0 = 0; i0 < n; i0 += 64) {
         const int i = i0 + (int)(threadIdx.x & 63);
-        const int x = i < n ? row_blocks(lengths[i], max_len) : 0;
-        const int64_t end = base + wave_scan(x);
-        const unsigned long long past = __ballot(end > at);
+        const uint32_t x = n <= 64 ? r.x : i < n ? row_blocks(lengths[i], max_len) : 0, end = n <= 64 ? r.end : wave_scan(x);
+        const unsigned long long past = __ballot(base + end > at);
         if (past) {
             const int lane = __ffsll(past) - 1;
             row = i0 + lane;
-            first = __shfl(end - x, lane);
+            first = base + (uint32_t)__builtin_amdgcn_readlane(end - x, lane);
             return;
         }
-        base = __shfl(end, 63);
+        base += (uint32_t)__builtin_amdgcn_readlane(end, 63);
     }
 }
 
@@ -190,14 +213,13 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, Attend
         for (int i = threadIdx.x; i < heads * DH; i += 64 * ATT_WAVES) out[b * a.out_row + (int64_t)head0 * DH + i] = from_f<T>(len > 0 ? NAN : 0.f);
         if ((int)threadIdx.x < heads && a.lse) a.lse[(int64_t)b * a.hq + head0 + threadIdx.x] = len > 0 ? NAN : -INFINITY;
     }
-    int64_t all, none;
-    count_blocks(a.lengths, c.n_seq, a.max_len, 0, all, none);
-    const int64_t parts = attend_parts(all, a.W);
+    const Batch batch = count_blocks(a.lengths, c.n_seq, a.max_len);
+    const int64_t parts = attend_parts(batch.all, a.W);
     if (w >= parts) return;
-    int64_t at = all * w / parts;
-    const int64_t end = all * (w + 1) / parts;
+    int64_t at = times_over(batch.all, w, parts);
+    const int64_t end = times_over(batch.all, w + 1, parts);
     int b; int64_t first;
-    find_row(a.lengths, c.n_seq, a.max_len, at, b, first);
+    find_row(batch, a.lengths, c.n_seq, a.max_len, at, b, first);
     const float scale = a.scale * LOG2E;
     Tile<T, DH> t;
     while (at < end) {
@@ -310,10 +332,14 @@ __global__ void __launch_bounds__(256) attend_finish_kernel(KvView c, AttendArgs
     if (!blocks) return;
     const int chunk = (int)blockIdx.x - joins;
     if (chunk >= 0 && chunk * FINISH_SLOTS >= len) return;
-    int64_t all, first;
-    count_blocks(a.lengths, c.n_seq, a.max_len, b, all, first);
-    const int64_t parts = attend_parts(all, a.W);
-    const int w0 = (int)(((first + 1) * parts - 1) / all), n = (int)(((first + blocks) * parts - 1) / all) - w0 + 1;
+    const Batch batch = count_blocks(a.lengths, c.n_seq, a.max_len);
+    const int64_t parts = attend_parts(batch.all, a.W), first = blocks_before(batch, a.lengths, c.n_seq, a.max_len, b);
+    // the last workgroup w with w * all / parts <= block
+    auto holder = [&](int64_t block) {
+        const int64_t x = (block + 1) * parts - 1;
+        return x < 1ll << 32 && batch.all < 1ll << 32 ? (int)((uint32_t)x / (uint32_t)batch.all) : (int)(x / batch.all);
+    };
+    const int w0 = holder(first), n = holder(first + blocks - 1) - w0 + 1;
     // piece p of the head of this group's index j
     auto slot = [&](int p, int j) { return ((int64_t)(2 * (w0 + p) + (p == 0 ? 1 : 0)) * c.hkv * a.tiles + hk * a.tiles + j / 16) * 16 + j % 16; };
     if (chunk < 0) {
