@@ -18,7 +18,7 @@ typedef f16_t  f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int ATT_BLOCK = 32;                 // slots of a block: never across pages
 constexpr int ATT_WAVES = 4;
-constexpr int ATT_LEAST = 8, ATT_MOST = 512;   // blocks of a workgroup, workgroups along the slots
+constexpr int ATT_LEAST = 2, ATT_MOST = 512;   // blocks of a workgroup at least, workgroups of a launch at most
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct AttendArgs {
@@ -322,11 +322,14 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, Attend
 // per value that walks the pieces one after the other, 5 with all of them asked for at once).
 constexpr int FINISH_SLOTS = 1024, FINISH_HEADS = 64;
 
-template <typename T>
+// WAVES waves join a head: all four where heads are few, one of them each where there are thousands, most of which have one piece and nothing to join (100 rows of 64
+// heads, the whole call: 72 us with a workgroup per head, 61 with a wave).
+template <typename T, int WAVES>
 __global__ void __launch_bounds__(256) attend_finish_kernel(KvView c, AttendArgs a, int joins) {
-    __shared__ float factor[ATT_MOST];
+    constexpr int THREADS = 64 * WAVES, TEAMS = 4 / WAVES;
+    __shared__ float factors[TEAMS][ATT_MOST];
     __shared__ f32x4 sums[256];
-    __shared__ float red[17];
+    __shared__ float red[8];
     const int b = blockIdx.z, hk = blockIdx.y, tid = threadIdx.x, group = a.hq / c.hkv, dh = c.dh;
     const int len = a.lengths[b], blocks = row_blocks(len, a.max_len);
     if (!blocks) return;
@@ -344,36 +347,52 @@ __global__ void __launch_bounds__(256) attend_finish_kernel(KvView c, AttendArgs
     auto slot = [&](int p, int j) { return ((int64_t)(2 * (w0 + p) + (p == 0 ? 1 : 0)) * c.hkv * a.tiles + hk * a.tiles + j / 16) * 16 + j % 16; };
     if (chunk < 0) {
         if (n == 1) return;
-        const int j = blockIdx.x;
-        float2 ml = make_float2(-INFINITY, 0.f), other = ml;
-        if (tid < n) ml = a.part_ml[slot(tid, j)];
-        if (tid + 256 < n) other = a.part_ml[slot(tid + 256, j)];
-        float top = wave_max(fmaxf(ml.x, other.x));
-        if ((tid & 63) == 0) red[tid >> 6] = top;
+        const int team = tid / THREADS, t = tid % THREADS, j = blockIdx.x * TEAMS + team;
+        const bool there = j < group;
+        float *factor = factors[team];
+        auto all_of = [&](float v, float *at, bool largest) {  // over the team
+            v = largest ? wave_max(v) : wave_sum(v);
+            if constexpr (WAVES == 1) return v;
+            if ((tid & 63) == 0) at[tid >> 6] = v;
+            __syncthreads();
+            return largest ? fmaxf(fmaxf(at[0], at[1]), fmaxf(at[2], at[3])) : at[0] + at[1] + at[2] + at[3];
+        };
+        float2 ml[ATT_MOST / THREADS];
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < ATT_MOST / THREADS; ++k) {
+            const int p = k * THREADS + t;
+            ml[k] = there && p < n ? a.part_ml[slot(p, j)] : make_float2(-INFINITY, 0.f);
+            top = fmaxf(top, ml[k].x);
+        }
+        top = all_of(top, red, true);
+#pragma unroll
+        for (int k = 0; k < ATT_MOST / THREADS; ++k) {
+            const float f = back_by(ml[k].x, top);
+            factor[k * THREADS + t] = f;
+            sum += ml[k].y * f;
+        }
+        sum = all_of(sum, red + 4, false);
         __syncthreads();
-        top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-        const float f = back_by(ml.x, top), fo = back_by(other.x, top);
-        factor[tid] = f;
-        if (tid + 256 < ATT_MOST) factor[tid + 256] = fo;
-        const float sum = block_sum(ml.y * f + other.y * fo, red);      // (its barriers stand between the factors' writes and reads)
-        // a thread adds four values of every (256 / quads)-th piece
-        const int quads = dh / 4, ways = 256 / quads, way = tid / quads, d = tid % quads * 4;
+        // a thread adds four values of every (THREADS / quads)-th piece
+        const int quads = dh / 4, ways = THREADS / quads, way = t / quads, d = t % quads * 4;
         f32x4 r = {0.f, 0.f, 0.f, 0.f};
-        if (way < ways) {
+        if (there && way < ways) {
 #pragma unroll 8
             for (int p = way; p < n; p += ways) r += *reinterpret_cast<const f32x4 *>(a.part + slot(p, j) * dh + d) * factor[p];
         }
         sums[tid] = r;
         __syncthreads();
-        if (way == 0) {
-            for (int v = 1; v < ways; ++v) r += sums[v * quads + tid];
+        if (there && way == 0) {
+            for (int v = 1; v < ways; ++v) r += sums[team * THREADS + v * quads + t];
             const float inv = 1.f / sum;
             T *to = static_cast<T *>(a.out) + b * a.out_row + (int64_t)(hk * group + j) * dh + d;
             for (int e = 0; e < 4; ++e) to[e] = from_f<T>(r[e] * inv);
         }
-        if (tid == 0 && a.lse) a.lse[(int64_t)b * a.hq + hk * group + j] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+        if (there && t == 0 && a.lse) a.lse[(int64_t)b * a.hq + hk * group + j] = (top + __builtin_amdgcn_logf(sum)) * LN2;
         return;
     }
+    float *factor = factors[0];
     const int s = chunk * FINISH_SLOTS + tid * 4, live = len - s;
     f32x4 w = {0.f, 0.f, 0.f, 0.f};
     for (int j0 = 0; j0 < group; j0 += FINISH_HEADS) {
@@ -413,13 +432,14 @@ __global__ void __launch_bounds__(256) attend_finish_kernel(KvView c, AttendArgs
 
 // How a call runs: workgroups along the slots, and its scratch.
 struct AttendPlan { int tiles, W; int64_t score_row; size_t part, part_ml, row_lse, scores, bytes; };
-static AttendPlan attend_plan(const KvView &c, int hq, int max_len, bool weighed) {
+static AttendPlan attend_plan(const KvView &c, int esize, int hq, int max_len, bool weighed) {
     AttendPlan p{};
     p.tiles = (hq / c.hkv + 15) / 16;
     const int64_t per = (int64_t)c.hkv * p.tiles, blocks = (int64_t)c.n_seq * ((max_len + ATT_BLOCK - 1) / ATT_BLOCK);
-    // Two workgroups a CU, the registers' limit, and never more: a third round of a few costs as much as a whole one (40 key heads, 16 rows: 94 us with 13 x 40
+    // As many workgroups as the registers let a CU hold, and never more: a third round of a few costs as much as a whole one (40 key heads, 16 rows: 94 us with 13 x 40
     // workgroups, 74 with 12 x 40).
-    int64_t W = ATT_MOST / per;
+    const bool two = esize == 2 ? c.dh <= 160 : c.dh <= (weighed ? 96 : 128);
+    int64_t W = (two ? ATT_MOST : ATT_MOST / 2) / per;
     if (W > (blocks + ATT_LEAST - 1) / ATT_LEAST) W = (blocks + ATT_LEAST - 1) / ATT_LEAST;
     p.W = W < 1 ? 1 : (int)W;
     p.score_row = (max_len + ATT_BLOCK - 1) / ATT_BLOCK * ATT_BLOCK;
@@ -454,8 +474,13 @@ static void launch_attend_t(const KvView &c, const AttendArgs &a, bool weighed, 
         case 224: launch_attend<T, 224>(c, a, weighed, st); break;
         default: launch_attend<T, 256>(c, a, weighed, st); break;
     }
-    const int joins = a.W > 1 ? a.hq / c.hkv : 0, chunks = weighed ? (a.max_len + FINISH_SLOTS - 1) / FINISH_SLOTS : 0;
-    if (joins + chunks) attend_finish_kernel<T><<<dim3(joins + chunks, c.hkv, c.n_seq), 256, 0, st>>>(c, a, joins);
+    const int chunks = weighed ? (a.max_len + FINISH_SLOTS - 1) / FINISH_SLOTS : 0;
+    const bool many = (int64_t)c.n_seq * a.hq > 1024;
+    const int joins = a.W == 1 ? 0 : many ? (a.hq / c.hkv + 3) / 4 : a.hq / c.hkv;
+    const dim3 grid(joins + chunks, c.hkv, c.n_seq);
+    if (joins + chunks == 0) return;
+    if (many) attend_finish_kernel<T, 1><<<grid, 256, 0, st>>>(c, a, joins);
+    else attend_finish_kernel<T, 4><<<grid, 256, 0, st>>>(c, a, joins);
 }
 
 }  // namespace poss
@@ -480,7 +505,7 @@ const char *attend_bad(const poss_kv_cache *c, int32_t hq, int32_t max_len) {
 extern "C" {
 
 size_t poss_kv_attend_scratch_bytes(const poss_kv_cache *cache, int32_t n_q_heads, int32_t max_len, int32_t weighed) {
-    return attend_bad(cache, n_q_heads, max_len) ? 0 : attend_plan(kv_view(*cache), n_q_heads, attend_max_len(*cache, max_len), weighed != 0).bytes;
+    return attend_bad(cache, n_q_heads, max_len) ? 0 : attend_plan(kv_view(*cache), (int)dtype_size(cache->dtype), n_q_heads, attend_max_len(*cache, max_len), weighed != 0).bytes;
 }
 
 int poss_kv_attend(const poss_kv_cache *cache, int32_t n_q_heads, const void *q, int64_t q_row, void *out, int64_t out_row, const int32_t *lengths, int32_t max_len, float scale,
@@ -499,7 +524,7 @@ int poss_kv_attend(const poss_kv_cache *cache, int32_t n_q_heads, const void *q,
     const KvView c = kv_view(*cache);
     const int most = attend_max_len(*cache, max_len);
     const bool weighed = weights_out != nullptr;
-    const AttendPlan p = attend_plan(c, n_q_heads, most, weighed);
+    const AttendPlan p = attend_plan(c, (int)dtype_size(cache->dtype), n_q_heads, most, weighed);
     if (scratch_bytes < p.bytes) return set_error(POSS_E_CAPACITY, "%s: needs %zu bytes of scratch, got %zu", who, p.bytes, scratch_bytes);
     char *base = static_cast<char *>(scratch);
     AttendArgs a{n_q_heads, p.tiles, q, q_row, out, out_row, lengths, most, scale, lse, weights, weights_out, p.W, reinterpret_cast<float *>(base + p.part),

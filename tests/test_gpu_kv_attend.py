@@ -96,7 +96,8 @@ class Case:
 SHAPES = [  # lengths, hq, hkv, dh, page
     ([1], 1, 1, 64, 32), ([0], 4, 2, 64, 32), ([2], 8, 1, 128, 64), ([31, 32, 33], 4, 4, 64, 32), ([17], 32, 8, 128, 64), ([64, 0, 1, 63, 65, 128, 129], 8, 2, 128, 64), ([500, 1, 0, 700], 5, 5, 64, 128),
     ([255, 256, 257], 6, 2, 96, 32), ([1000], 16, 1, 128, 64), ([333, 90], 34, 2, 64, 32), ([4000, 3, 0, 1500, 2049], 8, 2, 128, 128), ([3000], 40, 40, 128, 64), ([700, 701], 8, 1, 256, 32),
-    ([1, 2, 3, 4, 5] * 30, 4, 2, 32, 32), ([100, 1200], 48, 1, 160, 64), ([900], 9, 3, 192, 32), ([411, 60], 4, 2, 224, 128), ([9001], 8, 8, 64, 64)]
+    ([1, 2, 3, 4, 5] * 30, 4, 2, 32, 32), ([100, 1200], 48, 1, 160, 64), ([900], 9, 3, 192, 32), ([411, 60], 4, 2, 224, 128), ([9001], 8, 8, 64, 64),
+    ([300, 5, 0, 129] * 20 + [4000], 16, 2, 64, 32), ([90, 40] * 100, 6, 3, 96, 64)]
 
 
 @pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
