@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, E
 // where those are too many (equal weights), from two more histograms.
 __global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView c, EvictArgs a) {
     constexpr int BINS = 4096, EACH = BINS / EVICT_THREADS, AHEAD = 16;      // AHEAD: loads of an array on their way at a time
-    __shared__ int hist[BINS], red[2][3][EVICT_WAVES], pick[3];
+    __shared__ int hist[BINS], red[2][3][EVICT_WAVES], pick[3], taken;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const EvictHead e = evict_head(c, a);
     const int len = e.len, n = e.n;
@@ -228,16 +228,15 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView
         prefix = prefix << bits | (uint32_t)pick[0];
         want = pick[1]; share = pick[2];
     };
+    if (tid == 0) taken = 0;                                   // (seen by all behind digit()'s barriers)
     digit(20, 12);
     if (share <= BINS) {
-        if (tid == 0) pick[0] = 0;
-        __syncthreads();
         for (int i = i0; i < i1; i += 64 * AHEAD) {
             load(i);
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const uint32_t k = key_of(u);
-                if (i + 64 * u < i1 && k >> 20 == prefix) hist[atomicAdd(&pick[0], 1)] = (int)k;      // (in any order: they are counted)
+                if (i + 64 * u < i1 && k >> 20 == prefix) hist[atomicAdd(&taken, 1)] = (int)k;      // (in any order: they are counted)
             }
         }
         __syncthreads();

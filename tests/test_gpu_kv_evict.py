@@ -86,7 +86,7 @@ def test_evict_is_the_plain_rule(t, n_seq, slots, lengths, hkv, dh, page, budget
 
 
 @pytest.mark.parametrize("how", ["equal", "zero", "special", "rising", "falling", "near", "negative"])
-@pytest.mark.parametrize("slots", [64, 1500, 5000])
+@pytest.mark.parametrize("slots", [64, 1500, 5000, 20000])
 def test_weights_of_every_kind(how, slots):
     print(f"evict weights {how} slots {slots}", flush=True)
     cache, table, rng = make("bf16", 1, slots, 2, 64, 32, seed=slots)
