@@ -385,7 +385,7 @@ typedef struct poss_kv_cache {
 
 /* Rotary positions of a head's first rot_dim values: pair i is (x[i], x[i + rot_dim/2]) or, interleaved, (x[2i], x[2i+1]); it becomes
  * magnitude * (a cos - b sin, b cos + a sin) at the angle position * freq[i], formed in 64 bits.  The other values stay.  A program may fill in
- * frequencies of its own (finite ones). */
+ * frequencies of its own (finite ones; angles up to 2^45). */
 #define POSS_ROPE_PAIRS 128
 typedef struct poss_rope {
     int32_t rot_dim, interleaved;            /* rot_dim: even, 2 .. 2 * POSS_ROPE_PAIRS */
@@ -424,13 +424,14 @@ int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t ro
 /* Attention of one query row per sequence over the slots 0 .. lengths[b]-1: out[b][h] = sum_s p v, p = softmax(scale * q . k), query head h on key
  * head h / (n_q_heads / n_kv_heads).  q and out: [n_seq][n_q_heads][head_dim] of the cache's type, heads contiguous, q_row and out_row values apart, 16-byte
  * aligned with distances of whole 16 bytes.  lengths: DEVICE int32[n_seq]; max_len: the most that any of them is (0: all slots); it decides
- * how the work is split.  A length of zero or less gives zeros and an lse of -infinity; one above max_len, or a slot without a page, a row of NaN; scores that are all
+ * how the work is split and, with weights, the size of the scratch.  A length of zero or less gives zeros and an lse of -infinity; one above max_len, or a slot without a page, a row of NaN; scores that are all
  * -infinity, zeros over nothing: a row of NaN and an lse of -infinity.
  * lse (may be NULL): float32 [n_seq][n_q_heads], the logarithm of the sum of exponentials.
  * weights_out (may be NULL): float32 [n_seq][n_kv_heads][slots], the weights that the slots have been given so far: weights (the same form; NULL: zeros;
  * may be weights_out) plus this row's p, summed over the heads that share the key head.  Slots beyond the length are left as they were.
  * scratch: poss_kv_attend_scratch_bytes bytes, aligned to 256, for this call alone until it has run (two calls or graphs that may
- * run at the same time need one each).  Sums and statistics are float32; 16-bit probabilities carry 16 significant bits (bf16) or 11 (f16).
+ * run at the same time need one each).  Sums and statistics are float32; 16-bit caches take a
+ * probability as the sum of two numbers of their type, 16 significant bits or more.
  * The bits of a row may differ with the other rows' lengths; the same call gives the same bits. */
 size_t poss_kv_attend_scratch_bytes(const poss_kv_cache *cache, int32_t n_q_heads, int32_t max_len, int32_t weighed);
 int poss_kv_attend(const poss_kv_cache *cache, int32_t n_q_heads, const void *q, int64_t q_row, void *out, int64_t out_row,

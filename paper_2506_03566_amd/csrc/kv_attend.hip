@@ -138,7 +138,8 @@ template <typename T, int DH> struct Tile {
         for (int d = 0; d < DH / 16; ++d)
             for (int j = 0; j < 8; ++j) if (slot_of(j) >= n) v[d][j] = (T)0.f;
     }
-    // A probability enters as the sum of two 16-bit numbers: rounded once to 8 bits (bf16) it alone would be off by more than the result's half step.
+    // A probability enters as the sum of two 16-bit numbers: rounded once to 8 bits (bf16) it alone would be off by more than the result's half step.  fp16
+    // holds numbers below 2^-14 with fewer bits: there probabilities, and their sum with them, are 2^12 times larger (lift()), so that those of 2^-26 of the largest have all.
     __device__ __forceinline__ void add_values(const float *p, f32x4 *o) const {
         x8 hi, lo;
 #pragma unroll
@@ -191,6 +192,7 @@ template <int DH> struct Tile<float, DH> {
     }
 };
 
+template <typename T> constexpr float lift() { return __is_same(T, f16_t) ? 12.f : 0.f; }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 // 2^(m - to) for a running maximum that may be -infinity (nothing yet: 0).
 __device__ __forceinline__ float back_by(float m, float to) { return m == -INFINITY ? 0.f : exp2_of(m - to); }
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, Attend
 #pragma unroll
                     for (int d = 0; d < DH / 16; ++d) o[d] *= back;
                 }
-                const float ref = m == -INFINITY ? 0.f : m;
+                const float ref = (m == -INFINITY ? 0.f : m) - lift<T>();
 #pragma unroll
                 for (int x = 0; x < 8; ++x) { z[x] = exp2_of(z[x] - ref); l += z[x]; }
                 t.add_values(z, o);
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, Attend
                 T *to = out + b * a.out_row + (int64_t)(head0 + h) * DH + d;
                 for (int e = 0; e < 4; ++e) to[e] = from_f<T>(r[e] * inv);
                 if (d == 0) {
-                    const float lse2 = top + __builtin_amdgcn_logf(sum);
+                    const float lse2 = top + __builtin_amdgcn_logf(sum) - lift<T>();
                     if (a.lse) a.lse[(int64_t)b * a.hq + head0 + h] = lse2 * LN2;
                     if (WEIGHED) a.row_lse[(int64_t)b * a.hq + head0 + h] = lse2;
                 }
@@ -389,7 +391,7 @@ __global__ void __launch_bounds__(256) attend_finish_kernel(KvView c, AttendArgs
             T *to = static_cast<T *>(a.out) + b * a.out_row + (int64_t)(hk * group + j) * dh + d;
             for (int e = 0; e < 4; ++e) to[e] = from_f<T>(r[e] * inv);
         }
-        if (there && t == 0 && a.lse) a.lse[(int64_t)b * a.hq + hk * group + j] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+        if (there && t == 0 && a.lse) a.lse[(int64_t)b * a.hq + hk * group + j] = (top + __builtin_amdgcn_logf(sum) - lift<T>()) * LN2;
         return;
     }
     float *factor = factors[0];
@@ -406,7 +408,7 @@ __global__ void __launch_bounds__(256) attend_finish_kernel(KvView c, AttendArgs
                 for (int p = tid & 63; p < n; p += 64) top = fmaxf(top, a.part_ml[slot(p, j0 + j)].x);
                 top = wave_max(top);
                 for (int p = tid & 63; p < n; p += 64) { const float2 ml = a.part_ml[slot(p, j0 + j)]; sum += ml.y * back_by(ml.x, top); }
-                lse = top + __builtin_amdgcn_logf(wave_sum(sum));
+                lse = top + __builtin_amdgcn_logf(wave_sum(sum)) - lift<T>();
             }
             if ((tid & 63) == 0) factor[j] = lse;
         }

@@ -148,6 +148,24 @@ def test_loud_scores_scales_and_strides(t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+def test_many_small_probabilities_beside_a_large_one(t):
+    """Each 2^-15 to 2^-17 of the largest, together as much as it: what a 16-bit number cannot hold of one must not be lost of all."""
+    n = 40000
+    c = Case(t, [n], 2, 1, 64, 128, seed=8)
+    k, v, _ = c.cache.tensors
+    k[:] = torch.where(k.isnan(), k, 0)
+    c.q[:] = 0
+    c.q[:, :, 0] = 8.0
+    k[:, :, :, 0] = torch.where(k[:, :, :, 0].isnan(), k[:, :, :, 0], -11.0 + torch.rand_like(k[:, :, :, 0].float()).mul_(0.5).to(TYPES[t]) - 0.25)
+    k[c.table[0, 0], 0, 77, 0] = 0.0
+    v[:] = torch.where(v.isnan(), v, v.abs() + 0.5)
+    v[c.table[0, 0], 0, :, 77] = 0.0                         # the large one's value: the others' are the result
+    wo = torch.zeros(1, 1, c.slots, device="cuda")
+    out, lse = c.attend(weights_out=wo)
+    c.check(out, lse, 0.125, None, wo, torch.zeros_like(wo))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
 def test_pages_that_are_not_there_and_lengths_beyond_the_bound(t):
     """A row with such a slot is NaN, the others are as ever; nothing outside the pages is read."""
     c = Case(t, [200, 130, 64, 1], 4, 2, 64, 32, seed=5, slots=512)
