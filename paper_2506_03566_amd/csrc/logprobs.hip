@@ -4,6 +4,8 @@
 // maximum: large logits cancel nothing, and x / T cannot overflow where p has a value.
 #include "kv.h"
 
+#include <float.h>
+
 namespace poss {
 
 constexpr float LOG2_E = 1.4426950408889634f;
@@ -370,7 +372,7 @@ int poss_logprobs(int32_t dtype, const void *x, int64_t ldx, int32_t rows, int32
                   int32_t n_top, int32_t *top_ids, float *top_logp, void *scratch, size_t scratch_bytes, void *hip_stream) {
     const char *who = "poss_logprobs";
     if (kv_bad_dtype(dtype) || !logprobs_ok(rows, vocab, n_top) || n_tokens < 0 || (rows > 1 && ldx < vocab)) return set_error(POSS_E_INVALID_ARG, "%s: bad shape or type", who);
-    if (!(temperature > 0) || !(temperature < INFINITY)) return set_error(POSS_E_INVALID_ARG, "%s: temperature must be positive", who);
+    if (!(temperature >= FLT_MIN) || !(temperature < INFINITY)) return set_error(POSS_E_INVALID_ARG, "%s: temperature must be a positive number, not a subnormal one", who);
     if (rows == 0) return POSS_OK;
     if (!x || !scratch || (n_tokens && (!tokens || !logp)) || (n_top && (!top_ids || !top_logp))) return set_error(POSS_E_INVALID_ARG, "%s: null argument", who);
     if (!kv_aligned(x, dtype_size(dtype)) || !kv_aligned(tokens, 4) || !kv_aligned(logp, 4) || !kv_aligned(entropy, 4) || !kv_aligned(top_ids, 4) || !kv_aligned(top_logp, 4))

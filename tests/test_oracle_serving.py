@@ -186,7 +186,7 @@ def test_logprobs_refusals():
 
     def call(**kw):
         return lib.poss_logprobs(*{**good, **kw}.values(), None)
-    for kw in (dict(t=3), dict(rows=-1), dict(vocab=0), dict(ldx=999), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=math.inf), dict(temperature=math.nan), dict(n_tokens=-1), dict(n_top=33),
+    for kw in (dict(t=3), dict(rows=-1), dict(vocab=0), dict(ldx=999), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=math.inf), dict(temperature=math.nan), dict(temperature=1e-40), dict(n_tokens=-1), dict(n_top=33),
                dict(x=None), dict(tokens=None), dict(logp=None), dict(ids=None), dict(top=None), dict(scratch=None), dict(x=A + 1), dict(tokens=A + 2), dict(scratch=A + 64), dict(entropy=A + 2)):
         assert call(**kw) == P.E_INVALID_ARG, kw
     assert call(bytes=need - 1) == P.E_CAPACITY
