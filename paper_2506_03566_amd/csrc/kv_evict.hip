@@ -25,26 +25,29 @@ constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / 64;
 __device__ __forceinline__ int lanes_below(unsigned long long them) {      // of them, those before this lane
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(them >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)them, 0));
 }
-// Sum of a number per wave over the waves; one barrier.  red: two sets of EVICT_WAVES, used in turn.
+// Sum of a number per wave over the waves; one barrier.
+template <int WAVES>
 __device__ __forceinline__ int waves_sum(int x, int *red) {
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
     __syncthreads();
     int s = 0;
 #pragma unroll
-    for (int w = 0; w < EVICT_WAVES; ++w) s += red[w];
+    for (int w = 0; w < WAVES; ++w) s += red[w];
     return s;
 }
+template <int WAVES>
 __device__ __forceinline__ int block_newest(int newest, int *red) {
     for (int o = 32; o; o >>= 1) newest = max(newest, __shfl_xor(newest, o));
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = newest;
     __syncthreads();
-    for (int w = 0; w < EVICT_WAVES; ++w) newest = max(newest, red[w]);
+    for (int w = 0; w < WAVES; ++w) newest = max(newest, red[w]);
     return newest;
 }
 __device__ __forceinline__ uint32_t slot_key(float w, int pos, int first, int64_t border) { return pos < first || pos > border ? 0xffffffffu : weight_key(w); }
 
 // One head's rows of the arrays, and what every kernel does with them first: what lies beyond the new length, and a head that loses nothing.
 struct EvictHead { const float *w; const int32_t *pos; int32_t *kept; float *wo; int32_t *po; int len, n; };
+template <int THREADS>
 __device__ __forceinline__ EvictHead evict_head(const KvView &c, const EvictArgs &a) {
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const int64_t row = (int64_t)b * c.hkv + h, base = row * c.slots;
@@ -52,22 +55,23 @@ __device__ __forceinline__ EvictHead evict_head(const KvView &c, const EvictArgs
     e.len = e.len < 0 ? 0 : e.len > c.slots ? c.slots : e.len;
     e.n = e.len < a.budget ? e.len : a.budget;
     if (h == 0 && tid == 0) a.lengths_out[b] = e.n;
-    for (int i = e.n + tid; i < a.budget; i += EVICT_THREADS) e.kept[i] = -1;
-    for (int i = e.n + tid; i < c.slots; i += EVICT_THREADS) { e.wo[i] = 0.f; e.po[i] = -1; }
+    for (int i = e.n + tid; i < a.budget; i += THREADS) e.kept[i] = -1;
+    for (int i = e.n + tid; i < c.slots; i += THREADS) { e.wo[i] = 0.f; e.po[i] = -1; }
     if (e.n == e.len)
-        for (int i = tid; i < e.n; i += EVICT_THREADS) { e.kept[i] = i; e.wo[i] = e.w[i]; e.po[i] = e.pos[i]; }
+        for (int i = tid; i < e.n; i += THREADS) { e.kept[i] = i; e.wo[i] = e.w[i]; e.po[i] = e.pos[i]; }
     return e;
 }
 
-// One workgroup per sequence and key head, up to K * 1024 slots: slot k * 1024 + t is thread t's k-th, its key stays in a register.  The n-th largest key is found from the
+// One workgroup per sequence and key head, up to K * THREADS slots: slot k * THREADS + t is thread t's k-th, its key stays in a register.  The n-th largest key is found from the
 // highest bit down, two bits at a time, by counting the keys from each candidate on: counting is ballots, with no contention for
 // a histogram's few busy bins.  It ends as soon as exactly n keys are counted, for distinct weights long before the last bit.
-template <int K>
-__global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, EvictArgs a) {
-    __shared__ int red[2][3][EVICT_WAVES], before[K][EVICT_WAVES];
-    __shared__ uint16_t movers[K * EVICT_THREADS / 2];       // as many as there are holes, at most half of the slots
+template <int THREADS, int K>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView c, EvictArgs a) {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ int red[2][3][WAVES], before[K][WAVES];
+    __shared__ uint16_t movers[K * THREADS / 2];       // as many as there are holes, at most half of the slots
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const EvictHead e = evict_head(c, a);
+    const EvictHead e = evict_head<THREADS>(c, a);
     const int len = e.len, n = e.n;
     if (n == len) return;
     float w[K];
@@ -75,15 +79,15 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, E
     int newest = INT32_MIN;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int i = k * EVICT_THREADS + tid;
+        const int i = k * THREADS + tid;
         w[k] = i < len ? e.w[i] : 0.f;
         pos[k] = i < len ? e.pos[i] : INT32_MIN;
         newest = max(newest, pos[k]);
     }
-    const int64_t border = (int64_t)block_newest(newest, red[0][0]) - a.recent;
+    const int64_t border = (int64_t)block_newest<WAVES>(newest, red[0][0]) - a.recent;
     uint32_t key[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) key[k] = k * EVICT_THREADS + tid < len ? slot_key(w[k], pos[k], a.first, border) : 0;
+    for (int k = 0; k < K; ++k) key[k] = k * THREADS + tid < len ? slot_key(w[k], pos[k], a.first, border) : 0;
     uint32_t found = 0;                                      // the keys from here on are at least n
     int above = 0;                                           // the keys beyond it, once it is the n-th
     bool exact = false;                                      // just n keys from `found` on
@@ -100,7 +104,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, E
         for (int j = 0; j < 3; ++j) {
             many[j] = 0;
 #pragma unroll
-            for (int v = 0; v < EVICT_WAVES; ++v) many[j] += red[turn][j][v];
+            for (int v = 0; v < WAVES; ++v) many[j] += red[turn][j][v];
         }
         const int step = many[2] >= n ? 3 : many[1] >= n ? 2 : many[0] >= n ? 1 : 0;
         found |= (uint32_t)step << shift;
@@ -112,18 +116,18 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, E
         int more = 0;
 #pragma unroll
         for (int k = 0; k < K; ++k) more += __popcll(__ballot(key[k] > found));
-        above = waves_sum(more, red[turn][0]);
+        above = waves_sum<WAVES>(more, red[turn][0]);
         want = n - above;
     }
     uint32_t stays = 0;
     if (exact) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) if (k * EVICT_THREADS + tid < len && key[k] >= found) stays |= 1u << k;
+        for (int k = 0; k < K; ++k) if (k * THREADS + tid < len && key[k] >= found) stays |= 1u << k;
     } else {
         unsigned long long equal[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            equal[k] = __ballot(k * EVICT_THREADS + tid < len && key[k] == found);
+            equal[k] = __ballot(k * THREADS + tid < len && key[k] == found);
             if (lane == 0) before[k][wave] = __popcll(equal[k]);
         }
         __syncthreads();
@@ -131,9 +135,9 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, E
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             int mine = base;
-            for (int v = 0; v < EVICT_WAVES; ++v) { const int x = before[k][v]; base += x; if (v < wave) mine += x; }
+            for (int v = 0; v < WAVES; ++v) { const int x = before[k][v]; base += x; if (v < wave) mine += x; }
             const bool eq = equal[k] >> lane & 1;
-            if (k * EVICT_THREADS + tid < len && (key[k] > found || (eq && mine + lanes_below(equal[k]) < want))) stays |= 1u << k;
+            if (k * THREADS + tid < len && (key[k] > found || (eq && mine + lanes_below(equal[k]) < want))) stays |= 1u << k;
         }
         __syncthreads();
     }
@@ -141,7 +145,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, E
     unsigned long long holes[K], moves[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int i = k * EVICT_THREADS + tid;
+        const int i = k * THREADS + tid;
         holes[k] = __ballot(i < n && !(stays >> k & 1));
         moves[k] = __ballot(i >= n && (stays >> k & 1));
         if (lane == 0) before[k][wave] = __popcll(holes[k]) | __popcll(moves[k]) << 16;
@@ -151,14 +155,14 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_kernel(KvView c, E
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         int mine = base;
-        for (int v = 0; v < EVICT_WAVES; ++v) { const int x = before[k][v]; base += x; if (v < wave) mine += x; }
+        for (int v = 0; v < WAVES; ++v) { const int x = before[k][v]; base += x; if (v < wave) mine += x; }
         hole_at[k] = holes[k] >> lane & 1 ? (mine & 0xffff) + lanes_below(holes[k]) : -1;
-        if (moves[k] >> lane & 1) movers[(mine >> 16) + lanes_below(moves[k])] = (uint16_t)(k * EVICT_THREADS + tid);
+        if (moves[k] >> lane & 1) movers[(mine >> 16) + lanes_below(moves[k])] = (uint16_t)(k * THREADS + tid);
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int i = k * EVICT_THREADS + tid;
+        const int i = k * THREADS + tid;
         if (i >= n) continue;
         int from = i;
         if (hole_at[k] >= 0) { from = movers[hole_at[k]]; w[k] = e.w[from]; pos[k] = e.pos[from]; }
@@ -173,7 +177,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView
     constexpr int BINS = 4096, EACH = BINS / EVICT_THREADS, AHEAD = 16;      // AHEAD: loads of an array on their way at a time
     __shared__ int hist[BINS], red[2][3][EVICT_WAVES], pick[3], taken;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const EvictHead e = evict_head(c, a);
+    const EvictHead e = evict_head<EVICT_THREADS>(c, a);
     const int len = e.len, n = e.n;
     if (n == len) return;
     const int per = (len + 64 * EVICT_WAVES - 1) / (64 * EVICT_WAVES) * 64, i0 = wave * per + lane, i1 = min(len, (wave + 1) * per);
@@ -185,7 +189,7 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) newest = max(newest, pos[u]);
     }
-    const int64_t border = (int64_t)block_newest(newest, red[0][0]) - a.recent;
+    const int64_t border = (int64_t)block_newest<EVICT_WAVES>(newest, red[0][0]) - a.recent;
     float w[AHEAD];
     int pos[AHEAD];
     auto load = [&](int i) {                                   // slots i, i + 64 ..
@@ -406,10 +410,14 @@ extern "C" int poss_kv_evict(const poss_kv_cache *cache, const float *weights, c
     const KvView c = kv_view(*cache);
     const EvictArgs a{weights, positions, lengths, budget, first, recent, kept, weights_out, positions_out, lengths_out};
     const dim3 heads(c.hkv, c.n_seq);
-    if (c.slots <= 2 * EVICT_THREADS) evict_select_kernel<2><<<heads, EVICT_THREADS, 0, st>>>(c, a);
-    else if (c.slots <= 4 * EVICT_THREADS) evict_select_kernel<4><<<heads, EVICT_THREADS, 0, st>>>(c, a);
-    else if (c.slots <= 8 * EVICT_THREADS) evict_select_kernel<8><<<heads, EVICT_THREADS, 0, st>>>(c, a);
-    else if (c.slots <= 16 * EVICT_THREADS) evict_select_kernel<16><<<heads, EVICT_THREADS, 0, st>>>(c, a);
+#define POSS_SELECT(THREADS, K) if (c.slots <= THREADS * K) evict_select_kernel<THREADS, K><<<heads, THREADS, 0, st>>>(c, a)
+    POSS_SELECT(256, 3);
+    else POSS_SELECT(256, 6);
+    else POSS_SELECT(512, 4);
+    else POSS_SELECT(512, 8);
+    else POSS_SELECT(512, 16);
+    else POSS_SELECT(1024, 16);
+#undef POSS_SELECT
     else evict_select_long_kernel<<<heads, EVICT_THREADS, 0, st>>>(c, a);
     const int most = budget < c.slots ? budget : c.slots;
     const dim3 grid((most + MOVE_SLOTS - 1) / MOVE_SLOTS, c.hkv, c.n_seq);
