@@ -160,10 +160,11 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
     const int tid = threadIdx.x;
     const int64_t r = blockIdx.x;
     const float c = LOG2_E / a.temperature;
-    // this part's ids [lo, hi); tiles are counted from the 16-byte boundary at or before lo, so that whole pieces are aligned loads
+    // this part's ids [lo, hi); tiles are counted from the 16-byte boundary at or before the row, so that whole pieces are aligned loads, and parts are whole
+    // tiles: only a row's first and last one may be less
     const T *row = static_cast<const T *>(a.x) + r * a.ldx;
-    const int lo = (int)blockIdx.y * a.per, hi = min(a.vocab, lo + a.per);
-    const int start = lo - (int)(reinterpret_cast<uintptr_t>(row + lo) % 16 / sizeof(T));
+    const int shift = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)), start = (int)blockIdx.y * a.per - shift;
+    const int lo = max(start, 0), hi = min(a.vocab, start + a.per);
     auto whole = [&](int i0) { return i0 >= lo && i0 + LP_TILE <= hi; };
     auto fetch = [&](int i0, vec *raw) {                   // the pieces of this thread in the whole tile at id i0
 #pragma unroll
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LogprobsArgs a) {
         if constexpr (TOP == 2) {
             bool equal = false;                            // whether a value may equal the border
             if (i0 == start) { border = near_nth(top, a.n_top); equal = border > -INFINITY; }
-            else if ((tile & (tile - 1)) == 0) border = fmaxf(border, near_nth(tops, a.n_top));      // of the tiles before, at the 2nd, 4th, 8th ..: a tile puts fewer on the list
+            else if (tile > 1 && (tile & (tile - 1)) == 0) border = fmaxf(border, near_nth(tops, a.n_top));      // of 2, 4, 8 .. tiles before: a tile puts fewer on the list
             tops = fmaxf(tops, top);
             ++tile;
             if (__any(equal ? top >= border : top > border)) {
@@ -330,15 +331,15 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_join_kernel(LogprobsArgs 
     write_row<T>(a, r, joined, room);
 }
 
-// Parts of a row: as many as give the chip four workgroups a CU, none of less than a tile.  per: ids of each, whole pieces of 16 bytes.
+// Parts of a row: as many as give the chip four workgroups a CU, whole tiles each.  (A row that begins off alignment by less than 16 bytes has up to 7 ids more to cover.)
 static int logprobs_parts(int rows, int vocab, int *per = nullptr) {
+    const int tiles = (vocab + 7 + LP_TILE - 1) / LP_TILE;
     int p = rows ? 1024 / rows : 1;
-    const int most = (vocab + LP_TILE - 1) / LP_TILE;
-    p = p < most ? p : most;
+    p = p < tiles ? p : tiles;
     p = p < 1 ? 1 : p > LP_MOST_PARTS ? LP_MOST_PARTS : p;
-    const int ids = ((vocab + p - 1) / p + 7) / 8 * 8;
-    if (per) *per = ids;
-    return (vocab + ids - 1) / ids;
+    const int each = (tiles + p - 1) / p;
+    if (per) *per = each * LP_TILE;
+    return (tiles + each - 1) / each;
 }
 
 template <typename T>
