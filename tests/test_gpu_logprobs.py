@@ -109,6 +109,23 @@ def test_rows_of_every_kind(t, V):
         check(x, None, 20, temperature, P.logprobs(x, n_top=20, temperature=temperature))
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,V", [(1100, 9000), (1300, 4103), (500, 13001)])
+def test_many_rows_of_several_tiles(t, rows, V):
+    """One workgroup, or two, walk a row tile by tile; the best against a stable sort."""
+    print(f"logprobs tiles {t} {rows}x{V}", flush=True)
+    x = logits(np.random.default_rng(rows), rows, V, t)
+    logp, entropy, ids, top = (g.cpu().numpy() for g in P.logprobs(x, torch.zeros(rows, dtype=torch.int32, device="cuda"), n_top=7))
+    xs = x.double().cpu().numpy()
+    want = np.argsort(-xs, axis=1, kind="stable")[:, :7]
+    assert np.array_equal(ids, want)
+    lp, h = o.logprobs(xs)
+    r = 2.0 ** -22 * 40 + (V / 256 + 64) * 2.0 ** -24          # magnitudes of z, d and lse here are below 20
+    assert np.abs(top - np.take_along_axis(lp, want, 1)).max() <= r and np.abs(entropy - h).max() <= 8 * r
+    fine = np.isfinite(lp[:, 0])
+    assert np.array_equal(logp[~fine], lp[~fine, 0]) and np.abs(logp[fine] - lp[fine, 0]).max() <= r
+
+
 def test_many_rows_and_given_outputs():
     rng = np.random.default_rng(3)
     x = logits(rng, 700, 3001, "bf16")

@@ -45,7 +45,9 @@ def rows(rng, n, h, d, t, pad=0, shift=0, head_pad=0):
 @pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("n,h,d,rot,pad,shift,head_pad", [(1, 1, 2, 2, 0, 0, 0), (1, 8, 128, 128, 0, 0, 0), (3, 5, 128, 96, 0, 0, 0), (2, 3, 64, 64, 8, 0, 0), (7, 2, 80, 20, 3, 1, 0), (130, 4, 96, 32, 0, 0, 32),
-                                                          (5, 1, 256, 256, 0, 0, 0), (17, 3, 33, 16, 0, 0, 0), (1, 40, 128, 64, 0, 8, 0), (300, 1, 64, 2, 0, 0, 0), (2, 2, 300, 256, 1, 3, 5)])
+                                                          (5, 1, 256, 256, 0, 0, 0), (17, 3, 33, 16, 0, 0, 0), (1, 40, 128, 64, 0, 8, 0), (300, 1, 64, 2, 0, 0, 0), (2, 2, 300, 256, 1, 3, 5),
+                                                          (200, 5, 64, 64, 8, 0, 0), (261, 3, 128, 96, 0, 0, 0), (300, 2, 256, 256, 0, 0, 0), (250, 4, 96, 32, 0, 0, 32), (220, 40, 128, 128, 0, 8, 0),
+                                                          (220, 2, 64, 64, 1, 1, 0), (1001, 1, 32, 16, 0, 0, 0)])
 def test_rotary_against_float64(t, interleaved, n, h, d, rot, pad, shift, head_pad):
     print(f"rotary {t} interleaved {interleaved} {n}x{h}x{d} rot {rot} pad {pad} shift {shift} head_pad {head_pad}", flush=True)
     rng = np.random.default_rng(n * 100 + d)
@@ -108,7 +110,8 @@ def make_cache(rng, t, n_seq, per, hkv, dh, page, spare=2, apart=0):
 
 APPENDS = [  # n_seq, rows, hq, hkv, dh, page, kind of rows
     (1, 1, 4, 2, 64, 32, "decode"), (5, 5, 8, 8, 128, 64, "decode"), (2, 70, 2, 1, 96, 32, "prompt"), (1, 300, 8, 2, 128, 64, "prompt"), (3, 200, 5, 5, 64, 128, "prompt"), (2, 33, 7, 1, 256, 32, "any"),
-    (4, 90, 3, 3, 32, 64, "any"), (1, 129, 0, 4, 160, 128, "prompt"), (3, 65, 16, 2, 224, 32, "offset")]
+    (4, 90, 3, 3, 32, 64, "any"), (1, 129, 0, 4, 160, 128, "prompt"), (3, 65, 16, 2, 224, 32, "offset"),
+    (2, 260, 4, 3, 64, 32, "any"), (3, 400, 2, 2, 128, 64, "offset"), (210, 210, 4, 2, 96, 32, "decode"), (1, 700, 0, 1, 32, 128, "offset"), (5, 333, 6, 6, 160, 64, "prompt")]
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
@@ -132,7 +135,9 @@ def test_append(t, interleaved, n_seq, rows_, hq, hkv, dh, page, how):
     if rows_ > 4:
         slots[2], slots[4] = -1, slots_all                 # padding, and one past the end
     if rows_ > 40:
-        seq[17], seq[18], slots[30] = -1, n_seq, -2 ** 31
+        slots[30] = -2 ** 31
+        if how != "decode":
+            seq[17], seq[18] = -1, n_seq
     table = cache.tensors[2]
     if how == "any":
         table[0, 1] = -1                                   # pages that are not there
