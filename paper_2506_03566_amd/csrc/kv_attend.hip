@@ -19,6 +19,7 @@ typedef f16_t  f16x8 __attribute__((ext_vector_type(8)));
 constexpr int ATT_BLOCK = 32;                 // slots of a block: never across pages
 constexpr int ATT_WAVES = 4;
 constexpr int ATT_LEAST = 2, ATT_MOST = 512;   // blocks of a workgroup at least, workgroups of a launch at most
+constexpr int ATT_ROW = 2 * ATT_WAVES;        // blocks of a row that one workgroup takes
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct AttendArgs {
@@ -26,7 +27,7 @@ struct AttendArgs {
     const void *q; int64_t q_row; void *out; int64_t out_row;
     const int32_t *lengths; int max_len; float scale;
     float *lse; const float *weights; float *weights_out;
-    int W;                // workgroups along the batch's slots
+    int W;                // workgroups along the batch's slots; 0: one for each row
     float *part;          // [2 W][hkv * tiles][16][dh]
     float2 *part_ml;      // [2 W][hkv * tiles][16]
     float *scores; int64_t score_row;   // [n_seq][hq][score_row], log2 domain
@@ -202,26 +203,32 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, Attend
     constexpr int ROW = DH + 4;
     __shared__ float lds_o[ATT_WAVES * 16 * ROW];
     __shared__ float2 lds_ml[ATT_WAVES][16];
+    __shared__ float lds_lse[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g4 = lane >> 4;
     const int w = blockIdx.x, hk = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles;
     const int group = a.hq / c.hkv, head0 = hk * group + tile * 16, heads = min(16, group - tile * 16);
     const T *ks = static_cast<const T *>(c.k), *vs = static_cast<const T *>(c.v), *qs = static_cast<const T *>(a.q);
     T *out = static_cast<T *>(a.out);
     const int P = 1 << c.shift;
+    const bool by_rows = a.W == 0;                             // a workgroup is a row
     // rows without a block are nobody's: workgroup b % W writes row b
-    for (int b = w; b < c.n_seq; b += a.W) {
+    for (int b = w; b < c.n_seq; b += by_rows ? c.n_seq : a.W) {
         const int len = a.lengths[b];
         if (row_blocks(len, a.max_len)) continue;
         for (int i = threadIdx.x; i < heads * DH; i += 64 * ATT_WAVES) out[b * a.out_row + (int64_t)head0 * DH + i] = from_f<T>(len > 0 ? NAN : 0.f);
         if ((int)threadIdx.x < heads && a.lse) a.lse[(int64_t)b * a.hq + head0 + threadIdx.x] = len > 0 ? NAN : -INFINITY;
     }
-    const Batch batch = count_blocks(a.lengths, c.n_seq, a.max_len);
-    const int64_t parts = attend_parts(batch.all, a.W);
-    if (w >= parts) return;
-    int64_t at = times_over(batch.all, w, parts);
-    const int64_t end = times_over(batch.all, w + 1, parts);
-    int b; int64_t first;
-    find_row(batch, a.lengths, c.n_seq, a.max_len, at, b, first);
+    int64_t at = 0, end, first = 0;
+    int b = w;
+    if (by_rows) end = row_blocks(a.lengths[w], a.max_len);
+    else {
+        const Batch batch = count_blocks(a.lengths, c.n_seq, a.max_len);
+        const int64_t parts = attend_parts(batch.all, a.W);
+        if (w >= parts) return;
+        at = times_over(batch.all, w, parts);
+        end = times_over(batch.all, w + 1, parts);
+        find_row(batch, a.lengths, c.n_seq, a.max_len, at, b, first);
+    }
     const float scale = a.scale * LOG2E;
     Tile<T, DH> t;
     while (at < end) {
@@ -307,7 +314,7 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, Attend
                 if (d == 0) {
                     const float lse2 = top + __builtin_amdgcn_logf(sum) - lift<T>();
                     if (a.lse) a.lse[(int64_t)b * a.hq + head0 + h] = lse2 * LN2;
-                    if (WEIGHED) a.row_lse[(int64_t)b * a.hq + head0 + h] = lse2;
+                    if (WEIGHED) { if (by_rows && a.tiles == 1) lds_lse[h] = lse2; else a.row_lse[(int64_t)b * a.hq + head0 + h] = lse2; }
                 }
             } else {
                 *reinterpret_cast<f32x4 *>(a.part + (slot * 16 + h) * DH + d) = r;
@@ -315,6 +322,18 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, Attend
             }
         }
         at = first + i1;
+        if constexpr (WEIGHED) {
+            if (by_rows && a.tiles == 1) {                     // all the key head's heads are here: their weights need no second launch
+                __syncthreads();
+                const int64_t row = ((int64_t)b * c.hkv + hk) * c.slots;
+                for (int s = threadIdx.x; s < len; s += 64 * ATT_WAVES) {
+                    const float *z = a.scores + ((int64_t)b * a.hq + head0) * a.score_row + s;
+                    float x = 0.f;
+                    for (int h = 0; h < heads; ++h) x += exp2_of(z[h * a.score_row] - lds_lse[h]);
+                    a.weights_out[row + s] = (a.weights ? a.weights[row + s] : 0.f) + x;
+                }
+            }
+        }
     }
 }
 
@@ -337,14 +356,17 @@ __global__ void __launch_bounds__(256) attend_finish_kernel(KvView c, AttendArgs
     if (!blocks) return;
     const int chunk = (int)blockIdx.x - joins;
     if (chunk >= 0 && chunk * FINISH_SLOTS >= len) return;
-    const Batch batch = count_blocks(a.lengths, c.n_seq, a.max_len);
-    const int64_t parts = attend_parts(batch.all, a.W), first = blocks_before(batch, a.lengths, c.n_seq, a.max_len, b);
-    // the last workgroup w with w * all / parts <= block
-    auto holder = [&](int64_t block) {
-        const int64_t x = (block + 1) * parts - 1;
-        return x < 1ll << 32 && batch.all < 1ll << 32 ? (int)((uint32_t)x / (uint32_t)batch.all) : (int)(x / batch.all);
-    };
-    const int w0 = holder(first), n = holder(first + blocks - 1) - w0 + 1;
+    int w0 = 0, n = 1;
+    if (a.W) {
+        const Batch batch = count_blocks(a.lengths, c.n_seq, a.max_len);
+        const int64_t parts = attend_parts(batch.all, a.W), first = blocks_before(batch, a.lengths, c.n_seq, a.max_len, b);
+        // the last workgroup w with w * all / parts <= block
+        auto holder = [&](int64_t block) {
+            const int64_t x = (block + 1) * parts - 1;
+            return x < 1ll << 32 && batch.all < 1ll << 32 ? (int)((uint32_t)x / (uint32_t)batch.all) : (int)(x / batch.all);
+        };
+        w0 = holder(first); n = holder(first + blocks - 1) - w0 + 1;
+    }
     // piece p of the head of this group's index j
     auto slot = [&](int p, int j) { return ((int64_t)(2 * (w0 + p) + (p == 0 ? 1 : 0)) * c.hkv * a.tiles + hk * a.tiles + j / 16) * 16 + j % 16; };
     if (chunk < 0) {
@@ -437,13 +459,16 @@ struct AttendPlan { int tiles, W; int64_t score_row; size_t part, part_ml, row_l
 static AttendPlan attend_plan(const KvView &c, int esize, int hq, int max_len, bool weighed) {
     AttendPlan p{};
     p.tiles = (hq / c.hkv + 15) / 16;
-    const int64_t per = (int64_t)c.hkv * p.tiles, blocks = (int64_t)c.n_seq * ((max_len + ATT_BLOCK - 1) / ATT_BLOCK);
+    const int64_t per = (int64_t)c.hkv * p.tiles, longest = (max_len + ATT_BLOCK - 1) / ATT_BLOCK, blocks = c.n_seq * longest;
     // As many workgroups as the registers let a CU hold, and never more: a third round of a few costs as much as a whole one (40 key heads, 16 rows: 94 us with 13 x 40
     // workgroups, 74 with 12 x 40).
     const bool two = esize == 2 ? c.dh <= 160 : c.dh <= (weighed ? 96 : 128);
     int64_t W = (two ? ATT_MOST : ATT_MOST / 2) / per;
     if (W > (blocks + ATT_LEAST - 1) / ATT_LEAST) W = (blocks + ATT_LEAST - 1) / ATT_LEAST;
     p.W = W < 1 ? 1 : (int)W;
+    // Rows of a few blocks are a workgroup each, without a join: up to two blocks a wave, or four where rows and heads are many (8 rows of up to 250 slots 12.8 -> 8.2 us,
+    // 64 of up to 500 weighed 28.7 -> 24.7; 4 of up to 1000 15.2 -> 18.8, so not those; 2 of up to 318 with one key head 12.2 -> 13.9).
+    if (longest <= ATT_ROW || (longest <= 2 * ATT_ROW && c.n_seq * per >= 64)) p.W = 0;
     p.score_row = (max_len + ATT_BLOCK - 1) / ATT_BLOCK * ATT_BLOCK;
     auto take = [&](size_t n) { const size_t at = p.bytes; p.bytes += (n + 255) / 256 * 256; return at; };
     if (p.W > 1) {
@@ -460,7 +485,7 @@ static AttendPlan attend_plan(const KvView &c, int esize, int hq, int max_len, b
 
 template <typename T, int DH>
 static void launch_attend(const KvView &c, const AttendArgs &a, bool weighed, hipStream_t st) {
-    const dim3 grid(a.W, c.hkv * a.tiles);
+    const dim3 grid(a.W ? a.W : c.n_seq, c.hkv * a.tiles);
     if (weighed) attend_kernel<T, DH, true><<<grid, 64 * ATT_WAVES, 0, st>>>(c, a);
     else attend_kernel<T, DH, false><<<grid, 64 * ATT_WAVES, 0, st>>>(c, a);
 }
@@ -476,9 +501,9 @@ static void launch_attend_t(const KvView &c, const AttendArgs &a, bool weighed, 
         case 224: launch_attend<T, 224>(c, a, weighed, st); break;
         default: launch_attend<T, 256>(c, a, weighed, st); break;
     }
-    const int chunks = weighed ? (a.max_len + FINISH_SLOTS - 1) / FINISH_SLOTS : 0;
+    const int chunks = weighed && (a.W || a.tiles > 1) ? (a.max_len + FINISH_SLOTS - 1) / FINISH_SLOTS : 0;
     const bool many = (int64_t)c.n_seq * a.hq > 1024;
-    const int joins = a.W == 1 ? 0 : many ? (a.hq / c.hkv + 3) / 4 : a.hq / c.hkv;
+    const int joins = a.W <= 1 ? 0 : many ? (a.hq / c.hkv + 3) / 4 : a.hq / c.hkv;
     const dim3 grid(joins + chunks, c.hkv, c.n_seq);
     if (joins + chunks == 0) return;
     if (many) attend_finish_kernel<T, 1><<<grid, 256, 0, st>>>(c, a, joins);
