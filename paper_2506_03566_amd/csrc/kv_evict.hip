@@ -170,12 +170,215 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView c, EvictAr
     }
 }
 
-// The same for any number of slots: what is read is read again for every pass, by each wave its own stretch of slots, 64 side by side, with a barrier only between passes.  The
-// 12 highest bits of the n-th key (sign, exponent, three bits of mantissa) come from a histogram, the others by counting among the keys that share them, in LDS;
-// where those are too many (equal weights), from two more histograms.
+// More slots: the 12 highest bits of the n-th key (sign, exponent, three bits of mantissa) come from a histogram, the others by counting among the keys that share
+// them, in LDS; where those are too many (equal weights), from two more histograms.  each(f): f of every key of this thread; 1024 threads.
+// The n-th key, how many of the keys equal to it stay (the first in slot order), and how many there are.
+constexpr int BINS = 4096;
+struct NthKey { uint32_t key; int want, share; };
+struct NthRoom { int hist[BINS], red[2][3][EVICT_WAVES], pick[3], taken; };
+template <class Each>
+__device__ __forceinline__ NthKey nth_key(Each each, int n, int len, NthRoom &room) {
+    constexpr int EACH = BINS / EVICT_THREADS, FEW = 8;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // the digit of `bits` bits at `shift` of the key that is the want-th largest of those with this prefix: prefix, want, and how many share the new prefix
+    uint32_t prefix = 0;
+    int want = n, share = len;
+    auto digit = [&](int shift, int bits) {
+        __syncthreads();
+        for (int i = tid; i < BINS; i += EVICT_THREADS) room.hist[i] = 0;
+        __syncthreads();
+        each([&](uint32_t k) { if (shift + bits == 32 || k >> (shift + bits & 31) == prefix) atomicAdd(&room.hist[k >> shift & ((1 << bits) - 1)], 1); });
+        __syncthreads();
+        // thread t looks at bins EACH t .. EACH t + EACH - 1, counted from the last
+        int mine[EACH], sum = 0;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) sum += mine[j] = room.hist[BINS - 1 - (tid * EACH + j)];
+        int at = sum;
+        for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(at, o); if (lane >= o) at += y; }
+        if (lane == 63) room.red[1][0][wave] = at;
+        __syncthreads();
+        at -= sum;
+        for (int v = 0; v < wave; ++v) at += room.red[1][0][v];
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            if (at < want && want <= at + mine[j]) { room.pick[0] = BINS - 1 - (tid * EACH + j); room.pick[1] = want - at; room.pick[2] = mine[j]; }
+            at += mine[j];
+        }
+        __syncthreads();
+        prefix = prefix << bits | (uint32_t)room.pick[0];
+        want = room.pick[1]; share = room.pick[2];
+    };
+    if (tid == 0) room.taken = 0;                              // (seen by all behind digit()'s barriers)
+    digit(20, 12);
+    if (share > BINS) {
+        digit(8, 12);
+        digit(0, 8);
+        return NthKey{prefix, want, share};
+    }
+    each([&](uint32_t k) { if (k >> 20 == prefix) room.hist[atomicAdd(&room.taken, 1)] = (int)k; });      // (in any order: they are counted)
+    __syncthreads();
+    if (share <= 64 * FEW) {                                   // few: one wave counts them bit by bit, without a barrier
+        if (wave == 0) {
+            uint32_t key[FEW], found = prefix << 20;
+#pragma unroll
+            for (int j = 0; j < FEW; ++j) key[j] = j * 64 + lane < share ? (uint32_t)room.hist[j * 64 + lane] : 0;
+            int from = share, beyond = 0;                      // keys from `found` on, and those beyond its stretch
+            for (int bit = 19; bit >= 0 && from != want; --bit) {
+                int many = 0;
+#pragma unroll
+                for (int j = 0; j < FEW; ++j) many += __popcll(__ballot(j * 64 + lane < share && key[j] >= (found | 1u << bit)));
+                if (many >= want) { found |= 1u << bit; from = many; } else beyond = many;
+            }
+            // with `from` of them exactly as many as stay, the lowest of these is the n-th and none of its equals goes
+            if (from == want) {
+                uint32_t low = ~0u;
+#pragma unroll
+                for (int j = 0; j < FEW; ++j) if (j * 64 + lane < share && key[j] >= found) low = min(low, key[j]);
+                for (int o = 32; o; o >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o));
+                found = low; beyond = want - 1; from = want;
+            }
+            if (lane == 0) { room.pick[0] = (int)found; room.pick[1] = want - beyond; room.pick[2] = from - beyond; }
+        }
+        __syncthreads();
+        return NthKey{(uint32_t)room.pick[0], room.pick[1], room.pick[2]};
+    }
+    uint32_t key[EACH], found = prefix << 20;
+    bool in[EACH];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) { in[j] = j * EVICT_THREADS + tid < share; key[j] = in[j] ? (uint32_t)room.hist[j * EVICT_THREADS + tid] : 0; }
+    // often all are the same number (weights of zero)
+    uint32_t differ = 0;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) if (in[j]) differ |= key[j] ^ (uint32_t)room.hist[0];
+    if (__any(differ) && lane == 0) room.pick[0] = -1;         // (`prefix` has been read from there: barriers behind that)
+    __syncthreads();
+    if (room.pick[0] != -1) return NthKey{(uint32_t)room.hist[0], want, share};
+    int turn = 0, beyond = 0, least = share;                   // keys above `found`'s stretch, and from it on
+    for (int shift = 18; shift >= 0; shift -= 2, turn ^= 1) {
+        int many[3] = {0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+#pragma unroll
+            for (int j = 0; j < 3; ++j) many[j] += __popcll(__ballot(in[k] && key[k] >= (found | (uint32_t)(j + 1) << shift)));
+        if (lane == 0)
+            for (int j = 0; j < 3; ++j) room.red[turn][j][wave] = many[j];
+        __syncthreads();
+        for (int j = 0; j < 3; ++j) {
+            many[j] = 0;
+#pragma unroll
+            for (int v = 0; v < EVICT_WAVES; ++v) many[j] += room.red[turn][j][v];
+        }
+        const int step = many[2] >= want ? 3 : many[1] >= want ? 2 : many[0] >= want ? 1 : 0;
+        found |= (uint32_t)step << shift;
+        if (step < 3) beyond = many[step];                     // (with step 3 what lies above is as before)
+        if (step) least = many[step - 1];
+    }
+    return NthKey{found, want - beyond, least - beyond};
+}
+
+// Up to K * 1024 slots, keys in registers: slot k * 1024 + t is thread t's k-th.
+template <int K>
+__global__ void __launch_bounds__(EVICT_THREADS) evict_select_wide_kernel(KvView c, EvictArgs a) {
+    constexpr int COUNTS = K * EVICT_WAVES, AHEAD = 8;
+    __shared__ NthRoom room;
+    __shared__ int before[COUNTS];
+    __shared__ uint16_t movers[K * EVICT_THREADS / 2];         // as many as there are holes, at most half of the slots
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const EvictHead e = evict_head<EVICT_THREADS>(c, a);
+    const int len = e.len, n = e.n;
+    if (n == len) return;
+    uint32_t key[K];
+    int newest = INT32_MIN;
+    {
+        int pos[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int i = k * EVICT_THREADS + tid;
+            pos[k] = i < len ? e.pos[i] : INT32_MIN;
+            newest = max(newest, pos[k]);
+        }
+        const int64_t border = (int64_t)block_newest<EVICT_WAVES>(newest, room.red[0][0]) - a.recent;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int i = k * EVICT_THREADS + tid;
+            key[k] = slot_key(i < len ? e.w[i] : 0.f, pos[k], a.first, border);
+        }
+    }
+    const NthKey nth = nth_key([&](auto f) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) if (k * EVICT_THREADS + tid < len) f(key[k]);
+    }, n, len, room);
+    // counts[k][wave], in slot order, become sums of those before
+    auto count_off = [&]() {
+        __syncthreads();
+        if (wave == 0) {
+            int x[COUNTS / 64], sum = 0;
+#pragma unroll
+            for (int j = 0; j < COUNTS / 64; ++j) sum += x[j] = before[lane * (COUNTS / 64) + j];
+            int at = sum;
+            for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(at, o); if (lane >= o) at += y; }
+            at -= sum;
+#pragma unroll
+            for (int j = 0; j < COUNTS / 64; ++j) { before[lane * (COUNTS / 64) + j] = at; at += x[j]; }
+        }
+        __syncthreads();
+    };
+    const bool ties = nth.want < nth.share;
+    uint32_t stays = 0;
+    if (ties) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const unsigned long long eq = __ballot(k * EVICT_THREADS + tid < len && key[k] == nth.key);
+            if (lane == 0) before[k * EVICT_WAVES + wave] = __popcll(eq);
+        }
+        count_off();
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const bool in = k * EVICT_THREADS + tid < len;
+        const unsigned long long eq = __ballot(in && key[k] == nth.key);
+        if (in && (key[k] > nth.key || (key[k] == nth.key && (!ties || before[k * EVICT_WAVES + wave] + lanes_below(eq) < nth.want)))) stays |= 1u << k;
+    }
+    // holes below n and movers from n on, counted off in the two halves of a number
+    __syncthreads();
+    auto holes_at = [&](int k) { return __ballot(k * EVICT_THREADS + tid < n && !(stays >> k & 1)); };
+    auto moves_at = [&](int k) { return __ballot(k * EVICT_THREADS + tid >= n && (stays >> k & 1)); };
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const unsigned long long holes = holes_at(k), moves = moves_at(k);
+        if (lane == 0) before[k * EVICT_WAVES + wave] = __popcll(holes) | __popcll(moves) << 16;
+    }
+    count_off();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const unsigned long long moves = moves_at(k);
+        if (moves >> lane & 1) movers[(before[k * EVICT_WAVES + wave] >> 16) + lanes_below(moves)] = (uint16_t)(k * EVICT_THREADS + tid);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k0 = 0; k0 < K; k0 += AHEAD) {
+        int from[AHEAD], pos[AHEAD];
+        float w[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int k = k0 + u, i = k * EVICT_THREADS + tid;
+            const unsigned long long holes = holes_at(k);
+            from[u] = i >= n ? -1 : holes >> lane & 1 ? movers[(before[k * EVICT_WAVES + wave] & 0xffff) + lanes_below(holes)] : i;
+            if (from[u] >= 0) { w[u] = e.w[from[u]]; pos[u] = e.pos[from[u]]; }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int i = (k0 + u) * EVICT_THREADS + tid;
+            if (from[u] >= 0) { e.kept[i] = from[u]; e.wo[i] = w[u]; e.po[i] = pos[u]; }
+        }
+    }
+}
+
+// The same for any number of slots: what is read is read again for every pass, by each wave its own stretch of slots, 64 side by side, with a barrier only between passes.
 __global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView c, EvictArgs a) {
-    constexpr int BINS = 4096, EACH = BINS / EVICT_THREADS, AHEAD = 16;      // AHEAD: loads of an array on their way at a time
-    __shared__ int hist[BINS], red[2][3][EVICT_WAVES], pick[3], taken;
+    constexpr int AHEAD = 16;                                  // loads of an array on their way at a time
+    __shared__ NthRoom room;
+    int (*const red)[3][EVICT_WAVES] = room.red;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const EvictHead e = evict_head<EVICT_THREADS>(c, a);
     const int len = e.len, n = e.n;
@@ -197,84 +400,15 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView
         for (int u = 0; u < AHEAD; ++u) { const bool in = i + 64 * u < i1; w[u] = in ? e.w[i + 64 * u] : 0.f; pos[u] = in ? e.pos[i + 64 * u] : 0; }
     };
     auto key_of = [&](int u) { return slot_key(w[u], pos[u], a.first, border); };
-    // the digit of `bits` bits at `shift` of the key that is the want-th largest of those with this prefix: prefix, want, and how many share the new prefix
-    uint32_t prefix = 0;
-    int want = n, share = len;
-    auto digit = [&](int shift, int bits) {
-        __syncthreads();
-        for (int i = tid; i < BINS; i += EVICT_THREADS) hist[i] = 0;
-        __syncthreads();
+    const NthKey nth = nth_key([&](auto f) {
         for (int i = i0; i < i1; i += 64 * AHEAD) {
             load(i);
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const uint32_t k = key_of(u);
-                if (i + 64 * u < i1 && (shift + bits == 32 || k >> (shift + bits & 31) == prefix)) atomicAdd(&hist[k >> shift & ((1 << bits) - 1)], 1);
-            }
+            for (int u = 0; u < AHEAD; ++u) if (i + 64 * u < i1) f(key_of(u));
         }
-        __syncthreads();
-        // thread t looks at bins EACH t .. EACH t + EACH - 1, counted from the last
-        int mine[EACH], sum = 0;
-#pragma unroll
-        for (int j = 0; j < EACH; ++j) sum += mine[j] = hist[BINS - 1 - (tid * EACH + j)];
-        int at = sum;
-        for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(at, o); if (lane >= o) at += y; }
-        if (lane == 63) red[1][0][wave] = at;
-        __syncthreads();
-        at -= sum;
-        for (int v = 0; v < wave; ++v) at += red[1][0][v];
-#pragma unroll
-        for (int j = 0; j < EACH; ++j) {
-            if (at < want && want <= at + mine[j]) { pick[0] = BINS - 1 - (tid * EACH + j); pick[1] = want - at; pick[2] = mine[j]; }
-            at += mine[j];
-        }
-        __syncthreads();
-        prefix = prefix << bits | (uint32_t)pick[0];
-        want = pick[1]; share = pick[2];
-    };
-    if (tid == 0) taken = 0;                                   // (seen by all behind digit()'s barriers)
-    digit(20, 12);
-    if (share <= BINS) {
-        for (int i = i0; i < i1; i += 64 * AHEAD) {
-            load(i);
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const uint32_t k = key_of(u);
-                if (i + 64 * u < i1 && k >> 20 == prefix) hist[atomicAdd(&taken, 1)] = (int)k;      // (in any order: they are counted)
-            }
-        }
-        __syncthreads();
-        uint32_t key[EACH], found = prefix << 20;
-        bool in[EACH];
-#pragma unroll
-        for (int j = 0; j < EACH; ++j) { in[j] = j * EVICT_THREADS + tid < share; key[j] = in[j] ? (uint32_t)hist[j * EVICT_THREADS + tid] : 0; }
-        int turn = 0, beyond = 0, least = share;               // keys above `found`'s stretch, and from it on
-        for (int shift = 18; shift >= 0; shift -= 2, turn ^= 1) {
-            int many[3] = {0, 0, 0};
-#pragma unroll
-            for (int k = 0; k < EACH; ++k)
-#pragma unroll
-                for (int j = 0; j < 3; ++j) many[j] += __popcll(__ballot(in[k] && key[k] >= (found | (uint32_t)(j + 1) << shift)));
-            if (lane == 0)
-                for (int j = 0; j < 3; ++j) red[turn][j][wave] = many[j];
-            __syncthreads();
-            for (int j = 0; j < 3; ++j) {
-                many[j] = 0;
-#pragma unroll
-                for (int v = 0; v < EVICT_WAVES; ++v) many[j] += red[turn][j][v];
-            }
-            const int step = many[2] >= want ? 3 : many[1] >= want ? 2 : many[0] >= want ? 1 : 0;
-            found |= (uint32_t)step << shift;
-            if (step < 3) beyond = many[step];                 // (with step 3 what lies above is as before)
-            if (step) least = many[step - 1];
-        }
-        prefix = found;
-        want -= beyond;
-        share = least - beyond;
-    } else {
-        digit(8, 12);
-        digit(0, 8);
-    }
+    }, n, len, room);
+    const uint32_t prefix = nth.key;
+    const int want = nth.want, share = nth.share;
     // kept: keys above the prefix, and the first `want` of the `share` with it.  Each wave counts its equal ones, then its holes and movers, then writes.
     __syncthreads();
     const bool ties = want < share;
@@ -416,8 +550,9 @@ extern "C" int poss_kv_evict(const poss_kv_cache *cache, const float *weights, c
     else POSS_SELECT(512, 4);
     else POSS_SELECT(512, 8);
     else POSS_SELECT(512, 16);
-    else POSS_SELECT(1024, 16);
 #undef POSS_SELECT
+    else if (c.slots <= 16 * EVICT_THREADS) evict_select_wide_kernel<16><<<heads, EVICT_THREADS, 0, st>>>(c, a);
+    else if (c.slots <= 32 * EVICT_THREADS) evict_select_wide_kernel<32><<<heads, EVICT_THREADS, 0, st>>>(c, a);
     else evict_select_long_kernel<<<heads, EVICT_THREADS, 0, st>>>(c, a);
     const int most = budget < c.slots ? budget : c.slots;
     const dim3 grid((most + MOVE_SLOTS - 1) / MOVE_SLOTS, c.hkv, c.n_seq);
