@@ -385,7 +385,7 @@ typedef struct poss_kv_cache {
 
 /* Rotary positions of a head's first rot_dim values: pair i is (x[i], x[i + rot_dim/2]) or, interleaved, (x[2i], x[2i+1]); it becomes
  * magnitude * (a cos - b sin, b cos + a sin) at the angle position * freq[i], formed in 64 bits.  The other values stay.  A program may fill in
- * frequencies of its own (finite ones; angles up to 2^45). */
+ * frequencies of its own (finite ones). */
 #define POSS_ROPE_PAIRS 128
 typedef struct poss_rope {
     int32_t rot_dim, interleaved;            /* rot_dim: even, 2 .. 2 * POSS_ROPE_PAIRS */

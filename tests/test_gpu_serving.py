@@ -270,3 +270,21 @@ def test_offsets_beyond_32_bits():
     y.normal_()
     P.rotary(y, tokens[:2].contiguous(), P.Rope(64), z)
     assert np.abs(f64(z) - o.rotate(f64(y), [7, 4999], np.array(P.Rope(64).frequencies))).max() <= 2.0 ** -6
+
+
+def test_rotary_turns_keys_as_a_context_does():
+    """Layer 0's keys of a prompt, multiplied here and rotated by the call, are those in the context's cache but for sums in another order."""
+    pair = Pair("t_mid_bf16")
+    cfg, ctx = pair.cfg, pair.ctx
+    from synth import make_prompt
+    prompt = make_prompt(cfg)
+    ctx.prefill(prompt)
+    k, _ = ctx.debug_read_kv(-1, 0, 0, len(prompt))
+    w = pair.dev_weights
+    h = w["embed"][torch.tensor(prompt, device="cuda").long()].float()
+    u = (h * torch.rsqrt(h.pow(2).mean(dim=1, keepdim=True) + cfg.rms_eps) * w["layer0.attn_norm"].float()).to(torch.bfloat16).float()
+    x = (u @ w["layer0.wk"].float().t()).view(len(prompt), cfg.n_kv_heads, cfg.head_dim)
+    got = P.rotary(x, torch.arange(len(prompt), device="cuda").int(), P.Rope(cfg.head_dim, cfg.rope_theta)).to(torch.bfloat16).float().cpu().numpy()
+    differ = got != k
+    assert differ.mean() < 0.01 and np.abs(got - k).max() <= 2.0 ** -7 * np.abs(k).max()
+    pair.close()
