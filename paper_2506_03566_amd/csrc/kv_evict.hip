@@ -6,7 +6,7 @@
 // the j-th hole is filled from the j-th of those.  No source is a destination, so the moves need no order.
 //
 // A workgroup per head chooses, bound by latency (1025 slots of 8 heads 12 us, 4096 of 256 heads 16, 18580 of one 31, 131072 of 8 238); a second launch moves.  Keys move as rows; a
-// value row gives and takes single values, so that whole lines are read and parts of lines written: 32 sequences of up to 4096 slots to 2000, 8 heads of 128, bf16: 60 us for 102 MB
+// value row gives and takes single values, so that whole lines are read and parts of lines written: 32 sequences of up to 4096 slots to 2000, 8 heads of 128, bf16: 60 us for 105 MB
 // read and 91 written, 17 us of them the keys'.  Reading and writing the destinations' lines whole took as long.
 #include "kv.h"
 

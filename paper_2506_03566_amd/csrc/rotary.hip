@@ -1,7 +1,7 @@
 // Rotary positions, alone and on the way into a paged cache (include/poss.h: poss_rope_fill, poss_rotary, poss_kv_append).
 //
 // Pairs (a, b) -> magnitude (a cos - b sin, b cos + a sin), in float32, rounded once.  Bound by memory: everything is read once and written once.  8192 rows of 32 + 8 + 8
-// heads of 128 (bf16, 201 MB): 45 us, 4.5 TB/s, with no more traffic than that (99 MB read, 98 MB written); 8192 x 40 heads alone 38 us.  A row alone 4.7 us: launch, position
+// heads of 128 (bf16, 201 MB): 45 us, 4.5 TB/s, with no more traffic than that (102 MB read, 101 MB written); 8192 x 40 heads alone 38 us.  A row alone 4.7 us: launch, position
 // and slot, the page, the row.
 #include "kv.h"
 
