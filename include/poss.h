@@ -428,7 +428,8 @@ int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t ro
  * -infinity, zeros over nothing: a row of NaN and an lse of -infinity.
  * lse (may be NULL): float32 [n_seq][n_q_heads], the logarithm of the sum of exponentials.
  * weights_out (may be NULL): float32 [n_seq][n_kv_heads][slots], the weights that the slots have been given so far: weights (the same form; NULL: zeros;
- * may be weights_out) plus this row's p, summed over the heads that share the key head.  Slots beyond the length are left as they were.
+ * may be weights_out) plus this row's p, summed over the heads that share the key head.  Slots beyond the length are left as they were, all of a row
+ * whose length is above max_len; a row with a slot without a page has weights of NaN.
  * scratch: poss_kv_attend_scratch_bytes bytes, aligned to 256, for this call alone until it has run (two calls or graphs that may
  * run at the same time need one each).  Sums and statistics are float32; 16-bit caches take a
  * probability as the sum of two numbers of their type, 16 significant bits or more.

@@ -97,7 +97,8 @@ SHAPES = [  # lengths, hq, hkv, dh, page
     ([1], 1, 1, 64, 32), ([0], 4, 2, 64, 32), ([2], 8, 1, 128, 64), ([31, 32, 33], 4, 4, 64, 32), ([17], 32, 8, 128, 64), ([64, 0, 1, 63, 65, 128, 129], 8, 2, 128, 64), ([500, 1, 0, 700], 5, 5, 64, 128),
     ([255, 256, 257], 6, 2, 96, 32), ([1000], 16, 1, 128, 64), ([333, 90], 34, 2, 64, 32), ([4000, 3, 0, 1500, 2049], 8, 2, 128, 128), ([3000], 40, 40, 128, 64), ([700, 701], 8, 1, 256, 32),
     ([1, 2, 3, 4, 5] * 30, 4, 2, 32, 32), ([100, 1200], 48, 1, 160, 64), ([900], 9, 3, 192, 32), ([411, 60], 4, 2, 224, 128), ([9001], 8, 8, 64, 64),
-    ([300, 5, 0, 129] * 20 + [4000], 16, 2, 64, 32), ([90, 40] * 100, 6, 3, 96, 64)]
+    ([300, 5, 0, 129] * 20 + [4000], 16, 2, 64, 32), ([90, 40] * 100, 6, 3, 96, 64), ([200, 31], 40, 1, 64, 32), ([400, 3] * 20, 8, 2, 64, 32),
+    ([255, 0, 256], 17, 1, 32, 128), ([512] * 40, 34, 2, 128, 64)]
 
 
 @pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
@@ -174,7 +175,9 @@ def test_pages_that_are_not_there_and_lengths_beyond_the_bound(t):
     table[2, 1] = 10 ** 6
     good = c.cache.tensors
     c.cache = P.KvCache(good[0], good[1], torch.from_numpy(table).cuda())
-    out, lse = c.attend()
+    wo = torch.zeros(4, 2, c.slots, device="cuda")
+    out, lse = c.attend(weights_out=wo)
+    assert bool(wo[0, :, :200].isnan().all()) and bool(wo[2, :, :64].isnan().all()) and not bool(wo[0, :, 200:].any()) and not bool(wo[[1, 3]].isnan().any())
     assert bool(out[[0, 2]].isnan().all()) and bool(lse[[0, 2]].isnan().all())
     c.check(out, lse, 0.125, rows=[1, 3])
     c.cache = P.KvCache(*good)
@@ -183,7 +186,7 @@ def test_pages_that_are_not_there_and_lengths_beyond_the_bound(t):
     out, lse = c.attend(lengths=lengths, weights_out=wo)
     assert bool(out[[1, 3]].isnan().all()) and bool(lse[[1, 3]].isnan().all()) and not bool(out[2].any()) and bool((lse[2] == -np.inf).all())
     c.check(out, lse, 0.125, rows=[0])
-    assert not bool(wo[2].any()) and not bool(wo[0].isnan().any())
+    assert not bool(wo[1:].any()) and not bool(wo[0].isnan().any())
     out, lse = c.attend(lengths=torch.tensor([200, 129, 64, 1], dtype=torch.int32, device="cuda"), max_len=199)
     assert bool(out[0].isnan().all()) and not bool(out[1:].isnan().any())
 
