@@ -86,16 +86,17 @@ __global__ void __launch_bounds__(1024) append_kernel(KvView c, AppendArgs a, po
 }
 
 // ------------------------------------------------------------------------------------------ whole pieces of 16 bytes, many rows
-// A wave's part of a row: pieces of 16 bytes, of both members' halves at once where pairs lie apart.  units: of one head; of_units: 2^32 / units, rounded up.
-struct Units { int units; uint32_t of_units; };
+// A wave's part of a row: pieces of 16 bytes, of both members' halves at once where pairs lie apart.  units: of one head; of_units: 2^32 / units, rounded up; parts: waves
+// that share a row, 4 where rows alone would leave the chip idle (274 rows of 64 + 8 + 8 heads of 256: 26 -> 11 us), else 1.
+struct Units { int units; uint32_t of_units; int parts; };
 
 template <typename T, bool INTERLEAVED>
-__device__ __forceinline__ void rotate_pieces(const T *x, int64_t x_head, T *y, int64_t y_head, int heads, int rot, Units n, const float2 *cs) {
+__device__ __forceinline__ void rotate_pieces(const T *x, int64_t x_head, T *y, int64_t y_head, int heads, int rot, Units n, int part, const float2 *cs) {
     constexpr int E = 16 / sizeof(T);
     typedef T vec __attribute__((ext_vector_type(E)));
     const int half = rot >> 1, turned = INTERLEAVED ? rot / E : half / E, all = heads * n.units;
 #pragma unroll 2
-    for (int j = threadIdx.x & 63; j < all; j += 64) {
+    for (int j = part * 64 + (threadIdx.x & 63); j < all; j += 64 * n.parts) {
         const int h = (int)__umulhi((uint32_t)j, n.of_units), u = j - h * n.units;
         const T *xi = x + h * x_head;
         T *yi = y + h * y_head;
@@ -127,20 +128,20 @@ __device__ __forceinline__ void rotate_pieces(const T *x, int64_t x_head, T *y, 
     }
 }
 
-// A wave per row.
+// A wave per row, or n.parts of them.
 template <typename T, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) rotary_rows_kernel(const T *x, int64_t x_row, int64_t x_head, T *y, int64_t y_row, int64_t y_head, int rows, int heads, Units n,
                                                           const int32_t *__restrict__ positions, poss_rope rope, float sign) {
     __shared__ __align__(16) float2 cs[4][POSS_ROPE_PAIRS];
     const int wave = threadIdx.x >> 6;
-    const int64_t r = (int64_t)blockIdx.x * 4 + wave;
+    const int64_t r = n.parts == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
     if (r >= rows) return;
     rope_angles(rope, positions[r], sign, cs[wave], threadIdx.x & 63, 64);
     wave_lds_sync();
-    rotate_pieces<T, INTERLEAVED>(x + r * x_row, x_head, y + r * y_row, y_head, heads, rope.rot_dim, n, cs[wave]);
+    rotate_pieces<T, INTERLEAVED>(x + r * x_row, x_head, y + r * y_row, y_head, heads, rope.rot_dim, n, n.parts == 1 ? 0 : wave, cs[wave]);
 }
 
-// Queries and keys: a wave per row, in the first workgroups.  Values: behind them, a wave per square of eight by eight pieces - 16-bit types 64 rows by 64 dims -
+// Queries and keys: a wave per row (or n.parts), in the first workgroups.  Values: behind them, a wave per square of eight by eight pieces - 16-bit types 64 rows by 64 dims -
 // of which a lane turns a square of E by E values over in its registers, so that the rows of consecutive slots leave as whole lines of a value row.
 // That needs E rows with consecutive slots, the first at a multiple of E; squares are laid so for the rows that follow the call's first slot.
 // In other squares a lane takes a row and writes value by value: of consecutive slots 64 stand side by side (all squares so: 49 us for the 45 above).
@@ -151,17 +152,17 @@ __global__ void __launch_bounds__(256) append_rows_kernel(KvView c, AppendArgs a
     __shared__ __align__(16) float2 cs[4][POSS_ROPE_PAIRS];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, dh = c.dh;
     if ((int)blockIdx.x < row_groups) {
-        const int r = blockIdx.x * 4 + wave;
+        const int r = n.parts == 1 ? blockIdx.x * 4 + wave : blockIdx.x, part = n.parts == 1 ? 0 : wave;
         if (r >= a.rows) return;
         int b, slot;
         const int page = append_page(c, a, r, b, slot);
         if (rope.rot_dim) rope_angles(rope, a.positions[r], 1.f, cs[wave], lane, 64);
         wave_lds_sync();
-        rotate_pieces<T, INTERLEAVED>(static_cast<const T *>(a.q) + r * a.q_row, dh, static_cast<T *>(a.q_out) + r * a.q_out_row, dh, a.hq, rope.rot_dim, n, cs[wave]);
+        rotate_pieces<T, INTERLEAVED>(static_cast<const T *>(a.q) + r * a.q_row, dh, static_cast<T *>(a.q_out) + r * a.q_out_row, dh, a.hq, rope.rot_dim, n, part, cs[wave]);
         if (page < 0) return;
-        rotate_pieces<T, INTERLEAVED>(static_cast<const T *>(a.k) + r * a.k_row, dh, static_cast<T *>(c.k) + kv_key_at(c, page, 0, slot), (int64_t)dh << c.shift, c.hkv, rope.rot_dim, n,
+        rotate_pieces<T, INTERLEAVED>(static_cast<const T *>(a.k) + r * a.k_row, dh, static_cast<T *>(c.k) + kv_key_at(c, page, 0, slot), (int64_t)dh << c.shift, c.hkv, rope.rot_dim, n, part,
                                       cs[wave]);
-        note_positions(c, a, r, b, slot, lane, 64);
+        if (part == 0) note_positions(c, a, r, b, slot, lane, 64);
         return;
     }
     const int across = (c.hkv * dh + 8 * E - 1) / (8 * E);                     // squares of a row of values
@@ -205,11 +206,13 @@ __global__ void __launch_bounds__(256) append_rows_kernel(KvView c, AppendArgs a
     }
 }
 
+constexpr int ROWS_FULL = 2048;                              // two waves a SIMD
 // Whether a head of dh values, rot of them rotated, is whole pieces of 16 bytes, and how many units.
-static bool units_of(int dt, int dh, int rot, bool interleaved, Units &n) {
+static bool units_of(int dt, int rows, int dh, int rot, bool interleaved, Units &n) {
     const int E = dt == DT_F32 ? 4 : 8, half = rot / 2;
     if (dh % E || rot % E || (!interleaved && half % E)) return false;
     n.units = dh / E - (interleaved ? 0 : half / E);
+    n.parts = rows < ROWS_FULL ? 4 : 1;
     n.of_units = (uint32_t)(((1ull << 32) + n.units - 1) / n.units);
     return true;
 }
@@ -281,15 +284,16 @@ int poss_rotary(int32_t dtype, const void *x, int64_t x_row, int64_t x_head, voi
     const float sign = inverse ? -1.f : 1.f;
     const int64_t whole = 16 / (int64_t)e;
     const int threads = row_threads(heads);
-    Units n;
-    const bool pieces = rows >= ROWS_MANY && units_of(dtype, head_dim, rope->rot_dim, rope->interleaved, n) && (int64_t)heads * n.units < 1 << 24 && kv_aligned(x, 16) && kv_aligned(y, 16) &&
+    Units n{};
+    const bool pieces = rows >= ROWS_MANY && units_of(dtype, rows, head_dim, rope->rot_dim, rope->interleaved, n) && (int64_t)heads * n.units < 1 << 24 && kv_aligned(x, 16) && kv_aligned(y, 16) &&
                         x_row % whole == 0 && y_row % whole == 0 && x_head % whole == 0 && y_head % whole == 0;
+    const int row_groups = n.parts == 4 ? rows : (rows + 3) / 4;
 #define POSS_ROTARY(T)                                                                                                                                    \
     do {                                                                                                                                                  \
         const T *xt = static_cast<const T *>(x); T *yt = static_cast<T *>(y);                                                                             \
         if (!pieces) rotary_kernel<T><<<rows, threads, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, heads, head_dim, positions, *rope, sign);               \
-        else if (rope->interleaved) rotary_rows_kernel<T, true><<<(rows + 3) / 4, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, rows, heads, n, positions, *rope, sign); \
-        else rotary_rows_kernel<T, false><<<(rows + 3) / 4, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, rows, heads, n, positions, *rope, sign);  \
+        else if (rope->interleaved) rotary_rows_kernel<T, true><<<row_groups, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, rows, heads, n, positions, *rope, sign); \
+        else rotary_rows_kernel<T, false><<<row_groups, 256, 0, st>>>(xt, x_row, x_head, yt, y_row, y_head, rows, heads, n, positions, *rope, sign);  \
     } while (0)
     if (dtype == DT_F32) POSS_ROTARY(float); else if (dtype == DT_BF16) POSS_ROTARY(bf16_t); else POSS_ROTARY(f16_t);
 #undef POSS_ROTARY
@@ -319,10 +323,10 @@ int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t ro
     const poss_rope &r = rope ? *rope : none;
     const int64_t whole = 16 / (int64_t)e;
     const int threads = row_threads(n_q_heads + 2 * cache->n_kv_heads);
-    Units n;
-    const bool pieces = rows >= ROWS_MANY && units_of(cache->dtype, cache->head_dim, r.rot_dim, r.interleaved, n) && kv_aligned(k, 16) && kv_aligned(v, 16) && k_row % whole == 0 &&
+    Units n{};
+    const bool pieces = rows >= ROWS_MANY && units_of(cache->dtype, rows, cache->head_dim, r.rot_dim, r.interleaved, n) && kv_aligned(k, 16) && kv_aligned(v, 16) && k_row % whole == 0 &&
                         v_row % whole == 0 && (!n_q_heads || (kv_aligned(q, 16) && kv_aligned(q_out, 16) && q_row % whole == 0 && q_out_row % whole == 0));
-    const int row_groups = (rows + 3) / 4;
+    const int row_groups = n.parts == 4 ? rows : (rows + 3) / 4;
     const int64_t squares = ((int64_t)rows + whole - 1 + 8 * whole - 1) / (8 * whole) * ((kv_len + 8 * whole - 1) / (8 * whole));      // (the first rows may begin inside a piece)
     const int64_t groups = row_groups + (squares + 3) / 4;
 #define POSS_APPEND(T)                                                                                                     \
