@@ -69,7 +69,8 @@ SHAPES = [  # n_seq, slots, lengths, hkv, dh, page, budget, first, recent
     (1, 32, [32], 1, 64, 32, 31, 0, 0), (1, 64, [33], 2, 64, 32, 32, 4, 16), (3, 100, [100, 0, 1], 2, 128, 64, 50, 0, 10), (2, 96, [96, 95], 3, 32, 32, 1, 0, 0), (2, 96, [96, 40], 1, 96, 32, 1, 0, 1),
     (1, 1025, [1025], 8, 128, 64, 1024, 4, 256), (4, 2000, [2000, 1999, 700, 1300], 2, 64, 128, 700, 4, 100), (1, 5000, [5000], 2, 128, 64, 4000, 0, 0), (2, 300, [300, 299], 2, 256, 32, 300, 0, 0),
     (2, 200, [500, -3], 2, 64, 32, 64, 60, 4), (1, 9000, [8888], 1, 64, 128, 100, 3, 90), (2, 200, [200, 150], 1, 160, 64, 1000, 5, 10), (1, 40000, [40000], 2, 32, 128, 20001, 4, 1000),
-    (2, 3000, [3000, 2500], 2, 64, 64, 1500, 2, 100), (1, 1300, [1290], 2, 64, 32, 1289, 0, 1), (2, 8000, [8000, 10], 1, 32, 64, 7000, 9, 0), (1, 20000, [20000], 1, 32, 128, 19999, 0, 0)]
+    (2, 3000, [3000, 2500], 2, 64, 64, 1500, 2, 100), (1, 1300, [1290], 2, 64, 32, 1289, 0, 1), (2, 8000, [8000, 10], 1, 32, 64, 7000, 9, 0), (1, 20000, [20000], 1, 32, 128, 19999, 0, 0),
+    (1, 9000, [9000], 1, 32, 128, 8000, 0, 0), (2, 30000, [30000, 20000], 1, 32, 64, 15000, 10, 3000), (1, 70000, [66000], 1, 32, 128, 30000, 0, 500), (1, 12000, [12000], 2, 64, 64, 3, 1, 1)]
 
 
 @pytest.mark.parametrize("t", ["bf16", "f16", "f32"])

@@ -227,6 +227,26 @@ def test_a_contexts_own_cache_and_logits(name, over):
     pair.close()
 
 
+def test_each_sequence_of_a_batch_hands_out_its_own_cache():
+    """Two sequences with the same prompt, a third with another: the same attention over the first two's caches, not over the third's; both kinds of cache, and with
+    layers in 4 bits."""
+    from synth import make_prompt
+    for mx in (False, True):
+        pair = Pair("t_mid_bf16", lib_over=dict(batch=3, **({"mx": True} if mx else {})))
+        cfg, ctx = pair.cfg, pair.ctx
+        prompt = make_prompt(cfg)
+        for b in range(3):
+            ctx.prefill(prompt if b < 2 else prompt[::-1].copy() if isinstance(prompt, np.ndarray) else prompt[::-1], seq=b)
+        q = torch.randn(1, cfg.n_q_heads, cfg.head_dim, device="cuda").to(torch.bfloat16)
+        n = torch.tensor([len(prompt) - 1], dtype=torch.int32, device="cuda")
+        for which, layer in ((-1, cfg.n_layers - 1), (0, 0)):
+            outs = [P.kv_attend(ctx.kv_cache(b, which, layer), q, n, torch.empty_like(q)) for b in range(3)]
+            assert torch.equal(outs[0], outs[1]) and not torch.equal(outs[0], outs[2]) and not bool(outs[2].isnan().any())
+        with pytest.raises(P.PossError):
+            ctx.kv_cache(3)
+        pair.close()
+
+
 def test_offsets_beyond_32_bits():
     """Pages whose values lie past 2^31 and bytes past 2^33, and rows of logits as far apart."""
     per_page = 8 * 128 * 128
