@@ -3,11 +3,13 @@
 Same names as include/poss.h, which says what each call does.  Tensors of a call are on one GPU; work goes to torch's current stream there
 unless a stream is given.  Small calls take a few microseconds: what these functions do for a call is kept short.
 """
+import contextlib
 import ctypes
 
 from .binding import POSS_OK, PossError, PossKvCache, PossRope, _mx, _mx_call, _mx_empty, _mx_refuse, _mx_type
 
 LOGPROBS_TOP = 32
+_AS_IT_IS = contextlib.nullcontext()
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
 
@@ -218,31 +220,43 @@ def logprobs(logits, tokens=None, n_top=0, temperature=1.0, logp=None, entropy=N
         _mx_refuse("logits must have contiguous rows that do not overlap")
     if n_top < 0 or n_top > min(LOGPROBS_TOP, vocab):
         _mx_refuse("n_top must be at most %d and the vocabulary" % LOGPROBS_TOP)
-    f32, i32 = torch.float32, torch.int32
-
-    def new(shape, dtype):
-        if stream is None:
-            return logits.new_empty(shape, dtype=dtype)
-        with torch.cuda.stream(stream):
-            return logits.new_empty(shape, dtype=dtype)
     n_tokens = tp = lp = 0
-    tensors = [logits]
-    if tokens is not None:
-        n_tokens = 1 if tokens.dim() == 1 else tokens.shape[1] if tokens.dim() == 2 else _mx_refuse("tokens must be [rows] or [rows, n]")
-        tp = _ints(tokens, (rows,) if tokens.dim() == 1 else (rows, n_tokens), "tokens")
-        if logp is None:
-            logp = new(tokens.shape, f32)
-        lp = _floats(logp, tokens.shape, "logp")
-        tensors += (tokens, logp)
-    tops = (rows, n_top)
-    entropy = new((rows,), f32) if entropy is None else entropy
-    top_ids = new(tops, i32) if top_ids is None else top_ids
-    top_logp = new(tops, f32) if top_logp is None else top_logp
-    ep, ip, op = _floats(entropy, (rows,), "entropy"), _ints(top_ids, tops, "top_ids"), _floats(top_logp, tops, "top_logp")
+    tensors = [logits]                                     # (what is allocated here needs no look)
+    with torch.cuda.stream(stream) if stream is not None else _AS_IT_IS:
+        new, f32 = logits.new_empty, torch.float32
+        if tokens is not None:
+            n_tokens = 1 if tokens.dim() == 1 else tokens.shape[1] if tokens.dim() == 2 else _mx_refuse("tokens must be [rows] or [rows, n]")
+            tp = _ints(tokens, (rows,) if tokens.dim() == 1 else (rows, n_tokens), "tokens")
+            tensors.append(tokens)
+            if logp is None:
+                logp = new(tokens.shape, dtype=f32)
+                lp = logp.data_ptr()
+            else:
+                lp = _floats(logp, tokens.shape, "logp")
+                tensors.append(logp)
+        if entropy is None:
+            entropy = new((rows,), dtype=f32)
+            ep = entropy.data_ptr()
+        else:
+            ep = _floats(entropy, (rows,), "entropy")
+            tensors.append(entropy)
+        if top_ids is None:
+            top_ids = new((rows, n_top), dtype=torch.int32)
+            ip = top_ids.data_ptr()
+        else:
+            ip = _ints(top_ids, (rows, n_top), "top_ids")
+            tensors.append(top_ids)
+        if top_logp is None:
+            top_logp = new((rows, n_top), dtype=f32)
+            op = top_logp.data_ptr()
+        else:
+            op = _floats(top_logp, (rows, n_top), "top_logp")
+            tensors.append(top_logp)
     if scratch is None:
         scratch = logprobs_scratch(rows, vocab, n_top, logits.device, stream)
     elif not scratch.is_contiguous():
         _mx_refuse("scratch must be contiguous")
-    _mx_call(_mx.lib.poss_logprobs, stream, (*tensors, entropy, top_ids, top_logp, scratch), t, logits.data_ptr(), ld if rows > 1 else vocab, rows, vocab, temperature, tp, n_tokens,
+    tensors.append(scratch)
+    _mx_call(_mx.lib.poss_logprobs, stream, tensors, t, logits.data_ptr(), ld if rows > 1 else vocab, rows, vocab, temperature, tp, n_tokens,
              lp, ep, n_top, ip, op, scratch.data_ptr(), scratch.nbytes)
     return logp, entropy, top_ids, top_logp
