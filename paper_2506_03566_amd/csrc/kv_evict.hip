@@ -6,7 +6,7 @@
 // the j-th hole is filled from the j-th of those.  No source is a destination, so the moves need no order.
 //
 // A workgroup per head chooses, bound by latency (1025 slots of 8 heads 12 us, 4096 of 256 heads 16, 18580 of one 31, 131072 of 8 238); a second launch moves.  Keys move as rows; a
-// value row gives and takes single values, so that whole lines are read and parts of lines written: 32 sequences of up to 4096 slots to 2000, 8 heads of 128, bf16: 60 us for 105 MB
+// value row gives and takes single values, so that whole lines are read and parts of lines written: 32 sequences of up to 4096 slots to 2000, 8 heads of 128, bf16: 57 us for 105 MB
 // read and 91 written, 17 us of them the keys'.  Reading and writing the destinations' lines whole took as long.
 #include "kv.h"
 
@@ -480,16 +480,16 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView
     for (int i = n + tid; i < n + all; i += EVICT_THREADS) e.po[i] = -1;
 }
 
-// The slots 256 x .. below the budget of one sequence and head whose source is another: listed, then moved, keys in pieces of 16 bytes, values with a lane per
+// The slots 256 x .. below the budget of one sequence and head whose source is another, 64 (or 32) of the dims: listed, then moved, keys in pieces of 16 bytes, values with a lane per
 // slot: sources ascend with destinations, so that the values of 64 of them lie in a few lines of each value row.
 constexpr int MOVE_SLOTS = 256;
 template <typename T>
-__global__ void __launch_bounds__(256) evict_move_kernel(KvView c, const int32_t *__restrict__ kept, int budget) {
+__global__ void __launch_bounds__(256) evict_move_kernel(KvView c, const int32_t *__restrict__ kept, int budget, int splits) {
     constexpr int E = 16 / sizeof(T), AHEAD = 8;
     typedef T vec __attribute__((ext_vector_type(E)));
     __shared__ int64_t key_from[MOVE_SLOTS], key_to[MOVE_SLOTS], value_from[MOVE_SLOTS], value_to[MOVE_SLOTS];
     __shared__ int count;
-    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, to = blockIdx.x * MOVE_SLOTS + tid;
+    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, to = blockIdx.x / splits * MOVE_SLOTS + tid, dims = c.dh / splits, first = blockIdx.x % splits * dims;
     const int from = to < budget ? kept[((int64_t)b * c.hkv + h) * budget + to] : -1;
     int pf = -1, pt = -1;
     if (from >= 0 && from != to) { pf = kv_page(c, b, from); pt = kv_page(c, b, to); }
@@ -509,13 +509,13 @@ __global__ void __launch_bounds__(256) evict_move_kernel(KvView c, const int32_t
     const int n = count;
     if (n == 0) return;
     T *k = static_cast<T *>(c.k), *v = static_cast<T *>(c.v);
-    const int pieces = c.dh / E;
+    const int pieces = dims / E;
 #pragma unroll 2
     for (int x = tid; x < n * pieces; x += 256) {
-        const int i = x / pieces, d = (x - i * pieces) * E;
+        const int i = x / pieces, d = first + (x - i * pieces) * E;
         *reinterpret_cast<vec *>(k + key_to[i] + d) = *reinterpret_cast<const vec *>(k + key_from[i] + d);
     }
-    const int each = c.dh / 4, d0 = (tid >> 6) * each;       // a wave takes a quarter of the value rows (a multiple of AHEAD)
+    const int each = dims / 4, d0 = first + (tid >> 6) * each;      // a wave takes a quarter of the value rows (a multiple of AHEAD)
     for (int i = tid & 63; i < n; i += 64) {
         const T *vf = v + value_from[i];
         T *vt = v + value_to[i];
@@ -559,9 +559,10 @@ extern "C" int poss_kv_evict(const poss_kv_cache *cache, const float *weights, c
     else if (c.slots <= 32 * EVICT_THREADS) evict_select_wide_kernel<32><<<heads, EVICT_THREADS, 0, st>>>(c, a);
     else evict_select_long_kernel<<<heads, EVICT_THREADS, 0, st>>>(c, a);
     const int most = budget < c.slots ? budget : c.slots;
-    const dim3 grid((most + MOVE_SLOTS - 1) / MOVE_SLOTS, c.hkv, c.n_seq);
-    if (cache->dtype == DT_F32) evict_move_kernel<float><<<grid, 256, 0, st>>>(c, kept, budget);
-    else if (cache->dtype == DT_BF16) evict_move_kernel<bf16_t><<<grid, 256, 0, st>>>(c, kept, budget);
-    else evict_move_kernel<f16_t><<<grid, 256, 0, st>>>(c, kept, budget);
+    const int splits = c.dh % 64 ? c.dh / 32 : c.dh / 64;
+    const dim3 grid((most + MOVE_SLOTS - 1) / MOVE_SLOTS * splits, c.hkv, c.n_seq);
+    if (cache->dtype == DT_F32) evict_move_kernel<float><<<grid, 256, 0, st>>>(c, kept, budget, splits);
+    else if (cache->dtype == DT_BF16) evict_move_kernel<bf16_t><<<grid, 256, 0, st>>>(c, kept, budget, splits);
+    else evict_move_kernel<f16_t><<<grid, 256, 0, st>>>(c, kept, budget, splits);
     return kv_launched(who);
 }
