@@ -15,8 +15,6 @@
 namespace poss {
 
 typedef float  f32x4 __attribute__((ext_vector_type(4)));
-typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
-typedef f16_t  f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int ATT_BLOCK = 32;                 // slots of a block: never across pages
 constexpr int ATT_WAVES = 4;
