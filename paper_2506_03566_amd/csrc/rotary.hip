@@ -4,6 +4,7 @@
 // heads of 128 (bf16, 201 MB): 45 us, 4.5 TB/s, with no more traffic than that (102 MB read, 101 MB written); 8192 x 40 heads alone 38 us.  A row alone 4.7 us: launch, position
 // and slot, the page, the row.
 #include "kv.h"
+#include "pieces.h"
 
 #include <math.h>
 
@@ -86,10 +87,7 @@ __global__ void __launch_bounds__(1024) append_kernel(KvView c, AppendArgs a, po
 }
 
 // ------------------------------------------------------------------------------------------ whole pieces of 16 bytes, many rows
-// A wave's part of a row: pieces of 16 bytes, of both members' halves at once where pairs lie apart.  units: of one head; of_units: 2^32 / units, rounded up; parts: waves
-// that share a row, 4 where rows alone would leave the chip idle (274 rows of 64 + 8 + 8 heads of 256: 26 -> 11 us), else 1.
-struct Units { int units; uint32_t of_units; int parts; };
-
+// A wave's part of a row, in units of pieces.h; four waves share a row where rows alone would leave the chip idle (274 rows of 64 + 8 + 8 heads of 256: 26 -> 11 us).
 template <typename T, bool INTERLEAVED>
 __device__ __forceinline__ void rotate_pieces(const T *x, int64_t x_head, T *y, int64_t y_head, int heads, int rot, Units n, int part, const float2 *cs) {
     constexpr int E = 16 / sizeof(T);
@@ -97,7 +95,7 @@ __device__ __forceinline__ void rotate_pieces(const T *x, int64_t x_head, T *y, 
     const int half = rot >> 1, turned = INTERLEAVED ? rot / E : half / E, all = heads * n.units;
 #pragma unroll 2
     for (int j = part * 64 + (threadIdx.x & 63); j < all; j += 64 * n.parts) {
-        const int h = (int)__umulhi((uint32_t)j, n.of_units), u = j - h * n.units;
+        const int h = unit_head(j, n.of_units), u = j - h * n.units;
         const T *xi = x + h * x_head;
         T *yi = y + h * y_head;
         if (u >= turned) {                                 // values that stay
@@ -206,17 +204,6 @@ __global__ void __launch_bounds__(256) append_rows_kernel(KvView c, AppendArgs a
     }
 }
 
-constexpr int ROWS_FULL = 2048;                              // two waves a SIMD
-// Whether a head of dh values, rot of them rotated, is whole pieces of 16 bytes, and how many units.
-static bool units_of(int dt, int rows, int dh, int rot, bool interleaved, Units &n) {
-    const int E = dt == DT_F32 ? 4 : 8, half = rot / 2;
-    if (dh % E || rot % E || (!interleaved && half % E)) return false;
-    n.units = dh / E - (interleaved ? 0 : half / E);
-    n.parts = rows < ROWS_FULL ? 4 : 1;
-    n.of_units = (uint32_t)(((1ull << 32) + n.units - 1) / n.units);
-    return true;
-}
-
 }  // namespace poss
 
 // ------------------------------------------------------------------------------------------ C entry points (include/poss.h)
@@ -285,7 +272,7 @@ int poss_rotary(int32_t dtype, const void *x, int64_t x_row, int64_t x_head, voi
     const int64_t whole = 16 / (int64_t)e;
     const int threads = row_threads(heads);
     Units n{};
-    const bool pieces = rows >= ROWS_MANY && units_of(dtype, rows, head_dim, rope->rot_dim, rope->interleaved, n) && (int64_t)heads * n.units < 1 << 24 && kv_aligned(x, 16) && kv_aligned(y, 16) &&
+    const bool pieces = rows >= ROWS_MANY && units_of((int)whole, rows, heads, head_dim, rope->rot_dim, rope->interleaved, n) && kv_aligned(x, 16) && kv_aligned(y, 16) &&
                         x_row % whole == 0 && y_row % whole == 0 && x_head % whole == 0 && y_head % whole == 0;
     const int row_groups = n.parts == 4 ? rows : (rows + 3) / 4;
 #define POSS_ROTARY(T)                                                                                                                                    \
@@ -324,7 +311,7 @@ int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t ro
     const int64_t whole = 16 / (int64_t)e;
     const int threads = row_threads(n_q_heads + 2 * cache->n_kv_heads);
     Units n{};
-    const bool pieces = rows >= ROWS_MANY && units_of(cache->dtype, rows, cache->head_dim, r.rot_dim, r.interleaved, n) && kv_aligned(k, 16) && kv_aligned(v, 16) && k_row % whole == 0 &&
+    const bool pieces = rows >= ROWS_MANY && units_of((int)whole, rows, n_q_heads > cache->n_kv_heads ? n_q_heads : cache->n_kv_heads, cache->head_dim, r.rot_dim, r.interleaved, n) && kv_aligned(k, 16) && kv_aligned(v, 16) && k_row % whole == 0 &&
                         v_row % whole == 0 && (!n_q_heads || (kv_aligned(q, 16) && kv_aligned(q_out, 16) && q_row % whole == 0 && q_out_row % whole == 0));
     const int row_groups = n.parts == 4 ? rows : (rows + 3) / 4;
     const int64_t squares = ((int64_t)rows + whole - 1 + 8 * whole - 1) / (8 * whole) * ((kv_len + 8 * whole - 1) / (8 * whole));      // (the first rows may begin inside a piece)
