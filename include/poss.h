@@ -425,7 +425,8 @@ int poss_kv_append(const poss_kv_cache *cache, const poss_rope *rope, int32_t ro
  * head h / (n_q_heads / n_kv_heads).  q and out: [n_seq][n_q_heads][head_dim] of the cache's type, heads contiguous, q_row and out_row values apart, 16-byte
  * aligned with distances of whole 16 bytes.  lengths: DEVICE int32[n_seq]; max_len: the most that any of them is (0: all slots); it decides
  * how the work is split and, with weights, the size of the scratch.  A length of zero or less gives zeros and an lse of -infinity; one above max_len, or a slot without a page, a row of NaN; scores that are all
- * -infinity, zeros over nothing: a row of NaN and an lse of -infinity.
+ * -infinity, zeros over nothing: a row of NaN and an lse of -infinity.  An infinite value makes its dim infinite, however small its probability, and NaN beside one of the other
+ * sign or at a score of -infinity; it shows nowhere else.  (Values so large that float32 does not hold their sum over the slots give infinity or NaN too.)
  * lse (may be NULL): float32 [n_seq][n_q_heads], the logarithm of the sum of exponentials.
  * weights_out (may be NULL): float32 [n_seq][n_kv_heads][slots], the weights that the slots have been given so far: weights (the same form; NULL: zeros;
  * may be weights_out) plus this row's p, summed over the heads that share the key head.  Slots beyond the length are left as they were, all of a row

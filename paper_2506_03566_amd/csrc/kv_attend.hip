@@ -198,6 +198,43 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 // 2^(m - to) for a running maximum that may be -infinity (nothing yet: 0).
 __device__ __forceinline__ float back_by(float m, float to) { return m == -INFINITY ? 0.f : exp2_of(m - to); }
 
+__device__ __forceinline__ bool any_nan(f32x4 o) { return __builtin_isunordered(o[0], o[1]) || __builtin_isunordered(o[2], o[3]); }
+// An infinite value counts as such wherever its score is above -infinity.  Where its probability, the second number that stands for it or a factor on the way is 0, or that number is
+// below 0, NaN has come of it.  So this is what a sum over the slots s0 .. s1 - 1 has to be that is NaN while the probabilities are not: the infinities and NaN among the values (row d) times
+// 1, or times 0 where the score is -infinity.  (If there are none it is left: numbers whose sums float32 does not hold.)  A thread looks through the slots by itself, which
+// costs the tiles nothing (131072 slots of 8 key heads: 0.18 ms with one infinity, 0.49 with a slot of them, for 0.1; to take their blocks once more, with such values apart: 0.2 to 0.5 us for every call).
+template <typename T, int DH>
+__device__ __forceinline__ float sum_of_infinities(const T *q, const KvView &c, const int32_t *table, int hk, int d, int s0, int s1, float scale) {
+    constexpr int E = 16 / sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(E)));
+    float sum = 0.f;
+#pragma unroll 1
+    for (int s = s0; s < s1 && sum == sum; s += E) {           // (s0 is a block's first slot)
+        const int page = table[s >> c.shift];                  // (there: the row's probabilities are numbers)
+        const T *v = static_cast<const T *>(c.v) + kv_value_at(c, page, hk, d, s), *k = static_cast<const T *>(c.k) + kv_key_at(c, page, hk, s);
+        const vec x = *reinterpret_cast<const vec *>(v);
+        bool numbers = true;
+#pragma unroll
+        for (int e = 0; e < E; ++e) numbers &= fabsf(to_f(x[e])) < INFINITY;
+        if (numbers) continue;
+#pragma unroll 1
+        for (int e = 0; e < min(E, s1 - s); ++e) {
+            if (fabsf(to_f(v[e])) < INFINITY) continue;
+            float z = 0.f;
+#pragma unroll 1
+            for (int i = 0; i < DH; ++i) z += to_f(q[i]) * to_f(k[e * DH + i]);
+            sum += to_f(v[e]) * (z * scale == -INFINITY ? 0.f : 1.f);
+        }
+    }
+    return sum == 0.f ? NAN : sum;
+}
+// A piece's sums brought to another maximum; an infinity stays one, however small the factor.
+__device__ __forceinline__ f32x4 brought(f32x4 o, float f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fabsf(o[e]) == INFINITY ? o[e] : o[e] * f;
+    return o;
+}
+
 template <typename T, int DH, bool WEIGHED>
 __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, AttendArgs a) {
     constexpr int ROW = DH + 4;
@@ -307,6 +344,10 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attend_kernel(KvView c, Attend
                 sum += lds_ml[v][h].y * f;                 // (a wave that saw nothing adds 0, one that saw only NaN shows it: 0 * NaN)
                 r += ov * f;
             }
+            if (any_nan(r) && sum == sum)
+#pragma unroll 1
+                for (int e = 0; e < 4; ++e)
+                    if (r[e] != r[e]) r[e] = sum_of_infinities<T, DH>(qs + b * a.q_row + (int64_t)(head0 + h) * DH, c, table, hk, d + e, i0 * ATT_BLOCK, min(i1 * ATT_BLOCK, len), scale);
             if (starts && ends) {
                 const float inv = 1.f / sum;
                 T *to = out + b * a.out_row + (int64_t)(head0 + h) * DH + d;
@@ -404,6 +445,10 @@ __global__ void __launch_bounds__(256) attend_finish_kernel(KvView c, AttendArgs
         if (there && way < ways) {
 #pragma unroll 8
             for (int p = way; p < n; p += ways) r += *reinterpret_cast<const f32x4 *>(a.part + slot(p, j) * dh + d) * factor[p];
+            if (any_nan(r)) {
+                r = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int p = way; p < n; p += ways) r += brought(*reinterpret_cast<const f32x4 *>(a.part + slot(p, j) * dh + d), factor[p]);
+            }
         }
         sums[tid] = r;
         __syncthreads();
