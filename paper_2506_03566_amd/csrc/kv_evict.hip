@@ -481,50 +481,52 @@ __global__ void __launch_bounds__(EVICT_THREADS) evict_select_long_kernel(KvView
 }
 
 // The slots 256 x .. below the budget of one sequence and head whose source is another, 64 (or 32) of the dims: listed, then moved, keys in pieces of 16 bytes, values with a lane per
-// slot: sources ascend with destinations, so that the values of 64 of them lie in a few lines of each value row.
-constexpr int MOVE_SLOTS = 256;
+// slot: sources ascend with destinations, so that the values of 64 of them lie in a few lines of each value row.  A launch has MOVE_GROUPS times as many slots side by side at most (threads
+// are counted in 32 bits: 2^30 slots of heads of 256 dims, cut in four, are 2^32 of them); a workgroup goes on to others.
+constexpr int MOVE_SLOTS = 256, MOVE_GROUPS = 1024;
 template <typename T>
-__global__ void __launch_bounds__(256) evict_move_kernel(KvView c, const int32_t *__restrict__ kept, int budget, int splits) {
+__global__ void __launch_bounds__(256) evict_move_kernel(KvView c, const int32_t *__restrict__ kept, int budget, int splits, int most) {
     constexpr int E = 16 / sizeof(T), AHEAD = 8;
     typedef T vec __attribute__((ext_vector_type(E)));
     __shared__ int64_t key_from[MOVE_SLOTS], key_to[MOVE_SLOTS], value_from[MOVE_SLOTS], value_to[MOVE_SLOTS];
     __shared__ int count;
-    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, to = blockIdx.x / splits * MOVE_SLOTS + tid, dims = c.dh / splits, first = blockIdx.x % splits * dims;
-    const int from = to < budget ? kept[((int64_t)b * c.hkv + h) * budget + to] : -1;
-    int pf = -1, pt = -1;
-    if (from >= 0 && from != to) { pf = kv_page(c, b, from); pt = kv_page(c, b, to); }
-    const bool moves = pf >= 0 && pt >= 0;
-    if (tid == 0) count = 0;
-    __syncthreads();
-    // (the order between waves does not matter, a wave's own slots stay together)
-    const unsigned long long them = __ballot(moves);
-    int at = 0;
-    if ((tid & 63) == 0 && them) at = atomicAdd(&count, __popcll(them));
-    at = __shfl(at, 0) + lanes_below(them);
-    if (moves) {
-        key_from[at] = kv_key_at(c, pf, h, from); key_to[at] = kv_key_at(c, pt, h, to);
-        value_from[at] = kv_value_at(c, pf, h, 0, from); value_to[at] = kv_value_at(c, pt, h, 0, to);
-    }
-    __syncthreads();
-    const int n = count;
-    if (n == 0) return;
+    const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, dims = c.dh / splits, first = blockIdx.x % splits * dims;
     T *k = static_cast<T *>(c.k), *v = static_cast<T *>(c.v);
-    const int pieces = dims / E;
+    for (int chunk = blockIdx.x / splits; chunk * MOVE_SLOTS < most; chunk += MOVE_GROUPS) {
+        const int to = chunk * MOVE_SLOTS + tid, from = to < most ? kept[((int64_t)b * c.hkv + h) * budget + to] : -1;
+        int pf = -1, pt = -1;
+        if (from >= 0 && from != to) { pf = kv_page(c, b, from); pt = kv_page(c, b, to); }
+        const bool moves = pf >= 0 && pt >= 0;
+        if (chunk >= MOVE_GROUPS) __syncthreads();             // the lists of the slots before are done with
+        if (tid == 0) count = 0;
+        __syncthreads();
+        // (the order between waves does not matter, a wave's own slots stay together)
+        const unsigned long long them = __ballot(moves);
+        int at = 0;
+        if ((tid & 63) == 0 && them) at = atomicAdd(&count, __popcll(them));
+        at = __shfl(at, 0) + lanes_below(them);
+        if (moves) {
+            key_from[at] = kv_key_at(c, pf, h, from); key_to[at] = kv_key_at(c, pt, h, to);
+            value_from[at] = kv_value_at(c, pf, h, 0, from); value_to[at] = kv_value_at(c, pt, h, 0, to);
+        }
+        __syncthreads();
+        const int n = count, pieces = dims / E;
 #pragma unroll 2
-    for (int x = tid; x < n * pieces; x += 256) {
-        const int i = x / pieces, d = first + (x - i * pieces) * E;
-        *reinterpret_cast<vec *>(k + key_to[i] + d) = *reinterpret_cast<const vec *>(k + key_from[i] + d);
-    }
-    const int each = dims / 4, d0 = first + (tid >> 6) * each;      // a wave takes a quarter of the value rows (a multiple of AHEAD)
-    for (int i = tid & 63; i < n; i += 64) {
-        const T *vf = v + value_from[i];
-        T *vt = v + value_to[i];
-        for (int d = d0; d < d0 + each; d += AHEAD) {
-            T got[AHEAD];
+        for (int x = tid; x < n * pieces; x += 256) {
+            const int i = x / pieces, d = first + (x - i * pieces) * E;
+            *reinterpret_cast<vec *>(k + key_to[i] + d) = *reinterpret_cast<const vec *>(k + key_from[i] + d);
+        }
+        const int each = dims / 4, d0 = first + (tid >> 6) * each;      // a wave takes a quarter of the value rows (a multiple of AHEAD)
+        for (int i = tid & 63; i < n; i += 64) {
+            const T *vf = v + value_from[i];
+            T *vt = v + value_to[i];
+            for (int d = d0; d < d0 + each; d += AHEAD) {
+                T got[AHEAD];
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) got[j] = vf[(int64_t)(d + j) << c.shift];
+                for (int j = 0; j < AHEAD; ++j) got[j] = vf[(int64_t)(d + j) << c.shift];
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) vt[(int64_t)(d + j) << c.shift] = got[j];
+                for (int j = 0; j < AHEAD; ++j) vt[(int64_t)(d + j) << c.shift] = got[j];
+            }
         }
     }
 }
@@ -560,9 +562,10 @@ extern "C" int poss_kv_evict(const poss_kv_cache *cache, const float *weights, c
     else evict_select_long_kernel<<<heads, EVICT_THREADS, 0, st>>>(c, a);
     const int most = budget < c.slots ? budget : c.slots;
     const int splits = c.dh % 64 ? c.dh / 32 : c.dh / 64;
-    const dim3 grid((most + MOVE_SLOTS - 1) / MOVE_SLOTS * splits, c.hkv, c.n_seq);
-    if (cache->dtype == DT_F32) evict_move_kernel<float><<<grid, 256, 0, st>>>(c, kept, budget, splits);
-    else if (cache->dtype == DT_BF16) evict_move_kernel<bf16_t><<<grid, 256, 0, st>>>(c, kept, budget, splits);
-    else evict_move_kernel<f16_t><<<grid, 256, 0, st>>>(c, kept, budget, splits);
+    const int chunks = (most + MOVE_SLOTS - 1) / MOVE_SLOTS;
+    const dim3 grid((chunks < MOVE_GROUPS ? chunks : MOVE_GROUPS) * splits, c.hkv, c.n_seq);
+    if (cache->dtype == DT_F32) evict_move_kernel<float><<<grid, 256, 0, st>>>(c, kept, budget, splits, most);
+    else if (cache->dtype == DT_BF16) evict_move_kernel<bf16_t><<<grid, 256, 0, st>>>(c, kept, budget, splits, most);
+    else evict_move_kernel<f16_t><<<grid, 256, 0, st>>>(c, kept, budget, splits, most);
     return kv_launched(who);
 }
