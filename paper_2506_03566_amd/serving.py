@@ -121,6 +121,8 @@ class KvCache:
 def kv_append(cache, k, v, slots, positions=None, rope=None, seq=None, q=None, q_out=None, slot_positions=None, stream=None):
     """Rows k, v [rows, kv_heads, dim] into slots [rows] of sequences seq [rows] (None: row r is sequence r), keys rotated to positions [rows] by rope;
     q [rows, heads, dim] rotated into q_out (None: into q).  slot_positions: int32 [sequences, kv_heads, slots] that notes the positions.  Returns q_out."""
+    if k.dim() != 3 or (q is not None and q.dim() != 3):
+        _mx_refuse("k and q must be [rows, heads, dim]")
     rows = k.shape[0]
     if rows > 0x7fffffff:
         _mx_refuse("too many rows")
@@ -161,6 +163,8 @@ def kv_attend(cache, q, lengths, out, lse=None, weights=None, weights_out=None, 
     """out [sequences, heads, dim] = attention of q over each sequence's first lengths[b] slots; lse float32 [sequences, heads].  weights_out float32
     [sequences, kv_heads, slots] = weights (None: zeros; may be weights_out) + the probabilities, summed over the heads of a key head.  scale: 1 / sqrt(dim) unless given.
     max_len: the most any length is (0: all slots).  scratch: from kv_attend_scratch, not used by another call at the same time; allocated per call if not given."""
+    if q.dim() != 3:
+        _mx_refuse("q must be [sequences, heads, dim]")
     n, heads = cache.n_seq, q.shape[1]
     qr, orow = _heads(q, cache.dtype, n, heads, cache.dim, "q"), _heads(out, cache.dtype, n, heads, cache.dim, "out")
     tensors = [*cache.tensors, q, out, lengths]

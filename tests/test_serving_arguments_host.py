@@ -1,0 +1,40 @@
+"""What the Python calls over paged caches refuse by themselves, before any GPU work: with a PossError, not with whatever an index or a narrower integer makes of it."""
+import os
+
+import pytest
+
+import paper_2506_03566_amd as P
+from paper_2506_03566_amd.binding import PossKvCache
+
+
+def _cache():
+    if not os.path.exists(P.LIB_PATH):
+        pytest.skip("libposs.so not built (run __graft_entry__.build())")
+    import torch
+    P.Rope(32)                                             # (looks the library and the types up)
+    cache = P.KvCache.__new__(P.KvCache)
+    k, v, table = torch.zeros(4, 2, 32, 64), torch.zeros(4, 2, 64, 32), torch.zeros(2, 2, dtype=torch.int32)
+    cache._set(PossKvCache(0, 2, 64, 32, 4, 2, 2, 2, 4096, 4096, k.data_ptr(), v.data_ptr(), table.data_ptr()), torch.float32, (k, v, table))
+    return cache, torch
+
+
+def refused(f, *args, **kw):
+    with pytest.raises(P.PossError) as e:
+        f(*args, **kw)
+    assert e.value.code == P.E_INVALID_ARG
+
+
+def test_tensors_of_other_dimensions():
+    cache, torch = _cache()
+    q, out, lengths, ints = torch.zeros(2, 4, 64), torch.zeros(2, 4, 64), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    for bad in (q[0, 0, 0], q[0, 0], q[0], q[None]):
+        refused(P.kv_attend, cache, bad, lengths, out)
+        refused(P.kv_attend, cache, q, lengths, bad)
+    k = torch.zeros(3, 2, 64)
+    for bad in (k[0, 0, 0], k[0, 0], k[0], k[None]):
+        refused(P.kv_append, cache, bad, k, ints)
+        refused(P.kv_append, cache, k, bad, ints)
+        refused(P.kv_append, cache, k, k, ints, q=bad)
+        refused(P.kv_append, cache, k, k, ints, q=k, q_out=bad)
+    refused(P.kv_attend, cache, q, lengths, out)           # no GPU tensors
+    refused(P.kv_append, cache, k, k, ints)
