@@ -25,6 +25,11 @@ def _floats(t, shape, what):
     return t.data_ptr()
 
 
+def _count(n, what):
+    """n, which has to be of 31 bits: what is wider would lose its upper ones on the way."""
+    return n if 0 <= n <= 0x7fffffff else _mx_refuse("%s rejected: %d" % (what, n))
+
+
 def _heads(t, dtype, rows, heads, dim, what):
     """The row distance of [rows, heads, dim] whose heads are contiguous."""
     if t.dtype is not dtype or t.shape != (rows, heads, dim):
@@ -44,7 +49,7 @@ class Rope:
         if scaling not in _SCALINGS:
             _mx_refuse("scaling is one of %s" % ", ".join(_SCALINGS))
         self.c = PossRope()
-        rc = lib.poss_rope_fill(rot_dim, 1 if interleaved else 0, theta, _SCALINGS[scaling], factor, low, high, original, magnitude, ctypes.byref(self.c))
+        rc = lib.poss_rope_fill(_count(rot_dim, "rot_dim"), 1 if interleaved else 0, theta, _SCALINGS[scaling], factor, low, high, original, magnitude, ctypes.byref(self.c))
         if rc != POSS_OK:
             raise PossError(rc, lib.poss_last_error(None).decode())
         if frequencies is not None:
@@ -153,7 +158,7 @@ def kv_append(cache, k, v, slots, positions=None, rope=None, seq=None, q=None, q
 
 def kv_attend_scratch(cache, heads, max_len=0, weights=False, stream=None):
     """Scratch for kv_attend of `heads` query heads over this cache, with weights or without."""
-    need = _mx.lib.poss_kv_attend_scratch_bytes(cache.ref, heads, max_len, 1 if weights else 0)
+    need = _mx.lib.poss_kv_attend_scratch_bytes(cache.ref, _count(heads, "heads"), _count(max_len, "max_len"), 1 if weights else 0)
     if need == 0:
         _mx_refuse("shape rejected")
     return _mx_empty(need, cache.tensors[0].device, stream)
@@ -183,7 +188,7 @@ def kv_attend(cache, q, lengths, out, lse=None, weights=None, weights_out=None, 
     elif not scratch.is_contiguous():
         _mx_refuse("scratch must be contiguous")
     tensors.append(scratch)
-    _mx_call(_mx.lib.poss_kv_attend, stream, tensors, cache.ref, heads, q.data_ptr(), qr, out.data_ptr(), orow, _ints(lengths, (n,), "lengths"), max_len,
+    _mx_call(_mx.lib.poss_kv_attend, stream, tensors, cache.ref, heads, q.data_ptr(), qr, out.data_ptr(), orow, _ints(lengths, (n,), "lengths"), _count(max_len, "max_len"),
              cache.dim ** -0.5 if scale is None else scale, lp, wp, op, scratch.data_ptr(), scratch.nbytes)
     return out
 
@@ -205,7 +210,7 @@ def kv_evict(cache, weights, positions, lengths, budget, kept, weights_out, posi
 def logprobs_scratch(rows, vocab, n_top=0, device="cuda", stream=None):
     """Scratch for logprobs of this shape; one that is large enough serves others too."""
     lib = (_mx if _mx.lib else _mx.open()).lib
-    need = lib.poss_logprobs_scratch_bytes(rows, vocab, n_top) if max(rows, vocab) < 1 << 31 else 0
+    need = lib.poss_logprobs_scratch_bytes(_count(rows, "rows"), _count(vocab, "vocab"), _count(n_top, "n_top"))
     if need == 0:
         _mx_refuse("shape rejected")
     return _mx_empty(need, device, stream)

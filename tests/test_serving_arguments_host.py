@@ -38,3 +38,19 @@ def test_tensors_of_other_dimensions():
         refused(P.kv_append, cache, k, k, ints, q=k, q_out=bad)
     refused(P.kv_attend, cache, q, lengths, out)           # no GPU tensors
     refused(P.kv_append, cache, k, k, ints)
+
+
+def test_numbers_beyond_32_bits():
+    """ctypes keeps an integer's lowest 32 bits: 2^32 + 5 would be taken for 5."""
+    cache, torch = _cache()
+    q, out, lengths = torch.zeros(2, 4, 64), torch.zeros(2, 4, 64), torch.zeros(2, dtype=torch.int32)
+    for wide in ((1 << 32) + 5, 1 << 31, -(1 << 32) + 5, -(1 << 32)):
+        refused(P.kv_attend, cache, q, lengths, out, max_len=wide)
+        refused(P.kv_attend, cache, q, lengths, out, max_len=wide, scratch=torch.zeros(1 << 16, dtype=torch.uint8))
+        refused(P.kv_attend_scratch, cache, 4, max_len=wide)
+        refused(P.kv_attend_scratch, cache, wide - 1)
+        refused(P.logprobs_scratch, wide, 1000, 2, device="cpu")
+        refused(P.logprobs_scratch, 3, wide, 2, device="cpu")
+        refused(P.logprobs_scratch, 3, 1000, wide, device="cpu")
+        refused(P.Rope, wide - 1)
+    assert P.logprobs_scratch(3, 1000, 2, device="cpu").nbytes > 0 and P.kv_attend_scratch(cache, 4, max_len=5).nbytes > 0
