@@ -397,7 +397,7 @@ typedef struct poss_rope {
  * NONE w;  LINEAR w / factor;  BASE w of theta * factor^(rot_dim / (rot_dim - 2));
  * BANDS and RAMP g w + (1 - g) w / factor, BANDS with g = (turns - low) / (high - low) for turns = original * w / (2 pi), RAMP with
  * g = 1 - (i - lo) / (hi - lo) for lo, hi = the indices of `high` and `low` turns, floor and ceiling, within 0 .. rot_dim - 1; g kept in 0 .. 1.
- * factor, low, high and original are read by the scalings that name them.  HOST only, no GPU needed. */
+ * factor, low, high and original are read by the scalings that name them.  Frequencies have to come out finite, magnitude too as float32.  HOST only, no GPU needed. */
 #define POSS_ROPE_NONE   0
 #define POSS_ROPE_LINEAR 1
 #define POSS_ROPE_BASE   2

@@ -222,7 +222,7 @@ int poss_rope_fill(int32_t rot_dim, int32_t interleaved, double theta, int32_t s
     const char *who = "poss_rope_fill";
     if (!out) return set_error(POSS_E_INVALID_ARG, "%s: null argument", who);
     if (rot_dim < 2 || rot_dim > 2 * POSS_ROPE_PAIRS || rot_dim % 2) return set_error(POSS_E_INVALID_ARG, "%s: rot_dim must be even, 2 to %d", who, 2 * POSS_ROPE_PAIRS);
-    if (!(theta > 0) || !isfinite(theta) || !isfinite(magnitude)) return set_error(POSS_E_INVALID_ARG, "%s: theta must be positive, magnitude finite", who);
+    if (!(theta > 0) || !isfinite(theta) || !isfinite((float)magnitude)) return set_error(POSS_E_INVALID_ARG, "%s: theta must be positive, magnitude finite", who);
     if (scaling < POSS_ROPE_NONE || scaling > POSS_ROPE_RAMP) return set_error(POSS_E_INVALID_ARG, "%s: no such scaling", who);
     if (scaling != POSS_ROPE_NONE && (!(factor > 0) || !isfinite(factor))) return set_error(POSS_E_INVALID_ARG, "%s: factor must be positive", who);
     const bool parts = scaling == POSS_ROPE_BANDS || scaling == POSS_ROPE_RAMP;
@@ -250,6 +250,7 @@ int poss_rope_fill(int32_t rot_dim, int32_t interleaved, double theta, int32_t s
         if (scaling == POSS_ROPE_RAMP) g = 1 - (i - lo) / (hi - lo > 1e-3 ? hi - lo : 1e-3);
         g = g < 0 ? 0 : g > 1 ? 1 : g;
         r.freq[i] = g * w + (1 - g) * w / (scaling == POSS_ROPE_NONE || scaling == POSS_ROPE_BASE ? 1 : factor);
+        if (!isfinite(r.freq[i])) return set_error(POSS_E_INVALID_ARG, "%s: theta and factor give a frequency that is not finite", who);
     }
     *out = r;
     return POSS_OK;

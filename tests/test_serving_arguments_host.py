@@ -54,3 +54,14 @@ def test_numbers_beyond_32_bits():
         refused(P.logprobs_scratch, 3, 1000, wide, device="cpu")
         refused(P.Rope, wide - 1)
     assert P.logprobs_scratch(3, 1000, 2, device="cpu").nbytes > 0 and P.kv_attend_scratch(cache, 4, max_len=5).nbytes > 0
+
+
+def test_frequencies_and_magnitudes_that_are_not_finite():
+    """Numbers that are finite as they come but give none: an infinite frequency turns every angle into NaN, a magnitude beyond float32 every value."""
+    _cache()
+    import math
+    for kw in (dict(magnitude=1e39), dict(magnitude=-1e300), dict(theta=1e-320), dict(theta=1e-200, scaling="linear", factor=1e-200), dict(scaling="linear", factor=1e-320),
+               dict(theta=1e-320, scaling="bands", factor=2.0), dict(scaling="base", factor=1e-320)):
+        refused(P.Rope, 64, **kw)
+    for kw in (dict(magnitude=3e38), dict(theta=1e-300), dict(scaling="linear", factor=1e-300), dict(scaling="base", factor=1e300)):
+        assert all(math.isfinite(f) for f in P.Rope(64, **kw).frequencies)
