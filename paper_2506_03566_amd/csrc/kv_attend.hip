@@ -584,7 +584,7 @@ int poss_kv_attend(const poss_kv_cache *cache, int32_t n_q_heads, const void *q,
                    float *lse, const float *weights, float *weights_out, void *scratch, size_t scratch_bytes, void *hip_stream) {
     const char *who = "poss_kv_attend";
     if (const char *why = attend_bad(cache, n_q_heads, max_len)) return set_error(POSS_E_INVALID_ARG, "%s: %s", who, why);
-    if (!(scale > -INFINITY && scale < INFINITY)) return set_error(POSS_E_INVALID_ARG, "%s: scale must be finite", who);
+    if (!(fabsf(scale) * LOG2E < INFINITY)) return set_error(POSS_E_INVALID_ARG, "%s: scale, and scale times log2(e), must be finite", who);
     if (weights && !weights_out) return set_error(POSS_E_INVALID_ARG, "%s: weights without weights_out", who);
     if (cache->n_seq == 0) return POSS_OK;
     if (!q || !out || !lengths || !scratch) return set_error(POSS_E_INVALID_ARG, "%s: null argument", who);

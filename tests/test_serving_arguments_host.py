@@ -65,3 +65,15 @@ def test_frequencies_and_magnitudes_that_are_not_finite():
         refused(P.Rope, 64, **kw)
     for kw in (dict(magnitude=3e38), dict(theta=1e-300), dict(scaling="linear", factor=1e-300), dict(scaling="base", factor=1e300)):
         assert all(math.isfinite(f) for f in P.Rope(64, **kw).frequencies)
+
+
+def test_a_scale_that_float32_does_not_hold_in_the_log2_domain():
+    """Scores are formed times scale * log2(e): where that is infinite, a score of 0 would be NaN."""
+    cache, torch = _cache()
+    lib = P.load_library()
+    need = lib.poss_kv_attend_scratch_bytes(cache.ref, 4, 0, 0)
+    a = 1 << 20                                            # (never followed: the scratch is too small)
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        assert lib.poss_kv_attend(cache.ref, 4, a, 256, 2 * a, 256, a, 0, scale, None, None, None, a, need - 1, None) == P.E_INVALID_ARG
+        assert b"scale" in lib.poss_last_error(None)
+    assert lib.poss_kv_attend(cache.ref, 4, a, 256, 2 * a, 256, a, 0, 2.3e38, None, None, None, a, need - 1, None) == P.E_CAPACITY
