@@ -1,4 +1,4 @@
-"""Rotation of many rows against float64 where a wave takes whole pieces: heads of a single unit and of a few, rows on both sides of a wave each and past the last whole
+"""Rotation of many rows, alone and into a cache, against float64 where a wave takes whole pieces: heads of a single unit and of a few, rows on both sides of a wave each and past the last whole
 workgroup, heads that lie apart or in another order, parts of wider heads, in place.
 
 Tolerance.  The angle is the float64 product that the oracle forms too; cosine and sine, times the magnitude, are rounded once to float32 (half a step, 2^-24, each), the product b sin
@@ -83,3 +83,31 @@ def test_a_row_does_not_depend_on_how_many_there_are(t):
         whole = P.rotary(x, pos, rope)
         for n in (1, 199, 200, 2047, 2048):
             assert torch.equal(P.rotary(x[:n], pos[:n], rope), whole[:n]), (dh, n)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,n_seq,first", [(2047, 1, 0), (2048, 1, 5), (2049, 3, 0), (2051, 2, 3), (2600, 2600, 0)])
+def test_append_of_many_rows(t, rows, n_seq, first):
+    """On both sides of a wave a row, with rows past the last whole workgroup: what is where, and nothing elsewhere."""
+    print(f"append {t} {rows} rows of {n_seq} sequences from slot {first}", flush=True)
+    rng = np.random.default_rng(rows)
+    hq, hkv, dh, page = 3, 2, 32, 32
+    each = -(-rows // n_seq)
+    per = -(-(each + first) // page)
+    pages = n_seq * per
+    k, v = (torch.full((pages, hkv, *s), float("nan"), dtype=TYPES[t], device="cuda") for s in ((page, dh), (dh, page)))
+    table = rng.permutation(pages).reshape(n_seq, per).astype(np.int32)
+    cache = P.KvCache(k, v, torch.from_numpy(table).cuda())
+    seq, slots = (np.arange(rows) // each).astype(np.int32), (np.arange(rows) % each + first).astype(np.int32)
+    slots[11] = -1
+    positions = rng.integers(0, 100000, size=rows).astype(np.int32)
+    rope = P.Rope(dh, magnitude=0.75)
+    q, kn, vn = torch.from_numpy(rng.normal(size=(rows, hq + 2 * hkv, dh))).to(TYPES[t]).cuda().split([hq, hkv, hkv], dim=1)
+    q_out = torch.empty(rows, hq, dh, dtype=TYPES[t], device="cuda")
+    P.kv_append(cache, kn, vn, torch.from_numpy(slots).cuda(), torch.from_numpy(positions).cuda(), rope, seq=torch.from_numpy(seq).cuda(), q=q, q_out=q_out)
+    assert_rotated(q_out, f64(q), positions, rope, False, t)
+    there = np.flatnonzero(slots >= 0)
+    pg, at = torch.from_numpy(table[seq[there], slots[there] // page].astype(np.int64)).cuda(), torch.from_numpy(slots[there].astype(np.int64) % page).cuda()
+    assert_rotated(k[pg, :, at], f64(kn)[there], positions[there], rope, False, t)
+    assert torch.equal(v[pg, :, :, at], vn[torch.from_numpy(there).cuda()])
+    assert int((~k.isnan()).sum()) == int((~v.isnan()).sum()) == len(there) * hkv * dh
