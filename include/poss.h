@@ -464,7 +464,9 @@ int poss_logprobs(int32_t dtype, const void *x, int64_t ldx, int32_t rows, int32
                   void *scratch, size_t scratch_bytes, void *hip_stream);
 
 /* The cache of one sequence of a context in the form above (one sequence): which = -1: target layer `layer`; which = s >= 0: specialist s.  Slots 0 .. t-1
- * hold the committed tokens' keys (rotated) and values; queue work on the context's stream, between its calls. */
+ * hold the committed tokens' keys (rotated) and values; queue work on the context's stream, between its calls.  It is the context's memory: it takes slot s for token s and
+ * knows its length from its own calls alone, so that behind poss_kv_append to slots of committed tokens or poss_kv_evict it must not go on with the sequence: reset it (poss_reset,
+ * poss_reset_seq) and give it its prompt again. */
 int poss_get_kv_cache(poss_ctx *ctx, int32_t seq, int32_t which, int32_t layer, poss_kv_cache *out);
 
 #ifdef __cplusplus

@@ -372,7 +372,8 @@ class Poss:
         return out
 
     def kv_cache(self, seq=0, which=-1, layer=0):
-        """The cache of one sequence for kv_attend and the like: the target's layer `layer` (which -1) or specialist `which`.  The memory is this context's."""
+        """The cache of one sequence for kv_attend and the like: the target's layer `layer` (which -1) or specialist `which`.  The memory is this context's:
+        after kv_append over committed slots or kv_evict the sequence has to be reset and prefilled before the context goes on with it."""
         from .serving import KvCache
         c = PossKvCache()
         self._check(self.lib.poss_get_kv_cache(self.h, seq, which, layer, ctypes.byref(c)))
