@@ -1,7 +1,7 @@
 // Log-probabilities of given tokens, entropy and the best alternatives of rows of logits (include/poss.h: poss_logprobs).
 //
 // With m = max x, d = (x - m) / T:  S = sum e^d, log p = d - log S, entropy = log S - sum(e^d d) / S.  Everything is formed from differences to the
-// maximum: large logits cancel nothing, and x / T cannot overflow where p has a value.
+// maximum: large logits cancel nothing, and x / T cannot overflow where p has a value (logits 2^128 or more below the largest have none here, at any temperature).
 #include "kv.h"
 
 #include <float.h>
