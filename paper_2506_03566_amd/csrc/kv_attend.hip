@@ -199,10 +199,11 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float back_by(float m, float to) { return m == -INFINITY ? 0.f : exp2_of(m - to); }
 
 __device__ __forceinline__ bool any_nan(f32x4 o) { return __builtin_isunordered(o[0], o[1]) || __builtin_isunordered(o[2], o[3]); }
-// An infinite value counts as such wherever its score is above -infinity.  Where its probability, the second number that stands for it or a factor on the way is 0, or that number is
-// below 0, NaN has come of it.  So this is what a sum over the slots s0 .. s1 - 1 has to be that is NaN while the probabilities are not: the infinities and NaN among the values (row d) times
-// 1, or times 0 where the score is -infinity.  (If there are none it is left: numbers whose sums float32 does not hold.)  A thread looks through the slots by itself, which
-// costs the tiles nothing (131072 slots of 8 key heads: 0.18 ms with one infinity, 0.49 with a slot of them, for 0.1; to take their blocks once more, with such values apart: 0.2 to 0.5 us for every call).
+// An infinite value counts as such wherever its score is above -infinity.  Where its probability, the second number that stands for it or a factor on the way is 0, or that
+// number is below 0, NaN has come of it.  So this is what a sum over the slots s0 .. s1 - 1 has to be that is NaN while the probabilities are not: the infinities and NaN among
+// the values (row d) times 1, or times 0 where the score is -infinity.  (If there are none it is left: numbers whose sums float32 does not hold.)  A thread looks through the
+// slots by itself, which costs the tiles nothing (131072 slots of 8 key heads: 0.18 ms with one infinity, 0.49 with a slot of them, for 0.1); to take their blocks once
+// more, with such values apart, cost every call 0.2 to 0.5 us.
 template <typename T, int DH>
 __device__ __forceinline__ float sum_of_infinities(const T *q, const KvView &c, const int32_t *table, int hk, int d, int s0, int s1, float scale) {
     constexpr int E = 16 / sizeof(T);
